@@ -1,0 +1,356 @@
+// Products between the matrices of the Newton-Schulz steps: C = A B^T, both operands' rows contiguous along the contraction (X X^T,
+// A A, and B X with X^T kept beside X), in half precision on the matrix cores with fp32 sums.  Symmetric results compute the tiles on and below the
+// diagonal and write the others as transposes.  Split operands hold a second half per entry (22 bits); a tile then takes three products,
+// lead x lead and the two crossed ones, of the same fragments.
+#include <atomic>
+
+#include "prsgd_internal.h"
+#include "prsgd_ops_internal.h"
+
+namespace prsgd {
+
+namespace {
+
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+template <int ES> struct __attribute__((packed, aligned(ES))) Packed16 { u32x4_t v; };
+
+constexpr int kRowBytes = 128;             // of an operand row in a tile
+
+__device__ __forceinline__ float half_value(uint16_t h) { return (float)__builtin_bit_cast(_Float16, h); }
+__device__ __forceinline__ uint16_t half_bits(float f) { return __builtin_bit_cast(uint16_t, (_Float16)f); }
+// leading halves and remainders of eight values
+__device__ __forceinline__ void split8(const float* v, u32x4_t* hi, u32x4_t* lo) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint16_t h0 = half_bits(v[2 * e]), h1 = half_bits(v[2 * e + 1]);
+    (*hi)[e] = (uint32_t)h0 | (uint32_t)h1 << 16;
+    (*lo)[e] = (uint32_t)half_bits(v[2 * e] - half_value(h0)) | (uint32_t)half_bits(v[2 * e + 1] - half_value(h1)) << 16;
+  }
+}
+__device__ __forceinline__ float half_at(u32x4_t v, int e) { return half_value((uint16_t)(v[e / 2] >> (16 * (e & 1)))); }
+
+// halves of column c of a row
+template <bool SPLIT> __device__ __forceinline__ int half_col(int c) { return SPLIT ? (c >> 5) * 64 + (c & 31) : c; }
+
+// Requests of a tile of ROWS operand rows by NW wavefronts: 16-byte chunk q of row r stands at chunk lds_chunk(r, q).
+template <int ROWS, int NW> struct TileRequests {
+  static constexpr int NPT = ROWS * kRowBytes / 1024 / NW;
+  static_assert(ROWS * kRowBytes % (1024 * NW) == 0, "a tile splits evenly over the wavefronts");
+  uint32_t off[NPT];
+  // rows past the operand's n are copies of its last one, never stored
+  __device__ __forceinline__ void set(int ld, int n, int wave, int lane) {
+#pragma unroll
+    for (int q = 0; q < NPT; ++q) {
+      const int chunk = (q * NW + wave) * 64 + lane, lr = chunk >> 3;
+      off[q] = (uint32_t)min(lr, n - 1) * (uint32_t)ld * 2u + (uint32_t)lds_chunk(lr, chunk & 7) * 16u;
+    }
+  }
+  __device__ __forceinline__ void request(const uint16_t* base, uint32_t lds_tile, int q, int wave) const {
+    load_to_lds(base, off[q], lds_tile + (uint32_t)(q * NW + wave) * 1024u);
+  }
+};
+
+template <int N> __device__ __forceinline__ void wait_requests() {
+  static_assert(N <= 63, "vmcnt");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(N) : "memory");
+}
+
+__device__ __forceinline__ f16x8_t fragment(const unsigned char* tile, int block, int chunk, int lane) {
+  const int r = lane & 31;
+  return __builtin_bit_cast(f16x8_t, *reinterpret_cast<const u32x4_t*>(tile + (block * 32 + r) * kRowBytes + (lds_chunk(r, chunk) << 4)));
+}
+
+// Eight consecutive values of the result at row i, columns j.. of the caller's matrix, n of them inside it.
+template <typename T> __device__ __forceinline__ void user_store(const OrthMatrices& u, int64_t at_out, int n, const float* v) {
+  T* out = reinterpret_cast<T*>(u.out) + at_out;
+  float r[8];
+  if (u.m != nullptr) {                    // the parameters' update
+    if (n >= 8) {
+      if constexpr (sizeof(T) == 4) {
+        const u32x4_t lo = reinterpret_cast<const Packed16<4>*>(out)->v, hi = reinterpret_cast<const Packed16<4>*>(out + 4)->v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { r[e] = __uint_as_float(lo[e]); r[4 + e] = __uint_as_float(hi[e]); }
+      } else {
+        const u32x4_t x = reinterpret_cast<const Packed16<2>*>(out)->v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[e] = __uint_as_float((e & 1) != 0 ? x[e / 2] & 0xFFFF0000u : x[e / 2] << 16);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (sizeof(T) == 4) r[e] = e < n ? out[e] : 0.0f;
+        else r[e] = e < n ? bf16_to_f32(out[e]) : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = fmaf(-u.step, v[e], u.keep * r[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = v[e];
+  }
+  if constexpr (sizeof(T) == 4) {
+    if (n >= 8) {
+      reinterpret_cast<Packed16<4>*>(out)->v = (u32x4_t){__float_as_uint(r[0]), __float_as_uint(r[1]), __float_as_uint(r[2]), __float_as_uint(r[3])};
+      reinterpret_cast<Packed16<4>*>(out + 4)->v = (u32x4_t){__float_as_uint(r[4]), __float_as_uint(r[5]), __float_as_uint(r[6]), __float_as_uint(r[7])};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < n) out[e] = r[e];
+    }
+  } else {
+    const u32x4_t w = {f32x2_to_bf16x2_rne(r[0], r[1]), f32x2_to_bf16x2_rne(r[2], r[3]), f32x2_to_bf16x2_rne(r[4], r[5]), f32x2_to_bf16x2_rne(r[6], r[7])};
+    if (n >= 8) {
+      reinterpret_cast<Packed16<2>*>(out)->v = w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < n) out[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+    }
+  }
+}
+
+template <int BM, int BN, int S> constexpr int square_lds_bytes(int wm, int wn) {
+  const int stages = S * (BM + BN) * kRowBytes, strips = wm * wn * 32 * (BN / wn + 2) * 4;
+  return stages > strips ? stages : strips;
+}
+
+// WM x WN wavefronts, S tiles of 128 bytes' depth in LDS.
+template <int BM, int BN, int WM, int WN, int S, bool SPLIT, int EPI>
+__global__ void __launch_bounds__(64 * WM * WN) square_kernel(const SquareArgs p) {
+  constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, KK = SPLIT ? 2 : 4, PARTS = SPLIT ? 2 : 1;
+  constexpr bool SYMMETRIC = EPI == SQ_GRAM || EPI == SQ_POLY;
+  constexpr int STAGE = (BM + BN) * kRowBytes;
+  using ReqA = TileRequests<BM, NW>;
+  using ReqB = TileRequests<BN, NW>;
+  constexpr int PER = ReqA::NPT + ReqB::NPT;
+  static_assert(!SYMMETRIC || BM == BN, "tiles of a symmetric result");
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+
+  // Consecutive workgroups go to the XCDs in turn; each XCD gets a contiguous range of the tiles, so that a matrix stays in few L2s.
+  const int total = p.tiles * p.count, xcd = blockIdx.x & 7;
+  const int idx = xcd * (total >> 3) + min(xcd, total & 7) + (blockIdx.x >> 3);
+  const int g = idx / p.tiles, in = idx - g * p.tiles;
+  int ti, tj;
+  if (SYMMETRIC) {                         // row of the triangle
+    ti = (int)((sqrtf(8.0f * (float)in + 1.0f) - 1.0f) * 0.5f);
+    while (ti * (ti + 1) / 2 > in) --ti;
+    while ((ti + 1) * (ti + 2) / 2 <= in) ++ti;
+    tj = in - ti * (ti + 1) / 2;
+  } else {
+    ti = in / p.tiles_n;
+    tj = in - ti * p.tiles_n;
+  }
+  const int m0 = ti * BM, n0 = tj * BN;
+
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
+  const uint16_t* a = p.a + g * p.a_gs + (int64_t)m0 * p.lda;
+  const uint16_t* b = p.b + g * p.b_gs + (int64_t)n0 * p.ldb;
+  ReqA ra;
+  ReqB rb;
+  ra.set(p.lda, p.M - m0, wave, lane);
+  rb.set(p.ldb, p.N - n0, wave, lane);
+  const int n_k = p.groups;
+  auto request = [&](int t, int first, int last) __attribute__((always_inline)) {
+    const uint32_t stage = lds0 + (uint32_t)(t % S) * STAGE;
+#pragma unroll
+    for (int q = first; q < last; ++q) {
+      if (q < ReqA::NPT) ra.request(a + t * 64, stage, q, wave);
+      else rb.request(b + t * 64, stage + BM * kRowBytes, q - ReqA::NPT, wave);
+    }
+  };
+  f16x8_t fa[2][PARTS][TM], fb[2][PARTS][TN];
+  auto load = [&](int t, int kk, int set) __attribute__((always_inline)) {
+    const unsigned char* ta = smem + (t % S) * STAGE;
+    const unsigned char* tb = ta + BM * kRowBytes;
+    const int chunk = 2 * kk + (lane >> 5);
+#pragma unroll
+    for (int h = 0; h < PARTS; ++h) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) fa[set][h][i] = fragment(ta, wm * TM + i, 4 * h + chunk, lane);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) fb[set][h][j] = fragment(tb, wn * TN + j, 4 * h + chunk, lane);
+    }
+  };
+  f32x16_t acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+
+  // Tile t + 1 is met before the last slice of tile t is multiplied; from there on every fragment of tile t has been read, and its stage
+  // takes tile t + S.
+#pragma unroll
+  for (int t = 0; t < S; ++t)
+    if (t < n_k) request(t, 0, PER);
+  if (n_k >= S) wait_requests<(S - 1) * PER>(); else wait_requests<0>();
+  asm volatile("s_barrier" ::: "memory");
+  load(0, 0, 0);
+  for (int t = 0; t < n_k; ++t) {
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      const int set = kk & 1;
+      if (kk == KK - 1) {
+        if (t + S - 1 < n_k) wait_requests<(S - 2) * PER>(); else wait_requests<0>();
+        asm volatile("s_barrier" ::: "memory");
+        if (t + S < n_k) request(t + S, 0, PER);
+        if (t + 1 < n_k) load(t + 1, 0, set ^ 1);
+      } else {
+        load(t, kk + 1, set ^ 1);
+      }
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[set][0][i], fb[set][0][j], acc[i][j], 0, 0, 0);
+          if constexpr (SPLIT) {
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[set][0][i], fb[set][1][j], acc[i][j], 0, 0, 0);
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[set][1][i], fb[set][0][j], acc[i][j], 0, 0, 0);
+          }
+        }
+    }
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+
+  // Epilogue: a wavefront passes strips of 32 rows through LDS, first along the rows and then, as transposes, along the columns.
+  constexpr int W = BN / WN, P = W + 2, VPR = W / 8, RPP = 64 / VPR;      // strip columns, pitch, 8-value vectors of a row, rows per pass
+  float* strip = reinterpret_cast<float*>(smem) + wave * 32 * P;
+  const int c0 = n0 + wn * W;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int r0 = m0 + (wm * TM + i) * 32;
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) strip[(8 * (e / 4) + 4 * (lane >> 5) + (e % 4)) * P + j * 32 + (lane & 31)] = acc[i][j][e];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll(EPI == SQ_LAST ? 1 : 32 / RPP)
+    for (int q = 0; q < 32 / RPP; ++q) {
+      const int lr = q * RPP + lane / VPR, lc = lane % VPR * 8, r = r0 + lr, c = c0 + lc;
+      float* at = strip + lr * P + lc;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const f32x2_t x = *reinterpret_cast<const f32x2_t*>(at + e);
+        v[e] = x[0];
+        v[e + 1] = x[1];
+      }
+      const bool inside = r < p.M && c < p.N;
+      const int hc = half_col<SPLIT>(c);
+      if constexpr (EPI != SQ_GRAM) {
+        u32x4_t hi = {0, 0, 0, 0}, lo = {0, 0, 0, 0};
+        if (inside) {
+          const int64_t o = g * p.lin_gs + (int64_t)r * p.ld_lin + hc;
+          hi = *reinterpret_cast<const u32x4_t*>(p.lin + o);
+          if (SPLIT) lo = *reinterpret_cast<const u32x4_t*>(p.lin + o + 32);
+          else if (EPI != SQ_POLY) lo = *reinterpret_cast<const u32x4_t*>(p.lin_lo + o);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = fmaf(p.alpha, half_at(hi, e) + half_at(lo, e), p.beta * v[e]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= p.beta;
+      }
+      // padding columns of the halves hold zeros, and so do padding rows of transposes
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = r < p.M && c + e < p.N ? v[e] : 0.0f;
+      if constexpr (EPI == SQ_LAST) {
+        if (!p.transposed && inside) {
+          const int64_t o = g * p.user.out_matrix + r * p.user.out_row + c;
+          if (p.user.bf16) user_store<uint16_t>(p.user, o, p.N - c, v);
+          else user_store<float>(p.user, o, p.N - c, v);
+        }
+      } else if (r < p.M && hc < p.ldo) {
+        u32x4_t hi, lo;
+        split8(v, &hi, &lo);
+        const int64_t o = g * p.out_gs + (int64_t)r * p.ldo + hc;
+        *reinterpret_cast<u32x4_t*>(p.out + o) = hi;
+        if (SPLIT) *reinterpret_cast<u32x4_t*>(p.out + o + 32) = lo;
+        else if (EPI == SQ_NEXT) *reinterpret_cast<u32x4_t*>(p.out_lo + o) = lo;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) *reinterpret_cast<f32x2_t*>(at + e) = (f32x2_t){v[e], v[e + 1]};
+    }
+    __builtin_amdgcn_wave_barrier();
+    if (SYMMETRIC ? ti != tj : EPI == SQ_NEXT || p.transposed) {
+#pragma unroll(EPI == SQ_LAST ? 1 : W / 16)
+      for (int q = 0; q < W / 16; ++q) {
+        const int lc = q * 16 + lane % 16, lr = lane / 16 * 8, c = c0 + lc, r = r0 + lr;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = strip[(lr + e) * P + lc];
+        if (c >= p.N) continue;
+        if constexpr (EPI == SQ_LAST) {
+          if (r < p.M) {
+            const int64_t o = g * p.user.out_matrix + c * p.user.out_row + r;
+            if (p.user.bf16) user_store<uint16_t>(p.user, o, p.M - r, v);
+            else user_store<float>(p.user, o, p.M - r, v);
+          }
+        } else {
+          const int hr = half_col<SPLIT>(r);
+          if (hr < p.ldt) {
+            u32x4_t hi, lo;
+            split8(v, &hi, &lo);
+            const int64_t o = g * p.t_gs + (int64_t)c * p.ldt + hr;
+            *reinterpret_cast<u32x4_t*>(p.out_t + o) = hi;
+            if (SPLIT) *reinterpret_cast<u32x4_t*>(p.out_t + o + 32) = lo;
+          }
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+}
+
+template <int BM, int BN, int WM, int WN, int S, bool SPLIT, int EPI> hipError_t launch_as(SquareArgs p, hipStream_t s) {
+  constexpr int kLds = square_lds_bytes<BM, BN, S>(WM, WN);
+  static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
+  auto kernel = square_kernel<BM, BN, WM, WN, S, SPLIT, EPI>;
+  // the tiles can exceed the 64 KB default; setting the limit twice is harmless
+  static std::atomic<bool> configured{false};
+  if (!configured.load(std::memory_order_acquire)) {
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    if (e != hipSuccess) return e;
+    configured.store(true, std::memory_order_release);
+  }
+  p.tiles_m = (p.M + BM - 1) / BM;
+  p.tiles_n = (p.N + BN - 1) / BN;
+  p.tiles = EPI == SQ_GRAM || EPI == SQ_POLY ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)p.tiles * (unsigned)p.count), dim3(64 * WM * WN), kLds, s, p);
+  return hipGetLastError();
+}
+template <int BM, int BN, int WM, int WN, int S> hipError_t launch_tile(const SquareArgs& p, int epi, bool split, hipStream_t s) {
+  switch (epi * 2 + (split ? 1 : 0)) {
+    case 0: return launch_as<BM, BN, WM, WN, S, false, SQ_GRAM>(p, s);
+    case 1: return launch_as<BM, BN, WM, WN, S, true, SQ_GRAM>(p, s);
+    case 2: return launch_as<BM, BN, WM, WN, S, false, SQ_POLY>(p, s);
+    case 3: return launch_as<BM, BN, WM, WN, S, true, SQ_POLY>(p, s);
+    case 4: return launch_as<BM, BN, WM, WN, S, false, SQ_NEXT>(p, s);
+    case 5: return launch_as<BM, BN, WM, WN, S, true, SQ_NEXT>(p, s);
+    case 6: return launch_as<BM, BN, WM, WN, S, false, SQ_LAST>(p, s);
+    default: return launch_as<BM, BN, WM, WN, S, true, SQ_LAST>(p, s);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_square(SquareArgs p, int epi, bool split, hipStream_t s) {
+  const bool symmetric = epi == SQ_GRAM || epi == SQ_POLY;
+  // rounds that the 256 compute units take over the tiles, in units of a 64 x 64 tile's products
+  auto cost = [&](int b, double efficiency) {
+    const int64_t tm = (p.M + b - 1) / b, tn = (p.N + b - 1) / b;
+    const int64_t tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * p.count;
+    return (double)((tiles + 255) / 256) * (b / 64) * (b / 64) / efficiency;
+  };
+  const double c256 = cost(256, 1.0), c128 = cost(128, 0.7), c64 = cost(64, 0.35);
+  if (c256 <= c128 && c256 <= c64) return launch_tile<256, 256, 2, 2, 2>(p, epi, split, s);
+  if (c128 <= c64) return launch_tile<128, 128, 2, 2, 2>(p, epi, split, s);
+  return launch_tile<64, 64, 2, 2, 4>(p, epi, split, s);
+}
+
+}  // namespace prsgd

@@ -14,6 +14,7 @@
 
 #include "prsgd_aux.h"
 #include "prsgd_internal.h"
+#include "prsgd_ops_internal.h"
 
 using namespace prsgd;
 
@@ -309,6 +310,12 @@ int hip_fail(prsgd_ctx* ctx, hipError_t e, const char* what) {
   snprintf(buf, sizeof(buf), "%s: %s", what, hipGetErrorString(e));
   return set_err(ctx, PRSGD_EHIP, "%s", buf);
 }
+
+}  // namespace
+
+int prsgd::op_error(int code, const char* text) { return set_err(nullptr, code, "%s", text); }
+
+namespace {
 
 // Drains finished event pairs into the per-kind totals.
 int profile_flush(prsgd_ctx* ctx) {

@@ -1,0 +1,93 @@
+// Internal declarations of the operators on replica sets (prsgd_ops.h).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "prsgd_ops.h"
+
+namespace prsgd {
+
+// Sets the text of prsgd_last_error(NULL) of this thread and returns `code`.
+int op_error(int code, const char* text);
+
+constexpr int kMaxNormWidth = 16384;
+
+struct NormArgs {
+  const void* x; int64_t x_row;          // backward: dy
+  const void* res; int64_t res_row;      // nullptr: none; backward: dsum
+  const float* w; int64_t w_row;
+  void* sum; int64_t sum_row;            // backward: s (read)
+  void* y; int64_t y_row;                // rows of T, or bytes; backward: dx
+  float* stat;                           // forward: rstd (may be nullptr) or scales; backward: rstd (read)
+  float* dw; int64_t dw_row;             // backward: dw, or the workgroups' shares of it
+  uint32_t rows, rows_per_worker;
+  int width;
+  float eps;
+  int blocks;                            // backward: workgroups per worker
+};
+hipError_t launch_rms_norm(const NormArgs& p, bool bf16, bool fp8, hipStream_t s);
+// Workgroups per worker of the backward pass, and the floats of their shares of dw (0: a workgroup has its worker's rows to itself).
+int norm_back_blocks(int workers, int64_t rows_per_worker, int width, bool bf16);
+size_t norm_back_share_floats(int workers, int64_t rows_per_worker, int width, bool bf16);
+hipError_t launch_rms_norm_backward(NormArgs p, float* shares, int workers, bool bf16, hipStream_t s);
+
+// ---- orthogonalised updates ------------------------------------------------------------------
+
+constexpr int kMaxOrthSide = 32768, kMaxOrthSteps = 64;
+constexpr int kShortSide = 32;           // a side up to here goes through its Gram matrix in 64 bits
+constexpr int kNormParts = 64;           // workgroups that sum a matrix's squares
+// Operands are halves of X, A and B times 2^13: entries reach 8, and what a second half holds of an entry of 2^-12 (X_0 of
+// 4096 x 4096) is a normal number or loses less than 2^-36.
+constexpr float kHalfScale = 8192.0f;
+
+// What a call does with the matrices, whichever path computes.
+struct OrthMatrices {
+  const void* g; int64_t g_matrix, g_row;
+  void* out; int64_t out_matrix, out_row;      // result, or (m != nullptr) the parameters that it updates
+  float* m; int64_t m_matrix, m_row;           // momenta (nullptr: U = G)
+  float mu, g_part, m_part;                    // M <- mu M + G, U = g_part G + m_part M
+  float keep, step;                            // X <- keep X - step O
+  int count, rows, cols;
+  bool bf16;
+  float eps, a, b, c;
+  int steps;
+};
+
+// Storage of a matrix of halves [rows][ld]: rows of whole 64-half (128-byte) groups, which hold 64 columns, or (split) 32
+// columns' leading halves and then their remainders.
+constexpr int half_ld(int cols, bool split) { return split ? (cols + 31) / 32 * 64 : (cols + 63) / 64 * 64; }
+
+// A square-side product of every matrix: acc = A B^T over rows of halves, then an epilogue.
+enum SquareEpilogue {
+  SQ_GRAM = 0,    // out = acc (symmetric)
+  SQ_POLY = 1,    // out = b lin + c acc (symmetric)
+  SQ_NEXT = 2,    // out = a lin + acc, and its transpose
+  SQ_LAST = 3,    // result = a lin + acc, into the caller's matrices
+};
+struct SquareArgs {
+  const uint16_t* a; int64_t a_gs; int lda;
+  const uint16_t* b; int64_t b_gs; int ldb;
+  int M, N, groups;                            // groups: 64-half groups of a row
+  const uint16_t* lin; const uint16_t* lin_lo; int64_t lin_gs; int ld_lin;     // lin_lo: remainders (unsplit operands)
+  uint16_t* out; uint16_t* out_lo; int64_t out_gs; int ldo;
+  uint16_t* out_t; int64_t t_gs; int ldt;
+  float alpha, beta;                           // out = alpha lin + beta acc
+  int tiles_m, tiles_n, tiles;                 // tiles per matrix
+  int count;
+  bool transposed;                             // SQ_LAST: the caller's matrices hold the transpose
+  OrthMatrices user;
+};
+hipError_t launch_square(SquareArgs p, int epi, bool split, hipStream_t s);
+
+hipError_t launch_orth_squares(const OrthMatrices& p, double* parts, hipStream_t s);
+struct OrthHalves {                            // X [short][ld_x], X^T [long][ld_t]
+  uint16_t* x; uint16_t* x_lo; int64_t x_gs; int ld_x;
+  uint16_t* t; int64_t t_gs; int ld_t;
+};
+hipError_t launch_orth_load(const OrthMatrices& p, const double* parts, const OrthHalves& h, bool split, hipStream_t s);
+// Short sides: slices of the long side a matrix is cut into (1: one launch), and the doubles of their Gram matrices.
+int orth_short_slices(int count, int longer);
+hipError_t launch_orth_short(const OrthMatrices& p, double* grams, int slices, hipStream_t s);
+
+}  // namespace prsgd

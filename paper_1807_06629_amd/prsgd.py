@@ -1,7 +1,7 @@
 """Thin ctypes binding of libprsgd (argument marshalling only).
 
-Every function mirrors one entry point of include/prsgd.h (or include/prsgd_aux.h, the
-measurement and test aids) under the same name.  PyTorch is
+Every function mirrors one entry point of include/prsgd.h (or include/prsgd_ops.h, the operators on
+replica sets, or include/prsgd_aux.h, the measurement and test aids) under the same name.  PyTorch is
 used for device memory (the replica buffer and the workspace are torch tensors) and for the
 HIP stream; all arithmetic of the method runs in the library's kernels.  There is no CPU
 fallback: importing this module without a built libprsgd.so raises.
@@ -59,12 +59,25 @@ class prsgd_kernel_stat(ctypes.Structure):
                 ("total_ms", ctypes.c_double)]
 
 
+class prsgd_orth_config(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("count", ctypes.c_int32), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32),
+                ("steps", ctypes.c_int32), ("a", ctypes.c_float), ("b", ctypes.c_float), ("c", ctypes.c_float),
+                ("eps", ctypes.c_float)]
+
+
+class prsgd_norm_config(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("workers", ctypes.c_int32), ("rows_per_worker", ctypes.c_int64),
+                ("width", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
 def _load() -> ctypes.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError("libprsgd.so is not built; run `python -m paper_1807_06629_amd.build`")
     lib = ctypes.CDLL(LIB_PATH)
     cfgp = ctypes.POINTER(prsgd_config)
     vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+    f32 = ctypes.c_float
+    orthp, normp = ctypes.POINTER(prsgd_orth_config), ctypes.POINTER(prsgd_norm_config)
     sigs = {
         "prsgd_param_count": (sz, [cfgp]),
         "prsgd_param_stride": (sz, [cfgp]),
@@ -102,6 +115,13 @@ def _load() -> ctypes.CDLL:
         "prsgd_profile_read": (ctypes.c_int, [vp, ctypes.POINTER(prsgd_kernel_stat), i32]),
         "prsgd_destroy": (ctypes.c_int, [vp]),
         "prsgd_last_error": (ctypes.c_char_p, [vp]),
+        "prsgd_orthogonalize_workspace_bytes": (sz, [orthp]),
+        "prsgd_orthogonalize": (ctypes.c_int, [orthp, vp, i64, i64, vp, i64, i64, vp, vp]),
+        "prsgd_muon_step": (ctypes.c_int, [orthp, vp, i64, i64, vp, i64, i64, vp, i64, i64, f32, f32, i32, f32, f32, vp, vp]),
+        "prsgd_rms_norm": (ctypes.c_int, [normp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp]),
+        "prsgd_rms_norm_fp8": (ctypes.c_int, [normp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp]),
+        "prsgd_rms_norm_backward_workspace_bytes": (sz, [normp]),
+        "prsgd_rms_norm_backward": (ctypes.c_int, [normp, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, vp]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -416,3 +436,185 @@ def prsgd_destroy(h: Handle) -> None:
 def prsgd_last_error(h: Optional[Handle]) -> str:
     msg = _lib.prsgd_last_error(h.ctx if h is not None else None)
     return msg.decode() if msg else ""
+
+
+# ---- operators on replica sets (include/prsgd_ops.h) ---------------------------------------------------------------
+# Tensors are taken as they are: rows have to be contiguous, distances between rows and matrices are read off the strides.
+# Work goes to the current stream of the tensors' device.  Outputs and workspaces that are not given are allocated.
+
+NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
+_DTYPES = {torch.float32: PRSGD_F32, torch.bfloat16: PRSGD_BF16}
+
+
+def _enqueue(device: torch.device, fn, *args) -> None:
+    if device.index == torch.cuda.current_device():
+        _check(fn(*args, torch.cuda.current_stream(device).cuda_stream))
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, torch.cuda.current_stream(device).cuda_stream))
+
+
+def _workspace(given: Optional[torch.Tensor], nbytes: int, device: torch.device) -> torch.Tensor:
+    if given is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if given.device != device or given.numel() * given.element_size() < nbytes:
+        raise ValueError("the workspace must have %d bytes on %s" % (nbytes, device))
+    return given
+
+
+def _matrices(t: torch.Tensor, shape, name: str):
+    """Address, distance between matrices and distance between rows of a [count][rows][cols] or [rows][cols] tensor."""
+    if not t.is_cuda or tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be a device tensor of shape %s" % (name, tuple(shape)))
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError("rows of %s must be contiguous" % name)
+    return t.data_ptr(), t.stride(0) if t.dim() == 3 else 0, t.stride(-2)
+
+
+def _orth_config(dtype: torch.dtype, shape, coefficients, steps: int, eps: float) -> prsgd_orth_config:
+    if dtype not in _DTYPES:
+        raise ValueError("matrices must be float32 or bfloat16")
+    if len(shape) not in (2, 3):
+        raise ValueError("matrices must be [count][rows][cols] or [rows][cols]")
+    a, b, c = coefficients
+    return prsgd_orth_config(_DTYPES[dtype], shape[0] if len(shape) == 3 else 1, shape[-2], shape[-1], int(steps), a, b, c, eps)
+
+
+def prsgd_orthogonalize_workspace_bytes(shape: Sequence[int], dtype: torch.dtype, coefficients=NEWTON_SCHULZ, steps: int = 5,
+                                        eps: float = 1e-7) -> int:
+    """Of prsgd_orthogonalize and prsgd_muon_step on [count][rows][cols] or [rows][cols] matrices."""
+    cfg = _orth_config(dtype, tuple(shape), coefficients, steps, eps)
+    n = int(_lib.prsgd_orthogonalize_workspace_bytes(ctypes.byref(cfg)))
+    if n == 0 and cfg.count != 0:
+        raise PrsgdError(PRSGD_EINVAL, _lib.prsgd_last_error(None).decode())
+    return n
+
+
+def prsgd_orthogonalize(g: torch.Tensor, out: Optional[torch.Tensor] = None, coefficients=NEWTON_SCHULZ, steps: int = 5,
+                        eps: float = 1e-7, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Newton-Schulz orthogonalisation of every [rows][cols] matrix of g (out may be g)."""
+    cfg = _orth_config(g.dtype, g.shape, coefficients, steps, eps)
+    if out is None:
+        out = torch.empty(g.shape, dtype=g.dtype, device=g.device)
+    if out.dtype != g.dtype or out.device != g.device:
+        raise ValueError("out must have the type and device of g")
+    src, dst = _matrices(g, g.shape, "g"), _matrices(out, g.shape, "out")
+    n = int(_lib.prsgd_orthogonalize_workspace_bytes(ctypes.byref(cfg)))
+    ws = _workspace(workspace, n, g.device)
+    _enqueue(g.device, _lib.prsgd_orthogonalize, ctypes.byref(cfg), *src, *dst, ws.data_ptr())
+    return out
+
+
+def prsgd_muon_step(x: torch.Tensor, g: torch.Tensor, m: torch.Tensor, lr: float, momentum: float = 0.95, nesterov: bool = True,
+                    weight_decay: float = 0.0, scale: Optional[float] = None, coefficients=NEWTON_SCHULZ, steps: int = 5,
+                    eps: float = 1e-7, workspace: Optional[torch.Tensor] = None) -> None:
+    """Momentum, orthogonalisation and update of every [rows][cols] matrix of x, in place on x and m (fp32).
+
+    scale defaults to 0.2 sqrt(max(rows, cols))."""
+    cfg = _orth_config(x.dtype, x.shape, coefficients, steps, eps)
+    if g.dtype != x.dtype or m.dtype != torch.float32 or g.device != x.device or m.device != x.device:
+        raise ValueError("g must have the type of x, m must be float32, all on one device")
+    if scale is None:
+        scale = 0.2 * max(x.shape[-2:]) ** 0.5
+    xs, gs, ms = _matrices(x, x.shape, "x"), _matrices(g, x.shape, "g"), _matrices(m, x.shape, "m")
+    n = int(_lib.prsgd_orthogonalize_workspace_bytes(ctypes.byref(cfg)))
+    ws = _workspace(workspace, n, x.device)
+    _enqueue(x.device, _lib.prsgd_muon_step, ctypes.byref(cfg), *xs, *gs, *ms, lr, momentum, 1 if nesterov else 0, weight_decay,
+             scale, ws.data_ptr())
+
+
+def _norm_rows(t: Optional[torch.Tensor], like: torch.Tensor, name: str, dtype=None):
+    """Address and distance between rows of a [rows][width] tensor (0, 0 for none)."""
+    if t is None:
+        return 0, 0
+    if t.device != like.device or t.shape != like.shape or t.dtype != (dtype or like.dtype):
+        raise ValueError("%s must be a %s tensor of shape %s on %s" % (name, dtype or like.dtype, tuple(like.shape), like.device))
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError("rows of %s must be contiguous" % name)
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _norm_config(x: torch.Tensor, w: torch.Tensor, eps: float) -> prsgd_norm_config:
+    if not x.is_cuda or x.dim() != 2 or x.dtype not in _DTYPES:
+        raise ValueError("rows must be a [rows][width] device tensor of float32 or bfloat16")
+    workers = 1 if w.dim() == 1 else w.shape[0]
+    if w.dtype != torch.float32 or w.device != x.device or w.dim() not in (1, 2) or w.shape[-1] != x.shape[1] or \
+            (w.shape[-1] > 1 and w.stride(-1) != 1):
+        raise ValueError("weights must be float32, [width] or [workers][width], rows contiguous")
+    if workers == 0 or x.shape[0] % workers != 0:
+        raise ValueError("every worker must have the same number of rows")
+    return prsgd_norm_config(_DTYPES[x.dtype], workers, x.shape[0] // workers, x.shape[1], eps)
+
+
+def _weight_rows(w: torch.Tensor) -> int:
+    return w.stride(0) if w.dim() == 2 and w.shape[0] > 1 else 0
+
+
+def _row_vector(given: Optional[torch.Tensor], x: torch.Tensor, name: str) -> torch.Tensor:
+    if given is None:
+        return torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+    if given.dtype != torch.float32 or given.device != x.device or given.shape != (x.shape[0],) or not given.is_contiguous():
+        raise ValueError("%s must be %d contiguous floats" % (name, x.shape[0]))
+    return given
+
+
+def _norm_outputs(x, residual, sum_out, out, dtype):
+    if sum_out is None and residual is not None:
+        sum_out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if out is None:
+        out = torch.empty(x.shape, dtype=dtype, device=x.device)
+    return sum_out, out
+
+
+def prsgd_rms_norm(x: torch.Tensor, w: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                   out: Optional[torch.Tensor] = None, sum_out: Optional[torch.Tensor] = None,
+                   rstd: Optional[torch.Tensor] = None):
+    """(y, s, rstd) of s = x + residual, y = s rstd w for the rows of every worker ([workers * rows][width], w [workers][width] or
+    [width]).  Without a residual s is x itself, and is written only if sum_out is given."""
+    cfg = _norm_config(x, w, eps)
+    sum_out, out = _norm_outputs(x, residual, sum_out, out, x.dtype)
+    rstd = _row_vector(rstd, x, "rstd")
+    _enqueue(x.device, _lib.prsgd_rms_norm, ctypes.byref(cfg), *_norm_rows(x, x, "x"), *_norm_rows(residual, x, "residual"),
+             w.data_ptr(), _weight_rows(w), *_norm_rows(sum_out, x, "sum_out"), *_norm_rows(out, x, "out"), rstd.data_ptr())
+    return out, x if sum_out is None else sum_out, rstd
+
+
+def prsgd_rms_norm_fp8(x: torch.Tensor, w: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                       out: Optional[torch.Tensor] = None, sum_out: Optional[torch.Tensor] = None,
+                       scales: Optional[torch.Tensor] = None):
+    """(q, scales, s): prsgd_rms_norm's y as q * scales[:, None], q in torch.float8_e4m3fn."""
+    cfg = _norm_config(x, w, eps)
+    sum_out, out = _norm_outputs(x, residual, sum_out, out, torch.float8_e4m3fn)
+    scales = _row_vector(scales, x, "scales")
+    _enqueue(x.device, _lib.prsgd_rms_norm_fp8, ctypes.byref(cfg), *_norm_rows(x, x, "x"), *_norm_rows(residual, x, "residual"),
+             w.data_ptr(), _weight_rows(w), *_norm_rows(sum_out, x, "sum_out"),
+             *_norm_rows(out, x, "out", torch.float8_e4m3fn), scales.data_ptr())
+    return out, scales, x if sum_out is None else sum_out
+
+
+def prsgd_rms_norm_backward_workspace_bytes(x: torch.Tensor, w: torch.Tensor) -> int:
+    cfg = _norm_config(x, w, 0.0)
+    n = int(_lib.prsgd_rms_norm_backward_workspace_bytes(ctypes.byref(cfg)))
+    if n == 0:
+        raise PrsgdError(PRSGD_EINVAL, _lib.prsgd_last_error(None).decode())
+    return n
+
+
+def prsgd_rms_norm_backward(dy: torch.Tensor, s: torch.Tensor, rstd: torch.Tensor, w: torch.Tensor,
+                            dsum: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                            dw: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """(dx, dw) of prsgd_rms_norm: dx is the gradient of x and of the residual alike, dw has w's shape."""
+    cfg = _norm_config(dy, w, 0.0)
+    rstd = _row_vector(rstd, dy, "rstd")
+    if dx is None:
+        dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
+    if dw is None:
+        dw = torch.empty(w.shape, dtype=torch.float32, device=dy.device)
+    if dw.dtype != torch.float32 or dw.shape != w.shape or dw.device != dy.device or (dw.shape[-1] > 1 and dw.stride(-1) != 1):
+        raise ValueError("dw must be float32 of w's shape, rows contiguous")
+    n = int(_lib.prsgd_rms_norm_backward_workspace_bytes(ctypes.byref(cfg)))
+    ws = _workspace(workspace, max(n, 1), dy.device)
+    _enqueue(dy.device, _lib.prsgd_rms_norm_backward, ctypes.byref(cfg), *_norm_rows(dy, dy, "dy"), *_norm_rows(dsum, dy, "dsum"),
+             *_norm_rows(s, dy, "s"), rstd.data_ptr(), w.data_ptr(), _weight_rows(w), *_norm_rows(dx, dy, "dx"), dw.data_ptr(),
+             _weight_rows(dw), ws.data_ptr())
+    return dx, dw
