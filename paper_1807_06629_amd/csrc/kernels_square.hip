@@ -3,6 +3,7 @@
 // diagonal and write the others as transposes.  Split operands hold a second half per entry (22 bits); a tile then takes three products,
 // lead x lead and the two crossed ones, of the same fragments.
 #include <atomic>
+#include <type_traits>
 
 #include "prsgd_internal.h"
 #include "prsgd_ops_internal.h"
@@ -34,7 +35,9 @@ __device__ __forceinline__ float half_at(u32x4_t v, int e) { return half_value((
 // halves of column c of a row
 template <bool SPLIT> __device__ __forceinline__ int half_col(int c) { return SPLIT ? (c >> 5) * 64 + (c & 31) : c; }
 
-// Requests of a tile of ROWS operand rows by NW wavefronts: 16-byte chunk q of row r stands at chunk lds_chunk(r, q).
+// Place of a row's 16-byte chunk q in its 128 bytes
+__device__ __forceinline__ int chunk_place(int r, int q) { return q ^ ((r >> 1) & 7); }
+// Requests of a tile of ROWS operand rows by NW wavefronts.
 template <int ROWS, int NW> struct TileRequests {
   static constexpr int NPT = ROWS * kRowBytes / 1024 / NW;
   static_assert(ROWS * kRowBytes % (1024 * NW) == 0, "a tile splits evenly over the wavefronts");
@@ -44,7 +47,7 @@ template <int ROWS, int NW> struct TileRequests {
 #pragma unroll
     for (int q = 0; q < NPT; ++q) {
       const int chunk = (q * NW + wave) * 64 + lane, lr = chunk >> 3;
-      off[q] = (uint32_t)min(lr, n - 1) * (uint32_t)ld * 2u + (uint32_t)lds_chunk(lr, chunk & 7) * 16u;
+      off[q] = (uint32_t)min(lr, n - 1) * (uint32_t)ld * 2u + (uint32_t)chunk_place(lr, chunk & 7) * 16u;
     }
   }
   __device__ __forceinline__ void request(const uint16_t* base, uint32_t lds_tile, int q, int wave) const {
@@ -59,7 +62,7 @@ template <int N> __device__ __forceinline__ void wait_requests() {
 
 __device__ __forceinline__ f16x8_t fragment(const unsigned char* tile, int block, int chunk, int lane) {
   const int r = lane & 31;
-  return __builtin_bit_cast(f16x8_t, *reinterpret_cast<const u32x4_t*>(tile + (block * 32 + r) * kRowBytes + (lds_chunk(r, chunk) << 4)));
+  return __builtin_bit_cast(f16x8_t, *reinterpret_cast<const u32x4_t*>(tile + (block * 32 + r) * kRowBytes + (chunk_place(r, chunk) << 4)));
 }
 
 // Eight consecutive values of the result at row i, columns j.. of the caller's matrix, n of them inside it.
@@ -163,17 +166,13 @@ __global__ void __launch_bounds__(64 * WM * WN) square_kernel(const SquareArgs p
     }
   };
   f16x8_t fa[2][PARTS][TM], fb[2][PARTS][TN];
-  auto load = [&](int t, int kk, int set) __attribute__((always_inline)) {
+  constexpr int READS = PARTS * (TM + TN);
+  // fragment q of slice kk
+  auto load = [&](int t, int kk, int set, int q) __attribute__((always_inline)) {
     const unsigned char* ta = smem + (t % S) * STAGE;
-    const unsigned char* tb = ta + BM * kRowBytes;
-    const int chunk = 2 * kk + (lane >> 5);
-#pragma unroll
-    for (int h = 0; h < PARTS; ++h) {
-#pragma unroll
-      for (int i = 0; i < TM; ++i) fa[set][h][i] = fragment(ta, wm * TM + i, 4 * h + chunk, lane);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) fb[set][h][j] = fragment(tb, wn * TN + j, 4 * h + chunk, lane);
-    }
+    const int h = q / (TM + TN), x = q % (TM + TN), chunk = 4 * h + 2 * kk + (lane >> 5);
+    if (x < TM) fa[set][h][x] = fragment(ta, wm * TM + x, chunk, lane);
+    else fb[set][h][x - TM] = fragment(ta + BM * kRowBytes, wn * TN + x - TM, chunk, lane);
   };
   f32x16_t acc[TM][TN];
 #pragma unroll
@@ -184,27 +183,32 @@ __global__ void __launch_bounds__(64 * WM * WN) square_kernel(const SquareArgs p
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
 
   // Tile t + 1 is met before the last slice of tile t is multiplied; from there on every fragment of tile t has been read, and its stage
-  // takes tile t + S.
+  // takes tile t + S, half of it behind that slice and half behind the next.  Each row of a slice's products is followed by its share of
+  // the next slice's fragments and of the requests, so that neither waits in a burst of its own (a request takes 16 cycles of the compute
+  // unit's one path to its cache).
 #pragma unroll
   for (int t = 0; t < S; ++t)
     if (t < n_k) request(t, 0, PER);
   if (n_k >= S) wait_requests<(S - 1) * PER>(); else wait_requests<0>();
   asm volatile("s_barrier" ::: "memory");
-  load(0, 0, 0);
-  for (int t = 0; t < n_k; ++t) {
+#pragma unroll
+  for (int q = 0; q < READS; ++q) load(0, 0, 0, q);
+  auto step = [&](int t, auto whole_) __attribute__((always_inline)) {
+    constexpr bool WHOLE = decltype(whole_)::value;        // every tile that the step asks for exists
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
       const int set = kk & 1;
-      if (kk == KK - 1) {
-        if (t + S - 1 < n_k) wait_requests<(S - 2) * PER>(); else wait_requests<0>();
+      const bool last = kk == KK - 1;
+      if (last) {
+        if (WHOLE || t + S - 1 < n_k) wait_requests<(S - 2) * PER>(); else wait_requests<0>();
         asm volatile("s_barrier" ::: "memory");
-        if (t + S < n_k) request(t + S, 0, PER);
-        if (t + 1 < n_k) load(t + 1, 0, set ^ 1);
-      } else {
-        load(t, kk + 1, set ^ 1);
       }
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+      for (int i = 0; i < TM; ++i) {
+        if (!last || WHOLE || t + 1 < n_k) {
+#pragma unroll
+          for (int q = i * READS / TM; q < (i + 1) * READS / TM; ++q) load(last ? t + 1 : t, last ? 0 : kk + 1, set ^ 1, q);
+        }
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
           acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[set][0][i], fb[set][0][j], acc[i][j], 0, 0, 0);
@@ -213,8 +217,19 @@ __global__ void __launch_bounds__(64 * WM * WN) square_kernel(const SquareArgs p
             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[set][1][i], fb[set][0][j], acc[i][j], 0, 0, 0);
           }
         }
+        constexpr int HALF = PER / 2;
+        if (last && (WHOLE || t + S < n_k)) request(t + S, i * HALF / TM, (i + 1) * HALF / TM);
+        if (kk == 0 && t > 0 && (WHOLE || t - 1 + S < n_k)) request(t - 1 + S, HALF + i * (PER - HALF) / TM, HALF + (i + 1) * (PER - HALF) / TM);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
+  };
+  int t = 0;
+  if (n_k > S) {
+    step(0, std::true_type{});
+    for (t = 1; t + S < n_k; ++t) step(t, std::true_type{});
   }
+  for (; t < n_k; ++t) step(t, std::false_type{});
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 
   // Epilogue: a wavefront passes strips of 32 rows through LDS, first along the rows and then, as transposes, along the columns.
