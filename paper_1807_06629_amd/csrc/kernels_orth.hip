@@ -37,59 +37,126 @@ __device__ __forceinline__ double wave_sum(double v) {
   return v;
 }
 
-// Sums of squares in 64 bits (an fp32 sum overflows from elements of 1e19 on): kNormParts workgroups per matrix, strided rows.
+// Eight elements of U at a row's column c, n of them inside it (the others are zero); M moves on unless an earlier launch did that.
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+template <int ES> struct __attribute__((packed, aligned(ES))) Packed16 { u32x4_t v; };
+template <typename T> __device__ __forceinline__ void load8(const T* p, int n, float (&v)[8]) {
+  if (n >= 8) {
+    if constexpr (sizeof(T) == 4) {
+      const u32x4_t lo = reinterpret_cast<const Packed16<4>*>(p)->v, hi = reinterpret_cast<const Packed16<4>*>(p + 4)->v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { v[e] = __uint_as_float(lo[e]); v[4 + e] = __uint_as_float(hi[e]); }
+    } else {
+      const u32x4_t x = reinterpret_cast<const Packed16<2>*>(p)->v;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = __uint_as_float((e & 1) != 0 ? x[e / 2] & 0xFFFF0000u : x[e / 2] << 16);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < n ? value(p[e]) : 0.0f;
+  }
+}
+template <typename T> __device__ __forceinline__ void update8(const OrthMatrices& p, int g, int row, int c, int n, bool stepped, float (&u)[8]) {
+  load8(reinterpret_cast<const T*>(p.g) + g * p.g_matrix + row * p.g_row + c, n, u);
+  if (p.m == nullptr) return;
+  float* at = p.m + g * p.m_matrix + row * p.m_row + c;
+  float m[8];
+  load8(at, n, m);
+  if (!stepped) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m[e] = fmaf(p.mu, m[e], u[e]);
+    if (n >= 8) {
+      reinterpret_cast<Packed16<4>*>(at)->v = (u32x4_t){__float_as_uint(m[0]), __float_as_uint(m[1]), __float_as_uint(m[2]), __float_as_uint(m[3])};
+      reinterpret_cast<Packed16<4>*>(at + 4)->v = (u32x4_t){__float_as_uint(m[4]), __float_as_uint(m[5]), __float_as_uint(m[6]), __float_as_uint(m[7])};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < n) at[e] = m[e];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) u[e] = fmaf(p.m_part, m[e], p.g_part * u[e]);
+}
+
+// Sums of squares in 64 bits (an fp32 sum overflows from elements of 1e19 on), a share of the matrix per workgroup.
 template <typename T> __global__ void __launch_bounds__(kThreads) orth_squares_kernel(OrthMatrices p, double* parts) {
   const int g = blockIdx.y;
-  const uint32_t total = (uint32_t)p.rows * (uint32_t)p.cols;
+  const uint32_t per_row = (uint32_t)(p.cols + 7) / 8, total = (uint32_t)p.rows * per_row;
   double s = 0.0;
-  for (uint32_t i = blockIdx.x * kThreads + threadIdx.x; i < total; i += kNormParts * kThreads) {
-    const uint32_t row = i / (uint32_t)p.cols;
-    const double u = (double)update_at<T>(p, g, (int)row, (int)(i - row * (uint32_t)p.cols), false);
-    s = fma(u, u, s);
+#pragma unroll 2
+  for (uint32_t i = blockIdx.x * kThreads + threadIdx.x; i < total; i += gridDim.x * kThreads) {
+    const uint32_t row = i / per_row;
+    const int c = (int)(i - row * per_row) * 8;
+    float u[8];
+    update8<T>(p, g, (int)row, c, p.cols - c, false, u);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = fma((double)u[e], (double)u[e], s);
   }
   s = wave_sum(s);
   __shared__ double sums[kThreads / kWave];
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
   __syncthreads();
-  if (threadIdx.x == 0) parts[g * kNormParts + blockIdx.x] = ((sums[0] + sums[1]) + sums[2]) + sums[3];
+  if (threadIdx.x == 0) parts[g * gridDim.x + blockIdx.x] = ((sums[0] + sums[1]) + sums[2]) + sums[3];
 }
 
-// X_0 = U / (|U| + eps) times kHalfScale as halves, a tile of 64 x 64 elements per workgroup, along the rows and as the transpose.
-// direct / turned: the buffers whose rows are U's rows / columns.
-struct LoadBuffers {
-  uint16_t* direct; uint16_t* direct_lo; int64_t direct_gs; int ld_direct;
-  uint16_t* turned; uint16_t* turned_lo; int64_t turned_gs; int ld_turned;
-};
-template <typename T, bool SPLIT>
-__global__ void __launch_bounds__(kThreads) orth_load_kernel(OrthMatrices p, const double* parts, LoadBuffers b) {
+// X_0 = U / (|U| + eps) times kHalfScale as halves, a tile of 64 x 64 elements per workgroup.  TURNED: X is the transpose of U, by way of LDS.
+template <typename T, bool TURNED>
+__global__ void __launch_bounds__(kThreads) orth_load_kernel(OrthMatrices p, const double* parts, int n_parts, OrthHalves h) {
+  constexpr bool SPLIT = sizeof(T) == 4;
   __shared__ float tile[64][65];
-  const int g = blockIdx.z, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
-  const double scale = norm_scale(wave_sum(parts[g * kNormParts + lane]), p.eps) * (double)kHalfScale;
-#pragma unroll 4
-  for (int i = 0; i < 16; ++i) {
-    const int r = r0 + 4 * i + wave, c = c0 + lane;
-    float v = 0.0f;
-    if (r < p.rows && c < p.cols) v = (float)((double)update_at<T>(p, g, r, c, true) * scale);
-    tile[4 * i + wave][lane] = v;
-  }
-  __syncthreads();
-  auto write = [&](uint16_t* hi, uint16_t* lo, int64_t gs, int ld, int row, int col, int n_rows, float v) __attribute__((always_inline)) {
-    if (row >= n_rows) return;
-    const int h = SPLIT ? (col >> 5) * 64 + (col & 31) : col;
-    if (h >= ld) return;
-    const _Float16 lead = (_Float16)v;
-    uint16_t* at = hi + g * gs + (int64_t)row * ld + h;
-    *at = __builtin_bit_cast(uint16_t, lead);
-    const uint16_t rest = __builtin_bit_cast(uint16_t, (_Float16)(v - (float)lead));
-    if (SPLIT) at[32] = rest;
-    else if (lo != nullptr) lo[g * gs + (int64_t)row * ld + h] = rest;
+  const int g = blockIdx.z, r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
+  double squares = 0.0;
+  for (int i = threadIdx.x & 63; i < n_parts; i += kWave) squares += parts[g * n_parts + i];
+  const double scale = norm_scale(wave_sum(squares), p.eps) * (double)kHalfScale;
+  const int lane_row = threadIdx.x >> 3, lane_col = (threadIdx.x & 7) * 8;
+  const int rows = TURNED ? p.cols : p.rows, cols = TURNED ? p.rows : p.cols;           // of X
+  auto write = [&](int row, int col, const float (&v)[8]) __attribute__((always_inline)) {
+    const int hc = SPLIT ? (col >> 4) * 32 + (col & 15) : col;
+    if (row >= half_rows(rows) || hc >= h.ld_x) return;
+    u32x4_t hi, lo;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const _Float16 a = (_Float16)v[2 * e], b = (_Float16)v[2 * e + 1];
+      const _Float16 ra = (_Float16)(v[2 * e] - (float)a), rb = (_Float16)(v[2 * e + 1] - (float)b);
+      hi[e] = (uint32_t)__builtin_bit_cast(uint16_t, a) | (uint32_t)__builtin_bit_cast(uint16_t, b) << 16;
+      lo[e] = (uint32_t)__builtin_bit_cast(uint16_t, ra) | (uint32_t)__builtin_bit_cast(uint16_t, rb) << 16;
+    }
+    const int64_t at = g * h.x_gs + (int64_t)row * h.ld_x + hc;
+    *reinterpret_cast<u32x4_t*>(h.x + at) = hi;
+    if (SPLIT) *reinterpret_cast<u32x4_t*>(h.x + at + 16) = lo;
+    else *reinterpret_cast<u32x4_t*>(h.x_lo + at) = lo;
+    if (row >= rows) {
+      const u32x4_t zero = {0, 0, 0, 0};
+      *reinterpret_cast<u32x4_t*>(h.spare + at) = zero;
+      if (SPLIT) *reinterpret_cast<u32x4_t*>(h.spare + at + 16) = zero;
+    }
   };
-#pragma unroll 4
-  for (int i = 0; i < 16; ++i) {
-    const int k = 4 * i + wave;
-    write(b.direct, b.direct_lo, b.direct_gs, b.ld_direct, r0 + k, c0 + lane, p.rows, tile[k][lane]);
-    write(b.turned, b.turned_lo, b.turned_gs, b.ld_turned, c0 + k, r0 + lane, p.cols, tile[lane][k]);
+#pragma unroll
+  for (int i = 0; i < 64; i += 32) {
+    const int r = r0 + i + lane_row, c = c0 + lane_col;
+    float u[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    if (r < p.rows && c < p.cols) update8<T>(p, g, r, c, p.cols - c, true, u);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e] = c + e < p.cols ? (float)((double)u[e] * scale) : 0.0f;
+    if (r >= p.rows) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[e] = 0.0f;
+    }
+    if (TURNED) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) tile[i + lane_row][lane_col + e] = u[e];
+    } else {
+      write(r, c, u);
+    }
+  }
+  if (!TURNED) return;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 64; i += 32) {
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = tile[lane_col + e][i + lane_row];
+    write(c0 + i + lane_row, r0 + lane_col, v);
   }
 }
 
@@ -273,23 +340,22 @@ __global__ void __launch_bounds__(kThreads) orth_short_kernel(OrthMatrices p, Sh
 }  // namespace
 
 hipError_t launch_orth_squares(const OrthMatrices& p, double* parts, hipStream_t s) {
-  const dim3 grid(kNormParts, (unsigned)p.count);
+  const dim3 grid((unsigned)norm_parts(p.rows, p.cols), (unsigned)p.count);
   if (p.bf16) hipLaunchKernelGGL(orth_squares_kernel<uint16_t>, grid, dim3(kThreads), 0, s, p, parts);
   else hipLaunchKernelGGL(orth_squares_kernel<float>, grid, dim3(kThreads), 0, s, p, parts);
   return hipGetLastError();
 }
 
-hipError_t launch_orth_load(const OrthMatrices& p, const double* parts, const OrthHalves& h, bool split, hipStream_t s) {
-  LoadBuffers b;
-  if (p.rows <= p.cols) b = LoadBuffers{h.x, h.x_lo, h.x_gs, h.ld_x, h.t, nullptr, h.t_gs, h.ld_t};
-  else b = LoadBuffers{h.t, nullptr, h.t_gs, h.ld_t, h.x, h.x_lo, h.x_gs, h.ld_x};
+hipError_t launch_orth_load(const OrthMatrices& p, const double* parts, const OrthHalves& h, hipStream_t s) {
   const dim3 grid((unsigned)(p.cols + 63) / 64, (unsigned)(p.rows + 63) / 64, (unsigned)p.count);
+  const int n = norm_parts(p.rows, p.cols);
+  const bool turned = p.rows > p.cols;
   if (p.bf16) {
-    if (split) hipLaunchKernelGGL((orth_load_kernel<uint16_t, true>), grid, dim3(kThreads), 0, s, p, parts, b);
-    else hipLaunchKernelGGL((orth_load_kernel<uint16_t, false>), grid, dim3(kThreads), 0, s, p, parts, b);
+    if (turned) hipLaunchKernelGGL((orth_load_kernel<uint16_t, true>), grid, dim3(kThreads), 0, s, p, parts, n, h);
+    else hipLaunchKernelGGL((orth_load_kernel<uint16_t, false>), grid, dim3(kThreads), 0, s, p, parts, n, h);
   } else {
-    if (split) hipLaunchKernelGGL((orth_load_kernel<float, true>), grid, dim3(kThreads), 0, s, p, parts, b);
-    else hipLaunchKernelGGL((orth_load_kernel<float, false>), grid, dim3(kThreads), 0, s, p, parts, b);
+    if (turned) hipLaunchKernelGGL((orth_load_kernel<float, true>), grid, dim3(kThreads), 0, s, p, parts, n, h);
+    else hipLaunchKernelGGL((orth_load_kernel<float, false>), grid, dim3(kThreads), 0, s, p, parts, n, h);
   }
   return hipGetLastError();
 }

@@ -1,6 +1,6 @@
-// Products between the matrices of the Newton-Schulz steps: C = A B^T, both operands' rows contiguous along the contraction (X X^T,
-// A A, and B X with X^T kept beside X), in half precision on the matrix cores with fp32 sums.  Symmetric results compute the tiles on and below the
-// diagonal and write the others as transposes.  Split operands hold a second half per entry (22 bits); a tile then takes three products,
+// Products between the matrices of the Newton-Schulz steps, in half precision on the matrix cores with fp32 sums: X X^T and A A, whose
+// operands' rows are contiguous along the contraction, and B X, whose second operand is read out of LDS as its transpose.  Symmetric results
+// compute the tiles on and below the diagonal and write the others as transposes.  Split operands hold a second half per entry (22 bits); a tile then takes three products,
 // lead x lead and the two crossed ones, of the same fragments.
 #include <atomic>
 #include <type_traits>
@@ -17,8 +17,6 @@ typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 template <int ES> struct __attribute__((packed, aligned(ES))) Packed16 { u32x4_t v; };
 
-constexpr int kRowBytes = 128;             // of an operand row in a tile
-
 __device__ __forceinline__ float half_value(uint16_t h) { return (float)__builtin_bit_cast(_Float16, h); }
 __device__ __forceinline__ uint16_t half_bits(float f) { return __builtin_bit_cast(uint16_t, (_Float16)f); }
 // leading halves and remainders of eight values
@@ -32,22 +30,36 @@ __device__ __forceinline__ void split8(const float* v, u32x4_t* hi, u32x4_t* lo)
 }
 __device__ __forceinline__ float half_at(u32x4_t v, int e) { return half_value((uint16_t)(v[e / 2] >> (16 * (e & 1)))); }
 
-// halves of column c of a row
-template <bool SPLIT> __device__ __forceinline__ int half_col(int c) { return SPLIT ? (c >> 5) * 64 + (c & 31) : c; }
-
-// Place of a row's 16-byte chunk q in its 128 bytes
-__device__ __forceinline__ int chunk_place(int r, int q) { return q ^ ((r >> 1) & 7); }
-// Requests of a tile of ROWS operand rows by NW wavefronts.
-template <int ROWS, int NW> struct TileRequests {
-  static constexpr int NPT = ROWS * kRowBytes / 1024 / NW;
-  static_assert(ROWS * kRowBytes % (1024 * NW) == 0, "a tile splits evenly over the wavefronts");
+// halves of column c of a row; remainders of split columns stand kGroup halves behind
+constexpr int kGroup = 16;
+template <bool SPLIT> __device__ __forceinline__ int half_col(int c) { return SPLIT ? (c >> 4) * 32 + (c & 15) : c; }
+// A tile of an operand: ROWS rows (or columns) of the product by RB bytes' depth each, requested by NW wavefronts.  LDS has 64 banks, and
+// the 256 bytes that 16 lanes read at a time have to lie on different ones: a tile cannot be padded on its way, so pieces of a row are exchanged.
+//   rows contiguous along the contraction: [ROWS][RB], 16-byte chunk q of row r at chunk_place(r, q)
+//   TRANS: [depth][ROWS halves, or pairs of them], 32-byte unit u of contraction row c at u ^ unit_xor(c), for reads that transpose
+template <int RB> __device__ __forceinline__ int chunk_place(int r, int q) { return RB == 128 ? q ^ ((r >> 1) & 7) : q ^ ((r >> 2) & 3); }
+template <int ROW, bool SPLIT> __device__ __forceinline__ int unit_xor(int c) {      // ROW: bytes of a contraction row
+  static_assert(ROW % 256 == 0 || (ROW == 128 && !SPLIT), "rows of whole bank sets, or two to a set");
+  return SPLIT ? (c & 1) | (c & 2) << 1 : ROW == 128 ? c & 2 : (c & 3) << 1;
+}
+template <int ROWS, int RB, int NW, bool SPLIT, bool TRANS> struct TileRequests {
+  static constexpr int NPT = ROWS * RB / 1024 / NW;
+  static_assert(ROWS * RB % (1024 * NW) == 0, "a tile splits evenly over the wavefronts");
   uint32_t off[NPT];
-  // rows past the operand's n are copies of its last one, never stored
+  // n: rows (TRANS: halves of a row) of the operand from the tile's first on; what lies past them is a copy of the last, never stored
   __device__ __forceinline__ void set(int ld, int n, int wave, int lane) {
 #pragma unroll
     for (int q = 0; q < NPT; ++q) {
-      const int chunk = (q * NW + wave) * 64 + lane, lr = chunk >> 3;
-      off[q] = (uint32_t)min(lr, n - 1) * (uint32_t)ld * 2u + (uint32_t)chunk_place(lr, chunk & 7) * 16u;
+      const int chunk = (q * NW + wave) * 64 + lane;
+      if constexpr (TRANS) {
+        constexpr int ROW = ROWS * (SPLIT ? 4 : 2), CH = ROW / 16;
+        const int c = chunk / CH, pos = chunk % CH, from = ((((pos >> 1) ^ unit_xor<ROW, SPLIT>(c)) << 1) | (pos & 1)) * 8;
+        off[q] = ((uint32_t)c * (uint32_t)ld + (uint32_t)min(from, n - 8)) * 2u;
+      } else {
+        constexpr int CH = RB / 16;
+        const int r = chunk / CH;
+        off[q] = (uint32_t)min(r, n - 1) * (uint32_t)ld * 2u + (uint32_t)chunk_place<RB>(r, chunk % CH) * 16u;
+      }
     }
   }
   __device__ __forceinline__ void request(const uint16_t* base, uint32_t lds_tile, int q, int wave) const {
@@ -60,10 +72,41 @@ template <int N> __device__ __forceinline__ void wait_requests() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(N) : "memory");
 }
 
-__device__ __forceinline__ f16x8_t fragment(const unsigned char* tile, int block, int chunk, int lane) {
-  const int r = lane & 31;
-  return __builtin_bit_cast(f16x8_t, *reinterpret_cast<const u32x4_t*>(tile + (block * 32 + r) * kRowBytes + (chunk_place(r, chunk) << 4)));
-}
+// MFMA operands of 32-row blocks: lane (r = lane % 32, kb = lane / 32) holds contraction elements 8 kb .. 8 kb + 7 of row r.  Where a lane
+// reads depends on the slice and the half through an exchange, on the block through a constant: COUNT places are kept per lane.
+template <int RB, bool SPLIT> struct RowFragments {
+  static constexpr int PARTS = SPLIT ? 2 : 1, KK = RB / 32 / PARTS, COUNT = KK * PARTS;
+  int at[COUNT];
+  __device__ __forceinline__ void set(int first_block, int lane) {
+#pragma unroll
+    for (int x = 0; x < COUNT; ++x) at[x] = (first_block * 32 + (lane & 31)) * RB + (chunk_place<RB>(lane & 31, 2 * x + (lane >> 5)) << 4);
+  }
+  __device__ __forceinline__ f16x8_t read(const unsigned char* tile, int block, int kk, int h) const {
+    return __builtin_bit_cast(f16x8_t, *reinterpret_cast<const u32x4_t*>(tile + at[kk * PARTS + h] + block * 32 * RB));
+  }
+};
+// The same out of a TRANS tile, by two ds_read_b64_tr_b16: of every 16 lanes, lane r gives the address of four halves M[r], and lane i gets
+// M[4 j + i / 4][i % 4], j = 0..3.  The exchange takes in the lowest bits of the block.
+template <int ROWS, bool SPLIT> struct ColumnFragments {
+  static constexpr int ROW = ROWS * (SPLIT ? 4 : 2), COUNT = 4;
+  int at[COUNT];
+  __device__ __forceinline__ void set(int first_block, int lane) {
+    const int g = lane >> 4, r = lane & 15, c = 8 * (g >> 1) + (r >> 2);
+#pragma unroll
+    for (int x = 0; x < COUNT; ++x) {      // split: block x / 2, half x % 2; otherwise block x
+      const int unit = SPLIT ? 4 * (first_block + x / 2) + 2 * (g & 1) + x % 2 : 2 * (first_block + x) + (g & 1);
+      at[x] = c * ROW + (unit ^ unit_xor<ROW, SPLIT>(r >> 2)) * 32 + 8 * (r & 3);
+    }
+  }
+  __device__ __forceinline__ f16x8_t read(const unsigned char* tile, int block, int kk, int h) const {
+    typedef __attribute__((__vector_size__(4 * sizeof(__fp16)))) __fp16 f16x4_t;
+    typedef __attribute__((address_space(3))) f16x4_t* lds_f16x4_ptr;
+    const unsigned char* p = tile + (SPLIT ? at[block % 2 * 2 + h] + block / 2 * 256 : at[block % 4] + block / 4 * 256) + kk * 16 * ROW;
+    const f16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_f16x4_ptr)(p));
+    const f16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_f16x4_ptr)(p + 4 * ROW));
+    return __builtin_bit_cast(f16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
 
 // Eight consecutive values of the result at row i, columns j.. of the caller's matrix, n of them inside it.
 template <typename T> __device__ __forceinline__ void user_store(const OrthMatrices& u, int64_t at_out, int n, const float* v) {
@@ -114,21 +157,23 @@ template <typename T> __device__ __forceinline__ void user_store(const OrthMatri
   }
 }
 
-template <int BM, int BN, int S> constexpr int square_lds_bytes(int wm, int wn) {
-  const int stages = S * (BM + BN) * kRowBytes, strips = wm * wn * 32 * (BN / wn + 2) * 4;
+constexpr int strip_pitch(int columns) { return columns + 8; }     // the four rows between a register's two halves lie 32 banks apart
+template <int BM, int BN, int S, int RB> constexpr int square_lds_bytes(int wm, int wn) {
+  const int stages = S * (BM + BN) * RB, strips = wm * wn * 32 * strip_pitch(BN / wn) * 4;
   return stages > strips ? stages : strips;
 }
 
-// WM x WN wavefronts, S tiles of 128 bytes' depth in LDS.
-template <int BM, int BN, int WM, int WN, int S, bool SPLIT, int EPI>
-__global__ void __launch_bounds__(64 * WM * WN) square_kernel(const SquareArgs p) {
-  constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, KK = SPLIT ? 2 : 4, PARTS = SPLIT ? 2 : 1;
-  constexpr bool SYMMETRIC = EPI == SQ_GRAM || EPI == SQ_POLY;
-  constexpr int STAGE = (BM + BN) * kRowBytes;
-  using ReqA = TileRequests<BM, NW>;
-  using ReqB = TileRequests<BN, NW>;
-  constexpr int PER = ReqA::NPT + ReqB::NPT;
-  static_assert(!SYMMETRIC || BM == BN, "tiles of a symmetric result");
+// WM x WN wavefronts, S tiles of RB bytes' depth in LDS.
+template <int BM, int BN, int WM, int WN, int S, int RB, bool SPLIT, int EPI>
+__global__ void __launch_bounds__(64 * WM * WN, 2) square_kernel(const SquareArgs p) {
+  constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, PARTS = SPLIT ? 2 : 1, KK = RB / 32 / PARTS;
+  constexpr bool SYMMETRIC = EPI == SQ_GRAM || EPI == SQ_POLY, TRANS = !SYMMETRIC;
+  constexpr int STAGE = (BM + BN) * RB;
+  using User = std::conditional_t<SPLIT, float, uint16_t>;
+  using ReqA = TileRequests<BM, RB, NW, SPLIT, false>;
+  using ReqB = TileRequests<BN, RB, NW, SPLIT, TRANS>;
+  constexpr int PER = ReqA::NPT + ReqB::NPT, R = BN / BM;
+  static_assert(!SYMMETRIC || BN % BM == 0, "tiles of a symmetric result");
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
@@ -138,11 +183,16 @@ __global__ void __launch_bounds__(64 * WM * WN) square_kernel(const SquareArgs p
   const int idx = xcd * (total >> 3) + min(xcd, total & 7) + (blockIdx.x >> 3);
   const int g = idx / p.tiles, in = idx - g * p.tiles;
   int ti, tj;
-  if (SYMMETRIC) {                         // row of the triangle
-    ti = (int)((sqrtf(8.0f * (float)in + 1.0f) - 1.0f) * 0.5f);
-    while (ti * (ti + 1) / 2 > in) --ti;
-    while ((ti + 1) * (ti + 2) / 2 <= in) ++ti;
-    tj = in - ti * (ti + 1) / 2;
+  bool mirrored = false;
+  if (SYMMETRIC) {                         // squares of BN x BN on and below the diagonal, R tiles each
+    const int sq = in / R;
+    ti = (int)((sqrtf(8.0f * (float)sq + 1.0f) - 1.0f) * 0.5f);
+    while (ti * (ti + 1) / 2 > sq) --ti;
+    while ((ti + 1) * (ti + 2) / 2 <= sq) ++ti;
+    tj = sq - ti * (ti + 1) / 2;
+    mirrored = ti != tj;
+    ti = ti * R + in % R;
+    if (ti * BM >= p.M) return;
   } else {
     ti = in / p.tiles_n;
     tj = in - ti * p.tiles_n;
@@ -151,28 +201,32 @@ __global__ void __launch_bounds__(64 * WM * WN) square_kernel(const SquareArgs p
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
   const uint16_t* a = p.a + g * p.a_gs + (int64_t)m0 * p.lda;
-  const uint16_t* b = p.b + g * p.b_gs + (int64_t)n0 * p.ldb;
+  const uint16_t* b = p.b + g * p.b_gs + (TRANS ? (int64_t)half_col<SPLIT>(n0) : (int64_t)n0 * p.ldb);
+  const int64_t b_step = TRANS ? (int64_t)(RB / 2 / PARTS) * p.ldb : RB / 2;
   ReqA ra;
   ReqB rb;
   ra.set(p.lda, p.M - m0, wave, lane);
-  rb.set(p.ldb, p.N - n0, wave, lane);
-  const int n_k = p.groups;
+  rb.set(p.ldb, TRANS ? p.ldb - half_col<SPLIT>(n0) : p.N - n0, wave, lane);
+  const int n_k = p.lda * 2 / RB;
   auto request = [&](int t, int first, int last) __attribute__((always_inline)) {
     const uint32_t stage = lds0 + (uint32_t)(t % S) * STAGE;
 #pragma unroll
     for (int q = first; q < last; ++q) {
-      if (q < ReqA::NPT) ra.request(a + t * 64, stage, q, wave);
-      else rb.request(b + t * 64, stage + BM * kRowBytes, q - ReqA::NPT, wave);
+      if (q < ReqA::NPT) ra.request(a + t * (RB / 2), stage, q, wave);
+      else rb.request(b + t * b_step, stage + BM * RB, q - ReqA::NPT, wave);
     }
   };
   f16x8_t fa[2][PARTS][TM], fb[2][PARTS][TN];
   constexpr int READS = PARTS * (TM + TN);
+  RowFragments<RB, SPLIT> rows;
+  std::conditional_t<TRANS, ColumnFragments<BN, SPLIT>, RowFragments<RB, SPLIT>> cols;
+  rows.set(wm * TM, lane);
+  cols.set(wn * TN, lane);
   // fragment q of slice kk
-  auto load = [&](int t, int kk, int set, int q) __attribute__((always_inline)) {
-    const unsigned char* ta = smem + (t % S) * STAGE;
-    const int h = q / (TM + TN), x = q % (TM + TN), chunk = 4 * h + 2 * kk + (lane >> 5);
-    if (x < TM) fa[set][h][x] = fragment(ta, wm * TM + x, chunk, lane);
-    else fb[set][h][x - TM] = fragment(ta + BM * kRowBytes, wn * TN + x - TM, chunk, lane);
+  auto load = [&](const unsigned char* tile, int kk, int set, int q) __attribute__((always_inline)) {
+    const int h = q / (TM + TN), x = q % (TM + TN);
+    if (x < TM) fa[set][h][x] = rows.read(tile, x, kk, h);
+    else fb[set][h][x - TM] = cols.read(tile + BM * RB, x - TM, kk, h);
   };
   f32x16_t acc[TM][TN];
 #pragma unroll
@@ -183,7 +237,7 @@ __global__ void __launch_bounds__(64 * WM * WN) square_kernel(const SquareArgs p
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
 
   // Tile t + 1 is met before the last slice of tile t is multiplied; from there on every fragment of tile t has been read, and its stage
-  // takes tile t + S, half of it behind that slice and half behind the next.  Each row of a slice's products is followed by its share of
+  // takes tile t + S.  Each row of a slice's products is followed by its share of
   // the next slice's fragments and of the requests, so that neither waits in a burst of its own (a request takes 16 cycles of the compute
   // unit's one path to its cache).
 #pragma unroll
@@ -192,12 +246,15 @@ __global__ void __launch_bounds__(64 * WM * WN) square_kernel(const SquareArgs p
   if (n_k >= S) wait_requests<(S - 1) * PER>(); else wait_requests<0>();
   asm volatile("s_barrier" ::: "memory");
 #pragma unroll
-  for (int q = 0; q < READS; ++q) load(0, 0, 0, q);
-  auto step = [&](int t, auto whole_) __attribute__((always_inline)) {
+  for (int q = 0; q < READS; ++q) load(smem, 0, 0, q);
+  // set0: the fragments' set of the tile's first slice
+  auto step = [&](int t, auto set0_, auto whole_) __attribute__((always_inline)) {
     constexpr bool WHOLE = decltype(whole_)::value;        // every tile that the step asks for exists
+    const unsigned char* here = smem + (t % S) * STAGE;
+    const unsigned char* next = smem + ((t + 1) % S) * STAGE;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
-      const int set = kk & 1;
+      const int set = (decltype(set0_)::value + kk) & 1;
       const bool last = kk == KK - 1;
       if (last) {
         if (WHOLE || t + S - 1 < n_k) wait_requests<(S - 2) * PER>(); else wait_requests<0>();
@@ -207,7 +264,7 @@ __global__ void __launch_bounds__(64 * WM * WN) square_kernel(const SquareArgs p
       for (int i = 0; i < TM; ++i) {
         if (!last || WHOLE || t + 1 < n_k) {
 #pragma unroll
-          for (int q = i * READS / TM; q < (i + 1) * READS / TM; ++q) load(last ? t + 1 : t, last ? 0 : kk + 1, set ^ 1, q);
+          for (int q = i * READS / TM; q < (i + 1) * READS / TM; ++q) load(last ? next : here, last ? 0 : kk + 1, set ^ 1, q);
         }
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
@@ -217,23 +274,26 @@ __global__ void __launch_bounds__(64 * WM * WN) square_kernel(const SquareArgs p
             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[set][1][i], fb[set][0][j], acc[i][j], 0, 0, 0);
           }
         }
-        constexpr int HALF = PER / 2;
-        if (last && (WHOLE || t + S < n_k)) request(t + S, i * HALF / TM, (i + 1) * HALF / TM);
-        if (kk == 0 && t > 0 && (WHOLE || t - 1 + S < n_k)) request(t - 1 + S, HALF + i * (PER - HALF) / TM, HALF + (i + 1) * (PER - HALF) / TM);
+        if (last && (WHOLE || t + S < n_k)) request(t + S, i * PER / TM, (i + 1) * PER / TM);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
   };
+  using Set0 = std::integral_constant<int, 0>;
+  using Set1 = std::integral_constant<int, KK & 1>;        // of odd tiles
   int t = 0;
-  if (n_k > S) {
-    step(0, std::true_type{});
-    for (t = 1; t + S < n_k; ++t) step(t, std::true_type{});
+  for (; t + S + 1 < n_k; t += 2) {
+    step(t, Set0{}, std::true_type{});
+    step(t + 1, Set1{}, std::true_type{});
   }
-  for (; t < n_k; ++t) step(t, std::false_type{});
+  for (; t < n_k; t += 2) {
+    step(t, Set0{}, std::false_type{});
+    if (t + 1 < n_k) step(t + 1, Set1{}, std::false_type{});
+  }
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 
   // Epilogue: a wavefront passes strips of 32 rows through LDS, first along the rows and then, as transposes, along the columns.
-  constexpr int W = BN / WN, P = W + 2, VPR = W / 8, RPP = 64 / VPR;      // strip columns, pitch, 8-value vectors of a row, rows per pass
+  constexpr int W = BN / WN, P = strip_pitch(W), VPR = W / 8, RPP = 64 / VPR;      // strip columns, pitch, 8-value vectors of a row, rows per pass
   float* strip = reinterpret_cast<float*>(smem) + wave * 32 * P;
   const int c0 = n0 + wn * W;
 #pragma unroll
@@ -262,7 +322,7 @@ __global__ void __launch_bounds__(64 * WM * WN) square_kernel(const SquareArgs p
         if (inside) {
           const int64_t o = g * p.lin_gs + (int64_t)r * p.ld_lin + hc;
           hi = *reinterpret_cast<const u32x4_t*>(p.lin + o);
-          if (SPLIT) lo = *reinterpret_cast<const u32x4_t*>(p.lin + o + 32);
+          if (SPLIT) lo = *reinterpret_cast<const u32x4_t*>(p.lin + o + kGroup);
           else if (EPI != SQ_POLY) lo = *reinterpret_cast<const u32x4_t*>(p.lin_lo + o);
         }
 #pragma unroll
@@ -277,22 +337,21 @@ __global__ void __launch_bounds__(64 * WM * WN) square_kernel(const SquareArgs p
       if constexpr (EPI == SQ_LAST) {
         if (!p.transposed && inside) {
           const int64_t o = g * p.user.out_matrix + r * p.user.out_row + c;
-          if (p.user.bf16) user_store<uint16_t>(p.user, o, p.N - c, v);
-          else user_store<float>(p.user, o, p.N - c, v);
+          user_store<User>(p.user, o, p.N - c, v);
         }
       } else if (r < p.M && hc < p.ldo) {
         u32x4_t hi, lo;
         split8(v, &hi, &lo);
         const int64_t o = g * p.out_gs + (int64_t)r * p.ldo + hc;
         *reinterpret_cast<u32x4_t*>(p.out + o) = hi;
-        if (SPLIT) *reinterpret_cast<u32x4_t*>(p.out + o + 32) = lo;
+        if (SPLIT) *reinterpret_cast<u32x4_t*>(p.out + o + kGroup) = lo;
         else if (EPI == SQ_NEXT) *reinterpret_cast<u32x4_t*>(p.out_lo + o) = lo;
       }
 #pragma unroll
       for (int e = 0; e < 8; e += 2) *reinterpret_cast<f32x2_t*>(at + e) = (f32x2_t){v[e], v[e + 1]};
     }
     __builtin_amdgcn_wave_barrier();
-    if (SYMMETRIC ? ti != tj : EPI == SQ_NEXT || p.transposed) {
+    if (SYMMETRIC ? mirrored : EPI == SQ_LAST && p.transposed) {
 #pragma unroll(EPI == SQ_LAST ? 1 : W / 16)
       for (int q = 0; q < W / 16; ++q) {
         const int lc = q * 16 + lane % 16, lr = lane / 16 * 8, c = c0 + lc, r = r0 + lr;
@@ -303,8 +362,7 @@ __global__ void __launch_bounds__(64 * WM * WN) square_kernel(const SquareArgs p
         if constexpr (EPI == SQ_LAST) {
           if (r < p.M) {
             const int64_t o = g * p.user.out_matrix + c * p.user.out_row + r;
-            if (p.user.bf16) user_store<uint16_t>(p.user, o, p.M - r, v);
-            else user_store<float>(p.user, o, p.M - r, v);
+            user_store<User>(p.user, o, p.M - r, v);
           }
         } else {
           const int hr = half_col<SPLIT>(r);
@@ -313,7 +371,7 @@ __global__ void __launch_bounds__(64 * WM * WN) square_kernel(const SquareArgs p
             split8(v, &hi, &lo);
             const int64_t o = g * p.t_gs + (int64_t)c * p.ldt + hr;
             *reinterpret_cast<u32x4_t*>(p.out_t + o) = hi;
-            if (SPLIT) *reinterpret_cast<u32x4_t*>(p.out_t + o + 32) = lo;
+            if (SPLIT) *reinterpret_cast<u32x4_t*>(p.out_t + o + kGroup) = lo;
           }
         }
       }
@@ -322,10 +380,10 @@ __global__ void __launch_bounds__(64 * WM * WN) square_kernel(const SquareArgs p
   }
 }
 
-template <int BM, int BN, int WM, int WN, int S, bool SPLIT, int EPI> hipError_t launch_as(SquareArgs p, hipStream_t s) {
-  constexpr int kLds = square_lds_bytes<BM, BN, S>(WM, WN);
+template <int BM, int BN, int WM, int WN, int S, int RB, bool SPLIT, int EPI> hipError_t launch_as(SquareArgs p, hipStream_t s) {
+  constexpr int kLds = square_lds_bytes<BM, BN, S, RB>(WM, WN);
   static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
-  auto kernel = square_kernel<BM, BN, WM, WN, S, SPLIT, EPI>;
+  auto kernel = square_kernel<BM, BN, WM, WN, S, RB, SPLIT, EPI>;
   // the tiles can exceed the 64 KB default; setting the limit twice is harmless
   static std::atomic<bool> configured{false};
   if (!configured.load(std::memory_order_acquire)) {
@@ -333,22 +391,22 @@ template <int BM, int BN, int WM, int WN, int S, bool SPLIT, int EPI> hipError_t
     if (e != hipSuccess) return e;
     configured.store(true, std::memory_order_release);
   }
-  p.tiles_m = (p.M + BM - 1) / BM;
+  const int tiles_m = (p.M + BM - 1) / BM;
   p.tiles_n = (p.N + BN - 1) / BN;
-  p.tiles = EPI == SQ_GRAM || EPI == SQ_POLY ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
+  p.tiles = EPI == SQ_GRAM || EPI == SQ_POLY ? p.tiles_n * (p.tiles_n + 1) / 2 * (BN / BM) : tiles_m * p.tiles_n;
   hipLaunchKernelGGL(kernel, dim3((unsigned)p.tiles * (unsigned)p.count), dim3(64 * WM * WN), kLds, s, p);
   return hipGetLastError();
 }
-template <int BM, int BN, int WM, int WN, int S> hipError_t launch_tile(const SquareArgs& p, int epi, bool split, hipStream_t s) {
+template <int BM, int BN, int WM, int WN, int S, int RB> hipError_t launch_tile(const SquareArgs& p, int epi, bool split, hipStream_t s) {
   switch (epi * 2 + (split ? 1 : 0)) {
-    case 0: return launch_as<BM, BN, WM, WN, S, false, SQ_GRAM>(p, s);
-    case 1: return launch_as<BM, BN, WM, WN, S, true, SQ_GRAM>(p, s);
-    case 2: return launch_as<BM, BN, WM, WN, S, false, SQ_POLY>(p, s);
-    case 3: return launch_as<BM, BN, WM, WN, S, true, SQ_POLY>(p, s);
-    case 4: return launch_as<BM, BN, WM, WN, S, false, SQ_NEXT>(p, s);
-    case 5: return launch_as<BM, BN, WM, WN, S, true, SQ_NEXT>(p, s);
-    case 6: return launch_as<BM, BN, WM, WN, S, false, SQ_LAST>(p, s);
-    default: return launch_as<BM, BN, WM, WN, S, true, SQ_LAST>(p, s);
+    case 0: return launch_as<BM, BN, WM, WN, S, RB, false, SQ_GRAM>(p, s);
+    case 1: return launch_as<BM, BN, WM, WN, S, RB, true, SQ_GRAM>(p, s);
+    case 2: return launch_as<BM, BN, WM, WN, S, RB, false, SQ_POLY>(p, s);
+    case 3: return launch_as<BM, BN, WM, WN, S, RB, true, SQ_POLY>(p, s);
+    case 4: return launch_as<BM, BN, WM, WN, S, RB, false, SQ_NEXT>(p, s);
+    case 5: return launch_as<BM, BN, WM, WN, S, RB, true, SQ_NEXT>(p, s);
+    case 6: return launch_as<BM, BN, WM, WN, S, RB, false, SQ_LAST>(p, s);
+    default: return launch_as<BM, BN, WM, WN, S, RB, true, SQ_LAST>(p, s);
   }
 }
 
@@ -357,15 +415,15 @@ template <int BM, int BN, int WM, int WN, int S> hipError_t launch_tile(const Sq
 hipError_t launch_square(SquareArgs p, int epi, bool split, hipStream_t s) {
   const bool symmetric = epi == SQ_GRAM || epi == SQ_POLY;
   // rounds that the 256 compute units take over the tiles, in units of a 64 x 64 tile's products
-  auto cost = [&](int b, double efficiency) {
-    const int64_t tm = (p.M + b - 1) / b, tn = (p.N + b - 1) / b;
-    const int64_t tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * p.count;
-    return (double)((tiles + 255) / 256) * (b / 64) * (b / 64) / efficiency;
+  auto cost = [&](int bm, int bn, double efficiency) {
+    const int64_t tm = (p.M + bm - 1) / bm, tn = (p.N + bn - 1) / bn;
+    const int64_t tiles = (symmetric ? tn * (tn + 1) / 2 * (bn / bm) : tm * tn) * p.count;
+    return (double)((tiles + 255) / 256) * (bm / 64) * (bn / 64) / efficiency;
   };
-  const double c256 = cost(256, 1.0), c128 = cost(128, 0.7), c64 = cost(64, 0.35);
-  if (c256 <= c128 && c256 <= c64) return launch_tile<256, 256, 2, 2, 2>(p, epi, split, s);
-  if (c128 <= c64) return launch_tile<128, 128, 2, 2, 2>(p, epi, split, s);
-  return launch_tile<64, 64, 2, 2, 4>(p, epi, split, s);
+  const double large = cost(128, 256, 1.0), middle = cost(128, 128, 0.8), small = cost(64, 64, 0.5);
+  if (!split && large <= middle && large <= small) return launch_tile<128, 256, 2, 2, 3, 64>(p, epi, split, s);
+  if (middle <= small) return launch_tile<128, 128, 2, 2, 3, 64>(p, epi, split, s);
+  return launch_tile<64, 64, 2, 2, 4, 128>(p, epi, split, s);
 }
 
 }  // namespace prsgd

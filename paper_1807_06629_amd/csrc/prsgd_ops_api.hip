@@ -2,6 +2,8 @@
 #include <math.h>
 #include <stdio.h>
 
+#include <utility>
+
 #include "prsgd_internal.h"
 #include "prsgd_ops_internal.h"
 
@@ -100,9 +102,9 @@ const char* orth_config_error(const prsgd_orth_config* c) {
 // Workspace of the products' path: halves of every matrix, then the partial sums of squares.
 struct OrthPlan {
   bool split;
-  int r, longer, ld_x, ld_t;
-  size_t x, x_lo, t, a, b, parts, total;       // byte offsets
-  int64_t x_gs, t_gs, a_gs;                    // halves per matrix
+  int r, longer, ld_x, ld_a;
+  size_t x, x_lo, a, b, parts, total;          // byte offsets
+  int64_t x_gs, a_gs;                          // halves per matrix
 };
 OrthPlan orth_plan(const prsgd_orth_config* c) {
   OrthPlan p{};
@@ -110,19 +112,17 @@ OrthPlan orth_plan(const prsgd_orth_config* c) {
   p.r = c->rows < c->cols ? c->rows : c->cols;
   p.longer = c->rows < c->cols ? c->cols : c->rows;
   p.ld_x = half_ld(p.longer, p.split);
-  p.ld_t = half_ld(p.r, p.split);
-  p.x_gs = (int64_t)p.r * p.ld_x;
-  p.t_gs = (int64_t)p.longer * p.ld_t;
-  p.a_gs = (int64_t)p.r * p.ld_t;
+  p.ld_a = half_ld(p.r, p.split);
+  p.x_gs = (int64_t)half_rows(p.r) * p.ld_x;
+  p.a_gs = (int64_t)p.r * p.ld_a;
   const size_t n = (size_t)c->count;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t v = at; at += align256(bytes); return v; };
-  p.x = take(n * p.x_gs * 2);
+  p.x = take(2 * n * p.x_gs * 2);
   p.x_lo = p.split ? 0 : take(n * p.x_gs * 2);
-  p.t = take(2 * n * p.t_gs * 2);
   p.a = take(n * p.a_gs * 2);
   p.b = take(n * p.a_gs * 2);
-  p.parts = take(n * kNormParts * sizeof(double));
+  p.parts = take(n * norm_parts(c->rows, c->cols) * sizeof(double));
   p.total = at;
   return p;
 }
@@ -137,16 +137,16 @@ hipError_t run_squares(const prsgd_orth_config* c, const OrthMatrices& m, char* 
   const OrthPlan p = orth_plan(c);
   auto halves = [&](size_t offset) { return reinterpret_cast<uint16_t*>(ws + offset); };
   double* parts = reinterpret_cast<double*>(ws + p.parts);
-  uint16_t* x = halves(p.x);
+  uint16_t* x = halves(p.x);                   // every product reads all of X while the next one is written
+  uint16_t* y = x + (size_t)c->count * p.x_gs;
   uint16_t* x_lo = p.split ? nullptr : halves(p.x_lo);
-  uint16_t* t[2] = {halves(p.t), halves(p.t) + (size_t)c->count * p.t_gs};
   uint16_t* a = halves(p.a);
   uint16_t* b = halves(p.b);
   const float inv = 1.0f / kHalfScale;
 
   hipError_t e = launch_orth_squares(m, parts, s);
   if (e != hipSuccess) return e;
-  e = launch_orth_load(m, parts, OrthHalves{x, x_lo, p.x_gs, p.ld_x, t[0], p.t_gs, p.ld_t}, p.split, s);
+  e = launch_orth_load(m, parts, OrthHalves{x, x_lo, y, p.x_gs, p.ld_x}, s);
   for (int k = 0; k < c->steps && e == hipSuccess; ++k) {
     SquareArgs q{};
     q.count = c->count;
@@ -155,41 +155,38 @@ hipError_t run_squares(const prsgd_orth_config* c, const OrthMatrices& m, char* 
     q.a_gs = q.b_gs = p.x_gs;
     q.lda = q.ldb = p.ld_x;
     q.M = q.N = p.r;
-    q.groups = p.ld_x / 64;
     q.out = q.out_t = a;
     q.out_gs = q.t_gs = p.a_gs;
-    q.ldo = q.ldt = p.ld_t;
+    q.ldo = q.ldt = p.ld_a;
     q.beta = inv;
     if ((e = launch_square(q, SQ_GRAM, p.split, s)) != hipSuccess) break;
     // B = b A + c A A
     q.a = q.b = q.lin = a;
     q.a_gs = q.b_gs = q.lin_gs = p.a_gs;
-    q.lda = q.ldb = q.ld_lin = p.ld_t;
-    q.groups = p.ld_t / 64;
+    q.lda = q.ldb = q.ld_lin = p.ld_a;
     q.out = q.out_t = b;
     q.alpha = c->b;
     q.beta = c->c * inv;
     if ((e = launch_square(q, SQ_POLY, p.split, s)) != hipSuccess) break;
     // X <- a X + B X
     q.a = b;
-    q.b = t[k & 1];
-    q.b_gs = p.t_gs;
+    q.b = x;
+    q.b_gs = p.x_gs;
+    q.ldb = p.ld_x;
     q.N = p.longer;
     q.lin = x;
     q.lin_lo = x_lo;
     q.lin_gs = p.x_gs;
     q.ld_lin = p.ld_x;
     if (k + 1 < c->steps) {
-      q.out = x;
+      q.out = y;
       q.out_lo = x_lo;
       q.out_gs = p.x_gs;
       q.ldo = p.ld_x;
-      q.out_t = t[(k + 1) & 1];
-      q.t_gs = p.t_gs;
-      q.ldt = p.ld_t;
       q.alpha = c->a;
       q.beta = inv;
       e = launch_square(q, SQ_NEXT, p.split, s);
+      std::swap(x, y);
     } else {
       q.user = m;
       q.transposed = c->rows > c->cols;

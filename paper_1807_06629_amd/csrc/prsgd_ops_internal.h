@@ -36,7 +36,9 @@ hipError_t launch_rms_norm_backward(NormArgs p, float* shares, int workers, bool
 
 constexpr int kMaxOrthSide = 32768, kMaxOrthSteps = 64;
 constexpr int kShortSide = 32;           // a side up to here goes through its Gram matrix in 64 bits
-constexpr int kNormParts = 64;           // workgroups that sum a matrix's squares
+// Workgroups that sum a matrix's squares: enough to fill the device where a matrix is large.
+constexpr int kMaxNormParts = 256;
+constexpr int norm_parts(int rows, int cols) { return (int64_t)rows * cols < (1 << 20) ? 64 : kMaxNormParts; }
 // Operands are halves of X, A and B times 2^13: entries reach 8, and what a second half holds of an entry of 2^-12 (X_0 of
 // 4096 x 4096) is a normal number or loses less than 2^-36.
 constexpr float kHalfScale = 8192.0f;
@@ -54,26 +56,27 @@ struct OrthMatrices {
   int steps;
 };
 
-// Storage of a matrix of halves [rows][ld]: rows of whole 64-half (128-byte) groups, which hold 64 columns, or (split) 32
-// columns' leading halves and then their remainders.
+// Storage of a matrix of halves [rows][ld]: rows of whole 128-byte lines.  Split (matrices of fp32): of every 16 columns the leading halves and then
+// the remainders.
 constexpr int half_ld(int cols, bool split) { return split ? (cols + 31) / 32 * 64 : (cols + 63) / 64 * 64; }
+constexpr int half_rows(int rows) { return (rows + 63) / 64 * 64; }      // of X, which products contract over: padding rows hold zeros
 
-// A square-side product of every matrix: acc = A B^T over rows of halves, then an epilogue.
+// A product of every matrix, then an epilogue: acc = A B^T for the symmetric ones, A B for the others.
 enum SquareEpilogue {
   SQ_GRAM = 0,    // out = acc (symmetric)
   SQ_POLY = 1,    // out = b lin + c acc (symmetric)
-  SQ_NEXT = 2,    // out = a lin + acc, and its transpose
+  SQ_NEXT = 2,    // out = a lin + acc
   SQ_LAST = 3,    // result = a lin + acc, into the caller's matrices
 };
 struct SquareArgs {
   const uint16_t* a; int64_t a_gs; int lda;
   const uint16_t* b; int64_t b_gs; int ldb;
-  int M, N, groups;                            // groups: 64-half groups of a row
-  const uint16_t* lin; const uint16_t* lin_lo; int64_t lin_gs; int ld_lin;     // lin_lo: remainders (unsplit operands)
+  int M, N;
+  const uint16_t* lin; const uint16_t* lin_lo; int64_t lin_gs; int ld_lin;     // lin_lo: remainders of unsplit X
   uint16_t* out; uint16_t* out_lo; int64_t out_gs; int ldo;
-  uint16_t* out_t; int64_t t_gs; int ldt;
+  uint16_t* out_t; int64_t t_gs; int ldt;      // where transposed tiles of a symmetric result go (out)
   float alpha, beta;                           // out = alpha lin + beta acc
-  int tiles_m, tiles_n, tiles;                 // tiles per matrix
+  int tiles_n, tiles;                          // per matrix; filled in by the launcher
   int count;
   bool transposed;                             // SQ_LAST: the caller's matrices hold the transpose
   OrthMatrices user;
@@ -81,11 +84,9 @@ struct SquareArgs {
 hipError_t launch_square(SquareArgs p, int epi, bool split, hipStream_t s);
 
 hipError_t launch_orth_squares(const OrthMatrices& p, double* parts, hipStream_t s);
-struct OrthHalves {                            // X [short][ld_x], X^T [long][ld_t]
-  uint16_t* x; uint16_t* x_lo; int64_t x_gs; int ld_x;
-  uint16_t* t; int64_t t_gs; int ld_t;
-};
-hipError_t launch_orth_load(const OrthMatrices& p, const double* parts, const OrthHalves& h, bool split, hipStream_t s);
+// X [half_rows(short side)][ld_x]; spare: where the next one goes, whose padding rows are cleared with it
+struct OrthHalves { uint16_t* x; uint16_t* x_lo; uint16_t* spare; int64_t x_gs; int ld_x; };
+hipError_t launch_orth_load(const OrthMatrices& p, const double* parts, const OrthHalves& h, hipStream_t s);
 // Short sides: slices of the long side a matrix is cut into (1: one launch), and the doubles of their Gram matrices.
 int orth_short_slices(int count, int longer);
 hipError_t launch_orth_short(const OrthMatrices& p, double* grams, int slices, hipStream_t s);
