@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import os
 from dataclasses import dataclass
+from functools import lru_cache
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -441,67 +442,75 @@ def prsgd_last_error(h: Optional[Handle]) -> str:
 # ---- operators on replica sets (include/prsgd_ops.h) ---------------------------------------------------------------
 # Tensors are taken as they are: rows have to be contiguous, distances between rows and matrices are read off the strides.
 # Work goes to the current stream of the tensors' device.  Outputs and workspaces that are not given are allocated.
+# What only depends on sizes and options (the configuration, its workspace) is made once per set of them: a call on a few
+# rows is otherwise bound by this marshalling.
 
 NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
 _DTYPES = {torch.float32: PRSGD_F32, torch.bfloat16: PRSGD_BF16}
+_FP8 = torch.float8_e4m3fn
+_current_device = torch._C._cuda_getDevice
+_current_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _enqueue(device: torch.device, fn, *args) -> None:
-    if device.index == torch.cuda.current_device():
-        _check(fn(*args, torch.cuda.current_stream(device).cuda_stream))
+def _enqueue(device: int, fn, *args) -> None:
+    if device == _current_device():
+        rc = fn(*args, _current_stream(device))
     else:
         with torch.cuda.device(device):
-            _check(fn(*args, torch.cuda.current_stream(device).cuda_stream))
+            rc = fn(*args, _current_stream(device))
+    if rc != PRSGD_OK:
+        _check(rc)
 
 
-def _workspace(given: Optional[torch.Tensor], nbytes: int, device: torch.device) -> torch.Tensor:
+def _workspace(given: Optional[torch.Tensor], nbytes: int, like: torch.Tensor) -> torch.Tensor:
     if given is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
-    if given.device != device or given.numel() * given.element_size() < nbytes:
-        raise ValueError("the workspace must have %d bytes on %s" % (nbytes, device))
+        given = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    elif given.device != like.device or given.numel() * given.element_size() < nbytes:
+        raise ValueError("the workspace must have %d bytes on %s" % (nbytes, like.device))
     return given
 
 
-def _matrices(t: torch.Tensor, shape, name: str):
+def _matrices(t: torch.Tensor, like: torch.Tensor, name: str, dtype: torch.dtype):
     """Address, distance between matrices and distance between rows of a [count][rows][cols] or [rows][cols] tensor."""
-    if not t.is_cuda or tuple(t.shape) != tuple(shape):
-        raise ValueError("%s must be a device tensor of shape %s" % (name, tuple(shape)))
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    if not t.is_cuda or t.dtype != dtype or (t is not like and (t.get_device() != like.get_device() or t.shape != like.shape)):
+        raise ValueError("%s must be a %s device tensor of shape %s" % (name, dtype, tuple(like.shape)))
+    st = t.stride()
+    if st[-1] != 1 and t.shape[-1] > 1:
         raise ValueError("rows of %s must be contiguous" % name)
-    return t.data_ptr(), t.stride(0) if t.dim() == 3 else 0, t.stride(-2)
+    return t.data_ptr(), st[0] if len(st) == 3 else 0, st[-2]
 
 
-def _orth_config(dtype: torch.dtype, shape, coefficients, steps: int, eps: float) -> prsgd_orth_config:
+@lru_cache(maxsize=1024)
+def _orth_plan(dtype: torch.dtype, shape, coefficients, steps: int, eps: float):
+    """Configuration by reference, and the bytes of its workspace."""
     if dtype not in _DTYPES:
         raise ValueError("matrices must be float32 or bfloat16")
     if len(shape) not in (2, 3):
         raise ValueError("matrices must be [count][rows][cols] or [rows][cols]")
     a, b, c = coefficients
-    return prsgd_orth_config(_DTYPES[dtype], shape[0] if len(shape) == 3 else 1, shape[-2], shape[-1], int(steps), a, b, c, eps)
+    cfg = prsgd_orth_config(_DTYPES[dtype], shape[0] if len(shape) == 3 else 1, shape[-2], shape[-1], int(steps), a, b, c, eps)
+    n = int(_lib.prsgd_orthogonalize_workspace_bytes(ctypes.byref(cfg)))
+    if n == 0 and cfg.count != 0:
+        raise PrsgdError(PRSGD_EINVAL, _lib.prsgd_last_error(None).decode())
+    return ctypes.byref(cfg), n
 
 
 def prsgd_orthogonalize_workspace_bytes(shape: Sequence[int], dtype: torch.dtype, coefficients=NEWTON_SCHULZ, steps: int = 5,
                                         eps: float = 1e-7) -> int:
     """Of prsgd_orthogonalize and prsgd_muon_step on [count][rows][cols] or [rows][cols] matrices."""
-    cfg = _orth_config(dtype, tuple(shape), coefficients, steps, eps)
-    n = int(_lib.prsgd_orthogonalize_workspace_bytes(ctypes.byref(cfg)))
-    if n == 0 and cfg.count != 0:
-        raise PrsgdError(PRSGD_EINVAL, _lib.prsgd_last_error(None).decode())
-    return n
+    return _orth_plan(dtype, tuple(shape), tuple(coefficients), steps, eps)[1]
 
 
 def prsgd_orthogonalize(g: torch.Tensor, out: Optional[torch.Tensor] = None, coefficients=NEWTON_SCHULZ, steps: int = 5,
                         eps: float = 1e-7, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Newton-Schulz orthogonalisation of every [rows][cols] matrix of g (out may be g)."""
-    cfg = _orth_config(g.dtype, g.shape, coefficients, steps, eps)
+    cfg, nbytes = _orth_plan(g.dtype, g.shape, tuple(coefficients), steps, eps)
+    src = _matrices(g, g, "g", g.dtype)
     if out is None:
         out = torch.empty(g.shape, dtype=g.dtype, device=g.device)
-    if out.dtype != g.dtype or out.device != g.device:
-        raise ValueError("out must have the type and device of g")
-    src, dst = _matrices(g, g.shape, "g"), _matrices(out, g.shape, "out")
-    n = int(_lib.prsgd_orthogonalize_workspace_bytes(ctypes.byref(cfg)))
-    ws = _workspace(workspace, n, g.device)
-    _enqueue(g.device, _lib.prsgd_orthogonalize, ctypes.byref(cfg), *src, *dst, ws.data_ptr())
+    dst = _matrices(out, g, "out", g.dtype)
+    ws = _workspace(workspace, nbytes, g)
+    _enqueue(g.get_device(), _lib.prsgd_orthogonalize, cfg, *src, *dst, ws.data_ptr())
     return out
 
 
@@ -511,59 +520,83 @@ def prsgd_muon_step(x: torch.Tensor, g: torch.Tensor, m: torch.Tensor, lr: float
     """Momentum, orthogonalisation and update of every [rows][cols] matrix of x, in place on x and m (fp32).
 
     scale defaults to 0.2 sqrt(max(rows, cols))."""
-    cfg = _orth_config(x.dtype, x.shape, coefficients, steps, eps)
-    if g.dtype != x.dtype or m.dtype != torch.float32 or g.device != x.device or m.device != x.device:
-        raise ValueError("g must have the type of x, m must be float32, all on one device")
+    cfg, nbytes = _orth_plan(x.dtype, x.shape, tuple(coefficients), steps, eps)
+    xs, gs, ms = _matrices(x, x, "x", x.dtype), _matrices(g, x, "g", x.dtype), _matrices(m, x, "m", torch.float32)
     if scale is None:
         scale = 0.2 * max(x.shape[-2:]) ** 0.5
-    xs, gs, ms = _matrices(x, x.shape, "x"), _matrices(g, x.shape, "g"), _matrices(m, x.shape, "m")
-    n = int(_lib.prsgd_orthogonalize_workspace_bytes(ctypes.byref(cfg)))
-    ws = _workspace(workspace, n, x.device)
-    _enqueue(x.device, _lib.prsgd_muon_step, ctypes.byref(cfg), *xs, *gs, *ms, lr, momentum, 1 if nesterov else 0, weight_decay,
-             scale, ws.data_ptr())
+    ws = _workspace(workspace, nbytes, x)
+    _enqueue(x.get_device(), _lib.prsgd_muon_step, cfg, *xs, *gs, *ms, lr, momentum, 1 if nesterov else 0, weight_decay, scale,
+             ws.data_ptr())
 
 
-def _norm_rows(t: Optional[torch.Tensor], like: torch.Tensor, name: str, dtype=None):
-    """Address and distance between rows of a [rows][width] tensor (0, 0 for none)."""
-    if t is None:
-        return 0, 0
-    if t.device != like.device or t.shape != like.shape or t.dtype != (dtype or like.dtype):
-        raise ValueError("%s must be a %s tensor of shape %s on %s" % (name, dtype or like.dtype, tuple(like.shape), like.device))
-    if t.shape[1] > 1 and t.stride(1) != 1:
-        raise ValueError("rows of %s must be contiguous" % name)
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
-
-
-def _norm_config(x: torch.Tensor, w: torch.Tensor, eps: float) -> prsgd_norm_config:
-    if not x.is_cuda or x.dim() != 2 or x.dtype not in _DTYPES:
+@lru_cache(maxsize=1024)
+def _norm_plan(dtype: torch.dtype, shape, w_shape, eps: float):
+    """Configuration by reference, the bytes that the backward call works in, rows and width."""
+    if len(shape) != 2 or dtype not in _DTYPES:
         raise ValueError("rows must be a [rows][width] device tensor of float32 or bfloat16")
-    workers = 1 if w.dim() == 1 else w.shape[0]
-    if w.dtype != torch.float32 or w.device != x.device or w.dim() not in (1, 2) or w.shape[-1] != x.shape[1] or \
-            (w.shape[-1] > 1 and w.stride(-1) != 1):
-        raise ValueError("weights must be float32, [width] or [workers][width], rows contiguous")
-    if workers == 0 or x.shape[0] % workers != 0:
+    if len(w_shape) not in (1, 2) or w_shape[-1] != shape[1]:
+        raise ValueError("weights must be [width] or [workers][width]")
+    workers = 1 if len(w_shape) == 1 else w_shape[0]
+    if workers == 0 or shape[0] % workers != 0:
         raise ValueError("every worker must have the same number of rows")
-    return prsgd_norm_config(_DTYPES[x.dtype], workers, x.shape[0] // workers, x.shape[1], eps)
+    cfg = prsgd_norm_config(_DTYPES[dtype], workers, shape[0] // workers, shape[1], eps)
+    n = int(_lib.prsgd_rms_norm_backward_workspace_bytes(ctypes.byref(cfg)))
+    if n == 0:
+        raise PrsgdError(PRSGD_EINVAL, _lib.prsgd_last_error(None).decode())
+    return ctypes.byref(cfg), n, shape[0], shape[1]
 
 
-def _weight_rows(w: torch.Tensor) -> int:
-    return w.stride(0) if w.dim() == 2 and w.shape[0] > 1 else 0
+def _norm_rows(t: torch.Tensor, like: torch.Tensor, name: str, dtype: torch.dtype):
+    """Address and distance between rows of a [rows][width] tensor."""
+    if not t.is_cuda or t.dtype != dtype or (t is not like and (t.get_device() != like.get_device() or t.shape != like.shape)):
+        raise ValueError("%s must be a %s device tensor of shape %s" % (name, dtype, tuple(like.shape)))
+    row, element = t.stride()
+    if element != 1 and t.shape[1] > 1:
+        raise ValueError("rows of %s must be contiguous" % name)
+    return t.data_ptr(), row if row >= t.shape[1] or t.shape[0] > 1 else t.shape[1]
 
 
-def _row_vector(given: Optional[torch.Tensor], x: torch.Tensor, name: str) -> torch.Tensor:
-    if given is None:
-        return torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
-    if given.dtype != torch.float32 or given.device != x.device or given.shape != (x.shape[0],) or not given.is_contiguous():
+def _weight_rows(w: torch.Tensor, like: torch.Tensor, name: str):
+    """Address and distance between workers of [width] or [workers][width] weights (or their gradients)."""
+    st = w.stride()
+    if w.dtype != torch.float32 or w.get_device() != like.get_device() or (st[-1] != 1 and w.shape[-1] > 1):
+        raise ValueError("%s must be float32 on the device of the rows, its rows contiguous" % name)
+    return w.data_ptr(), st[0] if len(st) == 2 and w.shape[0] > 1 else 0
+
+
+def _row_vector(t: torch.Tensor, x: torch.Tensor, name: str) -> int:
+    if t.dtype != torch.float32 or t.get_device() != x.get_device() or t.shape != x.shape[:1] or not t.is_contiguous():
         raise ValueError("%s must be %d contiguous floats" % (name, x.shape[0]))
-    return given
+    return t.data_ptr()
 
 
-def _norm_outputs(x, residual, sum_out, out, dtype):
-    if sum_out is None and residual is not None:
-        sum_out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+def _norm_forward(fn, x, w, residual, eps, out, out_dtype, sum_out, stat, stat_name):
+    dtype = x.dtype
+    cfg, _, rows, width = _norm_plan(dtype, x.shape, w.shape, eps)
+    x_at, x_row = _norm_rows(x, x, "x", dtype)
+    w_at, w_row = _weight_rows(w, x, "w")
+    r_at = r_row = s_at = s_row = 0
+    if residual is not None:
+        r_at, r_row = _norm_rows(residual, x, "residual", dtype)
+        if sum_out is None:
+            sum_out = torch.empty_like(x)
+            s_at, s_row = sum_out.data_ptr(), width
+    if sum_out is None:
+        sum_out = x
+    elif s_row == 0:
+        s_at, s_row = _norm_rows(sum_out, x, "sum_out", dtype)
     if out is None:
-        out = torch.empty(x.shape, dtype=dtype, device=x.device)
-    return sum_out, out
+        out = torch.empty_like(x, dtype=out_dtype)
+        y_at, y_row = out.data_ptr(), width
+    else:
+        y_at, y_row = _norm_rows(out, x, "out", out_dtype)
+    if stat is None:
+        stat = x.new_empty(rows, dtype=torch.float32)
+        stat_at = stat.data_ptr()
+    else:
+        stat_at = _row_vector(stat, x, stat_name)
+    _enqueue(x.get_device(), fn, cfg, x_at, x_row, r_at, r_row, w_at, w_row, s_at, s_row, y_at, y_row, stat_at)
+    return out, sum_out, stat
 
 
 def prsgd_rms_norm(x: torch.Tensor, w: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
@@ -571,50 +604,44 @@ def prsgd_rms_norm(x: torch.Tensor, w: torch.Tensor, residual: Optional[torch.Te
                    rstd: Optional[torch.Tensor] = None):
     """(y, s, rstd) of s = x + residual, y = s rstd w for the rows of every worker ([workers * rows][width], w [workers][width] or
     [width]).  Without a residual s is x itself, and is written only if sum_out is given."""
-    cfg = _norm_config(x, w, eps)
-    sum_out, out = _norm_outputs(x, residual, sum_out, out, x.dtype)
-    rstd = _row_vector(rstd, x, "rstd")
-    _enqueue(x.device, _lib.prsgd_rms_norm, ctypes.byref(cfg), *_norm_rows(x, x, "x"), *_norm_rows(residual, x, "residual"),
-             w.data_ptr(), _weight_rows(w), *_norm_rows(sum_out, x, "sum_out"), *_norm_rows(out, x, "out"), rstd.data_ptr())
-    return out, x if sum_out is None else sum_out, rstd
+    return _norm_forward(_lib.prsgd_rms_norm, x, w, residual, eps, out, x.dtype, sum_out, rstd, "rstd")
 
 
 def prsgd_rms_norm_fp8(x: torch.Tensor, w: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
                        out: Optional[torch.Tensor] = None, sum_out: Optional[torch.Tensor] = None,
                        scales: Optional[torch.Tensor] = None):
     """(q, scales, s): prsgd_rms_norm's y as q * scales[:, None], q in torch.float8_e4m3fn."""
-    cfg = _norm_config(x, w, eps)
-    sum_out, out = _norm_outputs(x, residual, sum_out, out, torch.float8_e4m3fn)
-    scales = _row_vector(scales, x, "scales")
-    _enqueue(x.device, _lib.prsgd_rms_norm_fp8, ctypes.byref(cfg), *_norm_rows(x, x, "x"), *_norm_rows(residual, x, "residual"),
-             w.data_ptr(), _weight_rows(w), *_norm_rows(sum_out, x, "sum_out"),
-             *_norm_rows(out, x, "out", torch.float8_e4m3fn), scales.data_ptr())
-    return out, scales, x if sum_out is None else sum_out
+    q, s, scales = _norm_forward(_lib.prsgd_rms_norm_fp8, x, w, residual, eps, out, _FP8, sum_out, scales, "scales")
+    return q, scales, s
 
 
 def prsgd_rms_norm_backward_workspace_bytes(x: torch.Tensor, w: torch.Tensor) -> int:
-    cfg = _norm_config(x, w, 0.0)
-    n = int(_lib.prsgd_rms_norm_backward_workspace_bytes(ctypes.byref(cfg)))
-    if n == 0:
-        raise PrsgdError(PRSGD_EINVAL, _lib.prsgd_last_error(None).decode())
-    return n
+    return _norm_plan(x.dtype, x.shape, w.shape, 0.0)[1]
 
 
 def prsgd_rms_norm_backward(dy: torch.Tensor, s: torch.Tensor, rstd: torch.Tensor, w: torch.Tensor,
                             dsum: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
                             dw: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """(dx, dw) of prsgd_rms_norm: dx is the gradient of x and of the residual alike, dw has w's shape."""
-    cfg = _norm_config(dy, w, 0.0)
-    rstd = _row_vector(rstd, dy, "rstd")
+    dtype = dy.dtype
+    cfg, nbytes, _, width = _norm_plan(dtype, dy.shape, w.shape, 0.0)
+    dy_at, dy_row = _norm_rows(dy, dy, "dy", dtype)
+    s_at, s_row = _norm_rows(s, dy, "s", dtype)
+    w_at, w_row = _weight_rows(w, dy, "w")
+    ds_at, ds_row = (0, 0) if dsum is None else _norm_rows(dsum, dy, "dsum", dtype)
     if dx is None:
-        dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
+        dx = torch.empty_like(dy)
+        dx_at, dx_row = dx.data_ptr(), width
+    else:
+        dx_at, dx_row = _norm_rows(dx, dy, "dx", dtype)
     if dw is None:
-        dw = torch.empty(w.shape, dtype=torch.float32, device=dy.device)
-    if dw.dtype != torch.float32 or dw.shape != w.shape or dw.device != dy.device or (dw.shape[-1] > 1 and dw.stride(-1) != 1):
-        raise ValueError("dw must be float32 of w's shape, rows contiguous")
-    n = int(_lib.prsgd_rms_norm_backward_workspace_bytes(ctypes.byref(cfg)))
-    ws = _workspace(workspace, max(n, 1), dy.device)
-    _enqueue(dy.device, _lib.prsgd_rms_norm_backward, ctypes.byref(cfg), *_norm_rows(dy, dy, "dy"), *_norm_rows(dsum, dy, "dsum"),
-             *_norm_rows(s, dy, "s"), rstd.data_ptr(), w.data_ptr(), _weight_rows(w), *_norm_rows(dx, dy, "dx"), dw.data_ptr(),
-             _weight_rows(dw), ws.data_ptr())
+        dw = torch.empty(w.shape, dtype=torch.float32, device=w.device)
+        dw_at, dw_row = dw.data_ptr(), width
+    else:
+        if dw.shape != w.shape:
+            raise ValueError("dw must have the shape of w")
+        dw_at, dw_row = _weight_rows(dw, dy, "dw")
+    work = _workspace(workspace, nbytes, dy)
+    _enqueue(dy.get_device(), _lib.prsgd_rms_norm_backward, cfg, dy_at, dy_row, ds_at, ds_row, s_at, s_row,
+             _row_vector(rstd, dy, "rstd"), w_at, w_row, dx_at, dx_row, dw_at, dw_row, work.data_ptr())
     return dx, dw
