@@ -1,30 +1,13 @@
 // Newton-Schulz orthogonalisation around its products: the sums of squares (and the momentum step, which is where the update is first
 // read), the normalised update as halves in both orientations, and whole calls whose shorter side is at most kShortSide.
-#include "prsgd_internal.h"
-#include "prsgd_ops_internal.h"
+#include <atomic>
+
+#include "orth_rows.h"
 
 namespace prsgd {
 
 namespace {
 
-template <typename T> __device__ __forceinline__ float value(T v) {
-  if constexpr (sizeof(T) == 4) return v; else return bf16_to_f32(v);
-}
-template <typename T> __device__ __forceinline__ void put(T* p, float f) {
-  if constexpr (sizeof(T) == 4) *p = f; else *p = f32_to_bf16_rne(f);
-}
-// M <- mu M + G, and the element of U; `stepped`: an earlier launch has moved M on
-template <typename T> __device__ __forceinline__ float update_at(const OrthMatrices& p, int g, int row, int col, bool stepped) {
-  const float v = value(reinterpret_cast<const T*>(p.g)[g * p.g_matrix + row * p.g_row + col]);
-  if (p.m == nullptr) return v;
-  float* at = p.m + g * p.m_matrix + row * p.m_row + col;
-  float m = *at;
-  if (!stepped) {
-    m = fmaf(p.mu, m, v);
-    *at = m;
-  }
-  return fmaf(p.m_part, m, p.g_part * v);
-}
 // the scale that normalises; a zero matrix stays zero
 __device__ __forceinline__ double norm_scale(double squares, float eps) {
   const double d = sqrt(squares) + (double)eps;
@@ -35,47 +18,6 @@ __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
   for (int d = 1; d < kWave; d <<= 1) v += __shfl_xor(v, d);
   return v;
-}
-
-// Eight elements of U at a row's column c, n of them inside it (the others are zero); M moves on unless an earlier launch did that.
-typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
-template <int ES> struct __attribute__((packed, aligned(ES))) Packed16 { u32x4_t v; };
-template <typename T> __device__ __forceinline__ void load8(const T* p, int n, float (&v)[8]) {
-  if (n >= 8) {
-    if constexpr (sizeof(T) == 4) {
-      const u32x4_t lo = reinterpret_cast<const Packed16<4>*>(p)->v, hi = reinterpret_cast<const Packed16<4>*>(p + 4)->v;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) { v[e] = __uint_as_float(lo[e]); v[4 + e] = __uint_as_float(hi[e]); }
-    } else {
-      const u32x4_t x = reinterpret_cast<const Packed16<2>*>(p)->v;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = __uint_as_float((e & 1) != 0 ? x[e / 2] & 0xFFFF0000u : x[e / 2] << 16);
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < n ? value(p[e]) : 0.0f;
-  }
-}
-template <typename T> __device__ __forceinline__ void update8(const OrthMatrices& p, int g, int row, int c, int n, bool stepped, float (&u)[8]) {
-  load8(reinterpret_cast<const T*>(p.g) + g * p.g_matrix + row * p.g_row + c, n, u);
-  if (p.m == nullptr) return;
-  float* at = p.m + g * p.m_matrix + row * p.m_row + c;
-  float m[8];
-  load8(at, n, m);
-  if (!stepped) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) m[e] = fmaf(p.mu, m[e], u[e]);
-    if (n >= 8) {
-      reinterpret_cast<Packed16<4>*>(at)->v = (u32x4_t){__float_as_uint(m[0]), __float_as_uint(m[1]), __float_as_uint(m[2]), __float_as_uint(m[3])};
-      reinterpret_cast<Packed16<4>*>(at + 4)->v = (u32x4_t){__float_as_uint(m[4]), __float_as_uint(m[5]), __float_as_uint(m[6]), __float_as_uint(m[7])};
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < n) at[e] = m[e];
-    }
-  }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) u[e] = fmaf(p.m_part, m[e], p.g_part * u[e]);
 }
 
 // Sums of squares in 64 bits (an fp32 sum overflows from elements of 1e19 on), a share of the matrix per workgroup.
@@ -161,178 +103,276 @@ __global__ void __launch_bounds__(kThreads) orth_load_kernel(OrthMatrices p, con
 }
 
 // ---- short sides -------------------------------------------------------------------------------
-// With r = min(rows, cols) <= 32 every iterate is P U with P an r x r polynomial of the Gram matrix K = U U^T (all of them commute):
+// With r = min(rows, cols) <= kShortSide every iterate is P U with P an r x r polynomial of the Gram matrix K = U U^T (all of them
+// symmetric, and they commute):
 //   A_0 = K / (|U| + eps)^2,  Q = a + b A + c A A,  P <- Q P,  A <- Q A Q,   |U|^2 = trace K,
-// so U is read once for K and once for P U, 3 r^2 L operations in all instead of 3 r^2 L per step.  The Gram matrix squares the
-// condition; in 64 bits its smallest eigenvalues are as good as fp32 singular values are, in fp32 they may come out negative and grow.
-constexpr int kChunk = 128;              // long-side positions in LDS at a time
-constexpr int kPitch = kShortSide + 1;
+// so U is read for K and for P U, 3 r^2 L operations in all instead of 3 r^2 L per step, and a whole call is one launch or two.  The Gram
+// matrix squares the condition: in 64 bits its smallest eigenvalues are as good as fp32 singular values are, in fp32 they may come out
+// negative and grow.  K and the polynomials run on v_mfma_f64_16x16x4, P U on v_mfma_f32_16x16x4.
+// A symmetric matrix of NB x NB blocks of 16 is kept as operands: element q of lane (g = lane / 16, i = lane % 16) of block (x, y) is
+// M[16 x + i][16 y + 4 q + g].  That is what a product takes from either side, and the product's block (x, y) comes out as block (y, x).
+typedef double f64x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 struct ShortShape { int r, longer; bool tall; };
+template <int NB> struct Short {
+  static constexpr int ROWS = 16 * NB, CHUNK = NB <= 2 ? 256 : 128;        // long-side positions in LDS at a time
+  static constexpr int PITCH = CHUNK + 4;                                  // 16 rows x 4 positions on 64 banks
+  static constexpr int MATRIX = NB * NB * 256;                             // doubles of a matrix
+  static constexpr int U_BYTES = ROWS * PITCH * 4;
+  // four matrices; U lies on the last two of them where the two would not fit beside each other
+  static constexpr int U_AT = NB <= 2 ? 4 * MATRIX * 8 : 2 * MATRIX * 8;
+  static constexpr int LDS = U_AT + U_BYTES > 4 * MATRIX * 8 ? U_AT + U_BYTES : 4 * MATRIX * 8;
+  static_assert(LDS <= 160 * 1024, "LDS of a compute unit");
+};
 
-template <typename T>
-__device__ __forceinline__ void stage(const OrthMatrices& p, const ShortShape& s, int g, int l0, int n, bool stepped,
-                                      double scale, float (&u)[kShortSide][kChunk + 1]) {
-  for (int i = threadIdx.x; i < s.r * n; i += kThreads) {
-    int a, l;
-    if (s.tall) { l = i / s.r; a = i - l * s.r; } else { a = i / n; l = i - a * n; }
-    u[a][l] = (float)((double)(s.tall ? update_at<T>(p, g, l0 + l, a, stepped) : update_at<T>(p, g, a, l0 + l, stepped)) * scale);
+// U at long-side positions [l0, l0 + n), zeros up to a multiple of 16 positions; eight elements of a row of U at a time
+template <typename T, int NB>
+__device__ __forceinline__ void stage(const OrthMatrices& p, const ShortShape& s, int g, int l0, int n, bool stepped, float* u) {
+  constexpr int P = Short<NB>::PITCH;
+  const int m = (n + 15) & ~15, per_row = ((s.tall ? s.r : m) + 7) / 8, total = (s.tall ? m : s.r) * per_row;
+#pragma unroll 2
+  for (int i = threadIdx.x; i < total; i += kThreads) {
+    const int row = i / per_row, c = (i - row * per_row) * 8;
+    float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    if (s.tall) {
+      if (row < n) update8<T>(p, g, l0 + row, c, s.r - c, stepped, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (c + e < s.r) u[(c + e) * P + row] = v[e];
+    } else {
+      if (c < n) update8<T>(p, g, row, l0 + c, n - c, stepped, v);
+      f32x4_t* to = reinterpret_cast<f32x4_t*>(u + row * P + c);
+      to[0] = (f32x4_t){v[0], v[1], v[2], v[3]};
+      to[1] = (f32x4_t){v[4], v[5], v[6], v[7]};
+    }
+  }
+}
+// ... and the result from there to the caller's matrices
+template <typename T, int NB>
+__device__ __forceinline__ void unstage(const OrthMatrices& p, const ShortShape& s, int g, int l0, int n, const float* u) {
+  constexpr int P = Short<NB>::PITCH;
+  const int per_row = ((s.tall ? s.r : n) + 7) / 8, total = (s.tall ? n : s.r) * per_row;
+#pragma unroll 2
+  for (int i = threadIdx.x; i < total; i += kThreads) {
+    const int row = i / per_row, c = (i - row * per_row) * 8;
+    float v[8];
+    if (s.tall) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = u[min(c + e, s.r - 1) * P + row];
+      result8<T>(p, g * p.out_matrix + (int64_t)(l0 + row) * p.out_row + c, s.r - c, v);
+    } else {
+      const f32x4_t* from = reinterpret_cast<const f32x4_t*>(u + row * P + c);
+      const f32x4_t lo = from[0], hi = from[1];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { v[e] = lo[e]; v[4 + e] = hi[e]; }
+      result8<T>(p, g * p.out_matrix + (int64_t)row * p.out_row + l0 + c, n - c, v);
+    }
   }
 }
 
-// K over the long-side positions [l0, l1) into LDS.  A thread has a 2 x 2 block on or below the diagonal, and of the positions its share.
-template <typename T>
-__device__ __forceinline__ void gram_of(const OrthMatrices& p, const ShortShape& s, int g, int l0, int l1, bool stepped,
-                                        float (&u)[kShortSide][kChunk + 1], double (&share)[4][kThreads], double (&k)[kShortSide][kPitch]) {
-  const int rb = (s.r + 1) / 2, blocks = rb * (rb + 1) / 2, shares = kThreads / blocks;
-  const int t = threadIdx.x, block = t % blocks, part = t / blocks;
-  int bi = 0;
-  while ((bi + 1) * (bi + 2) / 2 <= block) ++bi;
-  const int bj = block - bi * (bi + 1) / 2;
-  const int i0 = 2 * bi, i1 = min(2 * bi + 1, s.r - 1), j0 = 2 * bj, j1 = min(2 * bj + 1, s.r - 1);
-  double a00 = 0.0, a01 = 0.0, a10 = 0.0, a11 = 0.0;
-  for (int l = l0; l < l1; l += kChunk) {
-    const int n = min(kChunk, l1 - l);
+// Place of element e of a lane of one block in the transposed block
+__device__ __forceinline__ int transposed_place(int e, int lane) { return (lane & 15) / 4 * 64 + (lane & 3) * 16 + 4 * e + (lane >> 4); }
+// K over the long-side positions [l0, l1) into the first matrix of LDS; U's last chunk stays there if U has a place of its own.
+template <typename T, int NB>
+__device__ __forceinline__ void gram_of(const OrthMatrices& p, const ShortShape& s, int g, int l0, int l1, double* lds, float* u) {
+  using S = Short<NB>;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, i = lane & 15, q4 = lane >> 4;
+  for (int e = t + s.r * S::PITCH; e < S::ROWS * S::PITCH; e += kThreads) u[e] = 0.0f;       // rows past the side
+  f64x4_t acc[NB * (NB + 1) / 2];
+#pragma unroll
+  for (int b = 0; b < NB * (NB + 1) / 2; ++b) acc[b] = (f64x4_t){0.0, 0.0, 0.0, 0.0};
+  for (int l = l0; l < l1; l += S::CHUNK) {
+    const int n = min(S::CHUNK, l1 - l);
+    if (l > l0) __syncthreads();
+    stage<T, NB>(p, s, g, l, n, false, u);
     __syncthreads();
-    stage<T>(p, s, g, l, n, stepped, 1.0, u);
-    __syncthreads();
-    if (part < shares)
-      for (int x = part; x < n; x += shares) {
-        const double xi0 = u[i0][x], xi1 = u[i1][x], xj0 = u[j0][x], xj1 = u[j1][x];
-        a00 = fma(xi0, xj0, a00);
-        a01 = fma(xi0, xj1, a01);
-        a10 = fma(xi1, xj0, a10);
-        a11 = fma(xi1, xj1, a11);
+    for (int x = wave; x < (n + 3) / 4; x += 4) {
+      double v[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) v[b] = u[(16 * b + i) * S::PITCH + 4 * x + q4];
+      int k = 0;
+#pragma unroll
+      for (int y = 0; y < NB; ++y)
+#pragma unroll
+        for (int x2 = 0; x2 <= y; ++x2, ++k) acc[k] = __builtin_amdgcn_mfma_f64_16x16x4f64(v[x2], v[y], acc[k], 0, 0, 0);
+    }
+  }
+  if (S::U_AT < 4 * S::MATRIX * 8) __syncthreads();
+  int k = 0;
+#pragma unroll
+  for (int y = 0; y < NB; ++y)
+#pragma unroll
+    for (int x = 0; x <= y; ++x, ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) lds[wave * S::MATRIX + (y * NB + x) * 256 + e * 64 + lane] = acc[k][e];
+  __syncthreads();
+  // the wavefronts' shares in ascending order; a block above the diagonal is the transpose of the one below
+  const int mirrored = transposed_place(wave, lane);       // thread: element wave of lane
+#pragma unroll
+  for (int y = 0; y < NB; ++y)
+#pragma unroll
+    for (int x = 0; x <= y; ++x) {
+      const int at = (y * NB + x) * 256 + t;
+      const double v = ((lds[at] + lds[S::MATRIX + at]) + lds[2 * S::MATRIX + at]) + lds[3 * S::MATRIX + at];
+      lds[at] = v;
+      if (x != y) lds[(x * NB + y) * 256 + mirrored] = v;
+    }
+  __syncthreads();
+}
+
+// d <- f(x y); every wavefront meets the others behind it.  (Blocks on and below the diagonal alone, with the others written as their
+// transposes, save a quarter of the products at NB = 4 and took as long: 55 against 52 us for a call on 64 x 64.)
+template <int NB, typename F>
+__device__ __forceinline__ void short_product(const double* x, const double* y, double* d, F&& f) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int b = wave; b < NB * NB; b += 4) {
+    const int i = b / NB, j = b % NB;
+    f64x4_t acc = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+    for (int k = 0; k < NB; ++k)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        acc = __builtin_amdgcn_mfma_f64_16x16x4f64(x[(i * NB + k) * 256 + q * 64 + lane], y[(j * NB + k) * 256 + q * 64 + lane], acc, 0, 0, 0);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int at = (j * NB + i) * 256 + e * 64 + lane;
+      d[at] = f(acc[e], at, i == j && 4 * e + (lane >> 4) == (lane & 15));
+    }
+  }
+  __syncthreads();
+}
+
+// P of the scaled Gram matrix in the first matrix of LDS, as operands in fp32; a single block stays in registers, in every wavefront
+template <int NB>
+__device__ __forceinline__ void polynomial_of(const OrthMatrices& p, double* lds, float (&pf)[NB][NB][4]) {
+  const int lane = threadIdx.x & 63;
+  const double a = p.a, b = p.b, c = p.c;
+  if constexpr (NB == 1) {
+    auto product = [](f64x4_t x, f64x4_t y) __attribute__((always_inline)) {
+      f64x4_t acc = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+      for (int q = 0; q < 4; ++q) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(x[q], y[q], acc, 0, 0, 0);
+      return acc;
+    };
+    f64x4_t m, poly = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) m[q] = lds[q * 64 + lane];
+    for (int step = 0; step < p.steps; ++step) {
+      const f64x4_t square = product(m, m);
+      f64x4_t f;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) f[q] = fma(c, square[q], fma(b, m[q], 4 * q + (lane >> 4) == (lane & 15) ? a : 0.0));
+      poly = step == 0 ? f : product(f, poly);
+      if (step + 1 < p.steps) m = product(product(f, m), f);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) pf[0][0][q] = (float)poly[q];
+  } else {
+    constexpr int M = Short<NB>::MATRIX;
+    double* m = lds;
+    double* f = lds + M;
+    double* poly = lds + 2 * M;
+    double* spare = lds + 3 * M;
+    auto plain = [](double v, int, bool) { return v; };
+    for (int step = 0; step < p.steps; ++step) {
+      short_product<NB>(m, m, f, [&](double v, int at, bool diagonal) { return fma(c, v, fma(b, m[at], diagonal ? a : 0.0)); });
+      if (step == 0) {
+        for (int e = threadIdx.x; e < M; e += kThreads) poly[e] = f[e];
+      } else {
+        short_product<NB>(f, poly, spare, plain);
+        double* old = poly;
+        poly = spare;
+        spare = old;
       }
-  }
-  share[0][t] = a00;
-  share[1][t] = a01;
-  share[2][t] = a10;
-  share[3][t] = a11;
-  __syncthreads();
-  for (int e = t; e < 4 * blocks; e += kThreads) {
-    const int which = e / blocks, bk = e - which * blocks;
-    double v = 0.0;
-    for (int q = 0; q < shares; ++q) v += share[which][q * blocks + bk];
-    int i = 0;
-    while ((i + 1) * (i + 2) / 2 <= bk) ++i;
-    const int j = bk - i * (i + 1) / 2, x = 2 * i + (which >> 1), y = 2 * j + (which & 1);
-    if (x < s.r && y < s.r && (i != j || which != 1)) {
-      k[x][y] = v;
-      k[y][x] = v;
+      if (step + 1 < p.steps) {
+        short_product<NB>(f, m, spare, plain);
+        short_product<NB>(spare, f, m, plain);
+      }
     }
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < NB; ++x)
+#pragma unroll
+      for (int y = 0; y < NB; ++y)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) pf[x][y][q] = (float)poly[(x * NB + y) * 256 + q * 64 + lane];
+    if (Short<NB>::U_AT < 4 * M * 8) __syncthreads();
   }
-  __syncthreads();
 }
 
-// d <- x y for r x r matrices that commute and are symmetric (so y's columns are its rows), 2 x 2 elements a thread.  f: of the result.
-template <typename F>
-__device__ __forceinline__ void short_product(const double (&x)[kShortSide][kPitch], const double (&y)[kShortSide][kPitch],
-                                              double (&d)[kShortSide][kPitch], int r, F&& f) {
-  const int rb = (r + 1) / 2;
-  for (int t = threadIdx.x; t < rb * rb; t += kThreads) {
-    const int i0 = 2 * (t / rb), j0 = 2 * (t % rb), i1 = min(i0 + 1, r - 1), j1 = min(j0 + 1, r - 1);
-    double a00 = 0.0, a01 = 0.0, a10 = 0.0, a11 = 0.0;
-    for (int k = 0; k < r; ++k) {
-      const double xi0 = x[i0][k], xi1 = x[i1][k], yj0 = y[k][j0], yj1 = y[k][j1];
-      a00 = fma(xi0, yj0, a00);
-      a01 = fma(xi0, yj1, a01);
-      a10 = fma(xi1, yj0, a10);
-      a11 = fma(xi1, yj1, a11);
-    }
-    d[i0][j0] = f(a00, i0, j0);
-    if (j0 + 1 < r) d[i0][j1] = f(a01, i0, j1);
-    if (i0 + 1 < r) d[i1][j0] = f(a10, i1, j0);
-    if (i0 + 1 < r && j0 + 1 < r) d[i1][j1] = f(a11, i1, j1);
-  }
-  __syncthreads();
+template <int NB> __device__ __forceinline__ int slice_length(const ShortShape& s, int slices) {
+  constexpr int C = Short<NB>::CHUNK;
+  return ((s.longer + C - 1) / C + slices - 1) / slices * C;
 }
-
-template <typename T> __global__ void __launch_bounds__(kThreads) orth_short_gram_kernel(OrthMatrices p, ShortShape s, double* grams, int slices) {
-  __shared__ float u[kShortSide][kChunk + 1];
-  __shared__ double share[4][kThreads], k[kShortSide][kPitch];
-  const int g = blockIdx.y, per = ((s.longer + kChunk - 1) / kChunk + slices - 1) / slices * kChunk;
-  const int l0 = blockIdx.x * per, l1 = min(s.longer, l0 + per);
-  gram_of<T>(p, s, g, l0, l1, false, u, share, k);
-  double* out = grams + ((int64_t)g * slices + blockIdx.x) * s.r * s.r;
-  for (int e = threadIdx.x; e < s.r * s.r; e += kThreads) out[e] = k[e / s.r][e % s.r];
+template <typename T, int NB>
+__global__ void __launch_bounds__(kThreads) orth_short_gram_kernel(OrthMatrices p, ShortShape s, double* grams, int slices) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  double* lds = reinterpret_cast<double*>(smem);
+  const int g = blockIdx.y, per = slice_length<NB>(s, slices), l0 = min(s.longer, (int)blockIdx.x * per), l1 = min(s.longer, l0 + per);
+  gram_of<T, NB>(p, s, g, l0, l1, lds, reinterpret_cast<float*>(smem + Short<NB>::U_AT));
+  double* out = grams + ((int64_t)g * slices + blockIdx.x) * Short<NB>::MATRIX;
+  for (int e = threadIdx.x; e < Short<NB>::MATRIX; e += kThreads) out[e] = lds[e];
 }
 
 // ALONE: a matrix has one workgroup, which computes K itself.
-template <typename T, bool ALONE>
+template <typename T, int NB, bool ALONE>
 __global__ void __launch_bounds__(kThreads) orth_short_kernel(OrthMatrices p, ShortShape s, const double* grams, int slices) {
-  __shared__ float u[kShortSide][kChunk + 1];
-  __shared__ double share[4][kThreads];
-  __shared__ double m0[kShortSide][kPitch], m1[kShortSide][kPitch], m2[kShortSide][kPitch], m3[kShortSide][kPitch];
-  __shared__ float pf[kShortSide][kShortSide + 1];
-  const int g = blockIdx.y, r = s.r, per = ((s.longer + kChunk - 1) / kChunk + slices - 1) / slices * kChunk;
-  const int l0 = blockIdx.x * per, l1 = min(s.longer, l0 + per);
+  using S = Short<NB>;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  double* lds = reinterpret_cast<double*>(smem);
+  float* u = reinterpret_cast<float*>(smem + S::U_AT);
+  const int g = blockIdx.y, t = threadIdx.x, lane = t & 63, wave = t >> 6, i = lane & 15, q4 = lane >> 4;
+  const int per = slice_length<NB>(s, slices), l0 = min(s.longer, (int)blockIdx.x * per), l1 = min(s.longer, l0 + per);
   if (ALONE) {
-    gram_of<T>(p, s, g, 0, s.longer, false, u, share, m0);
+    gram_of<T, NB>(p, s, g, 0, s.longer, lds, u);
   } else {
-    for (int e = threadIdx.x; e < r * r; e += kThreads) {
+    for (int e = t; e < S::MATRIX; e += kThreads) {
       double v = 0.0;
-      for (int q = 0; q < slices; ++q) v += grams[((int64_t)g * slices + q) * r * r + e];
-      m0[e / r][e % r] = v;
+      for (int q = 0; q < slices; ++q) v += grams[((int64_t)g * slices + q) * S::MATRIX + e];
+      lds[e] = v;
     }
     __syncthreads();
   }
+  // the diagonal: element 4 q + g = i of block (x, x)
   double squares = 0.0;
-  for (int i = 0; i < r; ++i) squares += m0[i][i];
-  const double scale = norm_scale(squares, p.eps);
+  if (lane < S::ROWS) squares = lds[(lane / 16) * (NB + 1) * 256 + (lane % 16 / 4) * 64 + (lane % 4) * 16 + lane % 16];
+  const double scale = norm_scale(wave_sum(squares), p.eps);
   __syncthreads();
-  for (int e = threadIdx.x; e < r * r; e += kThreads) m0[e / r][e % r] *= scale * scale;
+  for (int e = t; e < S::MATRIX; e += kThreads) lds[e] *= scale * scale;
   __syncthreads();
+  float pf[NB][NB][4];
+  polynomial_of<NB>(p, lds, pf);
 
-  const double a = p.a, b = p.b, c = p.c;
-  auto plain = [](double v, int, int) { return v; };
-  // A in m0; Q to m1; products over m2; P in m3 (after the first step)
-  for (int step = 0; step < p.steps; ++step) {
-    short_product(m0, m0, m1, r, [&](double v, int i, int j) { return fma(c, v, fma(b, m0[i][j], i == j ? a : 0.0)); });
-    if (step > 0) {
-      short_product(m1, m3, m2, r, plain);
-      for (int e = threadIdx.x; e < r * r; e += kThreads) m3[e / r][e % r] = m2[e / r][e % r];
-    } else {
-      for (int e = threadIdx.x; e < r * r; e += kThreads) m3[e / r][e % r] = m1[e / r][e % r];
+  const bool staged = ALONE && NB <= 2 && s.longer <= S::CHUNK;            // U still lies in LDS
+  if (!staged)
+    for (int e = t + s.r * S::PITCH; e < S::ROWS * S::PITCH; e += kThreads) u[e] = 0.0f;
+  for (int l = l0; l < l1; l += S::CHUNK) {
+    const int n = min(S::CHUNK, l1 - l);
+    if (!staged) {
+      stage<T, NB>(p, s, g, l, n, true, u);
+      __syncthreads();
+    }
+    // P U, 16 positions at a time, in place
+    for (int x = wave; x < (n + 15) / 16; x += 4) {
+      f32x4_t o[NB];
+#pragma unroll
+      for (int a = 0; a < NB; ++a) o[a] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int k = 0; k < NB; ++k)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float v = (float)((double)u[(16 * k + 4 * q + q4) * S::PITCH + 16 * x + i] * scale);
+#pragma unroll
+          for (int a = 0; a < NB; ++a) o[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(pf[a][k][q], v, o[a], 0, 0, 0);
+        }
+#pragma unroll
+      for (int a = 0; a < NB; ++a)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[(16 * a + 4 * q4 + e) * S::PITCH + 16 * x + i] = o[a][e];
     }
     __syncthreads();
-    if (step + 1 < p.steps) {
-      short_product(m1, m0, m2, r, plain);
-      short_product(m2, m1, m0, r, plain);
-    }
-  }
-  for (int e = threadIdx.x; e < r * r; e += kThreads) pf[e / r][e % r] = (float)m3[e / r][e % r];
-  __syncthreads();
-
-  // P U, a column of 128 per pair of threads, half of the rows each
-  constexpr int H = kShortSide / 2;
-  T* out = reinterpret_cast<T*>(p.out) + g * p.out_matrix;
-  for (int l = l0; l < l1; l += kChunk) {
-    const int n = min(kChunk, l1 - l);
-    stage<T>(p, s, g, l, n, true, scale, u);
-    __syncthreads();
-    const int x = threadIdx.x % kChunk, i0 = threadIdx.x / kChunk * H;
-    float o[H];
-#pragma unroll
-    for (int i = 0; i < H; ++i) o[i] = 0.0f;
-    if (x < n)
-      for (int j = 0; j < r; ++j) {
-        const float v = u[j][x];
-#pragma unroll
-        for (int i = 0; i < H; ++i) o[i] = fmaf(pf[min(i0 + i, r - 1)][j], v, o[i]);
-      }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < H; ++i)
-      if (i0 + i < r && x < n) u[i0 + i][x] = o[i];
-    __syncthreads();
-    for (int i = threadIdx.x; i < r * n; i += kThreads) {
-      int q, at;
-      if (s.tall) { at = i / r; q = i - at * r; } else { q = i / n; at = i - q * n; }
-      T* to = out + (s.tall ? (l + at) * p.out_row + q : q * p.out_row + l + at);
-      const float v = u[q][at];
-      put(to, p.m == nullptr ? v : fmaf(-p.step, v, p.keep * value(*to)));
-    }
+    unstage<T, NB>(p, s, g, l, n, u);
     __syncthreads();
   }
 }
@@ -360,31 +400,52 @@ hipError_t launch_orth_load(const OrthMatrices& p, const double* parts, const Or
   return hipGetLastError();
 }
 
-int orth_short_slices(int count, int longer) {
-  const int chunks = (longer + kChunk - 1) / kChunk;
-  if (chunks <= 8) return 1;
+namespace {
+int short_blocks(int r) { return (r + 15) / 16; }
+int short_chunk(int r) { return short_blocks(r) <= 2 ? Short<2>::CHUNK : Short<4>::CHUNK; }
+
+template <typename T, int NB> hipError_t launch_short_as(const OrthMatrices& p, const ShortShape& shape, double* grams, int slices, hipStream_t s) {
+  constexpr int kLds = Short<NB>::LDS;
+  static std::atomic<bool> configured{false};              // past the 64 KB default; setting the limit twice is harmless
+  if (!configured.load(std::memory_order_acquire)) {
+    for (const void* k : {reinterpret_cast<const void*>(orth_short_gram_kernel<T, NB>), reinterpret_cast<const void*>(orth_short_kernel<T, NB, true>),
+                          reinterpret_cast<const void*>(orth_short_kernel<T, NB, false>)}) {
+      hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+      if (e != hipSuccess) return e;
+    }
+    configured.store(true, std::memory_order_release);
+  }
+  const dim3 grid((unsigned)slices, (unsigned)p.count);
+  if (slices == 1) {
+    hipLaunchKernelGGL((orth_short_kernel<T, NB, true>), grid, dim3(kThreads), kLds, s, p, shape, grams, slices);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((orth_short_gram_kernel<T, NB>), grid, dim3(kThreads), kLds, s, p, shape, grams, slices);
+  hipLaunchKernelGGL((orth_short_kernel<T, NB, false>), grid, dim3(kThreads), kLds, s, p, shape, grams, slices);
+  return hipGetLastError();
+}
+template <typename T> hipError_t launch_short(const OrthMatrices& p, const ShortShape& shape, double* grams, int slices, hipStream_t s) {
+  switch (short_blocks(shape.r)) {
+    case 1: return launch_short_as<T, 1>(p, shape, grams, slices, s);
+    case 2: return launch_short_as<T, 2>(p, shape, grams, slices, s);
+    case 3: return launch_short_as<T, 3>(p, shape, grams, slices, s);
+    default: return launch_short_as<T, 4>(p, shape, grams, slices, s);
+  }
+}
+}  // namespace
+
+size_t orth_short_doubles(int r) { return (size_t)short_blocks(r) * short_blocks(r) * 256; }
+int orth_short_slices(int count, int r, int longer) {
+  const int chunks = (longer + short_chunk(r) - 1) / short_chunk(r);
   int slices = (512 + count - 1) / count;
   if (slices > 16) slices = 16;
-  if (slices > chunks / 4) slices = chunks / 4;
-  return slices < 1 ? 1 : slices;
+  if (slices > chunks) slices = chunks;
+  return chunks <= 2 || slices < 2 ? 1 : slices;
 }
 
 hipError_t launch_orth_short(const OrthMatrices& p, double* grams, int slices, hipStream_t s) {
   const ShortShape shape{p.rows < p.cols ? p.rows : p.cols, p.rows < p.cols ? p.cols : p.rows, p.rows > p.cols};
-  const dim3 grid((unsigned)slices, (unsigned)p.count);
-  if (slices == 1) {
-    if (p.bf16) hipLaunchKernelGGL((orth_short_kernel<uint16_t, true>), grid, dim3(kThreads), 0, s, p, shape, grams, slices);
-    else hipLaunchKernelGGL((orth_short_kernel<float, true>), grid, dim3(kThreads), 0, s, p, shape, grams, slices);
-    return hipGetLastError();
-  }
-  if (p.bf16) {
-    hipLaunchKernelGGL(orth_short_gram_kernel<uint16_t>, grid, dim3(kThreads), 0, s, p, shape, grams, slices);
-    hipLaunchKernelGGL((orth_short_kernel<uint16_t, false>), grid, dim3(kThreads), 0, s, p, shape, grams, slices);
-  } else {
-    hipLaunchKernelGGL(orth_short_gram_kernel<float>, grid, dim3(kThreads), 0, s, p, shape, grams, slices);
-    hipLaunchKernelGGL((orth_short_kernel<float, false>), grid, dim3(kThreads), 0, s, p, shape, grams, slices);
-  }
-  return hipGetLastError();
+  return p.bf16 ? launch_short<uint16_t>(p, shape, grams, slices, s) : launch_short<float>(p, shape, grams, slices, s);
 }
 
 }  // namespace prsgd

@@ -5,17 +5,14 @@
 #include <atomic>
 #include <type_traits>
 
-#include "prsgd_internal.h"
-#include "prsgd_ops_internal.h"
+#include "orth_rows.h"
 
 namespace prsgd {
 
 namespace {
 
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
-typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
-template <int ES> struct __attribute__((packed, aligned(ES))) Packed16 { u32x4_t v; };
 
 __device__ __forceinline__ float half_value(uint16_t h) { return (float)__builtin_bit_cast(_Float16, h); }
 __device__ __forceinline__ uint16_t half_bits(float f) { return __builtin_bit_cast(uint16_t, (_Float16)f); }
@@ -107,55 +104,6 @@ template <int ROWS, bool SPLIT> struct ColumnFragments {
     return __builtin_bit_cast(f16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   }
 };
-
-// Eight consecutive values of the result at row i, columns j.. of the caller's matrix, n of them inside it.
-template <typename T> __device__ __forceinline__ void user_store(const OrthMatrices& u, int64_t at_out, int n, const float* v) {
-  T* out = reinterpret_cast<T*>(u.out) + at_out;
-  float r[8];
-  if (u.m != nullptr) {                    // the parameters' update
-    if (n >= 8) {
-      if constexpr (sizeof(T) == 4) {
-        const u32x4_t lo = reinterpret_cast<const Packed16<4>*>(out)->v, hi = reinterpret_cast<const Packed16<4>*>(out + 4)->v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { r[e] = __uint_as_float(lo[e]); r[4 + e] = __uint_as_float(hi[e]); }
-      } else {
-        const u32x4_t x = reinterpret_cast<const Packed16<2>*>(out)->v;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) r[e] = __uint_as_float((e & 1) != 0 ? x[e / 2] & 0xFFFF0000u : x[e / 2] << 16);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if constexpr (sizeof(T) == 4) r[e] = e < n ? out[e] : 0.0f;
-        else r[e] = e < n ? bf16_to_f32(out[e]) : 0.0f;
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = fmaf(-u.step, v[e], u.keep * r[e]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = v[e];
-  }
-  if constexpr (sizeof(T) == 4) {
-    if (n >= 8) {
-      reinterpret_cast<Packed16<4>*>(out)->v = (u32x4_t){__float_as_uint(r[0]), __float_as_uint(r[1]), __float_as_uint(r[2]), __float_as_uint(r[3])};
-      reinterpret_cast<Packed16<4>*>(out + 4)->v = (u32x4_t){__float_as_uint(r[4]), __float_as_uint(r[5]), __float_as_uint(r[6]), __float_as_uint(r[7])};
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < n) out[e] = r[e];
-    }
-  } else {
-    const u32x4_t w = {f32x2_to_bf16x2_rne(r[0], r[1]), f32x2_to_bf16x2_rne(r[2], r[3]), f32x2_to_bf16x2_rne(r[4], r[5]), f32x2_to_bf16x2_rne(r[6], r[7])};
-    if (n >= 8) {
-      reinterpret_cast<Packed16<2>*>(out)->v = w;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < n) out[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
-    }
-  }
-}
 
 constexpr int strip_pitch(int columns) { return columns + 8; }     // the four rows between a register's two halves lie 32 banks apart
 template <int BM, int BN, int S, int RB> constexpr int square_lds_bytes(int wm, int wn) {
@@ -337,7 +285,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) square_kernel(const SquareArg
       if constexpr (EPI == SQ_LAST) {
         if (!p.transposed && inside) {
           const int64_t o = g * p.user.out_matrix + r * p.user.out_row + c;
-          user_store<User>(p.user, o, p.N - c, v);
+          result8<User>(p.user, o, p.N - c, v);
         }
       } else if (r < p.M && hc < p.ldo) {
         u32x4_t hi, lo;
@@ -362,7 +310,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) square_kernel(const SquareArg
         if constexpr (EPI == SQ_LAST) {
           if (r < p.M) {
             const int64_t o = g * p.user.out_matrix + c * p.user.out_row + r;
-            user_store<User>(p.user, o, p.M - r, v);
+            result8<User>(p.user, o, p.M - r, v);
           }
         } else {
           const int hr = half_col<SPLIT>(r);

@@ -129,8 +129,8 @@ OrthPlan orth_plan(const prsgd_orth_config* c) {
 bool is_short(const prsgd_orth_config* c) { return c->rows <= kShortSide || c->cols <= kShortSide; }
 size_t short_bytes(const prsgd_orth_config* c) {
   const int r = c->rows < c->cols ? c->rows : c->cols, longer = c->rows < c->cols ? c->cols : c->rows;
-  const int slices = orth_short_slices(c->count, longer);
-  return align256(slices == 1 ? 256 : (size_t)c->count * slices * r * r * sizeof(double));
+  const int slices = orth_short_slices(c->count, r, longer);
+  return align256(slices == 1 ? 256 : (size_t)c->count * slices * orth_short_doubles(r) * sizeof(double));
 }
 
 hipError_t run_squares(const prsgd_orth_config* c, const OrthMatrices& m, char* ws, hipStream_t s) {
@@ -210,7 +210,7 @@ int run_orth(const prsgd_orth_config* c, OrthMatrices m, void* ws, void* stream,
   m.steps = c->steps;
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (is_short(c)) {
-    const int slices = orth_short_slices(c->count, c->rows < c->cols ? c->cols : c->rows);
+    const int slices = c->rows < c->cols ? orth_short_slices(c->count, c->rows, c->cols) : orth_short_slices(c->count, c->cols, c->rows);
     return hip_result(launch_orth_short(m, reinterpret_cast<double*>(ws), slices, s), what);
   }
   return hip_result(run_squares(c, m, reinterpret_cast<char*>(ws), s), what);

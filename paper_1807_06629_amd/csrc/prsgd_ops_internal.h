@@ -35,7 +35,7 @@ hipError_t launch_rms_norm_backward(NormArgs p, float* shares, int workers, bool
 // ---- orthogonalised updates ------------------------------------------------------------------
 
 constexpr int kMaxOrthSide = 32768, kMaxOrthSteps = 64;
-constexpr int kShortSide = 32;           // a side up to here goes through its Gram matrix in 64 bits
+constexpr int kShortSide = 64;           // a side up to here goes through its Gram matrix in 64 bits
 // Workgroups that sum a matrix's squares: enough to fill the device where a matrix is large.
 constexpr int kMaxNormParts = 256;
 constexpr int norm_parts(int rows, int cols) { return (int64_t)rows * cols < (1 << 20) ? 64 : kMaxNormParts; }
@@ -87,8 +87,9 @@ hipError_t launch_orth_squares(const OrthMatrices& p, double* parts, hipStream_t
 // X [half_rows(short side)][ld_x]; spare: where the next one goes, whose padding rows are cleared with it
 struct OrthHalves { uint16_t* x; uint16_t* x_lo; uint16_t* spare; int64_t x_gs; int ld_x; };
 hipError_t launch_orth_load(const OrthMatrices& p, const double* parts, const OrthHalves& h, hipStream_t s);
-// Short sides: slices of the long side a matrix is cut into (1: one launch), and the doubles of their Gram matrices.
-int orth_short_slices(int count, int longer);
+// Short sides: slices of the long side a matrix is cut into (1: one launch), and the doubles of a slice's Gram matrix.
+int orth_short_slices(int count, int r, int longer);
+size_t orth_short_doubles(int r);
 hipError_t launch_orth_short(const OrthMatrices& p, double* grams, int slices, hipStream_t s);
 
 }  // namespace prsgd

@@ -190,7 +190,7 @@ def test_results_do_not_change_from_run_to_run(P):
 
 
 def test_a_workspace_that_is_too_small_is_refused(P):
-    g = _matrices(2, 64, 64, F32)
+    g = _matrices(2, 80, 80, F32)
     with pytest.raises(ValueError):
         P.prsgd_orthogonalize(g, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
     with pytest.raises(ValueError):
