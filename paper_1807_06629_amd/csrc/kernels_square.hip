@@ -105,6 +105,36 @@ template <int ROWS, bool SPLIT> struct ColumnFragments {
   }
 };
 
+// Order of a matrix's tiles: strips kStrip tiles high, column by column, so that the tiles that an XCD works on at a time share more of
+// their operands in its L2 (of 32 tiles 4 rows and 8 columns, against 2 and 16 row by row).
+constexpr int kStrip = 4;
+__device__ __forceinline__ void strip_tile(int in, int tiles_m, int tiles_n, int* ti, int* tj) {
+  const int strip = in / (kStrip * tiles_n), first = strip * kStrip, high = min(kStrip, tiles_m - first), rest = in - first * tiles_n;
+  *tj = rest / high;
+  *ti = first + rest - *tj * high;
+}
+// The same over the squares on and below the diagonal, R tiles each.  Returns whether the tile's transpose is written too.
+template <int R> __device__ __forceinline__ bool triangle_tile(int in, int squares, int* ti, int* tj) {
+  int rest = in / R, first = 0, high = min(kStrip, squares);
+  while (rest >= high * first + high * (high + 1) / 2) {   // squares of the strip's rows
+    rest -= high * first + high * (high + 1) / 2;
+    first += kStrip;
+    high = min(kStrip, squares - first);
+  }
+  int row, col = rest / high;
+  if (col < first) {
+    row = first + rest - col * high;
+  } else {                                                 // the triangle at the strip's end
+    rest -= first * high;
+    col = first;
+    for (int left = high; rest >= left; --left, ++col) rest -= left;
+    row = col + rest;
+  }
+  *ti = row * R + in % R;
+  *tj = col;
+  return row != col;
+}
+
 constexpr int strip_pitch(int columns) { return columns + 8; }     // the four rows between a register's two halves lie 32 banks apart
 template <int BM, int BN, int S, int RB> constexpr int square_lds_bytes(int wm, int wn) {
   const int stages = S * (BM + BN) * RB, strips = wm * wn * 32 * strip_pitch(BN / wn) * 4;
@@ -123,6 +153,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) square_kernel(const SquareArg
   constexpr int PER = ReqA::NPT + ReqB::NPT, R = BN / BM;
   static_assert(!SYMMETRIC || BN % BM == 0, "tiles of a symmetric result");
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  fetch_kernel_args<sizeof(SquareArgs)>();
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
 
@@ -131,21 +162,34 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) square_kernel(const SquareArg
   const int idx = xcd * (total >> 3) + min(xcd, total & 7) + (blockIdx.x >> 3);
   const int g = idx / p.tiles, in = idx - g * p.tiles;
   int ti, tj;
-  bool mirrored = false;
-  if (SYMMETRIC) {                         // squares of BN x BN on and below the diagonal, R tiles each
-    const int sq = in / R;
-    ti = (int)((sqrtf(8.0f * (float)sq + 1.0f) - 1.0f) * 0.5f);
-    while (ti * (ti + 1) / 2 > sq) --ti;
-    while ((ti + 1) * (ti + 2) / 2 <= sq) ++ti;
-    tj = sq - ti * (ti + 1) / 2;
-    mirrored = ti != tj;
-    ti = ti * R + in % R;
-    if (ti * BM >= p.M) return;
-  } else {
-    ti = in / p.tiles_n;
-    tj = in - ti * p.tiles_n;
-  }
+  const bool mirrored = SYMMETRIC ? triangle_tile<R>(in, p.tiles_n, &ti, &tj) : false;
+  if (!SYMMETRIC) strip_tile(in, (p.M + BM - 1) / BM, p.tiles_n, &ti, &tj);
+  if (SYMMETRIC && ti * BM >= p.M) return;
   const int m0 = ti * BM, n0 = tj * BN;
+
+  // Strips of the epilogue: columns, pitch, 8-value vectors of a row, rows per pass
+  constexpr int W = BN / WN, P = strip_pitch(W), VPR = W / 8, RPP = 64 / VPR, PASSES = 32 / RPP;
+  const int c0 = n0 + wn * W;
+  // what the epilogue adds to the product at pass q of strip i
+  struct Linear { u32x4_t hi, lo; };
+  auto linear = [&](int i, int q) __attribute__((always_inline)) {
+    Linear v = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    const int r = m0 + (wm * TM + i) * 32 + q * RPP + lane / VPR, c = c0 + lane % VPR * 8;
+    if (EPI != SQ_GRAM && r < p.M && c < p.N) {
+      const int64_t o = g * p.lin_gs + (int64_t)r * p.ld_lin + half_col<SPLIT>(c);
+      v.hi = *reinterpret_cast<const u32x4_t*>(p.lin + o);
+      if (SPLIT) v.lo = *reinterpret_cast<const u32x4_t*>(p.lin + o + kGroup);
+      else if (EPI != SQ_POLY) v.lo = *reinterpret_cast<const u32x4_t*>(p.lin_lo + o);
+    }
+    return v;
+  };
+  // A workgroup with a single strip per wavefront asks for all of that first: behind the products it would wait for it once more.
+  constexpr bool AHEAD = TM == 1 && PASSES <= 2;
+  Linear ahead[AHEAD ? PASSES : 1];
+  if constexpr (AHEAD) {
+#pragma unroll
+    for (int q = 0; q < PASSES; ++q) ahead[q] = linear(0, q);
+  }
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
   const uint16_t* a = p.a + g * p.a_gs + (int64_t)m0 * p.lda;
@@ -241,9 +285,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) square_kernel(const SquareArg
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 
   // Epilogue: a wavefront passes strips of 32 rows through LDS, first along the rows and then, as transposes, along the columns.
-  constexpr int W = BN / WN, P = strip_pitch(W), VPR = W / 8, RPP = 64 / VPR;      // strip columns, pitch, 8-value vectors of a row, rows per pass
   float* strip = reinterpret_cast<float*>(smem) + wave * 32 * P;
-  const int c0 = n0 + wn * W;
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     const int r0 = m0 + (wm * TM + i) * 32;
@@ -252,8 +294,8 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) square_kernel(const SquareArg
 #pragma unroll
       for (int e = 0; e < 16; ++e) strip[(8 * (e / 4) + 4 * (lane >> 5) + (e % 4)) * P + j * 32 + (lane & 31)] = acc[i][j][e];
     __builtin_amdgcn_wave_barrier();
-#pragma unroll(EPI == SQ_LAST ? 1 : 32 / RPP)
-    for (int q = 0; q < 32 / RPP; ++q) {
+#pragma unroll(EPI == SQ_LAST && !AHEAD ? 1 : PASSES)
+    for (int q = 0; q < PASSES; ++q) {
       const int lr = q * RPP + lane / VPR, lc = lane % VPR * 8, r = r0 + lr, c = c0 + lc;
       float* at = strip + lr * P + lc;
       float v[8];
@@ -266,15 +308,11 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) square_kernel(const SquareArg
       const bool inside = r < p.M && c < p.N;
       const int hc = half_col<SPLIT>(c);
       if constexpr (EPI != SQ_GRAM) {
-        u32x4_t hi = {0, 0, 0, 0}, lo = {0, 0, 0, 0};
-        if (inside) {
-          const int64_t o = g * p.lin_gs + (int64_t)r * p.ld_lin + hc;
-          hi = *reinterpret_cast<const u32x4_t*>(p.lin + o);
-          if (SPLIT) lo = *reinterpret_cast<const u32x4_t*>(p.lin + o + kGroup);
-          else if (EPI != SQ_POLY) lo = *reinterpret_cast<const u32x4_t*>(p.lin_lo + o);
-        }
+        Linear x;
+        if constexpr (AHEAD) x = ahead[q];
+        else x = linear(i, q);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = fmaf(p.alpha, half_at(hi, e) + half_at(lo, e), p.beta * v[e]);
+        for (int e = 0; e < 8; ++e) v[e] = fmaf(p.alpha, half_at(x.hi, e) + half_at(x.lo, e), p.beta * v[e]);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= p.beta;
@@ -345,16 +383,12 @@ template <int BM, int BN, int WM, int WN, int S, int RB, bool SPLIT, int EPI> hi
   hipLaunchKernelGGL(kernel, dim3((unsigned)p.tiles * (unsigned)p.count), dim3(64 * WM * WN), kLds, s, p);
   return hipGetLastError();
 }
-template <int BM, int BN, int WM, int WN, int S, int RB> hipError_t launch_tile(const SquareArgs& p, int epi, bool split, hipStream_t s) {
-  switch (epi * 2 + (split ? 1 : 0)) {
-    case 0: return launch_as<BM, BN, WM, WN, S, RB, false, SQ_GRAM>(p, s);
-    case 1: return launch_as<BM, BN, WM, WN, S, RB, true, SQ_GRAM>(p, s);
-    case 2: return launch_as<BM, BN, WM, WN, S, RB, false, SQ_POLY>(p, s);
-    case 3: return launch_as<BM, BN, WM, WN, S, RB, true, SQ_POLY>(p, s);
-    case 4: return launch_as<BM, BN, WM, WN, S, RB, false, SQ_NEXT>(p, s);
-    case 5: return launch_as<BM, BN, WM, WN, S, RB, true, SQ_NEXT>(p, s);
-    case 6: return launch_as<BM, BN, WM, WN, S, RB, false, SQ_LAST>(p, s);
-    default: return launch_as<BM, BN, WM, WN, S, RB, true, SQ_LAST>(p, s);
+template <int BM, int BN, int WM, int WN, int S, int RB, bool SPLIT> hipError_t launch_tile(const SquareArgs& p, int epi, hipStream_t s) {
+  switch (epi) {
+    case SQ_GRAM: return launch_as<BM, BN, WM, WN, S, RB, SPLIT, SQ_GRAM>(p, s);
+    case SQ_POLY: return launch_as<BM, BN, WM, WN, S, RB, SPLIT, SQ_POLY>(p, s);
+    case SQ_NEXT: return launch_as<BM, BN, WM, WN, S, RB, SPLIT, SQ_NEXT>(p, s);
+    default: return launch_as<BM, BN, WM, WN, S, RB, SPLIT, SQ_LAST>(p, s);
   }
 }
 
@@ -368,10 +402,16 @@ hipError_t launch_square(SquareArgs p, int epi, bool split, hipStream_t s) {
     const int64_t tiles = (symmetric ? tn * (tn + 1) / 2 * (bn / bm) : tm * tn) * p.count;
     return (double)((tiles + 255) / 256) * (bm / 64) * (bn / 64) / efficiency;
   };
-  const double large = cost(128, 256, 1.0), middle = cost(128, 128, 0.8), small = cost(64, 64, 0.5);
-  if (!split && large <= middle && large <= small) return launch_tile<128, 256, 2, 2, 3, 64>(p, epi, split, s);
-  if (middle <= small) return launch_tile<128, 128, 2, 2, 3, 64>(p, epi, split, s);
-  return launch_tile<64, 64, 2, 2, 4, 128>(p, epi, split, s);
+  const double huge = cost(256, 256, 1.15), large = cost(128, 256, 1.0), middle = cost(128, 128, 0.8), small = cost(64, 64, 0.5);
+  if (split) {
+    // 128 x 256 would not leave a split product the registers for two workgroups per compute unit
+    if (middle <= small) return launch_tile<128, 128, 2, 2, 3, 64, true>(p, epi, s);
+    return launch_tile<64, 64, 2, 2, 4, 128, true>(p, epi, s);
+  }
+  if (huge <= large && huge <= middle && huge <= small) return launch_tile<256, 256, 4, 2, 2, 128, false>(p, epi, s);
+  if (large <= middle && large <= small) return launch_tile<128, 256, 2, 2, 3, 64, false>(p, epi, s);
+  if (middle <= small) return launch_tile<128, 128, 2, 2, 3, 64, false>(p, epi, s);
+  return launch_tile<64, 64, 2, 2, 4, 128, false>(p, epi, s);
 }
 
 }  // namespace prsgd
