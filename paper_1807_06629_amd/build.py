@@ -1,17 +1,19 @@
-"""Builds libprsgd.so (HIP, gfx950 only) in-tree with hipcc.
+"""Builds libprsgd.so (HIP, gfx950 only) in-tree with hipcc, and the Python module of its operators with g++.
 
     python -m paper_1807_06629_amd.build
 
 Each translation unit under csrc/ is compiled to an object in _build/ and the objects are
-linked into paper_1807_06629_amd/libprsgd.so.  Packed-FP32 instruction selection is turned off
+linked into paper_1807_06629_amd/libprsgd.so; csrc/binding becomes paper_1807_06629_amd/_ops.so beside it.  Packed-FP32 instruction selection is turned off
 for all device code.
 """
 from __future__ import annotations
 
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -19,6 +21,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libprsgd.so")
+BINDING = os.path.join(HERE, "_ops.so")
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
@@ -44,6 +47,18 @@ def _run(cmd):
     return out
 
 
+def _build_binding() -> str:
+    """Torch tensors to the operators' C calls: host code only, linked to the libprsgd.so beside it."""
+    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    return _run([shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+                 "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1", "-I", os.path.join(ROOT, "include"),
+                 "-I", sysconfig.get_paths()["include"], "-I", os.path.join(torch, "include"),
+                 "-I", os.path.join(torch, "include", "torch", "csrc", "api", "include"), "-I", os.path.join(rocm, "include"),
+                 os.path.join(CSRC, "binding", "ops_binding.cpp"), "-o", BINDING, "-L", os.path.join(torch, "lib"),
+                 "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip", "-L", HERE, "-l:libprsgd.so", "-Wl,-rpath,$ORIGIN"])
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     hipcc = _hipcc()
@@ -59,6 +74,9 @@ def build(verbose: bool = False) -> str:
             if verbose and log.strip():
                 print(log)
     log = _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objects])
+    if verbose and log.strip():
+        print(log)
+    log = _build_binding()
     if verbose and log.strip():
         print(log)
     return LIB

@@ -11,7 +11,6 @@ from __future__ import annotations
 import ctypes
 import os
 from dataclasses import dataclass
-from functools import lru_cache
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -132,6 +131,10 @@ def _load() -> ctypes.CDLL:
 
 
 _lib = _load()
+try:
+    from . import _ops
+except ImportError as e:
+    raise ImportError("_ops.so does not load; run `python -m paper_1807_06629_amd.build`") from e
 
 
 def make_config(n_workers: int, model: str, dims: Sequence[int], batch: int, rows_per_worker: int,
@@ -442,76 +445,25 @@ def prsgd_last_error(h: Optional[Handle]) -> str:
 # ---- operators on replica sets (include/prsgd_ops.h) ---------------------------------------------------------------
 # Tensors are taken as they are: rows have to be contiguous, distances between rows and matrices are read off the strides.
 # Work goes to the current stream of the tensors' device.  Outputs and workspaces that are not given are allocated.
-# What only depends on sizes and options (the configuration, its workspace) is made once per set of them: a call on a few
-# rows is otherwise bound by this marshalling.
+# The marshalling is compiled (csrc/binding): ValueError for a tensor that no call takes, PrsgdError for what the library refuses.
 
 NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
-_DTYPES = {torch.float32: PRSGD_F32, torch.bfloat16: PRSGD_BF16}
-_FP8 = torch.float8_e4m3fn
-_current_device = torch._C._cuda_getDevice
-_current_stream = torch._C._cuda_getCurrentRawStream
-
-
-def _enqueue(device: int, fn, *args) -> None:
-    if device == _current_device():
-        rc = fn(*args, _current_stream(device))
-    else:
-        with torch.cuda.device(device):
-            rc = fn(*args, _current_stream(device))
-    if rc != PRSGD_OK:
-        _check(rc)
-
-
-def _workspace(given: Optional[torch.Tensor], nbytes: int, like: torch.Tensor) -> torch.Tensor:
-    if given is None:
-        given = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
-    elif given.device != like.device or given.numel() * given.element_size() < nbytes:
-        raise ValueError("the workspace must have %d bytes on %s" % (nbytes, like.device))
-    return given
-
-
-def _matrices(t: torch.Tensor, like: torch.Tensor, name: str, dtype: torch.dtype):
-    """Address, distance between matrices and distance between rows of a [count][rows][cols] or [rows][cols] tensor."""
-    if not t.is_cuda or t.dtype != dtype or (t is not like and (t.get_device() != like.get_device() or t.shape != like.shape)):
-        raise ValueError("%s must be a %s device tensor of shape %s" % (name, dtype, tuple(like.shape)))
-    st = t.stride()
-    if st[-1] != 1 and t.shape[-1] > 1:
-        raise ValueError("rows of %s must be contiguous" % name)
-    return t.data_ptr(), st[0] if len(st) == 3 else 0, st[-2]
-
-
-@lru_cache(maxsize=1024)
-def _orth_plan(dtype: torch.dtype, shape, coefficients, steps: int, eps: float):
-    """Configuration by reference, and the bytes of its workspace."""
-    if dtype not in _DTYPES:
-        raise ValueError("matrices must be float32 or bfloat16")
-    if len(shape) not in (2, 3):
-        raise ValueError("matrices must be [count][rows][cols] or [rows][cols]")
-    a, b, c = coefficients
-    cfg = prsgd_orth_config(_DTYPES[dtype], shape[0] if len(shape) == 3 else 1, shape[-2], shape[-1], int(steps), a, b, c, eps)
-    n = int(_lib.prsgd_orthogonalize_workspace_bytes(ctypes.byref(cfg)))
-    if n == 0 and cfg.count != 0:
-        raise PrsgdError(PRSGD_EINVAL, _lib.prsgd_last_error(None).decode())
-    return ctypes.byref(cfg), n
+_ops.bind(_check)
 
 
 def prsgd_orthogonalize_workspace_bytes(shape: Sequence[int], dtype: torch.dtype, coefficients=NEWTON_SCHULZ, steps: int = 5,
                                         eps: float = 1e-7) -> int:
     """Of prsgd_orthogonalize and prsgd_muon_step on [count][rows][cols] or [rows][cols] matrices."""
-    return _orth_plan(dtype, tuple(shape), tuple(coefficients), steps, eps)[1]
+    if dtype not in (torch.float32, torch.bfloat16) or len(shape) not in (2, 3):
+        raise ValueError("matrices must be [count][rows][cols] or [rows][cols], float32 or bfloat16")
+    return _ops.orthogonalize_bytes(shape[0] if len(shape) == 3 else None, shape[-2], shape[-1], dtype == torch.bfloat16,
+                                    coefficients, steps, eps)
 
 
 def prsgd_orthogonalize(g: torch.Tensor, out: Optional[torch.Tensor] = None, coefficients=NEWTON_SCHULZ, steps: int = 5,
                         eps: float = 1e-7, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Newton-Schulz orthogonalisation of every [rows][cols] matrix of g (out may be g)."""
-    cfg, nbytes = _orth_plan(g.dtype, g.shape, tuple(coefficients), steps, eps)
-    src = _matrices(g, g, "g", g.dtype)
-    if out is None:
-        out = torch.empty(g.shape, dtype=g.dtype, device=g.device)
-    dst = _matrices(out, g, "out", g.dtype)
-    ws = _workspace(workspace, nbytes, g)
-    _enqueue(g.get_device(), _lib.prsgd_orthogonalize, cfg, *src, *dst, ws.data_ptr())
-    return out
+    return _ops.orthogonalize(g, out, coefficients, steps, eps, workspace)
 
 
 def prsgd_muon_step(x: torch.Tensor, g: torch.Tensor, m: torch.Tensor, lr: float, momentum: float = 0.95, nesterov: bool = True,
@@ -520,83 +472,9 @@ def prsgd_muon_step(x: torch.Tensor, g: torch.Tensor, m: torch.Tensor, lr: float
     """Momentum, orthogonalisation and update of every [rows][cols] matrix of x, in place on x and m (fp32).
 
     scale defaults to 0.2 sqrt(max(rows, cols))."""
-    cfg, nbytes = _orth_plan(x.dtype, x.shape, tuple(coefficients), steps, eps)
-    xs, gs, ms = _matrices(x, x, "x", x.dtype), _matrices(g, x, "g", x.dtype), _matrices(m, x, "m", torch.float32)
     if scale is None:
         scale = 0.2 * max(x.shape[-2:]) ** 0.5
-    ws = _workspace(workspace, nbytes, x)
-    _enqueue(x.get_device(), _lib.prsgd_muon_step, cfg, *xs, *gs, *ms, lr, momentum, 1 if nesterov else 0, weight_decay, scale,
-             ws.data_ptr())
-
-
-@lru_cache(maxsize=1024)
-def _norm_plan(dtype: torch.dtype, shape, w_shape, eps: float):
-    """Configuration by reference, the bytes that the backward call works in, rows and width."""
-    if len(shape) != 2 or dtype not in _DTYPES:
-        raise ValueError("rows must be a [rows][width] device tensor of float32 or bfloat16")
-    if len(w_shape) not in (1, 2) or w_shape[-1] != shape[1]:
-        raise ValueError("weights must be [width] or [workers][width]")
-    workers = 1 if len(w_shape) == 1 else w_shape[0]
-    if workers == 0 or shape[0] % workers != 0:
-        raise ValueError("every worker must have the same number of rows")
-    cfg = prsgd_norm_config(_DTYPES[dtype], workers, shape[0] // workers, shape[1], eps)
-    n = int(_lib.prsgd_rms_norm_backward_workspace_bytes(ctypes.byref(cfg)))
-    if n == 0:
-        raise PrsgdError(PRSGD_EINVAL, _lib.prsgd_last_error(None).decode())
-    return ctypes.byref(cfg), n, shape[0], shape[1]
-
-
-def _norm_rows(t: torch.Tensor, like: torch.Tensor, name: str, dtype: torch.dtype):
-    """Address and distance between rows of a [rows][width] tensor."""
-    if not t.is_cuda or t.dtype != dtype or (t is not like and (t.get_device() != like.get_device() or t.shape != like.shape)):
-        raise ValueError("%s must be a %s device tensor of shape %s" % (name, dtype, tuple(like.shape)))
-    row, element = t.stride()
-    if element != 1 and t.shape[1] > 1:
-        raise ValueError("rows of %s must be contiguous" % name)
-    return t.data_ptr(), row if row >= t.shape[1] or t.shape[0] > 1 else t.shape[1]
-
-
-def _weight_rows(w: torch.Tensor, like: torch.Tensor, name: str):
-    """Address and distance between workers of [width] or [workers][width] weights (or their gradients)."""
-    st = w.stride()
-    if w.dtype != torch.float32 or w.get_device() != like.get_device() or (st[-1] != 1 and w.shape[-1] > 1):
-        raise ValueError("%s must be float32 on the device of the rows, its rows contiguous" % name)
-    return w.data_ptr(), st[0] if len(st) == 2 and w.shape[0] > 1 else 0
-
-
-def _row_vector(t: torch.Tensor, x: torch.Tensor, name: str) -> int:
-    if t.dtype != torch.float32 or t.get_device() != x.get_device() or t.shape != x.shape[:1] or not t.is_contiguous():
-        raise ValueError("%s must be %d contiguous floats" % (name, x.shape[0]))
-    return t.data_ptr()
-
-
-def _norm_forward(fn, x, w, residual, eps, out, out_dtype, sum_out, stat, stat_name):
-    dtype = x.dtype
-    cfg, _, rows, width = _norm_plan(dtype, x.shape, w.shape, eps)
-    x_at, x_row = _norm_rows(x, x, "x", dtype)
-    w_at, w_row = _weight_rows(w, x, "w")
-    r_at = r_row = s_at = s_row = 0
-    if residual is not None:
-        r_at, r_row = _norm_rows(residual, x, "residual", dtype)
-        if sum_out is None:
-            sum_out = torch.empty_like(x)
-            s_at, s_row = sum_out.data_ptr(), width
-    if sum_out is None:
-        sum_out = x
-    elif s_row == 0:
-        s_at, s_row = _norm_rows(sum_out, x, "sum_out", dtype)
-    if out is None:
-        out = torch.empty_like(x, dtype=out_dtype)
-        y_at, y_row = out.data_ptr(), width
-    else:
-        y_at, y_row = _norm_rows(out, x, "out", out_dtype)
-    if stat is None:
-        stat = x.new_empty(rows, dtype=torch.float32)
-        stat_at = stat.data_ptr()
-    else:
-        stat_at = _row_vector(stat, x, stat_name)
-    _enqueue(x.get_device(), fn, cfg, x_at, x_row, r_at, r_row, w_at, w_row, s_at, s_row, y_at, y_row, stat_at)
-    return out, sum_out, stat
+    _ops.muon_step(x, g, m, lr, momentum, nesterov, weight_decay, scale, coefficients, steps, eps, workspace)
 
 
 def prsgd_rms_norm(x: torch.Tensor, w: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
@@ -604,44 +482,23 @@ def prsgd_rms_norm(x: torch.Tensor, w: torch.Tensor, residual: Optional[torch.Te
                    rstd: Optional[torch.Tensor] = None):
     """(y, s, rstd) of s = x + residual, y = s rstd w for the rows of every worker ([workers * rows][width], w [workers][width] or
     [width]).  Without a residual s is x itself, and is written only if sum_out is given."""
-    return _norm_forward(_lib.prsgd_rms_norm, x, w, residual, eps, out, x.dtype, sum_out, rstd, "rstd")
+    return _ops.rms_norm(x, w, residual, eps, out, sum_out, rstd, False)
 
 
 def prsgd_rms_norm_fp8(x: torch.Tensor, w: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
                        out: Optional[torch.Tensor] = None, sum_out: Optional[torch.Tensor] = None,
                        scales: Optional[torch.Tensor] = None):
     """(q, scales, s): prsgd_rms_norm's y as q * scales[:, None], q in torch.float8_e4m3fn."""
-    q, s, scales = _norm_forward(_lib.prsgd_rms_norm_fp8, x, w, residual, eps, out, _FP8, sum_out, scales, "scales")
+    q, s, scales = _ops.rms_norm(x, w, residual, eps, out, sum_out, scales, True)
     return q, scales, s
 
 
 def prsgd_rms_norm_backward_workspace_bytes(x: torch.Tensor, w: torch.Tensor) -> int:
-    return _norm_plan(x.dtype, x.shape, w.shape, 0.0)[1]
+    return _ops.rms_norm_backward_bytes(x, w)
 
 
 def prsgd_rms_norm_backward(dy: torch.Tensor, s: torch.Tensor, rstd: torch.Tensor, w: torch.Tensor,
                             dsum: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
                             dw: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """(dx, dw) of prsgd_rms_norm: dx is the gradient of x and of the residual alike, dw has w's shape."""
-    dtype = dy.dtype
-    cfg, nbytes, _, width = _norm_plan(dtype, dy.shape, w.shape, 0.0)
-    dy_at, dy_row = _norm_rows(dy, dy, "dy", dtype)
-    s_at, s_row = _norm_rows(s, dy, "s", dtype)
-    w_at, w_row = _weight_rows(w, dy, "w")
-    ds_at, ds_row = (0, 0) if dsum is None else _norm_rows(dsum, dy, "dsum", dtype)
-    if dx is None:
-        dx = torch.empty_like(dy)
-        dx_at, dx_row = dx.data_ptr(), width
-    else:
-        dx_at, dx_row = _norm_rows(dx, dy, "dx", dtype)
-    if dw is None:
-        dw = torch.empty(w.shape, dtype=torch.float32, device=w.device)
-        dw_at, dw_row = dw.data_ptr(), width
-    else:
-        if dw.shape != w.shape:
-            raise ValueError("dw must have the shape of w")
-        dw_at, dw_row = _weight_rows(dw, dy, "dw")
-    work = _workspace(workspace, nbytes, dy)
-    _enqueue(dy.get_device(), _lib.prsgd_rms_norm_backward, cfg, dy_at, dy_row, ds_at, ds_row, s_at, s_row,
-             _row_vector(rstd, dy, "rstd"), w_at, w_row, dx_at, dx_row, dw_at, dw_row, work.data_ptr())
-    return dx, dw
+    return _ops.rms_norm_backward(dy, s, rstd, w, dsum, dx, dw, workspace)
