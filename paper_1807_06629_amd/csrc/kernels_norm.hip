@@ -5,6 +5,7 @@
 // A row is held in the registers of TPR threads, E elements each (fp32 once unpacked), so that every array crosses HBM once and
 // the row's one reduction is all that stands between its loads and its stores.  The row maximum of the 8-bit form needs no second
 // one: max |y| = rstd max |s w|.  Bound by HBM from a few thousand rows on, by the latency of a launch below.
+#include <algorithm>
 #include <type_traits>
 
 #include "prsgd_internal.h"
@@ -290,20 +291,25 @@ __global__ void __launch_bounds__(threads_of<TPR>()) rms_norm_back_kernel(NormAr
   }
 }
 
-// dw of a worker from its workgroups' shares: a workgroup has 64 columns, its four wavefronts a quarter of the shares each.
-__global__ void __launch_bounds__(kThreads) norm_dw_kernel(const float* shares, int64_t share_row, int blocks, float* dw,
-                                                           int64_t dw_row, int width) {
+// dw of a worker from its workgroups' shares: a workgroup has 64 columns, its sixteen wavefronts a run of the shares each, added in order.
+constexpr int kShareWaves = 16;
+__global__ void __launch_bounds__(64 * kShareWaves) norm_dw_kernel(const float* shares, int64_t share_row, int blocks, float* dw,
+                                                                   int64_t dw_row, int width) {
   const int lane = threadIdx.x & 63, part = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
   const float* from = shares + (int64_t)blockIdx.y * blocks * share_row + c;
   float v = 0.0f;
   if (c < width) {
-#pragma unroll 4
-    for (int b = blocks * part / 4; b < blocks * (part + 1) / 4; ++b) v += from[b * share_row];
+#pragma unroll 8
+    for (int b = blocks * part / kShareWaves; b < blocks * (part + 1) / kShareWaves; ++b) v += from[b * share_row];
   }
-  __shared__ float sums[4][64];
+  __shared__ float sums[kShareWaves][64];
   sums[part][lane] = v;
   __syncthreads();
-  if (part == 0 && c < width) dw[(int64_t)blockIdx.y * dw_row + c] = ((v + sums[1][lane]) + sums[2][lane]) + sums[3][lane];
+  if (part == 0 && c < width) {
+#pragma unroll
+    for (int i = 1; i < kShareWaves; ++i) v += sums[i][lane];
+    dw[(int64_t)blockIdx.y * dw_row + c] = v;
+  }
 }
 
 __global__ void __launch_bounds__(kThreads) norm_dw_zero_kernel(float* dw, int64_t dw_row, int width) {
@@ -372,15 +378,18 @@ hipError_t launch_rms_norm(const NormArgs& p, bool bf16, bool fp8, hipStream_t s
   return with_shape(r, [&](auto tpr, auto e) { return launch_forward<float, decltype(tpr)::value, decltype(e)::value>(p, fp8, s); });
 }
 
-// 1024 workgroups in all where the rows last: four per compute unit, and shares of dw that stay far below the rows' own bytes.
+// Four workgroups per compute unit in all, where that leaves eight rows to each: a share of dw is written and read once, 8 bytes per
+// column, against 8 (bf16) to 16 per column of a row.  (4000 rows of 8192 in bf16, one worker: 65 us at four rows, 47 at eight.)
+// Fewer rows where the device would be left empty otherwise (16 x 64 rows of 1024 in fp32: 64 workgroups 10.8 us, 256 8.5), but not so
+// few that the second launch is all that it adds (64 x 8 rows of 128: 5.9 us in one launch, 8.4 in two).
 int norm_back_blocks(int workers, int64_t rows_per_worker, int width, bool bf16) {
   if (rows_per_worker <= 0) return 0;
   const RowShape r = row_shape((int64_t)workers * rows_per_worker, width, bf16);
   const int slots = r.tpr >= kThreads ? 1 : kThreads / r.tpr;
   const int64_t passes = (rows_per_worker + slots - 1) / slots;
-  int64_t blocks = (1024 + workers - 1) / workers;
-  if (blocks > (passes + 3) / 4) blocks = (passes + 3) / 4;
-  return (int)blocks;
+  if (passes <= 4) return 1;
+  const int64_t most = std::min<int64_t>(passes, std::max<int64_t>((rows_per_worker + 7) / 8, (256 + workers - 1) / workers));
+  return (int)std::min<int64_t>(most, (1024 + workers - 1) / workers);
 }
 
 size_t norm_back_share_floats(int workers, int64_t rows_per_worker, int width, bool bf16) {
@@ -404,7 +413,7 @@ hipError_t launch_rms_norm_backward(NormArgs p, float* shares, int workers, bool
   hipError_t e = bf16 ? with_shape(r, [&](auto tpr, auto el) { return launch_backward<uint16_t, decltype(tpr)::value, decltype(el)::value>(p, workers, s); })
                       : with_shape(r, [&](auto tpr, auto el) { return launch_backward<float, decltype(tpr)::value, decltype(el)::value>(p, workers, s); });
   if (e != hipSuccess || p.blocks <= 1) return e;
-  hipLaunchKernelGGL(norm_dw_kernel, dim3((p.width + 63) / 64, workers), dim3(kThreads), 0, s, shares, p.dw_row, p.blocks, dw, dw_row, p.width);
+  hipLaunchKernelGGL(norm_dw_kernel, dim3((p.width + 63) / 64, workers), dim3(64 * kShareWaves), 0, s, shares, p.dw_row, p.blocks, dw, dw_row, p.width);
   return hipGetLastError();
 }
 
