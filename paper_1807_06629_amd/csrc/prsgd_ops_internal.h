@@ -25,8 +25,9 @@ struct NormArgs {
   int width;
   float eps;
   int blocks;                            // backward: workgroups per worker
+  bool streamed;                         // rows past the caches (filled in by the launcher)
 };
-hipError_t launch_rms_norm(const NormArgs& p, bool bf16, bool fp8, hipStream_t s);
+hipError_t launch_rms_norm(NormArgs p, bool bf16, bool fp8, hipStream_t s);
 // Workgroups per worker of the backward pass, and the floats of their shares of dw (0: a workgroup has its worker's rows to itself).
 int norm_back_blocks(int workers, int64_t rows_per_worker, int width, bool bf16);
 size_t norm_back_share_floats(int workers, int64_t rows_per_worker, int width, bool bf16);
