@@ -200,8 +200,8 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) square_kernel(const SquareArg
   ra.set(p.lda, p.M - m0, wave, lane);
   rb.set(p.ldb, TRANS ? p.ldb - half_col<SPLIT>(n0) : p.N - n0, wave, lane);
   const int n_k = p.lda * 2 / RB;
-  auto request = [&](int t, int first, int last) __attribute__((always_inline)) {
-    const uint32_t stage = lds0 + (uint32_t)(t % S) * STAGE;
+  auto request = [&](int t, int place, int first, int last) __attribute__((always_inline)) {       // place: t mod S
+    const uint32_t stage = lds0 + (uint32_t)place * STAGE;
 #pragma unroll
     for (int q = first; q < last; ++q) {
       if (q < ReqA::NPT) ra.request(a + t * (RB / 2), stage, q, wave);
@@ -234,16 +234,18 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) square_kernel(const SquareArg
   // unit's one path to its cache).
 #pragma unroll
   for (int t = 0; t < S; ++t)
-    if (t < n_k) request(t, 0, PER);
+    if (t < n_k) request(t, t, 0, PER);
   if (n_k >= S) wait_requests<(S - 1) * PER>(); else wait_requests<0>();
   asm volatile("s_barrier" ::: "memory");
 #pragma unroll
   for (int q = 0; q < READS; ++q) load(smem, 0, 0, q);
   // set0: the fragments' set of the tile's first slice
+  int place = 0;
   auto step = [&](int t, auto set0_, auto whole_) __attribute__((always_inline)) {
     constexpr bool WHOLE = decltype(whole_)::value;        // every tile that the step asks for exists
-    const unsigned char* here = smem + (t % S) * STAGE;
-    const unsigned char* next = smem + ((t + 1) % S) * STAGE;
+    const int behind = place + 1 == S ? 0 : place + 1;
+    const unsigned char* here = smem + place * STAGE;
+    const unsigned char* next = smem + behind * STAGE;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
       const int set = (decltype(set0_)::value + kk) & 1;
@@ -266,10 +268,11 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) square_kernel(const SquareArg
             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[set][1][i], fb[set][0][j], acc[i][j], 0, 0, 0);
           }
         }
-        if (last && (WHOLE || t + S < n_k)) request(t + S, i * PER / TM, (i + 1) * PER / TM);
+        if (last && (WHOLE || t + S < n_k)) request(t + S, place, i * PER / TM, (i + 1) * PER / TM);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
+    place = behind;
   };
   using Set0 = std::integral_constant<int, 0>;
   using Set1 = std::integral_constant<int, KK & 1>;        // of odd tiles
