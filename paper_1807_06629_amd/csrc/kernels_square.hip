@@ -2,6 +2,13 @@
 // operands' rows are contiguous along the contraction, and B X, whose second operand is read out of LDS as its transpose.  Symmetric results
 // compute the tiles on and below the diagonal and write the others as transposes.  Split operands hold a second half per entry (22 bits); a tile then takes three products,
 // lead x lead and the two crossed ones, of the same fragments.
+// What is multiplied is held to 11 bits (22 if split), what is added (a X) to 22 either way: a rounding of the linear term is carried on
+// and grows as the smallest singular values do, 3.4445 per step, one in a factor of B X only turns singular vectors.  (Updates of rank
+// 32 at 512 x 512: error of the result 6e-4 so, 3e-2 with X in 11 bits throughout, 0.2 in bfloat16.)
+// Bound by the matrix cores and their power where matrices are large: 8 x 4096 x 4096 in half precision, B X 1084 us (1014 TFLOP/s, at 1.55 GHz;
+// a library's batched product of that size 1100), X X^T 581 us for 136 of 256 tiles (5 rounds of 256 where 4.25 would do).  16 x 1024 x 1024
+// split, B X 107 us: 965 TFLOP/s of the three products.  Bound by latency where they are small: no launch is under 5 us (4 x 4 tiles
+// of 64 x 64 with a contraction of 256: 5.3), most of it the way from one kernel's last store to the next one's first operands.
 #include <atomic>
 #include <type_traits>
 
