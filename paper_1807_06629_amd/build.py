@@ -56,7 +56,7 @@ def _build_binding() -> str:
                  "-I", sysconfig.get_paths()["include"], "-I", os.path.join(torch, "include"),
                  "-I", os.path.join(torch, "include", "torch", "csrc", "api", "include"), "-I", os.path.join(rocm, "include"),
                  os.path.join(CSRC, "binding", "ops_binding.cpp"), "-o", BINDING, "-L", os.path.join(torch, "lib"),
-                 "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip", "-L", HERE, "-l:libprsgd.so", "-Wl,-rpath,$ORIGIN"])
+                 "-ltorch_python", "-ltorch_cpu", "-ltorch_hip", "-lc10", "-lc10_hip", "-L", HERE, "-l:libprsgd.so", "-Wl,-rpath,$ORIGIN"])
 
 
 def build(verbose: bool = False) -> str:

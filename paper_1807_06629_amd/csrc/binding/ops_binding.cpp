@@ -4,6 +4,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -60,6 +61,11 @@ int32_t operand_type(const Tensor& t, const char* text) {
   return t.scalar_type() == at::kFloat ? PRSGD_F32 : PRSGD_BF16;
 }
 
+// The caching allocator without the dispatcher in front of it, which took as long again for each of a call's tensors
+Tensor device_empty(at::IntArrayRef sizes, at::ScalarType type, const Tensor& like) {
+  return Tensor(at::detail::empty_cuda(sizes, type, like.device(), std::nullopt));
+}
+
 // The tensors' device made current for the call, and its current stream.
 struct OnDevice {
   c10::DeviceIndex before;
@@ -102,17 +108,17 @@ NormCall norm_call(const Tensor& x, const Tensor& w, float eps) {
   return c;
 }
 Tensor row_vector(PyObject* o, const Tensor& x, const char* name) {
-  if (o == Py_None) return at::empty({x.size(0)}, x.options().dtype(at::kFloat));
+  if (o == Py_None) return device_empty({x.size(0)}, at::kFloat, x);
   const Tensor& t = tensor(o, name);
   if (t.scalar_type() != at::kFloat || t.device() != x.device() || t.dim() != 1 || t.size(0) != x.size(0) || !t.is_contiguous())
     throw Refused(std::string(name) + " must be contiguous float32, one value a row");
   return t;
 }
 Tensor given_or_empty(PyObject* o, const Tensor& like, at::ScalarType type, const char* name) {
-  return o == Py_None ? at::empty(like.sizes(), like.options().dtype(type)) : tensor(o, name);
+  return o == Py_None ? device_empty(like.sizes(), type, like) : tensor(o, name);
 }
 Tensor workspace(PyObject* o, size_t bytes, const Tensor& like) {
-  if (o == Py_None) return at::empty({(int64_t)bytes}, like.options().dtype(at::kByte));
+  if (o == Py_None) return device_empty({(int64_t)bytes}, at::kByte, like);
   const Tensor& t = tensor(o, "workspace");
   if (t.device() != like.device() || t.nbytes() < bytes || !t.is_contiguous()) throw Refused("the workspace must have " + std::to_string(bytes) + " bytes on the tensors' device");
   return t;
@@ -187,14 +193,21 @@ Matrices matrices_of(const Tensor& t, const Tensor& like, at::ScalarType type, c
 prsgd_orth_config orth_config(at::IntArrayRef shape, int32_t dtype, PyObject* coefficients, PyObject* steps, PyObject* eps) {
   prsgd_orth_config c{};
   require(shape.size() == 2 || shape.size() == 3, "matrices must be [count][rows][cols] or [rows][cols]");
-  require(PyTuple_Check(coefficients) && PyTuple_GET_SIZE(coefficients) == 3, "coefficients must be three numbers");
+  PyObject* three = PySequence_Fast(coefficients, "coefficients must be three numbers");
+  if (three == nullptr) throw Raised{};
+  const bool fits = PySequence_Fast_GET_SIZE(three) == 3;
+  double v[3] = {0.0, 0.0, 0.0};
+  for (int i = 0; fits && i < 3; ++i) v[i] = PyFloat_AsDouble(PySequence_Fast_GET_ITEM(three, i));
+  Py_DECREF(three);
+  if (PyErr_Occurred()) throw Raised{};
+  require(fits, "coefficients must be three numbers");
   c.dtype = dtype;
   c.count = shape.size() == 3 ? size32(shape[0]) : 1;
   c.rows = size32(shape[shape.size() - 2]);
   c.cols = size32(shape[shape.size() - 1]);
-  c.a = (float)number(PyTuple_GET_ITEM(coefficients, 0));
-  c.b = (float)number(PyTuple_GET_ITEM(coefficients, 1));
-  c.c = (float)number(PyTuple_GET_ITEM(coefficients, 2));
+  c.a = (float)v[0];
+  c.b = (float)v[1];
+  c.c = (float)v[2];
   c.steps = integer(steps);
   c.eps = (float)number(eps);
   return c;
