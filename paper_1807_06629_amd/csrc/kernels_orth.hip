@@ -111,8 +111,8 @@ __global__ void __launch_bounds__(kThreads) orth_load_kernel(OrthMatrices p, con
 // so U is read for K and for P U, 3 r^2 L operations in all instead of 3 r^2 L per step, and a whole call is one launch or two.  The Gram
 // matrix squares the condition: in 64 bits its smallest eigenvalues are as good as fp32 singular values are, in fp32 they may come out
 // negative and grow.  K and the polynomials run on v_mfma_f64_16x16x4, P U on v_mfma_f32_16x16x4.
-// 64 x (128 x 10) 8.3 us in one launch of 64 workgroups, latency from end to end.  Against the launches of the products' path: 64 x (64 x
-// 64) in fp32 52 and 68 us, 64 x (64 x 512) 82 and 95, 4 x (64 x 4096) 128 and 176; in bf16 8 x (64 x 1024) is the one slower, 91 and 73.
+// 64 x (128 x 10) 8.3 us in one launch of 64 workgroups, latency from end to end.  A call of this and of the products' path: 64 x (64 x
+// 64) in fp32 53 and 68 us, 64 x (64 x 512) 72 and 95, 4 x (64 x 4096) 79 and 176; in bf16 8 x (64 x 1024) 66 and 73, 64 x (64 x 512) 72 and 80.
 // A symmetric matrix of NB x NB blocks of 16 is kept as operands: element q of lane (g = lane / 16, i = lane % 16) of block (x, y) is
 // M[16 x + i][16 y + 4 q + g].  That is what a product takes from either side, and the product's block (x, y) comes out as block (y, x).
 typedef double f64x4_t __attribute__((ext_vector_type(4)));
@@ -447,8 +447,8 @@ template <typename T> hipError_t launch_short(const OrthMatrices& p, const Short
 }  // namespace
 
 size_t orth_short_doubles(int r) { return (size_t)short_blocks(r) * short_blocks(r) * 256; }
-// Slices of the long side: two chunks stay in one launch, which saves the second; more are dealt to up to 512 workgroups (8 x (16 x 1024)
-// in one launch 21 us, in four slices 12).
+// Slices of the long side: two chunks stay in one launch, which saves the second; more are dealt to as many workgroups as the device holds (8 x
+// (16 x 1024) in one launch 21 us, in four slices 12).
 int orth_short_slices(int count, int r, int longer) {
   const int chunks = (longer + short_chunk(r) - 1) / short_chunk(r);
   int slices = (short_blocks(r) == 4 ? 256 : 512) / count;    // what the device holds at once
