@@ -197,3 +197,40 @@ def test_a_workspace_that_is_too_small_is_refused(P):
         P.prsgd_orthogonalize(g.transpose(1, 2)[:, :, ::2])
     with pytest.raises(P.PrsgdError):
         P.prsgd_orthogonalize(g, steps=0)
+
+
+@pytest.mark.parametrize("rows,cols", [(12, 90), (70, 90)])
+def test_offsets_beyond_32_bits(P, rows, cols):
+    """Two matrices 2.2e9 elements apart, in and out."""
+    far = 2_200_000_000
+    g = _matrices(2, rows, cols, BF16)
+    base = torch.empty(far + rows * cols, dtype=BF16, device="cuda")
+    apart = base.as_strided((2, rows, cols), (far, cols, 1))
+    apart.copy_(g)
+    assert torch.equal(P.prsgd_orthogonalize(apart), P.prsgd_orthogonalize(g))
+    out = P.prsgd_orthogonalize(g, out=apart)
+    assert torch.equal(out, P.prsgd_orthogonalize(g))
+
+
+@pytest.mark.parametrize("shape", [(4, 20, 700), (6, 200, 300)])
+def test_calls_on_two_streams_at_once(P, shape):
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    gs = [_matrices(*shape, F32, seed=k) for k in range(2)]
+    want = [P.prsgd_orthogonalize(g) for g in gs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(8):
+        for k, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[k].append(P.prsgd_orthogonalize(gs[k]))
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(torch.equal(o, want[k]) for o in got[k])
+
+
+def test_coefficients_may_be_any_sequence(P):
+    g = _matrices(2, 20, 30, F32)
+    assert torch.equal(P.prsgd_orthogonalize(g, coefficients=list(O.NS)), P.prsgd_orthogonalize(g))
+    for bad in ((1.5, -0.5), 3.0, "abc", (1.5, None, 0.0)):
+        with pytest.raises((ValueError, TypeError)):
+            P.prsgd_orthogonalize(g, coefficients=bad)
