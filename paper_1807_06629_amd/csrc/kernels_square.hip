@@ -120,13 +120,13 @@ __device__ __forceinline__ void strip_tile(int in, int tiles_m, int tiles_n, int
   *tj = rest / high;
   *ti = first + rest - *tj * high;
 }
-// The same over the squares on and below the diagonal, R tiles each.  Returns whether the tile's transpose is written too.
-template <int R> __device__ __forceinline__ bool triangle_tile(int in, int squares, int* ti, int* tj) {
-  int rest = in / R, first = 0, high = min(kStrip, squares);
-  while (rest >= high * first + high * (high + 1) / 2) {   // squares of the strip's rows
+// The same over the tiles on and below the diagonal.
+__device__ __forceinline__ void triangle_tile(int in, int tiles, int* ti, int* tj) {
+  int rest = in, first = 0, high = min(kStrip, tiles);
+  while (rest >= high * first + high * (high + 1) / 2) {   // tiles of the strip's rows
     rest -= high * first + high * (high + 1) / 2;
     first += kStrip;
-    high = min(kStrip, squares - first);
+    high = min(kStrip, tiles - first);
   }
   int row, col = rest / high;
   if (col < first) {
@@ -137,9 +137,8 @@ template <int R> __device__ __forceinline__ bool triangle_tile(int in, int squar
     for (int left = high; rest >= left; --left, ++col) rest -= left;
     row = col + rest;
   }
-  *ti = row * R + in % R;
+  *ti = row;
   *tj = col;
-  return row != col;
 }
 
 constexpr int strip_pitch(int columns) { return columns + 8; }     // the four rows between a register's two halves lie 32 banks apart
@@ -157,8 +156,8 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) square_kernel(const SquareArg
   using User = std::conditional_t<SPLIT, float, uint16_t>;
   using ReqA = TileRequests<BM, RB, NW, SPLIT, false>;
   using ReqB = TileRequests<BN, RB, NW, SPLIT, TRANS>;
-  constexpr int PER = ReqA::NPT + ReqB::NPT, R = BN / BM;
-  static_assert(!SYMMETRIC || BN % BM == 0, "tiles of a symmetric result");
+  constexpr int PER = ReqA::NPT + ReqB::NPT;
+  static_assert(!SYMMETRIC || BN == BM, "tiles of a symmetric result");
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   fetch_kernel_args<sizeof(SquareArgs)>();
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -169,9 +168,8 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) square_kernel(const SquareArg
   const int idx = xcd * (total >> 3) + min(xcd, total & 7) + (blockIdx.x >> 3);
   const int g = idx / p.tiles, in = idx - g * p.tiles;
   int ti, tj;
-  const bool mirrored = SYMMETRIC ? triangle_tile<R>(in, p.tiles_n, &ti, &tj) : false;
-  if (!SYMMETRIC) strip_tile(in, (p.M + BM - 1) / BM, p.tiles_n, &ti, &tj);
-  if (SYMMETRIC && ti * BM >= p.M) return;
+  if (SYMMETRIC) triangle_tile(in, p.tiles_n, &ti, &tj);
+  else strip_tile(in, (p.M + BM - 1) / BM, p.tiles_n, &ti, &tj);
   const int m0 = ti * BM, n0 = tj * BN;
 
   // Strips of the epilogue: columns, pitch, 8-value vectors of a row, rows per pass
@@ -347,7 +345,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) square_kernel(const SquareArg
       for (int e = 0; e < 8; e += 2) *reinterpret_cast<f32x2_t*>(at + e) = (f32x2_t){v[e], v[e + 1]};
     }
     __builtin_amdgcn_wave_barrier();
-    if (SYMMETRIC ? mirrored : EPI == SQ_LAST && p.transposed) {
+    if (SYMMETRIC ? ti != tj : EPI == SQ_LAST && p.transposed) {
 #pragma unroll(EPI == SQ_LAST ? 1 : W / 16)
       for (int q = 0; q < W / 16; ++q) {
         const int lc = q * 16 + lane % 16, lr = lane / 16 * 8, c = c0 + lc, r = r0 + lr;
@@ -389,7 +387,7 @@ template <int BM, int BN, int WM, int WN, int S, int RB, bool SPLIT, int EPI> hi
   }
   const int tiles_m = (p.M + BM - 1) / BM;
   p.tiles_n = (p.N + BN - 1) / BN;
-  p.tiles = EPI == SQ_GRAM || EPI == SQ_POLY ? p.tiles_n * (p.tiles_n + 1) / 2 * (BN / BM) : tiles_m * p.tiles_n;
+  p.tiles = EPI == SQ_GRAM || EPI == SQ_POLY ? p.tiles_n * (p.tiles_n + 1) / 2 : tiles_m * p.tiles_n;
   hipLaunchKernelGGL(kernel, dim3((unsigned)p.tiles * (unsigned)p.count), dim3(64 * WM * WN), kLds, s, p);
   return hipGetLastError();
 }
@@ -406,28 +404,23 @@ template <int BM, int BN, int WM, int WN, int S, int RB, bool SPLIT> hipError_t 
 
 hipError_t launch_square(SquareArgs p, int epi, bool split, hipStream_t s) {
   const bool symmetric = epi == SQ_GRAM || epi == SQ_POLY;
-  // Time of a launch in units of a 64 x 64 tile's products at the rate of 128 x 256 tiles: tiles per compute unit times their size over
-  // their efficiency.  Of tiles that a compute unit has several of in hand, parts of a round count as such; of the others whole rounds.
+  // Time of a launch in units of a 64 x 64 tile's products: tiles per compute unit times their size over their efficiency.  Of tiles that a
+  // compute unit has several of in hand, parts of a round count as such; of 256 x 256 tiles whole rounds.
   // Measured over 17 shapes from 64 x (128 x 256) to 8 x (2048 x 2048), every tile size for each of the three products: this takes the
-  // fastest or one within 4 % of a call.  Where it matters most: B X of 16 x (320 x 800) in bf16, call of 133 us in 64 x 64 tiles, 154 in
-  // 128 x 256; X X^T of 8 x (1000 x 4096), 887 us in 128 x 256, 1018 in 256 x 256; B X there 885 in 128 x 128, 1058 in 64 x 64.
-  auto cost = [&](int bm, int bn, bool whole, double efficiency) {
-    const int64_t tm = (p.M + bm - 1) / bm, tn = (p.N + bn - 1) / bn;
-    const int64_t tiles = (symmetric ? tn * (tn + 1) / 2 * (bn / bm) : tm * tn) * p.count;
+  // fastest or one within 4 % of a call.  Where it matters most: B X of 16 x (320 x 800) in bf16, call of 133 us in 64 x 64 tiles, 171 in
+  // 256 x 256; X X^T of 8 x (1000 x 4096), 895 us in 128 x 128, 1018 in 256 x 256; B X of 8 x (2048 x 2048) 2244 us in 64 x 64, 1942 in
+  // 128 x 128, 1766 in 256 x 256.  (128 x 256 tiles were nowhere better by more than 1 %.)  Split products keep to 128 x 128: larger tiles do not
+  // leave two workgroups per compute unit the registers.
+  auto cost = [&](int b, bool whole, double efficiency) {
+    const int64_t tm = (p.M + b - 1) / b, tn = (p.N + b - 1) / b;
+    const int64_t tiles = (symmetric ? tn * (tn + 1) / 2 : tm * tn) * p.count;
     const double rounds = whole ? (double)((tiles + 255) / 256) : tiles < 256 ? 1.0 : (double)tiles / 256.0;
-    return rounds * (bm / 64) * (bn / 64) / efficiency;
+    return rounds * (b / 64) * (b / 64) / efficiency;
   };
-  const double huge = cost(256, 256, true, 1.2), large = cost(128, 256, true, 1.0), middle = cost(128, 128, false, 0.9),
-               small = cost(64, 64, false, split ? 0.77 : 0.68);
-  if (split) {
-    // 128 x 256 would not leave a split product the registers for two workgroups per compute unit
-    if (middle <= small) return launch_tile<128, 128, 2, 2, 3, 64, true>(p, epi, s);
-    return launch_tile<64, 64, 2, 2, 4, 128, true>(p, epi, s);
-  }
-  if (huge <= large && huge <= middle && huge <= small) return launch_tile<256, 256, 4, 2, 2, 128, false>(p, epi, s);
-  if (large <= middle && large <= small) return launch_tile<128, 256, 2, 2, 3, 64, false>(p, epi, s);
-  if (middle <= small) return launch_tile<128, 128, 2, 2, 3, 64, false>(p, epi, s);
-  return launch_tile<64, 64, 2, 2, 4, 128, false>(p, epi, s);
+  const double huge = cost(256, true, 1.2), middle = cost(128, false, 0.9), small = cost(64, false, split ? 0.77 : 0.68);
+  if (split) return middle <= small ? launch_tile<128, 128, 2, 2, 3, 64, true>(p, epi, s) : launch_tile<64, 64, 2, 2, 4, 128, true>(p, epi, s);
+  if (huge <= middle && huge <= small) return launch_tile<256, 256, 4, 2, 2, 128, false>(p, epi, s);
+  return middle <= small ? launch_tile<128, 128, 2, 2, 3, 64, false>(p, epi, s) : launch_tile<64, 64, 2, 2, 4, 128, false>(p, epi, s);
 }
 
 }  // namespace prsgd

@@ -234,3 +234,17 @@ def test_coefficients_may_be_any_sequence(P):
     for bad in ((1.5, -0.5), 3.0, "abc", (1.5, None, 0.0)):
         with pytest.raises((ValueError, TypeError)):
             P.prsgd_orthogonalize(g, coefficients=bad)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("count,rows,cols", [(24, 2050, 140), (24, 140, 2050), (9, 4000, 1001)])
+def test_the_largest_tiles_either_way_up(P, count, rows, cols, dtype):
+    g = _matrices(count, rows, cols, dtype, seed=7)
+    assert _err(P.prsgd_orthogonalize(g), O.orthogonalize(g)) <= TOL[dtype]
+    x, m = g.float().mul(100).to(dtype), torch.zeros(count, rows, cols, device="cuda")
+    want, _ = O.muon_step(x, g, m, nesterov=True, **STEP)
+    P.prsgd_muon_step(x, g, m, STEP["lr"], momentum=STEP["mu"], weight_decay=STEP["weight_decay"], scale=STEP["scale"])
+    # as in test_muon_step: the update's error, and the roundings of x
+    o = STEP["lr"] * STEP["scale"] * O.orthogonalize(g).flatten(1).norm(dim=1)
+    rounding = 2.0 ** (-8 if dtype == BF16 else -23) * want.flatten(1).norm(dim=1)
+    assert bool(((x.double() - want).flatten(1).norm(dim=1) <= TOL[dtype] * o + rounding).all())
