@@ -4,7 +4,9 @@
 // lead x lead and the two crossed ones, of the same fragments.
 // What is multiplied is held to 11 bits (22 if split), what is added (a X) to 22 either way: a rounding of the linear term is carried on
 // and grows as the smallest singular values do, 3.4445 per step, one in a factor of B X only turns singular vectors.  (Updates of rank
-// 32 at 512 x 512: error of the result 6e-4 so, 3e-2 with X in 11 bits throughout, 0.2 in bfloat16.)
+// 32 at 512 x 512: error of the result 9e-4 so, 3e-2 with X in 11 bits throughout, 0.2 in bfloat16.)  B's diagonal, which holds most of
+// B where the spectrum is flat, is held to 22 bits as well and meets both halves of X, in the sums of B X's epilogue: 2.1e-3 -> 1.1e-3 at
+// 70 x 80, 1.5e-3 -> 8e-4 at 512 x 512 (where half of the singular values are 0, 1e-3 -> 1.4e-3), for at most 1 % of a call's time.
 // Bound by the matrix cores and their power where matrices are large: 8 x 4096 x 4096 in half precision, B X 1084 us (1014 TFLOP/s, at 1.55 GHz;
 // a library's batched product of that size 1100), X X^T 581 us for 136 of 256 tiles (5 rounds of 256 where 4.25 would do).  16 x 1024 x 1024
 // split, B X 107 us: 965 TFLOP/s of the three products.  Bound by latency where they are small: no launch is under 5 us (4 x 4 tiles
@@ -176,15 +178,16 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) square_kernel(const SquareArg
   constexpr int W = BN / WN, P = strip_pitch(W), VPR = W / 8, RPP = 64 / VPR, PASSES = 32 / RPP;
   const int c0 = n0 + wn * W;
   // what the epilogue adds to the product at pass q of strip i
-  struct Linear { u32x4_t hi, lo; };
+  struct Linear { u32x4_t hi, lo; f32x2_t diag; };
   auto linear = [&](int i, int q) __attribute__((always_inline)) {
-    Linear v = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    Linear v = {{0, 0, 0, 0}, {0, 0, 0, 0}, {0.0f, 0.0f}};
     const int r = m0 + (wm * TM + i) * 32 + q * RPP + lane / VPR, c = c0 + lane % VPR * 8;
     if (EPI != SQ_GRAM && r < p.M && c < p.N) {
       const int64_t o = g * p.lin_gs + (int64_t)r * p.ld_lin + half_col<SPLIT>(c);
       v.hi = *reinterpret_cast<const u32x4_t*>(p.lin + o);
       if (SPLIT) v.lo = *reinterpret_cast<const u32x4_t*>(p.lin + o + kGroup);
       else if (EPI != SQ_POLY) v.lo = *reinterpret_cast<const u32x4_t*>(p.lin_lo + o);
+      if (!SPLIT && TRANS) v.diag = *reinterpret_cast<const f32x2_t*>(p.diag + 2 * ((int64_t)g * p.M + r));
     }
     return v;
   };
@@ -319,8 +322,18 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) square_kernel(const SquareArg
         Linear x;
         if constexpr (AHEAD) x = ahead[q];
         else x = linear(i, q);
+        if constexpr (!SPLIT && TRANS) {
+          // (a + what the half of B_ii leaves out) X + B X with X's remainder at B_ii
+          const float whole = fmaf(p.diag_scale, x.diag[1], p.alpha), half = p.diag_scale * x.diag[0];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = fmaf(p.alpha, half_at(x.hi, e) + half_at(x.lo, e), p.beta * v[e]);
+          for (int e = 0; e < 8; ++e) {
+            const float rest = half_at(x.lo, e);
+            v[e] = fmaf(whole, half_at(x.hi, e) + rest, fmaf(half, rest, p.beta * v[e]));
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = fmaf(p.alpha, half_at(x.hi, e) + half_at(x.lo, e), p.beta * v[e]);
+        }
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= p.beta;
@@ -328,6 +341,15 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) square_kernel(const SquareArg
       // padding columns of the halves hold zeros, and so do padding rows of transposes
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = r < p.M && c + e < p.N ? v[e] : 0.0f;
+      if constexpr (!SPLIT && EPI == SQ_POLY) {
+        if ((unsigned)(r - c) < 8u && r < p.M) {           // the vector holds the diagonal entry of its row
+          float d = v[0];
+#pragma unroll
+          for (int e = 1; e < 8; ++e) d = r == c + e ? v[e] : d;
+          const float half = half_value(half_bits(d));
+          *reinterpret_cast<f32x2_t*>(p.diag + 2 * ((int64_t)g * p.M + r)) = (f32x2_t){half, d - half} * (1.0f / kHalfScale);
+        }
+      }
       if constexpr (EPI == SQ_LAST) {
         if (!p.transposed && inside) {
           const int64_t o = g * p.user.out_matrix + r * p.user.out_row + c;

@@ -103,7 +103,7 @@ const char* orth_config_error(const prsgd_orth_config* c) {
 struct OrthPlan {
   bool split;
   int r, longer, ld_x, ld_a;
-  size_t x, x_lo, a, b, parts, total;          // byte offsets
+  size_t x, x_lo, a, b, diag, parts, total;    // byte offsets
   int64_t x_gs, a_gs;                          // halves per matrix
 };
 OrthPlan orth_plan(const prsgd_orth_config* c) {
@@ -122,6 +122,7 @@ OrthPlan orth_plan(const prsgd_orth_config* c) {
   p.x_lo = p.split ? 0 : take(n * p.x_gs * 2);
   p.a = take(n * p.a_gs * 2);
   p.b = take(n * p.a_gs * 2);
+  p.diag = p.split ? 0 : take(n * p.r * 2 * sizeof(float));
   p.parts = take(n * norm_parts(c->rows, c->cols) * sizeof(double));
   p.total = at;
   return p;
@@ -150,6 +151,7 @@ hipError_t run_squares(const prsgd_orth_config* c, const OrthMatrices& m, char* 
   for (int k = 0; k < c->steps && e == hipSuccess; ++k) {
     SquareArgs q{};
     q.count = c->count;
+    if (!p.split) q.diag = reinterpret_cast<float*>(ws + p.diag);
     // A = X X^T
     q.a = q.b = x;
     q.a_gs = q.b_gs = p.x_gs;
@@ -185,6 +187,7 @@ hipError_t run_squares(const prsgd_orth_config* c, const OrthMatrices& m, char* 
       q.ldo = p.ld_x;
       q.alpha = c->a;
       q.beta = inv;
+      q.diag_scale = 1.0f;
       e = launch_square(q, SQ_NEXT, p.split, s);
       std::swap(x, y);
     } else {
@@ -192,6 +195,7 @@ hipError_t run_squares(const prsgd_orth_config* c, const OrthMatrices& m, char* 
       q.transposed = c->rows > c->cols;
       q.alpha = c->a * inv;
       q.beta = inv * inv;
+      q.diag_scale = inv;
       e = launch_square(q, SQ_LAST, p.split, s);
     }
   }

@@ -77,6 +77,8 @@ struct SquareArgs {
   uint16_t* out; uint16_t* out_lo; int64_t out_gs; int ldo;
   uint16_t* out_t; int64_t t_gs; int ldt;      // where transposed tiles of a symmetric result go (out)
   float alpha, beta;                           // out = alpha lin + beta acc
+  // Unsplit operands: B's diagonal, [M][2] per matrix: the half that the product takes and what it leaves out; both times diag_scale.
+  float* diag; float diag_scale;
   int tiles_n, tiles;                          // per matrix; filled in by the launcher
   int count;
   bool transposed;                             // SQ_LAST: the caller's matrices hold the transpose
