@@ -179,27 +179,36 @@ __global__ void __launch_bounds__(threads_of<TPR>()) rms_norm_kernel(NormArgs p)
       }
     row_reduce<TPR, FP8>(a, m, parity);
     float rstd = 1.0f / sqrtf(a * inv_width + p.eps), top = m * rstd;
-    if (!(a < INFINITY)) {                                 // squares (or products with w) past fp32: again at 2^-80 of the row's size
-      parity ^= 1;
-      a = m = 0.0f;
+    const bool past = !(a < INFINITY);
+    if (past || (FP8 && !(m < INFINITY))) {                // past fp32: squares again at 2^-80 of the row's size, |y| from normed elements
+      const float size = past ? 0x1p-80f : 1.0f;
+      if (past) {
+        parity ^= 1;
+        a = 0.0f;
 #pragma unroll
-      for (int q = 0; q < NV; ++q)
+        for (int q = 0; q < NV; ++q)
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float z = s[q][e] * 0x1p-80f;
-          a = fmaf(z, z, a);
-          if (FP8) m = fmaxf(m, fabsf(z * wv[q][e]));
-        }
-      row_reduce<TPR, FP8>(a, m, parity);
-      rstd = 1.0f / sqrtf(a * inv_width);
-      top = m * rstd;
-      rstd *= 0x1p-80f;
+          for (int e = 0; e < V; ++e) a = fmaf(s[q][e] * size, s[q][e] * size, a);
+        row_reduce<TPR, false>(a, m, parity);
+        rstd = 1.0f / sqrtf(a * inv_width);
+      }
+      if constexpr (FP8) {
+        parity ^= 1;
+        float none = top = 0.0f;
+#pragma unroll
+        for (int q = 0; q < NV; ++q)
+#pragma unroll
+          for (int e = 0; e < V; ++e) top = fmaxf(top, fabsf(s[q][e] * size * rstd * wv[q][e]));
+        row_reduce<TPR, true>(none, top, parity);
+        if (!(a < INFINITY)) top = NAN;                    // a row with a NaN or an infinity has no scale
+      }
+      rstd *= size;
     }
-    float k = rstd;
-    if constexpr (FP8) {                                   // a NaN stays one
+    float shrink = 1.0f;
+    if constexpr (FP8) {
       const float scale = (top < kFp8Least ? kFp8Least : top) / kFp8Max;
-      k = rstd / scale;
-      if (t == 0 && live) p.stat[row] = rstd == rstd ? scale : rstd;
+      shrink = 1.0f / scale;
+      if (t == 0 && live) p.stat[row] = scale;
     } else if (p.stat != nullptr && t == 0 && live) {
       p.stat[row] = rstd;
     }
@@ -211,7 +220,11 @@ __global__ void __launch_bounds__(threads_of<TPR>()) rms_norm_kernel(NormArgs p)
         store_row<NT>(reinterpret_cast<T*>(p.sum) + (int64_t)row * p.sum_row + c, n, Rows<T>::pack(s[q]));
       float y[V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) y[e] = s[q][e] * k * wv[q][e];
+      for (int e = 0; e < V; ++e) y[e] = s[q][e] * rstd * wv[q][e];
+      if constexpr (FP8) {                                 // last: rstd / scale may leave fp32 where y / scale does not
+#pragma unroll
+        for (int e = 0; e < V; ++e) y[e] *= shrink;
+      }
       if constexpr (FP8) store_fp8<V>(reinterpret_cast<uint8_t*>(p.y) + (int64_t)row * p.y_row + c, n, y);
       else store_row<NT>(reinterpret_cast<T*>(p.y) + (int64_t)row * p.y_row + c, n, Rows<T>::pack(y));
     }

@@ -263,3 +263,32 @@ def test_what_the_binding_refuses(P):
             bad()
     with pytest.raises(P.PrsgdError):
         P.prsgd_rms_norm(x, w, eps=-1.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width", [9, 100, 1000, 9000])
+@pytest.mark.parametrize("size", [1e3, 1e18, 1e30])
+def test_eight_bits_of_weights_whose_products_overflow(P, width, dtype, size):
+    """s w passes fp32 where y does not: scales go by y."""
+    x, w = _rows(6, width, dtype, 1, size), 1e36 * _weights(2, width)
+    x[0] = 1.0                                                      # a row beside that needs nothing of it
+    q, scales, _ = P.prsgd_rms_norm_fp8(x, w)
+    y = O.rms_norm(x, w)[0]
+    assert float((scales.double() / (y.abs().amax(1) / 448.0) - 1).abs().max()) <= SUMS
+    got = q.float().double() * scales.double()[:, None]
+    step = torch.maximum(y.abs() * 2.0 ** -4, 2.0 ** -10 * scales.double()[:, None])
+    assert bool(((got - y).abs() <= step * (1 + 1e-4)).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("eps", [1e-12, 1e-30])
+def test_eight_bits_of_zeros_under_a_small_eps(P, dtype, eps):
+    """rstd over the least scale passes fp32: zeros stay zeros."""
+    x = torch.zeros(5, 200, dtype=dtype, device="cuda")
+    x[3] = _rows(1, 200, dtype, 1, 1e-3)[0]
+    w = _weights(1, 200)
+    q, scales, _ = P.prsgd_rms_norm_fp8(x, w, eps=eps)
+    assert bool((q[[0, 1, 2, 4]].float() == 0).all()) and bool(((scales[[0, 1, 2, 4]].double() * 448 * 2.0 ** 100 - 1).abs() <= 2.0 ** -23).all())
+    y = O.rms_norm(x[3:4], w, eps=eps)[0]
+    got = q[3:4].float().double() * float(scales[3])
+    assert bool(((got - y).abs() <= torch.maximum(y.abs() * 2.0 ** -4, torch.full_like(y, 2.0 ** -10 * float(scales[3]))) * (1 + 1e-4)).all())
