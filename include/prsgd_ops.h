@@ -89,8 +89,8 @@ typedef struct {
 
 /*
  * y_dev <- y, sum_dev <- s, rstd_dev [rows] <- rstd.  res_dev, sum_dev and rstd_dev may be NULL (no residual, not wanted).
- * w_dev is fp32, w_row elements from worker to worker (0: all share one).  sum_dev may be x_dev or res_dev, and y_dev may be
- * x_dev, if the distances agree; otherwise outputs may not overlap anything.
+ * w_dev is fp32, w_row elements from worker to worker (0: all share one).  sum_dev and y_dev may each be x_dev or res_dev, if
+ * the distances agree; otherwise outputs may not overlap anything.
  */
 int prsgd_rms_norm(const prsgd_norm_config* cfg, const void* x_dev, int64_t x_row, const void* res_dev, int64_t res_row,
                    const float* w_dev, int64_t w_row, void* sum_dev, int64_t sum_row, void* y_dev, int64_t y_row,
@@ -98,7 +98,8 @@ int prsgd_rms_norm(const prsgd_norm_config* cfg, const void* x_dev, int64_t x_ro
 
 /*
  * The same with y in 8 bits: scale = max(max_j |y_j|, 2^-100) / 448 of each row, q = y / scale rounded to nearest even in
- * e4m3 (4 exponent bits, bias 7, largest 448, no infinities).  q_dev holds bytes, q_row bytes from row to row; scale_dev [rows].
+ * e4m3 (4 exponent bits, bias 7, largest 448, no infinities).  q_dev holds bytes, q_row bytes from row to row, and
+ * overlaps nothing; scale_dev [rows].
  */
 int prsgd_rms_norm_fp8(const prsgd_norm_config* cfg, const void* x_dev, int64_t x_row, const void* res_dev, int64_t res_row,
                        const float* w_dev, int64_t w_row, void* sum_dev, int64_t sum_row, uint8_t* q_dev, int64_t q_row,
@@ -108,7 +109,7 @@ int prsgd_rms_norm_fp8(const prsgd_norm_config* cfg, const void* x_dev, int64_t 
  * Gradients of prsgd_rms_norm from dy (of y) and dsum (of s along the residual path, may be NULL), with sh = s * rstd:
  *   dx = rstd * (w dy - sh mean(w dy sh)) + dsum     (the gradient of x and of res alike)
  *   dw_i = sum over worker i's rows of dy * sh       (fp32, dw_row elements from worker to worker)
- * s_dev and rstd_dev are what the forward call wrote.  dx_dev may be dy_dev or dsum_dev if the distances agree.
+ * s_dev and rstd_dev are what the forward call wrote.  dx_dev may be dy_dev, dsum_dev or s_dev if the distances agree.
  * workspace_dev: prsgd_rms_norm_backward_workspace_bytes.  Without rows, dw is zeroed.
  */
 size_t prsgd_rms_norm_backward_workspace_bytes(const prsgd_norm_config* cfg);

@@ -243,9 +243,11 @@ PyObject* muon_step(PyObject* const* a) {
   OnDevice on(x);
   const Matrices xs = matrices_of(x, x, x.scalar_type(), "x"), gs = matrices_of(tensor(a[1], "g"), x, x.scalar_type(), "g"),
                  ms = matrices_of(tensor(a[2], "m"), x, at::kFloat, "m");
+  const int nesterov = PyObject_IsTrue(a[5]);
+  if (nesterov < 0) throw Raised{};
   const Tensor ws = workspace(a[11], orth_bytes(c), x);
   finish(prsgd_muon_step(&c, xs.at, xs.matrix, xs.row, gs.at, gs.matrix, gs.row, static_cast<float*>(ms.at), ms.matrix, ms.row,
-                         (float)number(a[3]), (float)number(a[4]), PyObject_IsTrue(a[5]), (float)number(a[6]), (float)number(a[7]),
+                         (float)number(a[3]), (float)number(a[4]), nesterov, (float)number(a[6]), (float)number(a[7]),
                          ws.data_ptr(), on.stream()));
   Py_RETURN_NONE;
 }

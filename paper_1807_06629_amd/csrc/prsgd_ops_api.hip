@@ -53,7 +53,10 @@ int norm_forward(const prsgd_norm_config* c, const void* x, int64_t x_row, const
   if (!rows_ok(c, x_row, false) || (res != nullptr && !rows_ok(c, res_row, false)) || (sum != nullptr && !rows_ok(c, sum_row, true)) ||
       !rows_ok(c, y_row, true))
     return bad("norm: distance between rows out of range");
-  if ((sum == x && sum != nullptr && sum_row != x_row) || (sum != nullptr && sum == res && sum_row != res_row) || (y == x && y_row != x_row))
+  // 8-bit rows lie otherwise than what they would replace
+  if (y == sum || (fp8 && (y == x || y == res))) return bad("norm: buffers overlap");
+  auto elsewhere = [](const void* out, int64_t out_row, const void* in, int64_t in_row) { return out != nullptr && out == in && out_row != in_row; };
+  if (elsewhere(sum, sum_row, x, x_row) || elsewhere(sum, sum_row, res, res_row) || elsewhere(y, y_row, x, x_row) || elsewhere(y, y_row, res, res_row))
     return bad("norm: in place with another distance between rows");
   NormArgs p{};
   p.x = x;
@@ -327,7 +330,8 @@ int prsgd_rms_norm_backward(const prsgd_norm_config* cfg, const void* dy_dev, in
     if (!rows_ok(cfg, dy_row, false) || (dsum_dev != nullptr && !rows_ok(cfg, dsum_row, false)) || !rows_ok(cfg, s_row, false) ||
         !rows_ok(cfg, dx_row, true))
       return bad("norm: distance between rows out of range");
-    if ((dx_dev == dy_dev && dx_row != dy_row) || (dx_dev == dsum_dev && dx_row != dsum_row)) return bad("norm: in place with another distance between rows");
+    if ((dx_dev == dy_dev && dx_row != dy_row) || (dx_dev == dsum_dev && dx_row != dsum_row) || (dx_dev == s_dev && dx_row != s_row))
+      return bad("norm: in place with another distance between rows");
   }
   p.x = dy_dev;
   p.x_row = dy_row;

@@ -292,3 +292,16 @@ def test_eight_bits_of_zeros_under_a_small_eps(P, dtype, eps):
     y = O.rms_norm(x[3:4], w, eps=eps)[0]
     got = q[3:4].float().double() * float(scales[3])
     assert bool(((got - y).abs() <= torch.maximum(y.abs() * 2.0 ** -4, torch.full_like(y, 2.0 ** -10 * float(scales[3]))) * (1 + 1e-4)).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width", [5, 300, 5000])
+def test_result_over_the_residual_and_gradient_over_the_rows(P, width, dtype):
+    x, res, w, dy = _rows(14, width, dtype, 1), _rows(14, width, dtype, 2), _weights(2, width), _rows(14, width, dtype, 3)
+    y, s, rstd = P.prsgd_rms_norm(x, w, residual=res)
+    over = res.clone()
+    again = P.prsgd_rms_norm(x, w, residual=over, out=over)
+    assert again[0] is over and torch.equal(over, y) and torch.equal(again[1], s)
+    dx, dw = P.prsgd_rms_norm_backward(dy, s, rstd, w)
+    over, gw = P.prsgd_rms_norm_backward(dy, s, rstd, w, dx=s)
+    assert torch.equal(over, dx) and torch.equal(gw, dw) and over.data_ptr() == s.data_ptr()

@@ -130,3 +130,22 @@ def test_the_binding_refuses_what_has_no_kernel(P):
         P.prsgd_orthogonalize(torch.zeros(3, 4))                       # no device tensor
     with pytest.raises(ValueError):
         P.prsgd_rms_norm(torch.zeros(3, 4), torch.ones(4))
+
+
+@pytest.mark.parametrize("args", [
+    (AT, 50, 3 * AT, 50, AT, 50, 2 * AT, 50, 2 * AT, 50), (AT, 50, 3 * AT, 50, AT, 50, None, 0, 3 * AT, 51),
+    (AT, 50, 3 * AT, 0, AT, 50, None, 0, 3 * AT, 50), (AT, 50, 3 * AT, 50, AT, 50, 3 * AT, 50, 3 * AT, 50),
+])
+def test_norms_refuse_outputs_on_each_other_or_elsewhere_in_place(P, args):
+    assert P._lib.prsgd_rms_norm(ctypes.byref(_norm(P)), *args, None, None) == P.PRSGD_EINVAL
+
+
+@pytest.mark.parametrize("y", [AT, 2 * AT, 3 * AT])
+def test_norm_fp8_is_not_in_place(P, y):
+    assert P._lib.prsgd_rms_norm_fp8(ctypes.byref(_norm(P)), AT, 50, 2 * AT, 50, AT, 50, 3 * AT, 50, y, 50, AT, None) == P.PRSGD_EINVAL
+
+
+def test_norm_backward_refuses_other_distances_in_place(P):
+    for dx in (AT, 2 * AT, 3 * AT):                                    # dy, dsum and s
+        args = [AT, 50, 2 * AT, 50, 3 * AT, 50, AT, AT, 50, dx, 51, AT, 50, AT]
+        assert P._lib.prsgd_rms_norm_backward(ctypes.byref(_norm(P)), *args, None) == P.PRSGD_EINVAL
