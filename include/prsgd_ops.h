@@ -76,8 +76,8 @@ int prsgd_muon_step(const prsgd_orth_config* cfg, void* x_dev, int64_t x_matrix,
  *   s = x + res,   rstd = 1 / sqrt(mean(s^2) + eps),   y = s * rstd * w_i
  * for rows_per_worker rows of each of `workers` workers (worker i owns the i-th run of rows and the weights w_i).
  * Sums, statistics and products are fp32 and every output is rounded once; y and rstd go by s as summed, before it is rounded.
- * Rows whose squares overflow fp32 are summed again at a smaller scale.  A row that holds a NaN or an infinity gives NaN where that is
- * (in 8 bits: everywhere), and no other row notices.
+ * Rows whose squares overflow fp32, or vanish beside an eps as small, are summed again at another scale.  A row that holds a
+ * NaN or an infinity gives NaN where that is (in 8 bits: everywhere), zeros with an eps of 0 too, and no other row notices.
  */
 typedef struct {
   int32_t dtype;                   /* PRSGD_F32 | PRSGD_BF16: type of x, res, s, y and their gradients */

@@ -137,6 +137,7 @@ template <int TPR, bool MAX> __device__ __forceinline__ void row_reduce(float& a
 template <int TPR> constexpr int threads_of() { return TPR > kThreads ? TPR : kThreads; }
 constexpr float kFp8Max = 448.0f;
 constexpr float kFp8Least = 0x1p-100f;    // a row of zeros has a scale too
+constexpr float kLeastSquares = 0x1p-90f;
 
 template <typename T, int TPR, int E, bool FP8, bool NT>
 __global__ void __launch_bounds__(threads_of<TPR>()) rms_norm_kernel(NormArgs p) {
@@ -179,10 +180,12 @@ __global__ void __launch_bounds__(threads_of<TPR>()) rms_norm_kernel(NormArgs p)
       }
     row_reduce<TPR, FP8>(a, m, parity);
     float rstd = 1.0f / sqrtf(a * inv_width + p.eps), top = m * rstd;
-    const bool past = !(a < INFINITY);
-    if (past || (FP8 && !(m < INFINITY))) {                // past fp32: squares again at 2^-80 of the row's size, |y| from normed elements
-      const float size = past ? 0x1p-80f : 1.0f;
-      if (past) {
+    // Squares past fp32 are summed again at 2^-80 of the row's size, ones that vanish beside an eps that small at 2^80; |y| is taken
+    // from normed elements where its own product with w is past fp32.
+    const bool past = !(a < INFINITY), least = a < kLeastSquares && p.eps < kLeastSquares;
+    if (past || least || (FP8 && !(m < INFINITY))) {
+      const float size = past ? 0x1p-80f : least ? 0x1p80f : 1.0f;
+      if (past || least) {
         parity ^= 1;
         a = 0.0f;
 #pragma unroll
@@ -190,7 +193,7 @@ __global__ void __launch_bounds__(threads_of<TPR>()) rms_norm_kernel(NormArgs p)
 #pragma unroll
           for (int e = 0; e < V; ++e) a = fmaf(s[q][e] * size, s[q][e] * size, a);
         row_reduce<TPR, false>(a, m, parity);
-        rstd = 1.0f / sqrtf(a * inv_width);
+        rstd = 1.0f / sqrtf(a * inv_width + p.eps * size * size);
       }
       if constexpr (FP8) {
         parity ^= 1;

@@ -305,3 +305,17 @@ def test_result_over_the_residual_and_gradient_over_the_rows(P, width, dtype):
     dx, dw = P.prsgd_rms_norm_backward(dy, s, rstd, w)
     over, gw = P.prsgd_rms_norm_backward(dy, s, rstd, w, dx=s)
     assert torch.equal(over, dx) and torch.equal(gw, dw) and over.data_ptr() == s.data_ptr()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width", [9, 100, 1000, 9000])
+@pytest.mark.parametrize("size,eps", [(1e-15, 0.0), (1e-20, 1e-39), (1e-25, 0.0), (1e-35, 0.0), (1e-17, 1e-34)])
+def test_rows_whose_squares_vanish(P, width, dtype, size, eps):
+    x, w = _rows(6, width, dtype, 1, size), _weights(2, width)
+    x[0] = 1.0
+    y, _, rstd = P.prsgd_rms_norm(x, w, eps=eps)
+    want = O.rms_norm(x, w, eps=eps)
+    _close(y, want[0], dtype)
+    assert float((rstd.double() / want[2] - 1).abs().max()) <= SUMS
+    q, scales, _ = P.prsgd_rms_norm_fp8(x, w, eps=eps)
+    assert float((scales.double() / (want[0].abs().amax(1) / 448.0) - 1).abs().max()) <= SUMS
