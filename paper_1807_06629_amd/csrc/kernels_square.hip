@@ -11,6 +11,7 @@
 // a library's batched product of that size 1100), X X^T 581 us for 136 of 256 tiles (5 rounds of 256 where 4.25 would do).  16 x 1024 x 1024
 // split, B X 107 us: 965 TFLOP/s of the three products.  Bound by latency where they are small: no launch is under 5 us (4 x 4 tiles
 // of 64 x 64 with a contraction of 256: 5.3), most of it the way from one kernel's last store to the next one's first operands.
+#include <algorithm>
 #include <atomic>
 #include <type_traits>
 
@@ -428,21 +429,31 @@ hipError_t launch_square(SquareArgs p, int epi, bool split, hipStream_t s) {
   const bool symmetric = epi == SQ_GRAM || epi == SQ_POLY;
   // Time of a launch in units of a 64 x 64 tile's products: tiles per compute unit times their size over their efficiency.  Of tiles that a
   // compute unit has several of in hand, parts of a round count as such; of 256 x 256 tiles whole rounds.
-  // Measured over 17 shapes from 64 x (128 x 256) to 8 x (2048 x 2048), every tile size for each of the three products: this takes the
+  // Measured over 28 shapes from 64 x (128 x 256) to 8 x (2048 x 2048), every tile size for each of the three products: this takes the
   // fastest or one within 4 % of a call.  Where it matters most: B X of 16 x (320 x 800) in bf16, call of 133 us in 64 x 64 tiles, 171 in
   // 256 x 256; X X^T of 8 x (1000 x 4096), 895 us in 128 x 128, 1018 in 256 x 256; B X of 8 x (2048 x 2048) 2244 us in 64 x 64, 1942 in
   // 128 x 128, 1766 in 256 x 256.  (128 x 256 tiles were nowhere better by more than 1 %.)  Split products keep to 128 x 128: larger tiles do not
   // leave two workgroups per compute unit the registers.
-  auto cost = [&](int b, bool whole, double efficiency) {
+  // 128 x 128 tiles: three workgroups of four wavefronts to a compute unit where there are that many; where there are two or one to each,
+  // workgroups of eight wavefronts that hold more of the contraction in LDS.  Calls in bf16: X X^T of 1 x (2048 x 2048), 136 tiles, 398 us
+  // in four wavefronts and 370 in eight, of 1 x (2900 x 2900), 276 tiles, 986 and 925, B X of 12 x (512 x 1000), 384 tiles, 196 and
+  // 187; from 513 tiles on the other way around (B X of 16 x (768 x 768) 372 and 383).  In fp32 1 to 2 %.
+  auto tiles = [&](int b) {
     const int64_t tm = (p.M + b - 1) / b, tn = (p.N + b - 1) / b;
-    const int64_t tiles = (symmetric ? tn * (tn + 1) / 2 : tm * tn) * p.count;
-    const double rounds = whole ? (double)((tiles + 255) / 256) : tiles < 256 ? 1.0 : (double)tiles / 256.0;
-    return rounds * (b / 64) * (b / 64) / efficiency;
+    return (symmetric ? tn * (tn + 1) / 2 : tm * tn) * p.count;
   };
-  const double huge = cost(256, true, 1.2), middle = cost(128, false, 0.9), small = cost(64, false, split ? 0.77 : 0.68);
-  if (split) return middle <= small ? launch_tile<128, 128, 2, 2, 3, 64, true>(p, epi, s) : launch_tile<64, 64, 2, 2, 4, 128, true>(p, epi, s);
-  if (huge <= middle && huge <= small) return launch_tile<256, 256, 4, 2, 2, 128, false>(p, epi, s);
-  return middle <= small ? launch_tile<128, 128, 2, 2, 3, 64, false>(p, epi, s) : launch_tile<64, 64, 2, 2, 4, 128, false>(p, epi, s);
+  auto cost = [](int64_t n, int b, double efficiency) { return (n < 256 ? 1.0 : (double)n / 256.0) * (b / 64) * (b / 64) / efficiency; };
+  const int64_t n_middle = tiles(128), n_huge = (tiles(256) + 255) / 256 * 256;
+  const double middle = cost(n_middle, 128, n_middle > 256 ? 0.9 : split ? 1.4 : 1.34), small = cost(tiles(64), 64, split ? 0.77 : 0.68);
+  if (!split && cost(n_huge, 256, 1.2) <= std::min(middle, small)) return launch_tile<256, 256, 4, 2, 2, 128, false>(p, epi, s);
+  auto launch = [&](auto split_) {
+    constexpr bool SPLIT = decltype(split_)::value;
+    if (middle > small) return launch_tile<64, 64, 2, 2, 4, 128, SPLIT>(p, epi, s);
+    if (n_middle <= 256) return launch_tile<128, 128, 4, 2, 3, 128, SPLIT>(p, epi, s);
+    if (n_middle <= 512) return launch_tile<128, 128, 4, 2, 2, 128, SPLIT>(p, epi, s);
+    return launch_tile<128, 128, 2, 2, 3, 64, SPLIT>(p, epi, s);
+  };
+  return split ? launch(std::true_type{}) : launch(std::false_type{});
 }
 
 }  // namespace prsgd

@@ -248,3 +248,18 @@ def test_the_largest_tiles_either_way_up(P, count, rows, cols, dtype):
     o = STEP["lr"] * STEP["scale"] * O.orthogonalize(g).flatten(1).norm(dim=1)
     rounding = 2.0 ** (-8 if dtype == BF16 else -23) * want.flatten(1).norm(dim=1)
     assert bool(((x.double() - want).flatten(1).norm(dim=1) <= TOL[dtype] * o + rounding).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("count,rows,cols", [(4, 600, 1001), (4, 1001, 600), (10, 700, 721), (10, 721, 700), (8, 970, 1003), (8, 1003, 970)])
+def test_a_workgroup_or_two_to_every_compute_unit(P, count, rows, cols, dtype):
+    """Numbers of tiles between those of the small calls and of the large ones."""
+    g = _matrices(count, rows, cols, dtype, seed=8)
+    o = O.orthogonalize(g)
+    assert _err(P.prsgd_orthogonalize(g), o) <= TOL[dtype]
+    x, m = g.float().mul(100).to(dtype), torch.zeros(count, rows, cols, device="cuda")
+    want, _ = O.muon_step(x, g, m, nesterov=True, **STEP)
+    P.prsgd_muon_step(x, g, m, STEP["lr"], momentum=STEP["mu"], weight_decay=STEP["weight_decay"], scale=STEP["scale"])
+    step = STEP["lr"] * STEP["scale"] * o.flatten(1).norm(dim=1)
+    rounding = 2.0 ** (-8 if dtype == BF16 else -23) * want.flatten(1).norm(dim=1)
+    assert bool(((x.double() - want).flatten(1).norm(dim=1) <= TOL[dtype] * step + rounding).all())
