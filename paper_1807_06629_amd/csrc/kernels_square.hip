@@ -437,7 +437,9 @@ hipError_t launch_square(SquareArgs p, int epi, bool split, hipStream_t s) {
   // 128 x 128 tiles: three workgroups of four wavefronts to a compute unit where there are that many; where there are two or one to each,
   // workgroups of eight wavefronts that hold more of the contraction in LDS.  Calls in bf16: X X^T of 1 x (2048 x 2048), 136 tiles, 398 us
   // in four wavefronts and 370 in eight, of 1 x (2900 x 2900), 276 tiles, 986 and 925, B X of 12 x (512 x 1000), 384 tiles, 196 and
-  // 187; from 513 tiles on the other way around (B X of 16 x (768 x 768) 372 and 383).  In fp32 1 to 2 %.
+  // 187; from 513 tiles on the other way around (B X of 16 x (768 x 768) 372 and 383).  In fp32 1 to 2 %.  More rounds of tiles than one over
+  // a long contraction run in two workgroups of four, half as many barriers (bf16 2 x (4096 x 4096) 3280 and 3010 us, fp32 7950 and
+  // 7340); over a short one in three (bf16 30 x (700 x 700) 528 and 560).
   auto tiles = [&](int b) {
     const int64_t tm = (p.M + b - 1) / b, tn = (p.N + b - 1) / b;
     return (symmetric ? tn * (tn + 1) / 2 : tm * tn) * p.count;
@@ -451,6 +453,7 @@ hipError_t launch_square(SquareArgs p, int epi, bool split, hipStream_t s) {
     if (middle > small) return launch_tile<64, 64, 2, 2, 4, 128, SPLIT>(p, epi, s);
     if (n_middle <= 256) return launch_tile<128, 128, 4, 2, 3, 128, SPLIT>(p, epi, s);
     if (n_middle <= 512) return launch_tile<128, 128, 4, 2, 2, 128, SPLIT>(p, epi, s);
+    if (n_middle > 768 && p.lda >= 2048) return launch_tile<128, 128, 2, 2, 2, 128, SPLIT>(p, epi, s);
     return launch_tile<128, 128, 2, 2, 3, 64, SPLIT>(p, epi, s);
   };
   return split ? launch(std::true_type{}) : launch(std::false_type{});

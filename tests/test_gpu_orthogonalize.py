@@ -263,3 +263,13 @@ def test_a_workgroup_or_two_to_every_compute_unit(P, count, rows, cols, dtype):
     step = STEP["lr"] * STEP["scale"] * o.flatten(1).norm(dim=1)
     rounding = 2.0 ** (-8 if dtype == BF16 else -23) * want.flatten(1).norm(dim=1)
     assert bool(((x.double() - want).flatten(1).norm(dim=1) <= TOL[dtype] * step + rounding).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("count,rows,cols", [(56, 520, 2050), (56, 2050, 520), (5, 2050, 2100), (5, 2100, 2050)])
+def test_many_tiles_over_a_long_contraction(P, count, rows, cols, dtype):
+    g = _matrices(count, rows, cols, dtype, seed=9)
+    want = O.orthogonalize(g)
+    got = P.prsgd_orthogonalize(g)
+    assert _err(got, want) <= TOL[dtype]
+    assert torch.equal(P.prsgd_orthogonalize(g), got)
