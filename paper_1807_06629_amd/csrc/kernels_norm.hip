@@ -5,8 +5,8 @@
 // A row is held in the registers of TPR threads, E elements each (fp32 once unpacked), so that every array crosses HBM once and
 // the row's one reduction is all that stands between its loads and its stores.  The row maximum of the 8-bit form needs no second
 // one: max |y| = rstd max |s w|.  Bound by HBM from a few thousand rows on, by the latency of a launch below:
-//   forward, bf16, 65536 rows of 4096 (2.15 GB)   377 us, 5.7 TB/s (a large copy: 4.7);  one row 3.5 us, a call of it 6.7
-//   8 bits, bf16, 800 rows of 1000                4.9 us, a call 6.7
+//   forward, bf16, 65536 rows of 4096 (2.15 GB)   378 us, 5.7 TB/s (a large copy: 4.7);  one row 3.4 us, a call of it 5.9
+//   8 bits, bf16, 800 rows of 1000                4.9 us, a call 6.0
 //   backward, bf16, 32768 rows of 4096 (1.07 GB)  210 + 5 us, 5.0 TB/s;  fp32, 1024 rows of 1024  5.9 + 2.7 us
 #include <algorithm>
 #include <type_traits>
