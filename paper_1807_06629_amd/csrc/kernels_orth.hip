@@ -225,7 +225,10 @@ __device__ __forceinline__ void gram_of(const OrthMatrices& p, const ShortShape&
   __syncthreads();
 }
 
-// d <- f(x y); every wavefront meets the others behind it.  (Blocks on and below the diagonal alone, with the others written as their
+// d <- f(y x^T), blocks come out transposed; every wavefront meets the others behind it.  Operands are symmetric but for rounding, and the
+// order counts for that: A <- (Q A^T) Q^T turns an unsymmetric rounding of A's around and makes it q_i q_j times as large, as it does a
+// symmetric one between two directions; Q (Q A^T) would make it 2 |b| + 1 times as large where A is the identity (1e-3 of the result after 14
+// default steps at 2 x 7, NaN after 30 of (2, -1.5, 0.5)).  (Blocks on and below the diagonal alone, with the others written as their
 // transposes, save a quarter of the products at NB = 4 and took as long: 55 against 52 us for a call on 64 x 64.)
 template <int NB, typename F>
 __device__ __forceinline__ void short_product(const double* x, const double* y, double* d, F&& f) {
@@ -268,7 +271,7 @@ __device__ __forceinline__ void polynomial_of(const OrthMatrices& p, double* lds
 #pragma unroll
       for (int q = 0; q < 4; ++q) f[q] = fma(c, square[q], fma(b, m[q], 4 * q + (lane >> 4) == (lane & 15) ? a : 0.0));
       poly = step == 0 ? f : product(f, poly);
-      if (step + 1 < p.steps) m = product(product(f, m), f);
+      if (step + 1 < p.steps) m = product(f, product(m, f));
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q) pf[0][0][q] = (float)poly[q];
@@ -290,8 +293,8 @@ __device__ __forceinline__ void polynomial_of(const OrthMatrices& p, double* lds
         spare = old;
       }
       if (step + 1 < p.steps) {
-        short_product<NB>(f, m, spare, plain);
-        short_product<NB>(spare, f, m, plain);
+        short_product<NB>(m, f, spare, plain);
+        short_product<NB>(f, spare, m, plain);
       }
     }
     __syncthreads();
