@@ -35,7 +35,8 @@ extern "C" {
  * dtype  PRSGD_F32: products of operands held to 22 bits, results to fp32 accuracy.
  *        PRSGD_BF16: products of operands held to 11 bits (fp16, scaled by a power of two), which leaves less error than
  *        the final rounding to bfloat16 does.  Either way products are accumulated in fp32, X itself is carried to 22
- *        bits between steps, and the norm is summed in 64.  A side of up to 64 is taken through its Gram matrix in 64 bits.
+ *        bits between steps, and the norm is summed in 64.  A side of up to 64 is taken through its Gram matrix in 64 bits
+ *        while steps are few (10 at these coefficients), by products beyond.
  * Coefficients have to keep singular values in [0, 1] below 2 and the middle factor |b s^2 + c s^4| below 7 at every
  * step (PRSGD_EINVAL otherwise): the range of the operands.
  */

@@ -109,8 +109,8 @@ __global__ void __launch_bounds__(kThreads) orth_load_kernel(OrthMatrices p, con
 // symmetric, and they commute):
 //   A_0 = K / (|U| + eps)^2,  Q = a + b A + c A A,  P <- Q P,  A <- Q A Q,   |U|^2 = trace K,
 // so U is read for K and for P U, 3 r^2 L operations in all instead of 3 r^2 L per step, and a whole call is one launch or two.  The Gram
-// matrix squares the condition: in 64 bits its smallest eigenvalues are as good as fp32 singular values are, in fp32 they may come out
-// negative and grow.  K and the polynomials run on v_mfma_f64_16x16x4, P U on v_mfma_f32_16x16x4.
+// matrix squares the condition: in 64 bits its smallest eigenvalues are as good as fp32 singular values are for as many steps as the
+// host lets through here (10 at the default coefficients); rounded ones may be negative, and grow without bound in the end.  K and the polynomials run on v_mfma_f64_16x16x4, P U on v_mfma_f32_16x16x4.
 // 64 x (128 x 10) 8.3 us in one launch of 64 workgroups, latency from end to end.  A call of this and of the products' path: 64 x (64 x
 // 64) in fp32 53 and 68 us, 64 x (64 x 512) 72 and 95, 4 x (64 x 4096) 79 and 176; in bf16 8 x (64 x 1024) 66 and 73, 64 x (64 x 512) 72 and 80.
 // A symmetric matrix of NB x NB blocks of 16 is kept as operands: element q of lane (g = lane / 16, i = lane % 16) of block (x, y) is

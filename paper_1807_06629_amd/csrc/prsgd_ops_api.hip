@@ -79,24 +79,33 @@ int norm_forward(const prsgd_norm_config* c, const void* x, int64_t x_row, const
 
 // ---- orthogonalised updates --------------------------------------------------------------------
 
-const char* orth_config_error(const prsgd_orth_config* c) {
+// What the polynomial does over the steps, on a grid over where the singular values are (they start in [0, 1]).
+struct OrthBounds {
+  float gram_growth;                           // product over the steps of the largest slope of A -> Q A Q in an eigenvalue of A
+};
+const char* orth_config_error(const prsgd_orth_config* c, OrthBounds* bounds) {
   if (c == nullptr) return "orthogonalize: config is null";
   if (c->dtype != PRSGD_F32 && c->dtype != PRSGD_BF16) return "orthogonalize: unknown dtype";
   if (c->count < 0 || c->count > 65535) return "orthogonalize: count out of range (0..65535)";
   if (c->rows < 1 || c->rows > kMaxOrthSide || c->cols < 1 || c->cols > kMaxOrthSide) return "orthogonalize: sides out of range (1..32768)";
   if (c->steps < 1 || c->steps > kMaxOrthSteps) return "orthogonalize: steps out of range (1..64)";
   if (!(c->eps >= 0.0f) || isinf(c->eps)) return "orthogonalize: eps must be finite and not negative";
-  // Singular values start in [0, 1]: the largest that a step can leave, and the middle factor, on a grid over where they are.
+  *bounds = {1.0f};
   float top = 1.0f;
   for (int k = 0; k < c->steps; ++k) {
-    float next = 0.0f, middle = 0.0f;
+    float next = 0.0f, slope = c->a * c->a;
     for (int i = 1; i <= 32; ++i) {
-      const float s = top * (float)i / 32.0f, q = s * s * (c->b + c->c * s * s), v = fabsf(s * (c->a + q));
+      const float s = top * (float)i / 32.0f, l = s * s, q = l * (c->b + c->c * l), v = fabsf(s * (c->a + q));
       if (!(fabsf(q) < 7.0f) || !(v < 2.0f)) return "orthogonalize: coefficients leave the range of the products";
-      if (fabsf(q) > middle) middle = fabsf(q);
       if (v > next) next = v;
+      const float d = fabsf((c->a + q) * (c->a + q + 2.0f * l * (c->b + 2.0f * c->c * l)));
+      if (d > slope) slope = d;
     }
-    if (next == top) break;
+    bounds->gram_growth *= slope;
+    if (next == top) {                         // and so on
+      bounds->gram_growth *= powf(slope, (float)(c->steps - 1 - k));
+      break;
+    }
     top = next;
   }
   return nullptr;
@@ -130,7 +139,14 @@ OrthPlan orth_plan(const prsgd_orth_config* c) {
   p.total = at;
   return p;
 }
-bool is_short(const prsgd_orth_config* c) { return c->rows <= kShortSide || c->cols <= kShortSide; }
+// A short side goes through its Gram matrix while that holds.  An eigenvalue of it that is zero comes out as 2^-52 of the trace, of either
+// sign, and grows by the slope at 0, a^2, per step; a negative one leaves every bound once it is about -1 (NaN from 20 default steps on).  Up
+// to 2^36 it stays below 2^-16, and errors below those of products of X in fp32: 10 default steps (2e-3 to 6e-3 of the result
+// where the side is of lower rank, against 5e-3 to 1e-2), 18 of (2, -1.5, 0.5), 30 of (1.5, -0.5, 0).  Products carry X itself, which any number leaves
+// in its range.
+bool is_short(const prsgd_orth_config* c, const OrthBounds& b) {
+  return (c->rows <= kShortSide || c->cols <= kShortSide) && b.gram_growth <= 0x1p36f;
+}
 size_t short_bytes(const prsgd_orth_config* c) {
   const int r = c->rows < c->cols ? c->rows : c->cols, longer = c->rows < c->cols ? c->cols : c->rows;
   const int slices = orth_short_slices(c->count, r, longer);
@@ -205,7 +221,7 @@ hipError_t run_squares(const prsgd_orth_config* c, const OrthMatrices& m, char* 
   return e;
 }
 
-int run_orth(const prsgd_orth_config* c, OrthMatrices m, void* ws, void* stream, const char* what) {
+int run_orth(const prsgd_orth_config* c, const OrthBounds& bounds, OrthMatrices m, void* ws, void* stream, const char* what) {
   m.count = c->count;
   m.rows = c->rows;
   m.cols = c->cols;
@@ -216,7 +232,7 @@ int run_orth(const prsgd_orth_config* c, OrthMatrices m, void* ws, void* stream,
   m.c = c->c;
   m.steps = c->steps;
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  if (is_short(c)) {
+  if (is_short(c, bounds)) {
     const int slices = c->rows < c->cols ? orth_short_slices(c->count, c->rows, c->cols) : orth_short_slices(c->count, c->cols, c->rows);
     return hip_result(launch_orth_short(m, reinterpret_cast<double*>(ws), slices, s), what);
   }
@@ -234,17 +250,19 @@ bool matrices_ok(const prsgd_orth_config* c, int64_t matrix, int64_t row) {
 extern "C" {
 
 size_t prsgd_orthogonalize_workspace_bytes(const prsgd_orth_config* cfg) {
-  if (const char* e = orth_config_error(cfg)) {
+  OrthBounds bounds;
+  if (const char* e = orth_config_error(cfg, &bounds)) {
     bad(e);
     return 0;
   }
   if (cfg->count == 0) return 0;
-  return is_short(cfg) ? short_bytes(cfg) : orth_plan(cfg).total;
+  return is_short(cfg, bounds) ? short_bytes(cfg) : orth_plan(cfg).total;
 }
 
 int prsgd_orthogonalize(const prsgd_orth_config* cfg, const void* g_dev, int64_t g_matrix, int64_t g_row, void* out_dev,
                         int64_t out_matrix, int64_t out_row, void* workspace_dev, void* hip_stream) {
-  if (const char* e = orth_config_error(cfg)) return bad(e);
+  OrthBounds bounds;
+  if (const char* e = orth_config_error(cfg, &bounds)) return bad(e);
   if (cfg->count == 0) return PRSGD_OK;
   if (g_dev == nullptr || out_dev == nullptr || workspace_dev == nullptr) return bad("orthogonalize: null buffer");
   const int es = element_bytes(cfg->dtype);
@@ -258,13 +276,14 @@ int prsgd_orthogonalize(const prsgd_orth_config* cfg, const void* g_dev, int64_t
   m.out = out_dev;
   m.out_matrix = out_matrix;
   m.out_row = out_row;
-  return run_orth(cfg, m, workspace_dev, hip_stream, "orthogonalize");
+  return run_orth(cfg, bounds, m, workspace_dev, hip_stream, "orthogonalize");
 }
 
 int prsgd_muon_step(const prsgd_orth_config* cfg, void* x_dev, int64_t x_matrix, int64_t x_row, const void* g_dev, int64_t g_matrix,
                     int64_t g_row, float* m_dev, int64_t m_matrix, int64_t m_row, float lr, float mu, int32_t nesterov,
                     float weight_decay, float scale, void* workspace_dev, void* hip_stream) {
-  if (const char* e = orth_config_error(cfg)) return bad(e);
+  OrthBounds bounds;
+  if (const char* e = orth_config_error(cfg, &bounds)) return bad(e);
   if (!(mu >= 0.0f && mu < 1.0f)) return bad("muon_step: momentum must be in [0, 1)");
   if (!isfinite(lr) || !isfinite(weight_decay) || !isfinite(scale)) return bad("muon_step: rate, decay or scale is not finite");
   if (cfg->count == 0) return PRSGD_OK;
@@ -289,7 +308,7 @@ int prsgd_muon_step(const prsgd_orth_config* cfg, void* x_dev, int64_t x_matrix,
   m.m_part = nesterov != 0 ? mu : 1.0f;
   m.keep = 1.0f - lr * weight_decay;
   m.step = lr * scale;
-  return run_orth(cfg, m, workspace_dev, hip_stream, "muon_step");
+  return run_orth(cfg, bounds, m, workspace_dev, hip_stream, "muon_step");
 }
 
 int prsgd_rms_norm(const prsgd_norm_config* cfg, const void* x_dev, int64_t x_row, const void* res_dev, int64_t res_row,
