@@ -32,7 +32,7 @@ extern "C" {
  * The coefficients (3.4445, -4.7750, 2.0315) with 5 steps bring singular values from 0.0021 on to between 0.68 and 1.21 (the local extremes of p).
  * A zero matrix gives zeros; a NaN or an infinity makes its own matrix NaN and no other.
  *
- * dtype  PRSGD_F32: products of operands held to 22 bits, results to fp32 accuracy.
+ * dtype  PRSGD_F32: products of operands held to 22 bits, results to fp32 accuracy, also where ||G|| is small beside eps.
  *        PRSGD_BF16: products of operands held to 11 bits (fp16, scaled by a power of two), which leaves less error than
  *        the final rounding to bfloat16 does.  Either way products are accumulated in fp32, X itself is carried to 22
  *        bits between steps, and the norm is summed in 64.  A side of up to 64 is taken through its Gram matrix in 64 bits

@@ -43,7 +43,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) orth_squares_k
   if (threadIdx.x == 0) parts[g * gridDim.x + blockIdx.x] = ((sums[0] + sums[1]) + sums[2]) + sums[3];
 }
 
-// X_0 = U / (|U| + eps) times kHalfScale as halves, a tile of 64 x 64 elements per workgroup.  TURNED: X is the transpose of U, by way of LDS.
+// X_0 = U / (|U| + eps) times kHalfScale and 2^room as halves, a tile of 64 x 64 elements per workgroup.  TURNED: X is the transpose of U, by way of LDS.
 template <typename T, bool TURNED>
 __global__ void __launch_bounds__(kThreads) orth_load_kernel(OrthMatrices p, const double* parts, int n_parts, OrthHalves h) {
   constexpr bool SPLIT = sizeof(T) == 4;
@@ -51,7 +51,13 @@ __global__ void __launch_bounds__(kThreads) orth_load_kernel(OrthMatrices p, con
   const int g = blockIdx.z, r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
   double squares = 0.0;
   for (int i = threadIdx.x & 63; i < n_parts; i += kWave) squares += parts[g * n_parts + i];
-  const double scale = norm_scale(wave_sum(squares), p.eps) * (double)kHalfScale;
+  squares = wave_sum(squares);
+  const double normal = norm_scale(squares, p.eps), size = sqrt(squares) * normal;        // |X_0|, below 2^e
+  int e = 0;
+  if (size > 0.0) (void)frexp(size, &e);
+  const int room = min(max(-e, 0), kMostRoom);
+  const double scale = ldexp(normal * (double)kHalfScale, room);
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) h.room[g] = room;
   const int lane_row = threadIdx.x >> 3, lane_col = (threadIdx.x & 7) * 8;
   const int rows = TURNED ? p.cols : p.rows, cols = TURNED ? p.rows : p.cols;           // of X
   auto write = [&](int row, int col, const float (&v)[8]) __attribute__((always_inline)) {

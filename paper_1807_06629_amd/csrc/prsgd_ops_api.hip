@@ -2,6 +2,7 @@
 #include <math.h>
 #include <stdio.h>
 
+#include <algorithm>
 #include <utility>
 
 #include "prsgd_internal.h"
@@ -82,6 +83,7 @@ int norm_forward(const prsgd_norm_config* c, const void* x, int64_t x_row, const
 // What the polynomial does over the steps, on a grid over where the singular values are (they start in [0, 1]).
 struct OrthBounds {
   float gram_growth;                           // product over the steps of the largest slope of A -> Q A Q in an eigenvalue of A
+  uint8_t grown[kMaxOrthSteps];                // X in front of step k is below 2^grown[k] |X_0| (or 255)
 };
 const char* orth_config_error(const prsgd_orth_config* c, OrthBounds* bounds) {
   if (c == nullptr) return "orthogonalize: config is null";
@@ -90,23 +92,29 @@ const char* orth_config_error(const prsgd_orth_config* c, OrthBounds* bounds) {
   if (c->rows < 1 || c->rows > kMaxOrthSide || c->cols < 1 || c->cols > kMaxOrthSide) return "orthogonalize: sides out of range (1..32768)";
   if (c->steps < 1 || c->steps > kMaxOrthSteps) return "orthogonalize: steps out of range (1..64)";
   if (!(c->eps >= 0.0f) || isinf(c->eps)) return "orthogonalize: eps must be finite and not negative";
-  *bounds = {1.0f};
-  float top = 1.0f;
+  bounds->gram_growth = 1.0f;
+  float top = 1.0f, slope = 0.0f, factor = 0.0f, x_growth = 1.0f;
+  bool settled = false;                        // steps to come are like the last one
   for (int k = 0; k < c->steps; ++k) {
-    float next = 0.0f, slope = c->a * c->a;
-    for (int i = 1; i <= 32; ++i) {
-      const float s = top * (float)i / 32.0f, l = s * s, q = l * (c->b + c->c * l), v = fabsf(s * (c->a + q));
-      if (!(fabsf(q) < 7.0f) || !(v < 2.0f)) return "orthogonalize: coefficients leave the range of the products";
-      if (v > next) next = v;
-      const float d = fabsf((c->a + q) * (c->a + q + 2.0f * l * (c->b + 2.0f * c->c * l)));
-      if (d > slope) slope = d;
+    int e = 0;
+    if (k > 0) (void)frexpf(x_growth, &e);
+    bounds->grown[k] = (uint8_t)std::min(e, 255);
+    if (!settled) {
+      float next = 0.0f;
+      slope = c->a * c->a;
+      factor = fabsf(c->a);
+      for (int i = 1; i <= 32; ++i) {
+        const float s = top * (float)i / 32.0f, l = s * s, q = l * (c->b + c->c * l), f = c->a + q, v = fabsf(s * f);
+        if (!(fabsf(q) < 7.0f) || !(v < 2.0f)) return "orthogonalize: coefficients leave the range of the products";
+        next = std::max(next, v);
+        factor = std::max(factor, fabsf(f));
+        slope = std::max(slope, fabsf(f * (f + 2.0f * l * (c->b + 2.0f * c->c * l))));
+      }
+      settled = next == top;
+      top = next;
     }
     bounds->gram_growth *= slope;
-    if (next == top) {                         // and so on
-      bounds->gram_growth *= powf(slope, (float)(c->steps - 1 - k));
-      break;
-    }
-    top = next;
+    x_growth = std::min(x_growth * std::max(factor, 1.0f), 0x1p120f);
   }
   return nullptr;
 }
@@ -115,7 +123,7 @@ const char* orth_config_error(const prsgd_orth_config* c, OrthBounds* bounds) {
 struct OrthPlan {
   bool split;
   int r, longer, ld_x, ld_a;
-  size_t x, x_lo, a, b, diag, parts, total;    // byte offsets
+  size_t x, x_lo, a, b, diag, room, parts, total;    // byte offsets
   int64_t x_gs, a_gs;                          // halves per matrix
 };
 OrthPlan orth_plan(const prsgd_orth_config* c) {
@@ -135,6 +143,7 @@ OrthPlan orth_plan(const prsgd_orth_config* c) {
   p.a = take(n * p.a_gs * 2);
   p.b = take(n * p.a_gs * 2);
   p.diag = p.split ? 0 : take(n * p.r * 2 * sizeof(float));
+  p.room = take(n * sizeof(int));
   p.parts = take(n * norm_parts(c->rows, c->cols) * sizeof(double));
   p.total = at;
   return p;
@@ -153,7 +162,7 @@ size_t short_bytes(const prsgd_orth_config* c) {
   return align256(slices == 1 ? 256 : (size_t)c->count * slices * orth_short_doubles(r) * sizeof(double));
 }
 
-hipError_t run_squares(const prsgd_orth_config* c, const OrthMatrices& m, char* ws, hipStream_t s) {
+hipError_t run_squares(const prsgd_orth_config* c, const OrthBounds& bounds, const OrthMatrices& m, char* ws, hipStream_t s) {
   const OrthPlan p = orth_plan(c);
   auto halves = [&](size_t offset) { return reinterpret_cast<uint16_t*>(ws + offset); };
   double* parts = reinterpret_cast<double*>(ws + p.parts);
@@ -162,14 +171,18 @@ hipError_t run_squares(const prsgd_orth_config* c, const OrthMatrices& m, char* 
   uint16_t* x_lo = p.split ? nullptr : halves(p.x_lo);
   uint16_t* a = halves(p.a);
   uint16_t* b = halves(p.b);
+  int* room = reinterpret_cast<int*>(ws + p.room);
   const float inv = 1.0f / kHalfScale;
 
   hipError_t e = launch_orth_squares(m, parts, s);
   if (e != hipSuccess) return e;
-  e = launch_orth_load(m, parts, OrthHalves{x, x_lo, y, p.x_gs, p.ld_x}, s);
+  e = launch_orth_load(m, parts, OrthHalves{x, x_lo, y, p.x_gs, p.ld_x, room}, s);
   for (int k = 0; k < c->steps && e == hipSuccess; ++k) {
     SquareArgs q{};
     q.count = c->count;
+    q.room = room;
+    q.grown = bounds.grown[k];
+    q.grown_next = bounds.grown[std::min(k + 1, c->steps - 1)];
     if (!p.split) q.diag = reinterpret_cast<float*>(ws + p.diag);
     // A = X X^T
     q.a = q.b = x;
@@ -236,7 +249,7 @@ int run_orth(const prsgd_orth_config* c, const OrthBounds& bounds, OrthMatrices 
     const int slices = c->rows < c->cols ? orth_short_slices(c->count, c->rows, c->cols) : orth_short_slices(c->count, c->cols, c->rows);
     return hip_result(launch_orth_short(m, reinterpret_cast<double*>(ws), slices, s), what);
   }
-  return hip_result(run_squares(c, m, reinterpret_cast<char*>(ws), s), what);
+  return hip_result(run_squares(c, bounds, m, reinterpret_cast<char*>(ws), s), what);
 }
 
 // matrices of a caller: rows apart by at least a row, matrices by at least a matrix (inputs and outputs alike)

@@ -43,6 +43,10 @@ constexpr int norm_parts(int rows, int cols) { return (int64_t)rows * cols < (1 
 // Operands are halves of X, A and B times 2^13: entries reach 8, and what a second half holds of an entry of 2^-12 (X_0 of
 // 4096 x 4096) is a normal number or loses less than 2^-36.
 constexpr float kHalfScale = 8192.0f;
+// Matrices whose norm is small beside eps give an X_0 that halves at this scale would hold in few bits or none (of norm 1e-5 at 1000 x 1000: ten
+// bits).  X is stored 2^room times as large then, room being what |X_0| leaves below 1, and less by what the steps may have made of it:
+// 2^max(0, room - grown[k]) in front of step k.  A and B need none of it, they are added to the coefficient a.
+constexpr int kMostRoom = 100;           // an X_0 below 2^-100 loses bits again, as the result does in its own type from 2^-126 on
 
 // What a call does with the matrices, whichever path computes.
 struct OrthMatrices {
@@ -76,19 +80,21 @@ struct SquareArgs {
   const uint16_t* lin; const uint16_t* lin_lo; int64_t lin_gs; int ld_lin;     // lin_lo: remainders of unsplit X
   uint16_t* out; uint16_t* out_lo; int64_t out_gs; int ldo;
   uint16_t* out_t; int64_t t_gs; int ldt;      // where transposed tiles of a symmetric result go (out)
+  const int* room;                             // per matrix
   float alpha, beta;                           // out = alpha lin + beta acc
   // Unsplit operands: B's diagonal, [M][2] per matrix: the half that the product takes and what it leaves out; both times diag_scale.
   float* diag; float diag_scale;
   int tiles_n, tiles;                          // per matrix; filled in by the launcher
   int count;
   bool transposed;                             // SQ_LAST: the caller's matrices hold the transpose
+  uint8_t grown, grown_next;                   // of X in front of this step and behind it
   OrthMatrices user;
 };
 hipError_t launch_square(SquareArgs p, int epi, bool split, hipStream_t s);
 
 hipError_t launch_orth_squares(const OrthMatrices& p, double* parts, hipStream_t s);
 // X [half_rows(short side)][ld_x]; spare: where the next one goes, whose padding rows are cleared with it
-struct OrthHalves { uint16_t* x; uint16_t* x_lo; uint16_t* spare; int64_t x_gs; int ld_x; };
+struct OrthHalves { uint16_t* x; uint16_t* x_lo; uint16_t* spare; int64_t x_gs; int ld_x; int* room; };
 hipError_t launch_orth_load(const OrthMatrices& p, const double* parts, const OrthHalves& h, hipStream_t s);
 // Short sides: slices of the long side a matrix is cut into (1: one launch), and the doubles of a slice's Gram matrix.
 int orth_short_slices(int count, int r, int longer);
