@@ -124,7 +124,7 @@ Tensor workspace(PyObject* o, size_t bytes, const Tensor& like) {
   return t;
 }
 
-// x, w, residual, eps, out, sum_out, stat, in 8 bits -> out, s, stat
+// x, w, residual, eps, out, sum_out, stat, in 8 bits -> out, s (or None), stat
 PyObject* rms_norm(PyObject* const* a) {
   const Tensor& x = tensor(a[0], "x");
   const NormCall c = norm_call(x, tensor(a[1], "w"), (float)number(a[3]));
@@ -146,7 +146,10 @@ PyObject* rms_norm(PyObject* const* a) {
                                   static_cast<uint8_t*>(yr.at), yr.distance, st, on.stream())
              : prsgd_rms_norm(&c.cfg, xr.at, xr.distance, rr.at, rr.distance, c.w, c.w_row, sr.at, sr.distance, yr.at, yr.distance, st,
                               on.stream()));
-  return Py_BuildValue("(NNN)", THPVariable_Wrap(out), THPVariable_Wrap(sum), THPVariable_Wrap(stat));
+  // rows that were their own sum are gone once the result has their place
+  const bool gone = a[2] == Py_None && a[5] == Py_None && x.numel() > 0 && yr.at == xr.at;
+  if (gone) Py_INCREF(Py_None);
+  return Py_BuildValue("(NNN)", THPVariable_Wrap(out), gone ? Py_None : THPVariable_Wrap(sum), THPVariable_Wrap(stat));
 }
 
 size_t back_bytes(const NormCall& c) {

@@ -481,7 +481,7 @@ def prsgd_rms_norm(x: torch.Tensor, w: torch.Tensor, residual: Optional[torch.Te
                    out: Optional[torch.Tensor] = None, sum_out: Optional[torch.Tensor] = None,
                    rstd: Optional[torch.Tensor] = None):
     """(y, s, rstd) of s = x + residual, y = s rstd w for the rows of every worker ([workers * rows][width], w [workers][width] or
-    [width]).  Without a residual s is x itself, and is written only if sum_out is given."""
+    [width]).  Without a residual s is x itself, and is written only if sum_out is given; None if y has taken x's place (out=x)."""
     return _ops.rms_norm(x, w, residual, eps, out, sum_out, rstd, False)
 
 
