@@ -5,6 +5,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -40,6 +41,17 @@ void finish(int status) {
 const Tensor& tensor(PyObject* o, const char* what) {
   if (!THPVariable_Check(o)) throw Refused(std::string(what) + " must be a tensor");
   return THPVariable_Unpack(o);
+}
+// A tensor that a call computes with or writes: no call records anything for autograd
+const Tensor& operand(PyObject* o, const char* what) {
+  const Tensor& t = tensor(o, what);
+  if (t.requires_grad() && c10::GradMode::is_enabled())
+    throw Refused(std::string(what) + " requires grad, and the operators record nothing: call them under torch.no_grad() or in a torch.autograd.Function");
+  return t;
+}
+// ... and one that it has written: autograd's check of what it saved has to see that
+void written(const Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
 double number(PyObject* o) {
   const double v = PyFloat_AsDouble(o);
@@ -109,32 +121,32 @@ NormCall norm_call(const Tensor& x, const Tensor& w, float eps) {
 }
 Tensor row_vector(PyObject* o, const Tensor& x, const char* name) {
   if (o == Py_None) return device_empty({x.size(0)}, at::kFloat, x);
-  const Tensor& t = tensor(o, name);
+  const Tensor& t = operand(o, name);
   if (t.scalar_type() != at::kFloat || t.device() != x.device() || t.dim() != 1 || t.size(0) != x.size(0) || !t.is_contiguous())
     throw Refused(std::string(name) + " must be contiguous float32, one value a row");
   return t;
 }
 Tensor given_or_empty(PyObject* o, const Tensor& like, at::ScalarType type, const char* name) {
-  return o == Py_None ? device_empty(like.sizes(), type, like) : tensor(o, name);
+  return o == Py_None ? device_empty(like.sizes(), type, like) : operand(o, name);
 }
 Tensor workspace(PyObject* o, size_t bytes, const Tensor& like) {
   if (o == Py_None) return device_empty({(int64_t)bytes}, at::kByte, like);
-  const Tensor& t = tensor(o, "workspace");
+  const Tensor& t = operand(o, "workspace");
   if (t.device() != like.device() || t.nbytes() < bytes || !t.is_contiguous()) throw Refused("the workspace must have " + std::to_string(bytes) + " bytes on the tensors' device");
   return t;
 }
 
 // x, w, residual, eps, out, sum_out, stat, in 8 bits -> out, s (or None), stat
 PyObject* rms_norm(PyObject* const* a) {
-  const Tensor& x = tensor(a[0], "x");
-  const NormCall c = norm_call(x, tensor(a[1], "w"), (float)number(a[3]));
+  const Tensor& x = operand(a[0], "x");
+  const NormCall c = norm_call(x, operand(a[1], "w"), (float)number(a[3]));
   const bool fp8 = a[7] == Py_True;
   const at::ScalarType type = x.scalar_type(), out_type = fp8 ? at::kFloat8_e4m3fn : type;
   OnDevice on(x);
   const Rows xr = rows_of(x, x, type, "x");
   Rows rr{nullptr, 0}, sr{nullptr, 0};
   Tensor sum = x;
-  if (a[2] != Py_None) rr = rows_of(tensor(a[2], "residual"), x, type, "residual");
+  if (a[2] != Py_None) rr = rows_of(operand(a[2], "residual"), x, type, "residual");
   if (a[2] != Py_None || a[5] != Py_None) {
     sum = given_or_empty(a[5], x, type, "sum_out");
     sr = rows_of(sum, x, type, "sum_out");
@@ -146,6 +158,9 @@ PyObject* rms_norm(PyObject* const* a) {
                                   static_cast<uint8_t*>(yr.at), yr.distance, st, on.stream())
              : prsgd_rms_norm(&c.cfg, xr.at, xr.distance, rr.at, rr.distance, c.w, c.w_row, sr.at, sr.distance, yr.at, yr.distance, st,
                               on.stream()));
+  written(out);
+  written(stat);
+  if (sr.at != nullptr) written(sum);
   // rows that were their own sum are gone once the result has their place
   const bool gone = a[2] == Py_None && a[5] == Py_None && x.numel() > 0 && yr.at == xr.at;
   if (gone) Py_INCREF(Py_None);
@@ -163,14 +178,14 @@ PyObject* rms_norm_backward_bytes(PyObject* const* a) {
 }
 // dy, s, rstd, w, dsum, dx, dw, workspace -> dx, dw
 PyObject* rms_norm_backward(PyObject* const* a) {
-  const Tensor& dy = tensor(a[0], "dy");
-  const Tensor& w = tensor(a[3], "w");
+  const Tensor& dy = operand(a[0], "dy");
+  const Tensor& w = operand(a[3], "w");
   const NormCall c = norm_call(dy, w, 0.0f);
   const at::ScalarType type = dy.scalar_type();
   OnDevice on(dy);
-  const Rows dyr = rows_of(dy, dy, type, "dy"), sr = rows_of(tensor(a[1], "s"), dy, type, "s");
+  const Rows dyr = rows_of(dy, dy, type, "dy"), sr = rows_of(operand(a[1], "s"), dy, type, "s");
   Rows dsr{nullptr, 0};
-  if (a[4] != Py_None) dsr = rows_of(tensor(a[4], "dsum"), dy, type, "dsum");
+  if (a[4] != Py_None) dsr = rows_of(operand(a[4], "dsum"), dy, type, "dsum");
   require(a[2] != Py_None, "rstd must be a tensor");
   const Tensor rstd = row_vector(a[2], dy, "rstd");
   Tensor dx = given_or_empty(a[5], dy, type, "dx"), dw = given_or_empty(a[6], w, at::kFloat, "dw");
@@ -181,6 +196,7 @@ PyObject* rms_norm_backward(PyObject* const* a) {
   const int64_t dw_row = dw.dim() == 2 && dw.size(0) > 1 ? dw.stride(0) : 0;
   finish(prsgd_rms_norm_backward(&c.cfg, dyr.at, dyr.distance, dsr.at, dsr.distance, sr.at, sr.distance, static_cast<const float*>(rstd.data_ptr()),
                                  c.w, c.w_row, dxr.at, dxr.distance, static_cast<float*>(dw.data_ptr()), dw_row, ws.data_ptr(), on.stream()));
+  for (const Tensor& t : {dx, dw, ws}) written(t);
   return Py_BuildValue("(NN)", THPVariable_Wrap(dx), THPVariable_Wrap(dw));
 }
 
@@ -227,7 +243,7 @@ PyObject* orthogonalize_bytes(PyObject* const* a) {
 }
 // g, out, coefficients, steps, eps, workspace -> out
 PyObject* orthogonalize(PyObject* const* a) {
-  const Tensor& g = tensor(a[0], "g");
+  const Tensor& g = operand(a[0], "g");
   const int32_t dtype = operand_type(g, "matrices must be a device tensor of float32 or bfloat16");
   const prsgd_orth_config c = orth_config(g.sizes(), dtype, a[2], a[3], a[4]);
   OnDevice on(g);
@@ -236,22 +252,26 @@ PyObject* orthogonalize(PyObject* const* a) {
   Tensor out = given_or_empty(a[1], g, g.scalar_type(), "out");
   const Matrices dst = matrices_of(out, g, g.scalar_type(), "out");
   finish(prsgd_orthogonalize(&c, src.at, src.matrix, src.row, dst.at, dst.matrix, dst.row, ws.data_ptr(), on.stream()));
+  written(out);
+  written(ws);
   return THPVariable_Wrap(out);
 }
 // x, g, m, lr, momentum, nesterov, weight decay, scale, coefficients, steps, eps, workspace
 PyObject* muon_step(PyObject* const* a) {
-  const Tensor& x = tensor(a[0], "x");
+  const Tensor& x = operand(a[0], "x");
   const int32_t dtype = operand_type(x, "matrices must be a device tensor of float32 or bfloat16");
   const prsgd_orth_config c = orth_config(x.sizes(), dtype, a[8], a[9], a[10]);
   OnDevice on(x);
-  const Matrices xs = matrices_of(x, x, x.scalar_type(), "x"), gs = matrices_of(tensor(a[1], "g"), x, x.scalar_type(), "g"),
-                 ms = matrices_of(tensor(a[2], "m"), x, at::kFloat, "m");
+  const Tensor& m = operand(a[2], "m");
+  const Matrices xs = matrices_of(x, x, x.scalar_type(), "x"), gs = matrices_of(operand(a[1], "g"), x, x.scalar_type(), "g"),
+                 ms = matrices_of(m, x, at::kFloat, "m");
   const int nesterov = PyObject_IsTrue(a[5]);
   if (nesterov < 0) throw Raised{};
   const Tensor ws = workspace(a[11], orth_bytes(c), x);
   finish(prsgd_muon_step(&c, xs.at, xs.matrix, xs.row, gs.at, gs.matrix, gs.row, static_cast<float*>(ms.at), ms.matrix, ms.row,
                          (float)number(a[3]), (float)number(a[4]), nesterov, (float)number(a[6]), (float)number(a[7]),
                          ws.data_ptr(), on.stream()));
+  for (const Tensor& t : {x, m, ws}) written(t);
   Py_RETURN_NONE;
 }
 
