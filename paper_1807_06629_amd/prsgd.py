@@ -131,10 +131,6 @@ def _load() -> ctypes.CDLL:
 
 
 _lib = _load()
-try:
-    from . import _ops
-except ImportError as e:
-    raise ImportError("_ops.so does not load; run `python -m paper_1807_06629_amd.build`") from e
 
 
 def make_config(n_workers: int, model: str, dims: Sequence[int], batch: int, rows_per_worker: int,
@@ -450,7 +446,22 @@ def prsgd_last_error(h: Optional[Handle]) -> str:
 # The marshalling is compiled (csrc/binding): ValueError for a tensor that no call takes, PrsgdError for what the library refuses.
 
 NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
-_ops.bind(_check)
+
+
+class _Operators:
+    """The compiled module, loaded by the first call of an operator: it is bound to one torch and one Python, the method's calls to neither."""
+
+    def __getattr__(self, name):
+        try:
+            from . import _ops as module
+        except ImportError as e:
+            raise ImportError("_ops.so does not load; run `python -m paper_1807_06629_amd.build`") from e
+        module.bind(_check)
+        self.__dict__.update((k, v) for k, v in vars(module).items() if not k.startswith("__"))
+        return getattr(module, name)
+
+
+_ops = _Operators()
 
 
 def prsgd_orthogonalize_workspace_bytes(shape: Sequence[int], dtype: torch.dtype, coefficients=NEWTON_SCHULZ, steps: int = 5,
