@@ -22,8 +22,10 @@ int hip_result(hipError_t e, const char* what) {
 size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 int element_bytes(int dtype) { return dtype == PRSGD_BF16 ? 2 : 4; }
 bool misaligned(const void* p, int bytes) { return (uintptr_t)p % (uintptr_t)bytes != 0; }
-// distances between rows (and matrices) whose products with the largest counts stay far inside 64 bits
+// distances between rows (and matrices) whose products with the counts, 2^16 matrices of 2^15 rows, stay far inside 64 bits; rows of norms,
+// up to 2^31 of them, are checked against their own number
 constexpr int64_t kMaxDistance = (int64_t)1 << 40;
+constexpr int64_t kMaxRowSpan = (int64_t)1 << 60;
 bool distance_ok(int64_t d, int64_t least) { return d >= least && d <= kMaxDistance; }
 
 // ---- norm ------------------------------------------------------------------------------------
@@ -39,7 +41,8 @@ const char* norm_config_error(const prsgd_norm_config* c) {
 }
 // inputs may repeat a row (distance 0), outputs may not
 bool rows_ok(const prsgd_norm_config* c, int64_t distance, bool output) {
-  return distance_ok(distance, output ? c->width : 0) && (distance == 0 || distance >= c->width);
+  if (!distance_ok(distance, output ? c->width : 0) || (distance != 0 && distance < c->width)) return false;
+  return distance <= kMaxRowSpan / std::max<int64_t>(1, c->workers * c->rows_per_worker);
 }
 
 int norm_forward(const prsgd_norm_config* c, const void* x, int64_t x_row, const void* res, int64_t res_row, const float* w,

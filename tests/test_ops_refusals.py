@@ -149,3 +149,16 @@ def test_norm_backward_refuses_other_distances_in_place(P):
     for dx in (AT, 2 * AT, 3 * AT):                                    # dy, dsum and s
         args = [AT, 50, 2 * AT, 50, 3 * AT, 50, AT, AT, 50, dx, 51, AT, 50, AT]
         assert P._lib.prsgd_rms_norm_backward(ctypes.byref(_norm(P)), *args, None) == P.PRSGD_EINVAL
+
+
+def test_norms_refuse_distances_whose_last_row_is_past_64_bits(P):
+    """The last of 2^31 - 1 rows of 2^40 elements' distance would start at 2^71."""
+    many = _norm(P, workers=1, rows_per_worker=(1 << 31) - 1)
+    far, ok = 1 << 40, (AT, 50)
+    for at in range(4):
+        d = [far if at == k else 50 for k in range(4)]
+        args = (AT, d[0], 2 * AT, d[1], AT, 50, 3 * AT, d[2], 4 * AT, d[3])
+        assert P._lib.prsgd_rms_norm(ctypes.byref(many), *args, None, None) == P.PRSGD_EINVAL
+        assert P._lib.prsgd_rms_norm_fp8(ctypes.byref(many), *args, AT, None) == P.PRSGD_EINVAL
+        back = (AT, d[0], 2 * AT, d[1], 3 * AT, d[2], AT, *ok, 4 * AT, d[3], *ok, AT)
+        assert P._lib.prsgd_rms_norm_backward(ctypes.byref(many), *back, None) == P.PRSGD_EINVAL
