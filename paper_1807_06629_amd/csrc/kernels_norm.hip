@@ -138,6 +138,7 @@ template <int TPR> constexpr int threads_of() { return TPR > kThreads ? TPR : kT
 constexpr float kFp8Max = 448.0f;
 constexpr float kFp8Least = 0x1p-100f;    // a row of zeros has a scale too
 constexpr float kLeastSquares = 0x1p-90f;
+constexpr float kLeastNormal = 0x1p-126f;
 
 template <typename T, int TPR, int E, bool FP8, bool NT>
 __global__ void __launch_bounds__(threads_of<TPR>()) rms_norm_kernel(NormArgs p) {
@@ -181,9 +182,10 @@ __global__ void __launch_bounds__(threads_of<TPR>()) rms_norm_kernel(NormArgs p)
     row_reduce<TPR, FP8>(a, m, parity);
     float rstd = 1.0f / sqrtf(a * inv_width + p.eps), top = m * rstd;
     // Squares past fp32 are summed again at 2^-80 of the row's size, ones that vanish beside an eps that small at 2^80; |y| is taken
-    // from normed elements where its own product with w is past fp32.
+    // from normed elements where their own products with w are past fp32 or below its normal numbers.  (All of them zero beside vanishing
+    // squares is no matter: rstd is 2^45 at most then, and the least scale that of 2^-100.)
     const bool past = !(a < INFINITY), least = a < kLeastSquares && p.eps < kLeastSquares;
-    if (past || least || (FP8 && !(m < INFINITY))) {
+    if (past || least || (FP8 && (!(m < INFINITY) || (m < kLeastNormal && (m > 0.0f || a > 0.0f))))) {
       const float size = past ? 0x1p-80f : least ? 0x1p80f : 1.0f;
       if (past || least) {
         parity ^= 1;

@@ -319,3 +319,21 @@ def test_rows_whose_squares_vanish(P, width, dtype, size, eps):
     assert float((rstd.double() / want[2] - 1).abs().max()) <= SUMS
     q, scales, _ = P.prsgd_rms_norm_fp8(x, w, eps=eps)
     assert float((scales.double() / (want[0].abs().amax(1) / 448.0) - 1).abs().max()) <= SUMS
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width,size,weight,eps", [(9, 1e-21, 1e-22, 1e-27), (100, 1e-21, 1e-22, 1e-27), (1000, 1e-21, 1e-22, 1e-27),
+                                                   (9000, 1e-21, 1e-22, 1e-27), (16384, 2.0 ** -51, 2.0 ** -98, 1e-40),
+                                                   (16384, 2.0 ** -51, 2.0 ** -100, 1e-40)])
+def test_eight_bits_of_weights_whose_products_vanish(P, width, size, weight, eps, dtype):
+    """s w is below fp32's normal numbers, or nothing at all, where y is not: scales go by y."""
+    x, w = _rows(6, width, dtype, 1, size), weight * _weights(2, width)
+    x[0] = 1.0                                                      # rows beside that need nothing of it
+    x[3] = 0.0
+    q, scales, _ = P.prsgd_rms_norm_fp8(x, w, eps=eps)
+    y = O.rms_norm(x, w, eps=eps)[0]
+    want = y.abs().amax(1).clamp(min=2.0 ** -100) / 448.0
+    assert float((scales.double() / want - 1).abs().max()) <= SUMS
+    got = q.float().double() * scales.double()[:, None]
+    step = torch.maximum(y.abs() * 2.0 ** -4, 2.0 ** -10 * scales.double()[:, None])
+    assert bool(((got - y).abs() <= step * (1 + 1e-4)).all())
