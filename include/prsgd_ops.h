@@ -63,7 +63,7 @@ int prsgd_orthogonalize(const prsgd_orth_config* cfg, const void* g_dev, int64_t
  * One step of momentum with an orthogonalised update on every worker's matrix X:
  *   M <- mu M + G,   U = G + mu M (nesterov != 0) or M,   O = orthogonalise(U),
  *   X <- (1 - lr * weight_decay) X - lr * scale * O.
- * x_dev and g_dev have cfg->dtype, momenta are fp32.  A scale of 0.2 sqrt(max(rows, cols)) gives updates of about the
+ * x_dev and g_dev have cfg->dtype, which also says how many bits the products hold; momenta are fp32.  A scale of 0.2 sqrt(max(rows, cols)) gives updates of about the
  * RMS that an elementwise adaptive step has.  The three buffers may not overlap.
  */
 int prsgd_muon_step(const prsgd_orth_config* cfg, void* x_dev, int64_t x_matrix, int64_t x_row,
@@ -77,7 +77,8 @@ int prsgd_muon_step(const prsgd_orth_config* cfg, void* x_dev, int64_t x_matrix,
  *   s = x + res,   rstd = 1 / sqrt(mean(s^2) + eps),   y = s * rstd * w_i
  * for rows_per_worker rows of each of `workers` workers (worker i owns the i-th run of rows and the weights w_i).
  * Sums, statistics and products are fp32 and every output is rounded once; y and rstd go by s as summed, before it is rounded.
- * Rows whose squares overflow fp32, or vanish beside an eps as small, are summed again at another scale.  A row that holds a
+ * Rows whose squares overflow fp32, or vanish beside an eps as small, are summed again at another scale (below an RMS of 2.9e-39 under an
+ * eps of 0 rstd itself overflows).  A row that holds a
  * NaN or an infinity gives NaN where that is (in 8 bits: everywhere), zeros with an eps of 0 too, and no other row notices.
  */
 typedef struct {

@@ -7,9 +7,11 @@
 // 32 at 512 x 512: error of the result 9e-4 so, 3e-2 with X in 11 bits throughout, 0.2 in bfloat16.)  B's diagonal, which holds most of
 // B where the spectrum is flat, is held to 22 bits as well and meets both halves of X, in the sums of B X's epilogue: 2.1e-3 -> 1.1e-3 at
 // 70 x 80, 1.5e-3 -> 8e-4 at 512 x 512 (where three quarters of the singular values are 0, 1e-3 -> 1.4e-3), for at most 1 % of a call's time.
-// Bound by the matrix cores and their power where matrices are large: 8 x 4096 x 4096 in half precision, B X 1122 us (980 TFLOP/s; on
-// another card 1084, 1014 TFLOP/s at 1.55 GHz; a library's batched product of that size 1100), X X^T 596 us for 136 of 256 tiles (5 rounds
-// of 256 where 4.25 would do).  16 x 1024 x 1024 split, B X 110 us: 934 TFLOP/s of the three products.  Bound by latency where they are small: no launch is under 5 us (4 x 4 tiles
+// Large matrices: 8 x 4096 x 4096 in half precision, B X 1122 us (980 TFLOP/s; on another card 1084, 1014 TFLOP/s).  The matrix cores are busy
+// 55 % of the cycles, at 1.7 GHz, and wavefronts wait 40 % of theirs: one workgroup to a compute unit, which meets at a barrier per 64 of depth and
+// has nothing beside its first requests and its epilogue.  A library's batched product of that size runs at 1100 TFLOP/s, 1000 us.  X X^T 596 us for
+// 136 of 256 tiles (5 rounds of 256 where 4.25 would do).  16 x 1024 x 1024 split, B X 110 us: 934 TFLOP/s of the three products.
+// Bound by latency where they are small: no launch is under 5 us (4 x 4 tiles
 // of 64 x 64 with a contraction of 256: 5.3), most of it the way from one kernel's last store to the next one's first operands.
 #include <algorithm>
 #include <atomic>

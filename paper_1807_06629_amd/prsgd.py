@@ -482,7 +482,8 @@ def prsgd_orthogonalize(g: torch.Tensor, out: Optional[torch.Tensor] = None, coe
 def prsgd_muon_step(x: torch.Tensor, g: torch.Tensor, m: torch.Tensor, lr: float, momentum: float = 0.95, nesterov: bool = True,
                     weight_decay: float = 0.0, scale: Optional[float] = None, coefficients=NEWTON_SCHULZ, steps: int = 5,
                     eps: float = 1e-7, workspace: Optional[torch.Tensor] = None) -> None:
-    """Momentum, orthogonalisation and update of every [rows][cols] matrix of x, in place on x and m (fp32).
+    """Momentum, orthogonalisation and update of every [rows][cols] matrix of x, in place on x and m (fp32).  The type of x, and of g, is also
+    that of the products: 22 bits for float32, 11 for bfloat16.
 
     scale defaults to 0.2 sqrt(max(rows, cols))."""
     if scale is None:
