@@ -275,6 +275,272 @@ PyObject* muon_step(PyObject* const* a) {
   Py_RETURN_NONE;
 }
 
+// ---- replicas of a model over tokens -----------------------------------------------------------
+
+// Matrices [workers][rows][cols] or [rows][cols] that go with the rows of all workers.
+struct Tables { void* at; int64_t workers, rows, cols, matrix, row; };
+Tables tables_of(const Tensor& t, const Tensor& like, at::ScalarType type, const char* name) {
+  if (t.device() != like.device() || t.scalar_type() != type || (t.dim() != 2 && t.dim() != 3))
+    throw Refused(std::string(name) + " must be [workers][rows][cols] or [rows][cols] on the device, and of the type, of the other operands");
+  if (t.size(-1) > 1 && t.stride(-1) != 1) throw Refused(std::string("rows of ") + name + " must be contiguous");
+  const bool many = t.dim() == 3;
+  return {t.data_ptr(), many ? t.size(0) : 1, t.size(-2), t.size(-1), many && t.size(0) > 1 ? t.stride(0) : 0, t.stride(-2)};
+}
+const int32_t* ids_of(const Tensor& t, const Tensor& like, const char* name) {
+  if (!t.is_cuda() || t.device() != like.device() || t.scalar_type() != at::kInt || t.dim() != 1 || (t.size(0) > 1 && t.stride(0) != 1))
+    throw Refused(std::string(name) + " must be contiguous int32, one value a row, on the rows' device");
+  return static_cast<const int32_t*>(t.data_ptr());
+}
+bool truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw Raised{};
+  return v != 0;
+}
+
+prsgd_embedding_config embedding_config(const Tensor& tokens, const Tables& t, int32_t dtype, float scale) {
+  prsgd_embedding_config c{};
+  require(t.workers > 0 && tokens.size(0) % t.workers == 0, "every worker must have the same number of tokens");
+  c.dtype = dtype;
+  c.workers = size32(t.workers);
+  c.rows_per_worker = tokens.size(0) / t.workers;
+  c.classes = size32(t.rows);
+  c.width = size32(t.cols);
+  c.scale = scale;
+  return c;
+}
+const char* const kTableType = "tables must be device tensors of float32 or bfloat16";
+// tokens, table, scale, out -> out
+PyObject* embedding(PyObject* const* a) {
+  const Tensor& tokens = operand(a[0], "tokens");
+  const Tensor& table = operand(a[1], "table");
+  const int32_t dtype = operand_type(table, kTableType);
+  const Tables t = tables_of(table, table, table.scalar_type(), "table");
+  const int32_t* ids = ids_of(tokens, table, "tokens");
+  const prsgd_embedding_config c = embedding_config(tokens, t, dtype, (float)number(a[2]));
+  OnDevice on(table);
+  Tensor out = a[3] == Py_None ? device_empty({tokens.size(0), t.cols}, table.scalar_type(), table) : operand(a[3], "out");
+  require(out.dim() == 2 && out.device() == table.device() && out.size(0) == tokens.size(0) && out.size(1) == t.cols, "out must be [rows][width] on the table's device");
+  const Rows yr = rows_of(out, out, table.scalar_type(), "out");
+  finish(prsgd_embedding(&c, ids, t.at, t.matrix, t.row, yr.at, yr.distance, on.stream()));
+  written(out);
+  return THPVariable_Wrap(out);
+}
+size_t embedding_bytes(const prsgd_embedding_config& c) {
+  const size_t n = prsgd_embedding_backward_workspace_bytes(&c);
+  if (n == 0) finish(PRSGD_EINVAL);
+  return n;
+}
+// tokens, table -> bytes
+PyObject* embedding_backward_bytes(PyObject* const* a) {
+  const Tensor& tokens = tensor(a[0], "tokens");
+  const Tensor& table = tensor(a[1], "table");
+  require(tokens.dim() == 1, "tokens must be [rows]");
+  const int32_t dtype = operand_type(table, kTableType);
+  return PyLong_FromSize_t(embedding_bytes(embedding_config(tokens, tables_of(table, table, table.scalar_type(), "table"), dtype, 1.0f)));
+}
+// dy, tokens, table, scale, dtable, workspace -> dtable
+PyObject* embedding_backward(PyObject* const* a) {
+  const Tensor& dy = operand(a[0], "dy");
+  const Tensor& tokens = operand(a[1], "tokens");
+  const Tensor& table = tensor(a[2], "table");             // its shape alone
+  const int32_t dtype = operand_type(table, kTableType);
+  const int32_t* ids = ids_of(tokens, table, "tokens");
+  const prsgd_embedding_config c = embedding_config(tokens, tables_of(table, table, table.scalar_type(), "table"), dtype, (float)number(a[3]));
+  require(dy.dim() == 2 && dy.device() == table.device() && dy.size(0) == tokens.size(0) && dy.size(1) == table.size(-1),
+          "dy must be [rows][width] on the table's device");
+  OnDevice on(table);
+  const Rows dyr = rows_of(dy, dy, table.scalar_type(), "dy");
+  Tensor dtable = given_or_empty(a[4], table, table.scalar_type(), "dtable");
+  require(dtable.sizes() == table.sizes(), "dtable must have the table's shape");
+  const Tables d = tables_of(dtable, table, table.scalar_type(), "dtable");
+  const Tensor ws = workspace(a[5], embedding_bytes(c), table);
+  finish(prsgd_embedding_backward(&c, ids, dyr.at, dyr.distance, d.at, d.matrix, d.row, ws.data_ptr(), on.stream()));
+  written(dtable);
+  written(ws);
+  return THPVariable_Wrap(dtable);
+}
+
+// Sequences of a scan: given, or as many as the starts or the states say, or one.
+struct ScanCall {
+  prsgd_scan_config cfg;
+  const int32_t* starts;
+};
+ScanCall scan_call(const Tensor& v, PyObject* sequences, PyObject* starts, PyObject* const* states, int n_states) {
+  ScanCall c{};
+  require(v.dim() == 2, "rows must be a [rows][width] tensor");
+  c.cfg.dtype = operand_type(v, "rows must be a device tensor of float32 or bfloat16");
+  int64_t n = sequences != Py_None ? integer(sequences) : -1;
+  if (starts != Py_None) {
+    const Tensor& t = operand(starts, "starts");
+    c.starts = ids_of(t, v, "starts");
+    if (n < 0) n = t.size(0) - 1;
+    require(t.size(0) == n + 1 && n >= 1, "starts must have one value more than there are sequences");
+  }
+  for (int i = 0; i < n_states && n < 0; ++i)
+    if (states[i] != Py_None) {
+      const Tensor& t = operand(states[i], "states");
+      require(t.dim() == 2, "states must be [sequences][width]");
+      n = t.size(0);
+    }
+  c.cfg.sequences = n < 0 ? 1 : size32(n);
+  c.cfg.rows = v.size(0);
+  c.cfg.width = size32(v.size(1));
+  return c;
+}
+Rows states_of(const Tensor& t, const Tensor& v, const ScanCall& c, const char* name) {
+  if (t.dim() != 2 || t.device() != v.device() || t.scalar_type() != at::kFloat || t.size(0) != c.cfg.sequences || t.size(1) != v.size(1))
+    throw Refused(std::string(name) + " must be float32 [sequences][width] on the rows' device");
+  return rows_of(t, t, at::kFloat, name);
+}
+Tensor states_given_or_empty(PyObject* o, const Tensor& v, const ScanCall& c, const char* name) {
+  return o == Py_None ? device_empty({c.cfg.sequences, v.size(1)}, at::kFloat, v) : operand(o, name);
+}
+// v, gate, sequences, starts, initial, out, last -> h, last
+PyObject* gated_scan(PyObject* const* a) {
+  const Tensor& v = operand(a[0], "v");
+  PyObject* const states[] = {a[4], a[6]};
+  ScanCall c = scan_call(v, a[2], a[3], states, 2);
+  const at::ScalarType type = v.scalar_type();
+  OnDevice on(v);
+  const Rows vr = rows_of(v, v, type, "v"), gr = rows_of(operand(a[1], "gate"), v, type, "gate");
+  Rows ir{nullptr, 0};
+  if (a[4] != Py_None) ir = states_of(operand(a[4], "initial"), v, c, "initial");
+  c.cfg.clear = a[5] == Py_None && c.starts != nullptr ? 1 : 0;
+  Tensor h = given_or_empty(a[5], v, type, "out"), last = states_given_or_empty(a[6], v, c, "last");
+  const Rows hr = rows_of(h, v, type, "out"), lr = states_of(last, v, c, "last");
+  finish(prsgd_gated_scan(&c.cfg, c.starts, vr.at, vr.distance, gr.at, gr.distance, static_cast<const float*>(ir.at), ir.distance, hr.at,
+                          hr.distance, static_cast<float*>(lr.at), lr.distance, on.stream()));
+  written(h);
+  written(last);
+  return Py_BuildValue("(NN)", THPVariable_Wrap(h), THPVariable_Wrap(last));
+}
+// dh, v, gate, h, sequences, starts, initial, dlast, dv, dgate, dinitial -> dv, dgate, dinitial
+PyObject* gated_scan_backward(PyObject* const* a) {
+  const Tensor& v = operand(a[1], "v");
+  PyObject* const states[] = {a[6], a[7], a[10]};
+  ScanCall c = scan_call(v, a[4], a[5], states, 3);
+  const at::ScalarType type = v.scalar_type();
+  OnDevice on(v);
+  const Rows dhr = rows_of(operand(a[0], "dh"), v, type, "dh"), vr = rows_of(v, v, type, "v"), gr = rows_of(operand(a[2], "gate"), v, type, "gate"),
+             hr = rows_of(operand(a[3], "h"), v, type, "h");
+  Rows ir{nullptr, 0}, dlr{nullptr, 0};
+  if (a[6] != Py_None) ir = states_of(operand(a[6], "initial"), v, c, "initial");
+  if (a[7] != Py_None) dlr = states_of(operand(a[7], "dlast"), v, c, "dlast");
+  if (c.starts != nullptr) c.cfg.clear = (a[8] == Py_None ? 1 : 0) + (a[9] == Py_None ? 2 : 0);
+  Tensor dv = given_or_empty(a[8], v, type, "dv"), dgate = given_or_empty(a[9], v, type, "dgate"),
+         dinitial = states_given_or_empty(a[10], v, c, "dinitial");
+  const Rows dvr = rows_of(dv, v, type, "dv"), dgr = rows_of(dgate, v, type, "dgate"), dir = states_of(dinitial, v, c, "dinitial");
+  finish(prsgd_gated_scan_backward(&c.cfg, c.starts, dhr.at, dhr.distance, vr.at, vr.distance, gr.at, gr.distance, hr.at, hr.distance,
+                                   static_cast<const float*>(ir.at), ir.distance, static_cast<const float*>(dlr.at), dlr.distance, dvr.at,
+                                   dvr.distance, dgr.at, dgr.distance, static_cast<float*>(dir.at), dir.distance, on.stream()));
+  for (const Tensor& t : {dv, dgate, dinitial}) written(t);
+  return Py_BuildValue("(NNN)", THPVariable_Wrap(dv), THPVariable_Wrap(dgate), THPVariable_Wrap(dinitial));
+}
+
+// x, p, seed, step, layer, residual, out -> out
+PyObject* dropout(PyObject* const* a) {
+  const Tensor& x = operand(a[0], "x");
+  prsgd_dropout_config c{};
+  require(x.dim() == 2, "rows must be a [rows][width] tensor");
+  c.dtype = operand_type(x, "rows must be a device tensor of float32 or bfloat16");
+  c.layer = integer(a[4]);
+  c.rows = x.size(0);
+  c.width = size32(x.size(1));
+  c.p = (float)number(a[1]);
+  auto word = [](PyObject* o) {
+    const unsigned long long v = PyLong_AsUnsignedLongLong(o);
+    if (v == (unsigned long long)-1 && PyErr_Occurred()) throw Raised{};
+    return (uint64_t)v;
+  };
+  c.seed = word(a[2]);
+  const int64_t* step = nullptr;
+  if (THPVariable_Check(a[3])) {
+    const Tensor& t = operand(a[3], "step");
+    require(t.scalar_type() == at::kLong && t.device() == x.device() && t.numel() == 1, "step must be a number or an int64 tensor of one on the rows' device");
+    step = static_cast<const int64_t*>(t.data_ptr());
+  } else {
+    c.step = word(a[3]);
+  }
+  OnDevice on(x);
+  const Rows xr = rows_of(x, x, x.scalar_type(), "x");
+  Rows rr{nullptr, 0};
+  if (a[5] != Py_None) rr = rows_of(operand(a[5], "residual"), x, x.scalar_type(), "residual");
+  Tensor out = given_or_empty(a[6], x, x.scalar_type(), "out");
+  const Rows yr = rows_of(out, x, x.scalar_type(), "out");
+  finish(prsgd_dropout(&c, step, xr.at, xr.distance, rr.at, rr.distance, yr.at, yr.distance, on.stream()));
+  written(out);
+  return THPVariable_Wrap(out);
+}
+
+struct XentCall {
+  prsgd_xent_config cfg;
+  Tables w;
+};
+XentCall xent_call(const Tensor& h, const Tensor& w, PyObject* classes_first) {
+  XentCall c{};
+  require(h.dim() == 2, "rows must be a [rows][width] tensor");
+  c.cfg.dtype = operand_type(h, "rows must be a device tensor of float32 or bfloat16");
+  c.w = tables_of(w, h, h.scalar_type(), "w");
+  c.cfg.classes_first = truth(classes_first) ? 1 : 0;
+  require(c.w.workers > 0 && h.size(0) % c.w.workers == 0, "every worker must have the same number of rows");
+  require((c.cfg.classes_first != 0 ? c.w.cols : c.w.rows) == h.size(1), "w must be [width][classes], or [classes][width] with classes_first, of the rows' width");
+  c.cfg.workers = size32(c.w.workers);
+  c.cfg.rows_per_worker = h.size(0) / c.w.workers;
+  c.cfg.width = size32(h.size(1));
+  c.cfg.classes = size32(c.cfg.classes_first != 0 ? c.w.rows : c.w.cols);
+  return c;
+}
+size_t xent_bytes(const XentCall& c, bool backward) {
+  const size_t n = backward ? prsgd_linear_cross_entropy_backward_workspace_bytes(&c.cfg) : prsgd_linear_cross_entropy_workspace_bytes(&c.cfg);
+  if (n == 0) finish(PRSGD_EINVAL);
+  return n;
+}
+// h, w, classes_first, backward -> bytes
+PyObject* linear_cross_entropy_bytes(PyObject* const* a) {
+  return PyLong_FromSize_t(xent_bytes(xent_call(tensor(a[0], "h"), tensor(a[1], "w"), a[2]), a[3] == Py_True));
+}
+const int32_t* labels_of(PyObject* o, const Tensor& h) {
+  const Tensor& t = operand(o, "labels");
+  const int32_t* at = ids_of(t, h, "labels");
+  require(t.size(0) == h.size(0), "labels must have one value a row");
+  return at;
+}
+// h, w, labels, classes_first, loss, lse, workspace -> loss, lse
+PyObject* linear_cross_entropy(PyObject* const* a) {
+  const Tensor& h = operand(a[0], "h");
+  const XentCall c = xent_call(h, operand(a[1], "w"), a[3]);
+  const int32_t* labels = labels_of(a[2], h);
+  OnDevice on(h);
+  const Rows hr = rows_of(h, h, h.scalar_type(), "h");
+  Tensor loss = row_vector(a[4], h, "loss"), lse = row_vector(a[5], h, "lse");
+  const Tensor ws = workspace(a[6], xent_bytes(c, false), h);
+  finish(prsgd_linear_cross_entropy(&c.cfg, hr.at, hr.distance, c.w.at, c.w.matrix, c.w.row, labels, static_cast<float*>(loss.data_ptr()),
+                                    static_cast<float*>(lse.data_ptr()), ws.data_ptr(), on.stream()));
+  for (const Tensor& t : {loss, lse, ws}) written(t);
+  return Py_BuildValue("(NN)", THPVariable_Wrap(loss), THPVariable_Wrap(lse));
+}
+// dloss, h, w, labels, lse, classes_first, dh, dw, workspace -> dh, dw
+PyObject* linear_cross_entropy_backward(PyObject* const* a) {
+  const Tensor& h = operand(a[1], "h");
+  const Tensor& w = operand(a[2], "w");
+  const XentCall c = xent_call(h, w, a[5]);
+  const int32_t* labels = labels_of(a[3], h);
+  OnDevice on(h);
+  const Rows hr = rows_of(h, h, h.scalar_type(), "h");
+  require(a[0] != Py_None && a[4] != Py_None, "dloss and lse must be tensors");
+  const Tensor dloss = row_vector(a[0], h, "dloss"), lse = row_vector(a[4], h, "lse");
+  Tensor dh = given_or_empty(a[6], h, h.scalar_type(), "dh"), dw = given_or_empty(a[7], w, h.scalar_type(), "dw");
+  const Rows dhr = rows_of(dh, h, h.scalar_type(), "dh");
+  require(dw.sizes() == w.sizes(), "dw must have w's shape");
+  const Tables d = tables_of(dw, h, h.scalar_type(), "dw");
+  const Tensor ws = workspace(a[8], xent_bytes(c, true), h);
+  finish(prsgd_linear_cross_entropy_backward(&c.cfg, static_cast<const float*>(dloss.data_ptr()), hr.at, hr.distance, c.w.at, c.w.matrix, c.w.row,
+                                             labels, static_cast<const float*>(lse.data_ptr()), dhr.at, dhr.distance, d.at, d.matrix, d.row,
+                                             ws.data_ptr(), on.stream()));
+  for (const Tensor& t : {dh, dw, ws}) written(t);
+  return Py_BuildValue("(NN)", THPVariable_Wrap(dh), THPVariable_Wrap(dw));
+}
+
 PyObject* bind(PyObject* const* a) {
   Py_XDECREF(g_check);
   g_check = a[0];
@@ -307,6 +573,15 @@ PyMethodDef methods[] = {PRSGD_METHOD(bind, 1),
                          PRSGD_METHOD(orthogonalize, 6),
                          PRSGD_METHOD(orthogonalize_bytes, 7),
                          PRSGD_METHOD(muon_step, 12),
+                         PRSGD_METHOD(embedding, 4),
+                         PRSGD_METHOD(embedding_backward, 6),
+                         PRSGD_METHOD(embedding_backward_bytes, 2),
+                         PRSGD_METHOD(gated_scan, 7),
+                         PRSGD_METHOD(gated_scan_backward, 11),
+                         PRSGD_METHOD(dropout, 7),
+                         PRSGD_METHOD(linear_cross_entropy, 7),
+                         PRSGD_METHOD(linear_cross_entropy_backward, 9),
+                         PRSGD_METHOD(linear_cross_entropy_bytes, 4),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_ops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

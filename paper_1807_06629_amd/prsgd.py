@@ -70,6 +70,26 @@ class prsgd_norm_config(ctypes.Structure):
                 ("width", ctypes.c_int32), ("eps", ctypes.c_float)]
 
 
+class prsgd_embedding_config(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("workers", ctypes.c_int32), ("rows_per_worker", ctypes.c_int64),
+                ("classes", ctypes.c_int32), ("width", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class prsgd_scan_config(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("sequences", ctypes.c_int32), ("rows", ctypes.c_int64), ("width", ctypes.c_int32),
+                ("clear", ctypes.c_int32)]
+
+
+class prsgd_dropout_config(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("layer", ctypes.c_int32), ("rows", ctypes.c_int64), ("width", ctypes.c_int32),
+                ("p", ctypes.c_float), ("seed", ctypes.c_uint64), ("step", ctypes.c_uint64)]
+
+
+class prsgd_xent_config(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("workers", ctypes.c_int32), ("rows_per_worker", ctypes.c_int64),
+                ("width", ctypes.c_int32), ("classes", ctypes.c_int32), ("classes_first", ctypes.c_int32)]
+
+
 def _load() -> ctypes.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError("libprsgd.so is not built; run `python -m paper_1807_06629_amd.build`")
@@ -78,6 +98,8 @@ def _load() -> ctypes.CDLL:
     vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     f32 = ctypes.c_float
     orthp, normp = ctypes.POINTER(prsgd_orth_config), ctypes.POINTER(prsgd_norm_config)
+    embp, scanp = ctypes.POINTER(prsgd_embedding_config), ctypes.POINTER(prsgd_scan_config)
+    dropp, xentp = ctypes.POINTER(prsgd_dropout_config), ctypes.POINTER(prsgd_xent_config)
     sigs = {
         "prsgd_param_count": (sz, [cfgp]),
         "prsgd_param_stride": (sz, [cfgp]),
@@ -122,6 +144,16 @@ def _load() -> ctypes.CDLL:
         "prsgd_rms_norm_fp8": (ctypes.c_int, [normp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp]),
         "prsgd_rms_norm_backward_workspace_bytes": (sz, [normp]),
         "prsgd_rms_norm_backward": (ctypes.c_int, [normp, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, vp]),
+        "prsgd_embedding": (ctypes.c_int, [embp, vp, vp, i64, i64, vp, i64, vp]),
+        "prsgd_embedding_backward_workspace_bytes": (sz, [embp]),
+        "prsgd_embedding_backward": (ctypes.c_int, [embp, vp, vp, i64, vp, i64, i64, vp, vp]),
+        "prsgd_gated_scan": (ctypes.c_int, [scanp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp]),
+        "prsgd_gated_scan_backward": (ctypes.c_int, [scanp, vp] + [vp, i64] * 9 + [vp]),
+        "prsgd_dropout": (ctypes.c_int, [dropp, vp, vp, i64, vp, i64, vp, i64, vp]),
+        "prsgd_linear_cross_entropy_workspace_bytes": (sz, [xentp]),
+        "prsgd_linear_cross_entropy": (ctypes.c_int, [xentp, vp, i64, vp, i64, i64, vp, vp, vp, vp, vp]),
+        "prsgd_linear_cross_entropy_backward_workspace_bytes": (sz, [xentp]),
+        "prsgd_linear_cross_entropy_backward": (ctypes.c_int, [xentp, vp, vp, i64, vp, i64, i64, vp, vp, vp, i64, vp, i64, i64, vp, vp]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -516,3 +548,69 @@ def prsgd_rms_norm_backward(dy: torch.Tensor, s: torch.Tensor, rstd: torch.Tenso
                             dw: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """(dx, dw) of prsgd_rms_norm: dx is the gradient of x and of the residual alike, dw has w's shape."""
     return _ops.rms_norm_backward(dy, s, rstd, w, dsum, dx, dw, workspace)
+
+
+def prsgd_embedding(tokens: torch.Tensor, table: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Rows of the workers' tables by token, times scale: tokens int32 [workers * rows], table [workers][classes][width] or
+    [classes][width]; tokens that are no row of the table (padding, -1) give zeros."""
+    return _ops.embedding(tokens, table, scale, out)
+
+
+def prsgd_embedding_backward_workspace_bytes(tokens: torch.Tensor, table: torch.Tensor) -> int:
+    return _ops.embedding_backward_bytes(tokens, table)
+
+
+def prsgd_embedding_backward(dy: torch.Tensor, tokens: torch.Tensor, table: torch.Tensor, scale: float = 1.0,
+                             dtable: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient of prsgd_embedding's table, of which the shape and type are taken and nothing is read."""
+    return _ops.embedding_backward(dy, tokens, table, scale, dtable, workspace)
+
+
+def prsgd_gated_scan(v: torch.Tensor, gate: torch.Tensor, sequences: Optional[int] = None, starts: Optional[torch.Tensor] = None,
+                     initial: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, last: Optional[torch.Tensor] = None):
+    """(h, last) of h_t = f h_{t-1} + (1 - f) v_t, f = sigmoid(gate), along every sequence of v and gate [rows][width]: from initial
+    (fp32 [sequences][width], zeros if None) to last, which may be initial.  Sequences are equal runs of rows, or packed ones that
+    start at starts (int32 [sequences + 1] on the device); rows that none of them has are left as they are in `out`, zeros if that is not given.
+    Their number is that of starts, of initial, or one, where it is not given."""
+    return _ops.gated_scan(v, gate, sequences, starts, initial, out, last)
+
+
+def prsgd_gated_scan_backward(dh: torch.Tensor, v: torch.Tensor, gate: torch.Tensor, h: torch.Tensor, sequences: Optional[int] = None,
+                              starts: Optional[torch.Tensor] = None, initial: Optional[torch.Tensor] = None,
+                              dlast: Optional[torch.Tensor] = None, dv: Optional[torch.Tensor] = None,
+                              dgate: Optional[torch.Tensor] = None, dinitial: Optional[torch.Tensor] = None):
+    """(dv, dgate, dinitial) of prsgd_gated_scan from dh and dlast (fp32, zeros if None); h is what it returned."""
+    return _ops.gated_scan_backward(dh, v, gate, h, sequences, starts, initial, dlast, dv, dgate, dinitial)
+
+
+def prsgd_dropout(x: torch.Tensor, p: float, seed: int, step=0, layer: int = 0, residual: Optional[torch.Tensor] = None,
+                  out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """residual + x with elements dropped with probability p (to 2^-16) and the others scaled to keep the mean; rows [rows][width].
+
+    The mask is a function of (seed, step, layer, place), so that the gradient of x is this call on dy without the residual.  step is a
+    number or an int64 device tensor of one, which is read when the call runs: replays of a captured call go by what it holds then."""
+    return _ops.dropout(x, p, seed, step, layer, residual, out)
+
+
+def prsgd_linear_cross_entropy_workspace_bytes(h: torch.Tensor, w: torch.Tensor, classes_first: bool = False) -> int:
+    return _ops.linear_cross_entropy_bytes(h, w, classes_first, False)
+
+
+def prsgd_linear_cross_entropy(h: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, classes_first: bool = False,
+                               loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                               workspace: Optional[torch.Tensor] = None):
+    """(loss, lse) of every row of h [workers * rows][width], whose logits are its product with its worker's matrix: w
+    [workers][width][classes] or [width][classes], or (classes_first, as an embedding's table) [workers][classes][width] or
+    [classes][width].  labels are int32; a row whose label is no class (padding, -1) has a loss of 0."""
+    return _ops.linear_cross_entropy(h, w, labels, classes_first, loss, lse, workspace)
+
+
+def prsgd_linear_cross_entropy_backward_workspace_bytes(h: torch.Tensor, w: torch.Tensor, classes_first: bool = False) -> int:
+    return _ops.linear_cross_entropy_bytes(h, w, classes_first, True)
+
+
+def prsgd_linear_cross_entropy_backward(dloss: torch.Tensor, h: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, lse: torch.Tensor,
+                                        classes_first: bool = False, dh: Optional[torch.Tensor] = None,
+                                        dw: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """(dh, dw) of prsgd_linear_cross_entropy from dloss (fp32, one value a row), in the types and shapes of h and w."""
+    return _ops.linear_cross_entropy_backward(dloss, h, w, labels, lse, classes_first, dh, dw, workspace)
