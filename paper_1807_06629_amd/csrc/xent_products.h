@@ -1,0 +1,203 @@
+// The products of the cross entropy and its gradients, with what each does with its tiles.
+//   PX_STATS  z^T = W^T h^T    a tile of logits becomes the maximum, the sum of exponentials and the label's logit of each of its rows
+//   PX_DZ     z = h W          ... becomes dz, in the rows' type
+//   PX_DH     dh = dz W^T      summed over the pieces of the classes in fp32
+//   PX_DW     dW = h^T dz
+// (PX_STATS has the classes along the accumulators' rows, 16 of them a lane, so that most of a row's reduction stays in registers.)
+#pragma once
+
+#include <math.h>
+
+#include <atomic>
+#include <type_traits>
+
+#include "gemm_tile.h"
+#include "orth_rows.h"
+#include "prsgd_token_internal.h"
+
+namespace prsgd {
+
+// One matrix of every worker: element (i, c), c the contraction index, at p + g * gs + i * ld + c, or (transposed) + c * ld + i.
+struct Operand { const void* p; int64_t gs, ld; bool dz; };
+struct ProductArgs {
+  Operand a, b;
+  int M, N, K;                           // rows of A, rows of B, contraction
+  int tiles_m, tiles_n, groups;          // tiles: filled in by the launcher
+  // of the rows, `rows` in every worker
+  const int32_t* labels;
+  const float* lse; const float* dloss;
+  int64_t rows;
+  int class0, classes;                   // first class of the piece; of all
+  float2* stats; int stat_tiles; float* picked;      // PX_STATS
+  void* out; int64_t out_gs, out_ld;     // the others
+  float* sums;                           // PX_DH over several pieces: [groups][M][N] fp32
+  bool first_piece, last_piece;
+  uint32_t* real;                        // rows with a label, 32 to a word, (rows + 63) / 64 * 2 words a worker: PX_DZ of the first piece writes them
+};
+enum ProductEpilogue { PX_STATS = 0, PX_DZ = 1, PX_DH = 2, PX_DW = 3 };
+
+template <typename T> constexpr bool kIsBf16 = std::is_same_v<T, uint16_t>;
+__host__ __device__ constexpr int64_t real_words(int64_t rows) { return (rows + 63) / 64 * 2; }
+
+// (m, s) of the union of two sets of logits, s the sum of exp(z - m)
+__device__ __forceinline__ void join_stats(float& m, float& s, float m2, float s2) {
+  const float top = fmaxf(m, m2);
+  // a set without logits, or of logits of -infinity alone, has no sum
+  s = (s == 0.0f ? 0.0f : s * expf(m - top)) + (s2 == 0.0f ? 0.0f : s2 * expf(m2 - top));
+  m = top;
+}
+
+// Rows of the accumulators: element e of a 32 x 32 block lies at row acc_row(e, lane), column lane % 32.
+__device__ __forceinline__ int acc_row(int e, int lane) { return 8 * (e / 4) + 4 * (lane >> 5) + (e & 3); }
+
+constexpr int kStripPad = 8;             // floats: the four rows between a register's two halves lie 32 banks apart
+template <int BM, int BN, int WM, int WN, int EPI> constexpr int epilogue_lds_bytes() {
+  return EPI == PX_STATS ? WM * BN * (int)sizeof(float2) : WM * WN * 32 * (BN / WN + kStripPad) * 4;
+}
+
+// Workgroup-wide: the last reads of the operands' tiles in smem are over.
+template <typename T, int EPI, int BM, int BN, int WM, int WN>
+__device__ __forceinline__ void product_epilogue(const ProductArgs& p, const f32x16_t (&acc)[BM / WM / 32][BN / WN / 32], int g, int m0, int n0, int ti,
+                                                 int wm, int wn, int lane, unsigned char* smem) {
+  constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
+  if constexpr (EPI == PX_STATS) {
+    float2* shared = reinterpret_cast<float2*>(smem);        // [WM][BN]
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int col = (wn * TN + j) * 32 + (lane & 31), row = n0 + col;
+      const bool live = row < p.N;
+      const int label = live ? p.labels[g * p.rows + row] : -1;
+      float m = -INFINITY, s = 0.0f;
+      bool odd = false;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int c = m0 + (wm * TM + i) * 32 + acc_row(e, lane);
+          if (c < p.M) {
+            m = fmaxf(m, acc[i][j][e]);
+            odd = odd || !(acc[i][j][e] <= INFINITY);          // fmaxf passes over what is no number
+            if (c == label) p.picked[g * p.rows + row] = acc[i][j][e];
+          }
+        }
+      const float top = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int c = m0 + (wm * TM + i) * 32 + acc_row(e, lane);
+          if (c < p.M) s += expf(acc[i][j][e] - top);
+        }
+      if (odd) s = NAN;
+      join_stats(m, s, __shfl_xor(m, 32), __shfl_xor(s, 32));
+      if (lane < 32) shared[wm * BN + col] = make_float2(m, s);
+    }
+    __syncthreads();
+    for (int col = threadIdx.x; col < BN; col += WM * WN * kWave) {
+      if (n0 + col >= p.N) continue;
+      float2 v = shared[col];
+#pragma unroll
+      for (int w = 1; w < WM; ++w) {
+        const float2 o = shared[w * BN + col];
+        join_stats(v.x, v.y, o.x, o.y);
+      }
+      p.stats[(g * p.rows + n0 + col) * p.stat_tiles + ti] = v;
+    }
+  } else {
+    // a wavefront passes strips of 32 rows through LDS, from where a lane takes eight columns of a row at a time
+    constexpr int W = BN / WN, P = W + kStripPad, VPR = W / 8, RPP = kWave / VPR, PASSES = 32 / RPP;
+    float* strip = reinterpret_cast<float*>(smem) + (wm * WN + wn) * 32 * P;
+    const int c = n0 + wn * W + lane % VPR * 8, n = p.N - c;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int r0 = m0 + (wm * TM + i) * 32;
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) strip[acc_row(e, lane) * P + j * 32 + (lane & 31)] = acc[i][j][e];
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int q = 0; q < PASSES; ++q) {
+        const int lr = q * RPP + lane / VPR, r = r0 + lr;
+        const float* at = strip + lr * P + lane % VPR * 8;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = at[e];
+        const bool live = r < p.M;
+        if constexpr (EPI == PX_DZ) {
+          const int64_t row = g * p.rows + (live ? r : 0);
+          const int label = p.labels[row];
+          const bool real = live && (unsigned)label < (unsigned)p.classes;
+          const float lse = p.lse[row], weight = p.dloss[row];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = real && e < n ? weight * (expf(v[e] - lse) - (p.class0 + c + e == label ? 1.0f : 0.0f)) : 0.0f;
+          // zeros behind the last class, up to the end of the tile or of the rows of dz (a multiple of eight)
+          if (live && c < p.out_ld) store8(reinterpret_cast<T*>(p.out) + g * p.out_gs + (int64_t)r * p.out_ld + c, 8, v);
+        } else {
+          if (!live || n <= 0) continue;
+          if constexpr (EPI == PX_DH) {
+            const bool real = (unsigned)p.labels[g * p.rows + r] < (unsigned)p.classes;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = real ? v[e] : 0.0f;
+            if (p.sums != nullptr) {
+              float* sum = p.sums + ((int64_t)g * p.M + r) * p.N + c;
+              if (!p.first_piece) {
+                float before[8];
+                load8(sum, n, before);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += before[e];
+              }
+              if (!p.last_piece) {
+                store8(sum, n, v);
+                continue;
+              }
+            }
+          }
+          store8(reinterpret_cast<T*>(p.out) + g * p.out_gs + (int64_t)r * p.out_ld + c, n, v);
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    if constexpr (EPI == PX_DZ) {
+      if (p.first_piece && n0 == 0 && wn == 0) {
+        // rows of this wavefront: words of 32, and zeros behind the last row to the end of a pair of words
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          const int r0 = m0 + (wm * TM + i) * 32, r = r0 + (lane & 31);
+          const bool real = r < p.M && (unsigned)p.labels[g * p.rows + r] < (unsigned)p.classes;
+          const uint64_t bits = __ballot(real);
+          if (lane == 0 && r0 / 32 < real_words(p.M)) p.real[g * real_words(p.M) + r0 / 32] = (uint32_t)bits;
+        }
+      }
+    }
+  }
+}
+
+// Consecutive workgroups go to the XCDs in turn; each gets a contiguous range of the tiles, so that what neighbours share stays in its L2.
+struct TilePosition { int g, ti, tj; };
+__device__ __forceinline__ TilePosition tile_of_workgroup(const ProductArgs& p) {
+  const int tiles = p.tiles_m * p.tiles_n, total = tiles * p.groups, xcd = blockIdx.x & 7;
+  const int idx = xcd * (total >> 3) + min(xcd, total & 7) + (int)(blockIdx.x >> 3), g = idx / tiles, in = idx - g * tiles;
+  // strips four tiles high, column by column
+  constexpr int kHigh = 4;
+  const int strip = in / (kHigh * p.tiles_n), first = strip * kHigh, high = min(kHigh, p.tiles_m - first), rest = in - first * p.tiles_n;
+  return {g, first + rest % high, rest / high};
+}
+
+// Limit of a kernel's dynamic LDS, raised once (twice is harmless).
+template <auto KERNEL> hipError_t allow_lds(int bytes) {
+  if (bytes <= 64 * 1024) return hipSuccess;
+  static std::atomic<bool> configured{false};
+  if (configured.load(std::memory_order_acquire)) return hipSuccess;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) configured.store(true, std::memory_order_release);
+  return e;
+}
+
+// transposed: (A, B) as (element (i, c) at c * ld + i).  Operands of any alignment and size (kernels_xent_any.hip) ...
+hipError_t launch_product_any(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, bool bf16, hipStream_t s);
+// ... and bf16 operands whose rows start at 16 bytes and are as long in whole (kernels_xent_bf16.hip).
+bool product_aligned(const ProductArgs& p, bool a_transposed, bool b_transposed);
+hipError_t launch_product_bf16(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, hipStream_t s);
+
+}  // namespace prsgd

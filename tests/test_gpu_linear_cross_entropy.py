@@ -98,6 +98,25 @@ def test_whole_tiles(P, dtype, first):
 
 
 @pytest.mark.parametrize("first", [False, True])
+@pytest.mark.parametrize("workers,rows,width,classes", [(33, 256, 512, 1024), (40, 250, 520, 1000), (40, 300, 264, 1004), (3, 2000, 1032, 1928), (130, 70, 200, 136)])
+def test_tiles_of_every_size(P, workers, rows, width, classes, first):
+    """Enough tiles for the larger ones, whole and ragged; rows without a label in every tile, in whole tiles, and nowhere."""
+    h, w, labels = _case(workers, rows, width, classes, BF16, first)
+    by_worker = labels.view(workers, rows)
+    by_worker[0] = by_worker[0].clamp(0, classes - 1)
+    by_worker[1, rows // 2:] = -1
+    by_worker[2, :rows // 2] = -1
+    h.view(workers, rows, width)[1, rows // 2:] = float("nan")
+    lse = P.prsgd_linear_cross_entropy(h, w, labels, classes_first=first)[1]
+    clean = h.clone()
+    clean.view(workers, rows, width)[1, rows // 2:] = 0.0
+    _check_forward(P, clean, w, labels, first)
+    got = P.prsgd_linear_cross_entropy_backward(_rand(9, workers * rows), h, w, labels, lse, classes_first=first)
+    want = _check_backward(P, _rand(9, workers * rows), clean, w, labels, torch.where(lse.isnan(), 0.0, lse), first)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("first", [False, True])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_several_pieces_of_the_classes(P, dtype, first):
     """128 MiB of dz are less than these classes take."""
