@@ -164,10 +164,16 @@ typedef struct {
                                       2 zeros in dgate; 3 both                                       */
 } prsgd_scan_config;
 
-/* last_dev may be NULL, and may be initial_dev if the distances agree.  No other buffers may overlap. */
+/* Bytes of workspace of either call below: 0 if they need none (few long sequences do) or the configuration is invalid. */
+size_t prsgd_gated_scan_workspace_bytes(const prsgd_scan_config* cfg);
+
+/*
+ * last_dev may be NULL, and may be initial_dev if the distances agree.  No other buffers may overlap.  workspace_dev may be NULL
+ * where none is needed.
+ */
 int prsgd_gated_scan(const prsgd_scan_config* cfg, const int32_t* starts_dev, const void* v_dev, int64_t v_row,
                      const void* gate_dev, int64_t gate_row, const float* initial_dev, int64_t initial_row, void* h_dev,
-                     int64_t h_row, float* last_dev, int64_t last_row, void* hip_stream);
+                     int64_t h_row, float* last_dev, int64_t last_row, void* workspace_dev, void* hip_stream);
 
 /*
  * Gradients from dh and dlast (NULL: zeros), with g_t = dh_t + f_{t+1} g_{t+1} (behind the last row: dlast):
@@ -178,7 +184,7 @@ int prsgd_gated_scan_backward(const prsgd_scan_config* cfg, const int32_t* start
                               const void* v_dev, int64_t v_row, const void* gate_dev, int64_t gate_row, const void* h_dev,
                               int64_t h_row, const float* initial_dev, int64_t initial_row, const float* dlast_dev,
                               int64_t dlast_row, void* dv_dev, int64_t dv_row, void* dgate_dev, int64_t dgate_row,
-                              float* dinitial_dev, int64_t dinitial_row, void* hip_stream);
+                              float* dinitial_dev, int64_t dinitial_row, void* workspace_dev, void* hip_stream);
 
 /*
  * Dropout: y = res + keep x / (1 - q), q = round(65536 p) / 65536, with a mask that is a function of (seed, step, layer, row, column):

@@ -395,7 +395,15 @@ Rows states_of(const Tensor& t, const Tensor& v, const ScanCall& c, const char* 
 Tensor states_given_or_empty(PyObject* o, const Tensor& v, const ScanCall& c, const char* name) {
   return o == Py_None ? device_empty({c.cfg.sequences, v.size(1)}, at::kFloat, v) : operand(o, name);
 }
-// v, gate, sequences, starts, initial, out, last -> h, last
+size_t scan_workspace(const ScanCall& c) {
+  const size_t n = prsgd_gated_scan_workspace_bytes(&c.cfg);
+  return n;                                                // 0 of what is refused: the call says so
+}
+// v, sequences -> bytes
+PyObject* gated_scan_bytes(PyObject* const* a) {
+  return PyLong_FromSize_t(scan_workspace(scan_call(tensor(a[0], "v"), a[1], Py_None, nullptr, 0)));
+}
+// v, gate, sequences, starts, initial, out, last, workspace -> h, last
 PyObject* gated_scan(PyObject* const* a) {
   const Tensor& v = operand(a[0], "v");
   PyObject* const states[] = {a[4], a[6]};
@@ -408,13 +416,16 @@ PyObject* gated_scan(PyObject* const* a) {
   c.cfg.clear = a[5] == Py_None && c.starts != nullptr ? 1 : 0;
   Tensor h = given_or_empty(a[5], v, type, "out"), last = states_given_or_empty(a[6], v, c, "last");
   const Rows hr = rows_of(h, v, type, "out"), lr = states_of(last, v, c, "last");
+  const size_t bytes = scan_workspace(c);
+  const Tensor ws = bytes > 0 ? workspace(a[7], bytes, v) : Tensor();
   finish(prsgd_gated_scan(&c.cfg, c.starts, vr.at, vr.distance, gr.at, gr.distance, static_cast<const float*>(ir.at), ir.distance, hr.at,
-                          hr.distance, static_cast<float*>(lr.at), lr.distance, on.stream()));
+                          hr.distance, static_cast<float*>(lr.at), lr.distance, bytes > 0 ? ws.data_ptr() : nullptr, on.stream()));
   written(h);
   written(last);
+  if (bytes > 0) written(ws);
   return Py_BuildValue("(NN)", THPVariable_Wrap(h), THPVariable_Wrap(last));
 }
-// dh, v, gate, h, sequences, starts, initial, dlast, dv, dgate, dinitial -> dv, dgate, dinitial
+// dh, v, gate, h, sequences, starts, initial, dlast, dv, dgate, dinitial, workspace -> dv, dgate, dinitial
 PyObject* gated_scan_backward(PyObject* const* a) {
   const Tensor& v = operand(a[1], "v");
   PyObject* const states[] = {a[6], a[7], a[10]};
@@ -430,10 +441,14 @@ PyObject* gated_scan_backward(PyObject* const* a) {
   Tensor dv = given_or_empty(a[8], v, type, "dv"), dgate = given_or_empty(a[9], v, type, "dgate"),
          dinitial = states_given_or_empty(a[10], v, c, "dinitial");
   const Rows dvr = rows_of(dv, v, type, "dv"), dgr = rows_of(dgate, v, type, "dgate"), dir = states_of(dinitial, v, c, "dinitial");
+  const size_t bytes = scan_workspace(c);
+  const Tensor ws = bytes > 0 ? workspace(a[11], bytes, v) : Tensor();
   finish(prsgd_gated_scan_backward(&c.cfg, c.starts, dhr.at, dhr.distance, vr.at, vr.distance, gr.at, gr.distance, hr.at, hr.distance,
                                    static_cast<const float*>(ir.at), ir.distance, static_cast<const float*>(dlr.at), dlr.distance, dvr.at,
-                                   dvr.distance, dgr.at, dgr.distance, static_cast<float*>(dir.at), dir.distance, on.stream()));
+                                   dvr.distance, dgr.at, dgr.distance, static_cast<float*>(dir.at), dir.distance,
+                                   bytes > 0 ? ws.data_ptr() : nullptr, on.stream()));
   for (const Tensor& t : {dv, dgate, dinitial}) written(t);
+  if (bytes > 0) written(ws);
   return Py_BuildValue("(NNN)", THPVariable_Wrap(dv), THPVariable_Wrap(dgate), THPVariable_Wrap(dinitial));
 }
 
@@ -576,8 +591,9 @@ PyMethodDef methods[] = {PRSGD_METHOD(bind, 1),
                          PRSGD_METHOD(embedding, 4),
                          PRSGD_METHOD(embedding_backward, 6),
                          PRSGD_METHOD(embedding_backward_bytes, 2),
-                         PRSGD_METHOD(gated_scan, 7),
-                         PRSGD_METHOD(gated_scan_backward, 11),
+                         PRSGD_METHOD(gated_scan, 8),
+                         PRSGD_METHOD(gated_scan_backward, 12),
+                         PRSGD_METHOD(gated_scan_bytes, 2),
                          PRSGD_METHOD(dropout, 7),
                          PRSGD_METHOD(linear_cross_entropy, 7),
                          PRSGD_METHOD(linear_cross_entropy_backward, 9),

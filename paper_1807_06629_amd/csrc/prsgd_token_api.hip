@@ -76,9 +76,14 @@ const char* scan_error(const prsgd_scan_config* c, const int32_t* starts, int cl
   if (misaligned(starts, 4)) return "gated_scan: misaligned buffer";
   return nullptr;
 }
+size_t scan_bytes(const prsgd_scan_config* c) {
+  const int parts = scan_parts(c->sequences, c->rows, c->width);
+  return parts > 1 ? (size_t)c->sequences * parts * c->width * sizeof(float2) : 0;
+}
 struct ScanBuffer { const void* at; int64_t row; bool output, needed; };
 // Rows in the sequences' type and states in fp32: present, aligned, distances, and outputs nowhere else.
-const char* scan_buffers_error(const prsgd_scan_config* c, const ScanBuffer* rows, int n_rows, const ScanBuffer* states, int n_states) {
+const char* scan_buffers_error(const prsgd_scan_config* c, const ScanBuffer* rows, int n_rows, const ScanBuffer* states, int n_states, const void* workspace) {
+  if ((workspace == nullptr && scan_bytes(c) > 0) || misaligned(workspace, 256)) return "gated_scan: null or misaligned workspace";
   const int es = element_bytes(c->dtype);
   for (int i = 0; i < n_rows; ++i) {
     if (c->rows == 0) break;
@@ -196,13 +201,23 @@ int prsgd_embedding_backward(const prsgd_embedding_config* cfg, const int32_t* t
                                               reinterpret_cast<hipStream_t>(hip_stream)), "embedding backward");
 }
 
+size_t prsgd_gated_scan_workspace_bytes(const prsgd_scan_config* cfg) {
+  // sequences that are given no starts have to be equal in the call itself
+  const int32_t* const some = reinterpret_cast<const int32_t*>(sizeof(int32_t));
+  if (const char* e = scan_error(cfg, some, 3)) {
+    bad(e);
+    return 0;
+  }
+  return scan_bytes(cfg);
+}
+
 int prsgd_gated_scan(const prsgd_scan_config* cfg, const int32_t* starts_dev, const void* v_dev, int64_t v_row, const void* gate_dev,
                      int64_t gate_row, const float* initial_dev, int64_t initial_row, void* h_dev, int64_t h_row, float* last_dev,
-                     int64_t last_row, void* hip_stream) {
+                     int64_t last_row, void* workspace_dev, void* hip_stream) {
   if (const char* e = scan_error(cfg, starts_dev, 1)) return bad(e);
   const ScanBuffer rows[] = {{v_dev, v_row, false, true}, {gate_dev, gate_row, false, true}, {h_dev, h_row, true, true}};
   const ScanBuffer states[] = {{initial_dev, initial_row, false, false}, {last_dev, last_row, true, false}};
-  if (const char* e = scan_buffers_error(cfg, rows, 3, states, 2)) return bad(e);
+  if (const char* e = scan_buffers_error(cfg, rows, 3, states, 2, workspace_dev)) return bad(e);
   if (last_dev != nullptr && last_dev == initial_dev && last_row != initial_row) return bad("gated_scan: state in place with another distance");
   ScanArgs p{};
   p.starts = starts_dev;
@@ -218,6 +233,8 @@ int prsgd_gated_scan(const prsgd_scan_config* cfg, const int32_t* starts_dev, co
   p.last_row = last_row;
   p.sequences = cfg->sequences;
   p.clear = cfg->clear;
+  p.parts = scan_parts(cfg->sequences, cfg->rows, cfg->width);
+  p.joint = reinterpret_cast<float2*>(workspace_dev);
   p.rows = cfg->rows;
   p.width = cfg->width;
   return hip_result(launch_gated_scan(p, cfg->dtype == PRSGD_BF16, false, reinterpret_cast<hipStream_t>(hip_stream)), "gated_scan");
@@ -226,12 +243,13 @@ int prsgd_gated_scan(const prsgd_scan_config* cfg, const int32_t* starts_dev, co
 int prsgd_gated_scan_backward(const prsgd_scan_config* cfg, const int32_t* starts_dev, const void* dh_dev, int64_t dh_row, const void* v_dev,
                               int64_t v_row, const void* gate_dev, int64_t gate_row, const void* h_dev, int64_t h_row,
                               const float* initial_dev, int64_t initial_row, const float* dlast_dev, int64_t dlast_row, void* dv_dev,
-                              int64_t dv_row, void* dgate_dev, int64_t dgate_row, float* dinitial_dev, int64_t dinitial_row, void* hip_stream) {
+                              int64_t dv_row, void* dgate_dev, int64_t dgate_row, float* dinitial_dev, int64_t dinitial_row, void* workspace_dev,
+                              void* hip_stream) {
   if (const char* e = scan_error(cfg, starts_dev, 3)) return bad(e);
   const ScanBuffer rows[] = {{dh_dev, dh_row, false, true}, {v_dev, v_row, false, true},   {gate_dev, gate_row, false, true},
                              {h_dev, h_row, false, true},   {dv_dev, dv_row, true, true}, {dgate_dev, dgate_row, true, true}};
   const ScanBuffer states[] = {{initial_dev, initial_row, false, false}, {dlast_dev, dlast_row, false, false}, {dinitial_dev, dinitial_row, true, false}};
-  if (const char* e = scan_buffers_error(cfg, rows, 6, states, 3)) return bad(e);
+  if (const char* e = scan_buffers_error(cfg, rows, 6, states, 3, workspace_dev)) return bad(e);
   if (dinitial_dev != nullptr && dinitial_dev == initial_dev) return bad("gated_scan: buffers overlap");
   if (dinitial_dev != nullptr && dinitial_dev == dlast_dev && dinitial_row != dlast_row) return bad("gated_scan: state in place with another distance");
   ScanArgs p{};
@@ -256,6 +274,8 @@ int prsgd_gated_scan_backward(const prsgd_scan_config* cfg, const int32_t* start
   p.last_row = dinitial_row;
   p.sequences = cfg->sequences;
   p.clear = cfg->clear;
+  p.parts = scan_parts(cfg->sequences, cfg->rows, cfg->width);
+  p.joint = reinterpret_cast<float2*>(workspace_dev);
   p.rows = cfg->rows;
   p.width = cfg->width;
   return hip_result(launch_gated_scan(p, cfg->dtype == PRSGD_BF16, true, reinterpret_cast<hipStream_t>(hip_stream)), "gated_scan backward");

@@ -147,8 +147,9 @@ def _load() -> ctypes.CDLL:
         "prsgd_embedding": (ctypes.c_int, [embp, vp, vp, i64, i64, vp, i64, vp]),
         "prsgd_embedding_backward_workspace_bytes": (sz, [embp]),
         "prsgd_embedding_backward": (ctypes.c_int, [embp, vp, vp, i64, vp, i64, i64, vp, vp]),
-        "prsgd_gated_scan": (ctypes.c_int, [scanp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp]),
-        "prsgd_gated_scan_backward": (ctypes.c_int, [scanp, vp] + [vp, i64] * 9 + [vp]),
+        "prsgd_gated_scan_workspace_bytes": (sz, [scanp]),
+        "prsgd_gated_scan": (ctypes.c_int, [scanp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp]),
+        "prsgd_gated_scan_backward": (ctypes.c_int, [scanp, vp] + [vp, i64] * 9 + [vp, vp]),
         "prsgd_dropout": (ctypes.c_int, [dropp, vp, vp, i64, vp, i64, vp, i64, vp]),
         "prsgd_linear_cross_entropy_workspace_bytes": (sz, [xentp]),
         "prsgd_linear_cross_entropy": (ctypes.c_int, [xentp, vp, i64, vp, i64, i64, vp, vp, vp, vp, vp]),
@@ -566,21 +567,28 @@ def prsgd_embedding_backward(dy: torch.Tensor, tokens: torch.Tensor, table: torc
     return _ops.embedding_backward(dy, tokens, table, scale, dtable, workspace)
 
 
+def prsgd_gated_scan_workspace_bytes(v: torch.Tensor, sequences: int) -> int:
+    """Of prsgd_gated_scan and its gradients; 0 where none is needed."""
+    return _ops.gated_scan_bytes(v, sequences)
+
+
 def prsgd_gated_scan(v: torch.Tensor, gate: torch.Tensor, sequences: Optional[int] = None, starts: Optional[torch.Tensor] = None,
-                     initial: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, last: Optional[torch.Tensor] = None):
+                     initial: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, last: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None):
     """(h, last) of h_t = f h_{t-1} + (1 - f) v_t, f = sigmoid(gate), along every sequence of v and gate [rows][width]: from initial
     (fp32 [sequences][width], zeros if None) to last, which may be initial.  Sequences are equal runs of rows, or packed ones that
     start at starts (int32 [sequences + 1] on the device); rows that none of them has are left as they are in `out`, zeros if that is not given.
     Their number is that of starts, of initial, or one, where it is not given."""
-    return _ops.gated_scan(v, gate, sequences, starts, initial, out, last)
+    return _ops.gated_scan(v, gate, sequences, starts, initial, out, last, workspace)
 
 
 def prsgd_gated_scan_backward(dh: torch.Tensor, v: torch.Tensor, gate: torch.Tensor, h: torch.Tensor, sequences: Optional[int] = None,
                               starts: Optional[torch.Tensor] = None, initial: Optional[torch.Tensor] = None,
                               dlast: Optional[torch.Tensor] = None, dv: Optional[torch.Tensor] = None,
-                              dgate: Optional[torch.Tensor] = None, dinitial: Optional[torch.Tensor] = None):
+                              dgate: Optional[torch.Tensor] = None, dinitial: Optional[torch.Tensor] = None,
+                              workspace: Optional[torch.Tensor] = None):
     """(dv, dgate, dinitial) of prsgd_gated_scan from dh and dlast (fp32, zeros if None); h is what it returned."""
-    return _ops.gated_scan_backward(dh, v, gate, h, sequences, starts, initial, dlast, dv, dgate, dinitial)
+    return _ops.gated_scan_backward(dh, v, gate, h, sequences, starts, initial, dlast, dv, dgate, dinitial, workspace)
 
 
 def prsgd_dropout(x: torch.Tensor, p: float, seed: int, step=0, layer: int = 0, residual: Optional[torch.Tensor] = None,

@@ -63,6 +63,29 @@ def test_packed_sequences_and_empty_ones(P, cuts, dtype):
     _check(P, rows, 70, dtype, len(cuts) - 1, torch.tensor(cuts, dtype=torch.int32, device="cuda"))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cuts", [(1024, None), (1100, None), (2500, None), (2200, [1, 2190]), (4400, [0, 4000, 4001, 4001, 4390])])
+def test_few_long_sequences_are_cut_into_parts(P, rows, cuts, dtype):
+    n = 1 if cuts is None else len(cuts) - 1
+    assert P.prsgd_gated_scan_workspace_bytes(torch.empty(rows, 12, device="cuda", dtype=dtype), n) > 0
+    _check(P, rows, 12, dtype, n, None if cuts is None else torch.tensor(cuts, dtype=torch.int32, device="cuda"), shift=3.0)
+
+
+def test_parts_and_any_workspace(P):
+    """Bits are those of any run, whatever the workspace held."""
+    v, gate, dh = (_rand(k, 3000, 40, dtype=BF16) for k in (1, 2, 3))
+    h, last = P.prsgd_gated_scan(v, gate)
+    back = P.prsgd_gated_scan_backward(dh, v, gate, h, dlast=last)
+    n = P.prsgd_gated_scan_workspace_bytes(v, 1)
+    for fill in (0, 0xFF):
+        ws = torch.full((n,), fill, dtype=torch.uint8, device="cuda")
+        again = P.prsgd_gated_scan(v, gate, workspace=ws)
+        assert torch.equal(h, again[0]) and torch.equal(last, again[1])
+        assert all(torch.equal(a, b) for a, b in zip(back, P.prsgd_gated_scan_backward(dh, v, gate, h, dlast=last, workspace=ws)))
+    with pytest.raises(ValueError):
+        P.prsgd_gated_scan(v, gate, workspace=torch.empty(n - 8, dtype=torch.uint8, device="cuda"))
+
+
 def test_rows_that_no_sequence_has(P):
     rows, width = 50, 20
     starts = torch.tensor([7, 20, 41], dtype=torch.int32, device="cuda")

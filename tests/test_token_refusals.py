@@ -52,8 +52,8 @@ def _vary(good, changes):
 
 EMB = [A, B, 350, 50, C, 50]                                 # tokens, table, matrix, row, y, row
 EMB_BACK = [A, B, 50, C, 350, 50, D]                         # tokens, dy, row, dtable, matrix, row, workspace
-SCAN = [None, A, 50, B, 50, C, 50, D, 50, E, 50]             # starts, v, gate, initial, h, last
-SCAN_BACK = [None, A, 50, B, 50, C, 50, D, 50, E, 50, F, 50, G, 50, 8 * A, 50, 9 * A, 50]
+SCAN = [None, A, 50, B, 50, C, 50, D, 50, E, 50, None]       # starts, v, gate, initial, h, last, workspace
+SCAN_BACK = [None, A, 50, B, 50, C, 50, D, 50, E, 50, F, 50, G, 50, 8 * A, 50, 9 * A, 50, None]
 DROP = [None, A, 50, B, 50, C, 50]                           # step, x, res, y
 XENT = [A, 50, B, 350, 7, C, D, E, F]                        # h, w, labels, loss, lse, workspace
 XENT_BACK = [A, B, 50, C, 350, 7, D, E, F, 50, G, 350, 7, 8 * A]      # dloss, h, w, labels, lse, dh, dw, workspace
@@ -98,7 +98,7 @@ def test_scan_refuses_its_configuration(P, kw):
 
 @pytest.mark.parametrize("args", _vary(SCAN, [(0, A + 2), (1, None), (1, A + 1), (2, 49), (3, None), (3, B + 2), (4, 49), (5, C + 2), (6, 49), (6, -50), (7, None),
                                               (7, D + 2), (7, A), (7, B), (7, C), (7, E), (8, 0), (8, 49), (9, E + 2), (9, A), (10, 49), (10, 0)]) +
-                         [[None, A, 50, B, 50, C, 50, D, 50, C, 51]])
+                         [[None, A, 50, B, 50, C, 50, D, 50, C, 51, None], SCAN[:11] + [F + 64]])
 def test_scan_refuses_its_buffers(P, args):
     assert _call(P, "prsgd_gated_scan", _scan(P), args) == P.PRSGD_EINVAL
     assert _call(P, "prsgd_gated_scan", _scan(P, clear=2), SCAN) == P.PRSGD_EINVAL
@@ -107,9 +107,18 @@ def test_scan_refuses_its_buffers(P, args):
 @pytest.mark.parametrize("args", _vary(SCAN_BACK, [(1, None), (3, None), (5, None), (7, None), (13, None), (15, None), (1, A + 2), (7, D + 1), (9, E + 2),
                                                    (13, A), (13, B), (13, D), (13, 8 * A), (15, C), (15, E), (17, E), (17, A), (17, G), (2, 49), (8, 7), (14, 0),
                                                    (16, 49), (18, 0), (12, 3)]) +
-                         [[None, A, 50, B, 50, C, 50, D, 50, E, 50, F, 50, G, 50, 8 * A, 50, F, 51]])
+                         [[None, A, 50, B, 50, C, 50, D, 50, E, 50, F, 50, G, 50, 8 * A, 50, F, 51, None]])
 def test_scan_backward_refuses_its_buffers(P, args):
     assert _call(P, "prsgd_gated_scan_backward", _scan(P), args) == P.PRSGD_EINVAL
+
+
+def test_few_long_sequences_need_a_workspace(P):
+    cfg = _scan(P, sequences=1, rows=1 << 15)
+    n = P._lib.prsgd_gated_scan_workspace_bytes(ctypes.byref(cfg))
+    assert 0 < n <= 64 * 50 * 8
+    assert _call(P, "prsgd_gated_scan", cfg, SCAN) == P.PRSGD_EINVAL and _call(P, "prsgd_gated_scan_backward", cfg, SCAN_BACK) == P.PRSGD_EINVAL
+    assert P._lib.prsgd_gated_scan_workspace_bytes(ctypes.byref(_scan(P))) == 0
+    assert P._lib.prsgd_gated_scan_workspace_bytes(ctypes.byref(_scan(P, width=0))) == 0 and "width" in P.prsgd_last_error(None)
 
 
 @pytest.mark.parametrize("kw", [dict(dtype=3), dict(layer=-1), dict(layer=32768), dict(rows=-1), dict(rows=1 << 31), dict(width=0), dict(width=32769), dict(p=-0.1),
@@ -168,11 +177,11 @@ def test_nothing_to_do_is_no_error(P):
 
 
 def test_workspaces_stay_bounded(P):
-    """Of the logits' gradients 128 MiB are held, or 256 classes of them."""
+    """Of the logits' gradients 128 MiB are held, or 256 classes of them; with them dh's sums, a bit a row, and what rounds each up to 256 bytes."""
     cfg = _xent(P, dtype=1, workers=8, rows_per_worker=8192, width=64, classes=1 << 20)
-    assert P._lib.prsgd_linear_cross_entropy_backward_workspace_bytes(ctypes.byref(cfg)) <= (128 << 20) + 8 * 8192 * 64 * 4 + 4096
+    assert P._lib.prsgd_linear_cross_entropy_backward_workspace_bytes(ctypes.byref(cfg)) <= (128 << 20) + 8 * 8192 * 64 * 4 + 8 * 8192 // 8 + 4096
     cfg = _xent(P, dtype=0, workers=1, rows_per_worker=1 << 20, width=64, classes=1000)
-    assert P._lib.prsgd_linear_cross_entropy_backward_workspace_bytes(ctypes.byref(cfg)) <= (1 << 20) * (256 + 64) * 4 + 4096
+    assert P._lib.prsgd_linear_cross_entropy_backward_workspace_bytes(ctypes.byref(cfg)) <= (1 << 20) * (256 + 64) * 4 + (1 << 20) // 8 + 4096
 
 
 def test_the_binding_refuses_what_has_no_kernel(P):
