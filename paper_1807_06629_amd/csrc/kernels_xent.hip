@@ -14,10 +14,12 @@ namespace prsgd {
 namespace {
 
 // A product by the kernel that takes its operands.
-hipError_t launch_product(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, bool bf16, hipStream_t s) {
+hipError_t launch_product(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, bool bf16, hipStream_t s, int* tiles_m = nullptr) {
+  int none;
+  if (tiles_m == nullptr) tiles_m = &none;
   if (p.M == 0 || p.N == 0) return hipSuccess;               // no rows: what remains is the zeros of dW
-  if (bf16 && product_aligned(p, a_transposed, b_transposed)) return launch_product_bf16(p, epi, a_transposed, b_transposed, s);
-  return launch_product_any(p, epi, a_transposed, b_transposed, bf16, s);
+  if (bf16 && product_aligned(p, a_transposed, b_transposed)) return launch_product_bf16(p, epi, a_transposed, b_transposed, tiles_m, s);
+  return launch_product_any(p, epi, a_transposed, b_transposed, bf16, tiles_m, s);
 }
 
 // Loss and lse of every row from its tiles' statistics: a wavefront a row.
@@ -41,7 +43,6 @@ __global__ void __launch_bounds__(kThreads) join_tiles_kernel(XentArgs p, const 
   }
 }
 
-constexpr int kClassTile = 128;
 constexpr size_t kPieceBytes = (size_t)128 << 20;          // of dz
 
 }  // namespace
@@ -58,12 +59,12 @@ hipError_t launch_xent(const XentArgs& x, const XentPlan& plan, char* ws, bool b
   p.rows = x.rows;
   p.classes = x.classes;
   p.stats = reinterpret_cast<float2*>(ws + plan.stats);
-  p.stat_tiles = plan.tiles;
   p.picked = reinterpret_cast<float*>(ws + plan.picked);
-  const hipError_t e = launch_product(p, PX_STATS, !x.classes_first, false, bf16, s);
+  int tiles = 0;
+  const hipError_t e = launch_product(p, PX_STATS, !x.classes_first, false, bf16, s, &tiles);
   if (e != hipSuccess) return e;
   const unsigned grid = (unsigned)std::min<int64_t>((x.rows * x.workers + 3) / 4, 256 * 64);
-  hipLaunchKernelGGL(join_tiles_kernel, dim3(grid), dim3(kThreads), 0, s, x, (const float2*)p.stats, (const float*)p.picked, plan.tiles);
+  hipLaunchKernelGGL(join_tiles_kernel, dim3(grid), dim3(kThreads), 0, s, x, (const float2*)p.stats, (const float*)p.picked, tiles);
   return hipGetLastError();
 }
 
@@ -122,8 +123,7 @@ XentPlan xent_plan(int workers, int64_t rows, int width, int classes, bool bf16,
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t v = at; at += (bytes + 255) / 256 * 256; return v; };
   if (!backward) {
-    e.tiles = (classes + kClassTile - 1) / kClassTile;
-    e.stats = take(n * e.tiles * sizeof(float2));
+    e.stats = take(n * ((classes + kLeastTile - 1) / kLeastTile) * sizeof(float2));
     e.picked = take(n * sizeof(float));
   } else {
     const int whole = (classes + 255) / 256;               // in 256 classes

@@ -142,31 +142,31 @@ template <typename T, int BM, int BN, bool TA, bool TB, int EPI> __global__ void
   product_epilogue<T, EPI, BM, BN, WM, WN>(p, acc, g, m0, n0, at.ti, wm, wn, lane, smem);
 }
 
-template <typename T, int BM, int BN, bool TA, bool TB, int EPI> hipError_t launch_tile(ProductArgs p, hipStream_t s) {
+template <typename T, int BM, int BN, bool TA, bool TB, int EPI> hipError_t launch_tile(ProductArgs p, int* tiles_m, hipStream_t s) {
   constexpr int kStages = 2 * product_stage_bytes(BM, BN, (int)sizeof(T)), kEpilogue = epilogue_lds_bytes<BM, BN, 2, 2, EPI>();
   constexpr int kLds = kStages > kEpilogue ? kStages : kEpilogue;
   static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
   constexpr auto kernel = product_kernel<T, BM, BN, TA, TB, EPI>;
   if (const hipError_t e = allow_lds<kernel>(kLds); e != hipSuccess) return e;
-  p.tiles_m = (p.M + BM - 1) / BM;
+  *tiles_m = p.tiles_m = (p.M + BM - 1) / BM;
   p.tiles_n = (p.N + BN - 1) / BN;
   hipLaunchKernelGGL(kernel, dim3((unsigned)p.tiles_m * (unsigned)p.tiles_n * (unsigned)p.groups), dim3(kThreads), kLds, s, p);
   return hipGetLastError();
 }
-template <typename T> hipError_t launch(const ProductArgs& p, int epi, bool ta, bool tb, hipStream_t s) {
+template <typename T> hipError_t launch(const ProductArgs& p, int epi, bool ta, bool tb, int* tiles_m, hipStream_t s) {
   constexpr int B = 128;
   switch (epi) {
-    case PX_STATS: return ta ? launch_tile<T, B, B, true, false, PX_STATS>(p, s) : launch_tile<T, B, B, false, false, PX_STATS>(p, s);
-    case PX_DZ: return tb ? launch_tile<T, B, B, false, true, PX_DZ>(p, s) : launch_tile<T, B, B, false, false, PX_DZ>(p, s);
-    case PX_DH: return tb ? launch_tile<T, B, B, false, true, PX_DH>(p, s) : launch_tile<T, B, B, false, false, PX_DH>(p, s);
-    default: return launch_tile<T, B, B, true, true, PX_DW>(p, s);
+    case PX_STATS: return ta ? launch_tile<T, B, B, true, false, PX_STATS>(p, tiles_m, s) : launch_tile<T, B, B, false, false, PX_STATS>(p, tiles_m, s);
+    case PX_DZ: return tb ? launch_tile<T, B, B, false, true, PX_DZ>(p, tiles_m, s) : launch_tile<T, B, B, false, false, PX_DZ>(p, tiles_m, s);
+    case PX_DH: return tb ? launch_tile<T, B, B, false, true, PX_DH>(p, tiles_m, s) : launch_tile<T, B, B, false, false, PX_DH>(p, tiles_m, s);
+    default: return launch_tile<T, B, B, true, true, PX_DW>(p, tiles_m, s);
   }
 }
 
 }  // namespace
 
-hipError_t launch_product_any(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, bool bf16, hipStream_t s) {
-  return bf16 ? launch<uint16_t>(p, epi, a_transposed, b_transposed, s) : launch<float>(p, epi, a_transposed, b_transposed, s);
+hipError_t launch_product_any(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, bool bf16, int* tiles_m, hipStream_t s) {
+  return bf16 ? launch<uint16_t>(p, epi, a_transposed, b_transposed, tiles_m, s) : launch<float>(p, epi, a_transposed, b_transposed, tiles_m, s);
 }
 
 }  // namespace prsgd

@@ -195,27 +195,29 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) product_bf16_kernel(const Pro
   product_epilogue<uint16_t, EPI, BM, BN, WM, WN>(p, acc, g, m0, n0, place_of.ti, wm, wn, lane, smem);
 }
 
-template <int BM, int BN, int WM, int WN, int S, bool TA, bool TB, int EPI> hipError_t launch_tile(ProductArgs p, hipStream_t s) {
+template <int BM, int BN, int WM, int WN, int S, bool TA, bool TB, int EPI> hipError_t launch_tile(ProductArgs p, int* tiles_m, hipStream_t s) {
   static_assert(S >= 2, "a step's tile and the next one");
   constexpr int kLds = lds_bytes<BM, BN, WM, WN, S, EPI>();
   static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
   constexpr auto kernel = product_bf16_kernel<BM, BN, WM, WN, S, TA, TB, EPI>;
   if (const hipError_t e = allow_lds<kernel>(kLds); e != hipSuccess) return e;
-  p.tiles_m = (p.M + BM - 1) / BM;
+  *tiles_m = p.tiles_m = (p.M + BM - 1) / BM;
   p.tiles_n = (p.N + BN - 1) / BN;
   hipLaunchKernelGGL(kernel, dim3((unsigned)p.tiles_m * (unsigned)p.tiles_n * (unsigned)p.groups), dim3(64 * WM * WN), kLds, s, p);
   return hipGetLastError();
 }
 
-template <bool TA, bool TB, int EPI> hipError_t launch(const ProductArgs& p, hipStream_t s) {
+template <bool TA, bool TB, int EPI> hipError_t launch(const ProductArgs& p, int* tiles_m, hipStream_t s) {
+  // Time of a launch in units of a 64 x 64 tile's products: tiles per compute unit times their size over their efficiency.  Of tiles that a compute unit has
+  // several of in hand, parts of a round count as such; of 256 x 256 tiles whole rounds.
   auto tiles = [&](int64_t b) { return ((p.M + b - 1) / b) * ((p.N + b - 1) / b) * p.groups; };
-  if constexpr (EPI == PX_STATS) {
-    return launch_tile<128, 128, 2, 2, 2, TA, TB, EPI>(p, s);
-  } else {
-    if (tiles(256) >= 128) return launch_tile<256, 256, 4, 2, 2, TA, TB, EPI>(p, s);
-    if (tiles(128) >= 128) return launch_tile<128, 128, 2, 2, 2, TA, TB, EPI>(p, s);
-    return launch_tile<64, 64, 2, 2, 4, TA, TB, EPI>(p, s);
-  }
+  auto cost = [](int64_t n, int b, double efficiency) { return (n < 256 ? 1.0 : (double)n / 256.0) * (b / 64) * (b / 64) / efficiency; };
+  const int64_t n_middle = tiles(128), n_huge = (tiles(256) + 255) / 256 * 256;
+  const double middle = cost(n_middle, 128, n_middle > 256 ? 0.9 : 1.34), small = cost(tiles(64), 64, 0.68), huge = cost(n_huge, 256, 1.2);
+  if (huge <= middle && huge <= small) return launch_tile<256, 256, 4, 2, 2, TA, TB, EPI>(p, tiles_m, s);
+  if (middle > small) return launch_tile<64, 64, 2, 2, 4, TA, TB, EPI>(p, tiles_m, s);
+  if (n_middle <= 256) return launch_tile<128, 128, 4, 2, 3, TA, TB, EPI>(p, tiles_m, s);
+  return launch_tile<128, 128, 2, 2, 2, TA, TB, EPI>(p, tiles_m, s);
 }
 
 bool operand_aligned(const Operand& o, int64_t contiguous, int64_t other, int groups) {
@@ -231,12 +233,12 @@ bool product_aligned(const ProductArgs& p, bool a_transposed, bool b_transposed)
          operand_aligned(p.b, whole(p.b, b_transposed ? p.N : p.K), b_transposed ? p.K : p.N, p.groups);
 }
 
-hipError_t launch_product_bf16(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, hipStream_t s) {
+hipError_t launch_product_bf16(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, int* tiles_m, hipStream_t s) {
   switch (epi) {
-    case PX_STATS: return a_transposed ? launch<true, false, PX_STATS>(p, s) : launch<false, false, PX_STATS>(p, s);
-    case PX_DZ: return b_transposed ? launch<false, true, PX_DZ>(p, s) : launch<false, false, PX_DZ>(p, s);
-    case PX_DH: return b_transposed ? launch<false, true, PX_DH>(p, s) : launch<false, false, PX_DH>(p, s);
-    default: return launch<true, true, PX_DW>(p, s);
+    case PX_STATS: return a_transposed ? launch<true, false, PX_STATS>(p, tiles_m, s) : launch<false, false, PX_STATS>(p, tiles_m, s);
+    case PX_DZ: return b_transposed ? launch<false, true, PX_DZ>(p, tiles_m, s) : launch<false, false, PX_DZ>(p, tiles_m, s);
+    case PX_DH: return b_transposed ? launch<false, true, PX_DH>(p, tiles_m, s) : launch<false, false, PX_DH>(p, tiles_m, s);
+    default: return launch<true, true, PX_DW>(p, tiles_m, s);
   }
 }
 

@@ -95,7 +95,6 @@ struct XentArgs {
   bool classes_first;
 };
 struct XentPlan {
-  int tiles;                             // forward: tiles of classes
   int piece, pieces;                     // backward: classes of a piece
   size_t stats, picked, dz, sums, real, total;       // byte offsets
 };

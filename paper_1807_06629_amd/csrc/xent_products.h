@@ -28,7 +28,7 @@ struct ProductArgs {
   const float* lse; const float* dloss;
   int64_t rows;
   int class0, classes;                   // first class of the piece; of all
-  float2* stats; int stat_tiles; float* picked;      // PX_STATS
+  float2* stats; float* picked;          // PX_STATS: [rows of all workers][tiles_m]
   void* out; int64_t out_gs, out_ld;     // the others
   float* sums;                           // PX_DH over several pieces: [groups][M][N] fp32
   bool first_piece, last_piece;
@@ -38,6 +38,12 @@ enum ProductEpilogue { PX_STATS = 0, PX_DZ = 1, PX_DH = 2, PX_DW = 3 };
 
 template <typename T> constexpr bool kIsBf16 = std::is_same_v<T, uint16_t>;
 __host__ __device__ constexpr int64_t real_words(int64_t rows) { return (rows + 63) / 64 * 2; }
+
+// exp of what is at most about zero.  bf16: on the hardware's base 2, which leaves |x| 2^-24 of the result, at most 2^-24 of the largest term.
+template <typename T> __device__ __forceinline__ float exp_of(float x) {
+  if constexpr (kIsBf16<T>) return __builtin_amdgcn_exp2f(x * 1.44269504f);
+  else return expf(x);
+}
 
 // (m, s) of the union of two sets of logits, s the sum of exp(z - m)
 __device__ __forceinline__ void join_stats(float& m, float& s, float m2, float s2) {
@@ -86,7 +92,7 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& p, const f32
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int c = m0 + (wm * TM + i) * 32 + acc_row(e, lane);
-          if (c < p.M) s += expf(acc[i][j][e] - top);
+          if (c < p.M) s += exp_of<T>(acc[i][j][e] - top);
         }
       if (odd) s = NAN;
       join_stats(m, s, __shfl_xor(m, 32), __shfl_xor(s, 32));
@@ -101,7 +107,7 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& p, const f32
         const float2 o = shared[w * BN + col];
         join_stats(v.x, v.y, o.x, o.y);
       }
-      p.stats[(g * p.rows + n0 + col) * p.stat_tiles + ti] = v;
+      p.stats[(g * p.rows + n0 + col) * p.tiles_m + ti] = v;
     }
   } else {
     // a wavefront passes strips of 32 rows through LDS, from where a lane takes eight columns of a row at a time
@@ -130,7 +136,7 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& p, const f32
           const bool real = live && (unsigned)label < (unsigned)p.classes;
           const float lse = p.lse[row], weight = p.dloss[row];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = real && e < n ? weight * (expf(v[e] - lse) - (p.class0 + c + e == label ? 1.0f : 0.0f)) : 0.0f;
+          for (int e = 0; e < 8; ++e) v[e] = real && e < n ? weight * (exp_of<T>(v[e] - lse) - (p.class0 + c + e == label ? 1.0f : 0.0f)) : 0.0f;
           // zeros behind the last class, up to the end of the tile or of the rows of dz (a multiple of eight)
           if (live && c < p.out_ld) store8(reinterpret_cast<T*>(p.out) + g * p.out_gs + (int64_t)r * p.out_ld + c, 8, v);
         } else {
@@ -195,9 +201,11 @@ template <auto KERNEL> hipError_t allow_lds(int bytes) {
 }
 
 // transposed: (A, B) as (element (i, c) at c * ld + i).  Operands of any alignment and size (kernels_xent_any.hip) ...
-hipError_t launch_product_any(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, bool bf16, hipStream_t s);
+// tiles_m: how many tiles the rows of A were cut into, of kLeastTile rows at least
+constexpr int kLeastTile = 64;
+hipError_t launch_product_any(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, bool bf16, int* tiles_m, hipStream_t s);
 // ... and bf16 operands whose rows start at 16 bytes and are as long in whole (kernels_xent_bf16.hip).
 bool product_aligned(const ProductArgs& p, bool a_transposed, bool b_transposed);
-hipError_t launch_product_bf16(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, hipStream_t s);
+hipError_t launch_product_bf16(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, int* tiles_m, hipStream_t s);
 
 }  // namespace prsgd
