@@ -13,13 +13,53 @@ namespace prsgd {
 
 namespace {
 
+// Parts that a contraction is cut into where its product has few tiles: 512 tiles of 64 x 64 in all, a part at least eight steps of 64.
+int splits_of(int64_t m, int64_t n, int64_t k, int groups) {
+  const int64_t tiles = (m + 63) / 64 * ((n + 63) / 64) * groups;
+  return tiles == 0 ? 1 : (int)std::max<int64_t>(std::min<int64_t>(512 / tiles, k / 512), 1);
+}
+size_t parts_bytes(int64_t m, int64_t n, int64_t k, int groups) {
+  const int splits = splits_of(m, n, k, groups);
+  return splits > 1 ? (size_t)splits * groups * m * n * sizeof(float) : 0;
+}
+
+// dh or dW of the parts: a lane eight columns.
+template <typename T, int EPI> __global__ void __launch_bounds__(kThreads) join_parts_kernel(ProductArgs p) {
+  const int64_t per_row = (p.N + 7) / 8, matrix = (int64_t)p.M * p.N, total = per_row * p.M * p.groups;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
+    const int64_t row = i / per_row, g = row / p.M;
+    const int r = (int)(row - g * p.M), c = (int)(i - row * per_row) * 8, n = p.N - c;
+    const float* from = p.parts + row * p.N + c;
+    float v[8];
+    load8(from, n, v);
+#pragma unroll 4
+    for (int q = 1; q < p.splits; ++q) {
+      float more[8];
+      load8(from + q * matrix * p.groups, n, more);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += more[e];
+    }
+    finish<T, EPI>(p, (int)g, r, c, n, v);
+  }
+}
+
 // A product by the kernel that takes its operands.
-hipError_t launch_product(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, bool bf16, hipStream_t s, int* tiles_m = nullptr) {
-  int none;
-  if (tiles_m == nullptr) tiles_m = &none;
+hipError_t launch_product(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, bool bf16, Cut* cut, hipStream_t s) {
+  *cut = {0, 1};
   if (p.M == 0 || p.N == 0) return hipSuccess;               // no rows: what remains is the zeros of dW
-  if (bf16 && product_aligned(p, a_transposed, b_transposed)) return launch_product_bf16(p, epi, a_transposed, b_transposed, tiles_m, s);
-  return launch_product_any(p, epi, a_transposed, b_transposed, bf16, tiles_m, s);
+  if (bf16 && product_aligned(p, a_transposed, b_transposed)) return launch_product_bf16(p, epi, a_transposed, b_transposed, cut, s);
+  return launch_product_any(p, epi, a_transposed, b_transposed, bf16, cut, s);
+}
+template <int EPI> hipError_t launch_gradient(ProductArgs p, bool a_transposed, bool b_transposed, bool bf16, hipStream_t s) {
+  Cut cut;
+  p.splits = splits_of(p.M, p.N, p.K, p.groups);
+  const hipError_t e = launch_product(p, EPI, a_transposed, b_transposed, bf16, &cut, s);
+  if (e != hipSuccess || cut.splits == 1) return e;
+  p.splits = cut.splits;
+  const unsigned grid = (unsigned)std::min<int64_t>(((int64_t)(p.N + 7) / 8 * p.M * p.groups + kThreads - 1) / kThreads, 256 * 16);
+  if (bf16) hipLaunchKernelGGL((join_parts_kernel<uint16_t, EPI>), dim3(grid), dim3(kThreads), 0, s, p);
+  else hipLaunchKernelGGL((join_parts_kernel<float, EPI>), dim3(grid), dim3(kThreads), 0, s, p);
+  return hipGetLastError();
 }
 
 // Loss and lse of every row from its tiles' statistics: a wavefront a row.
@@ -60,11 +100,12 @@ hipError_t launch_xent(const XentArgs& x, const XentPlan& plan, char* ws, bool b
   p.classes = x.classes;
   p.stats = reinterpret_cast<float2*>(ws + plan.stats);
   p.picked = reinterpret_cast<float*>(ws + plan.picked);
-  int tiles = 0;
-  const hipError_t e = launch_product(p, PX_STATS, !x.classes_first, false, bf16, s, &tiles);
+  p.splits = 1;
+  Cut cut;
+  const hipError_t e = launch_product(p, PX_STATS, !x.classes_first, false, bf16, &cut, s);
   if (e != hipSuccess) return e;
   const unsigned grid = (unsigned)std::min<int64_t>((x.rows * x.workers + 3) / 4, 256 * 64);
-  hipLaunchKernelGGL(join_tiles_kernel, dim3(grid), dim3(kThreads), 0, s, x, (const float2*)p.stats, (const float*)p.picked, tiles);
+  hipLaunchKernelGGL(join_tiles_kernel, dim3(grid), dim3(kThreads), 0, s, x, (const float2*)p.stats, (const float*)p.picked, cut.tiles_m);
   return hipGetLastError();
 }
 
@@ -94,8 +135,11 @@ hipError_t launch_xent_backward(const XentArgs& x, const XentPlan& plan, char* w
     p.out = ws + plan.dz;
     p.out_ld = dz.ld;
     p.out_gs = dz.gs;
-    hipError_t e = launch_product(p, PX_DZ, false, !x.classes_first, bf16, s);
+    p.splits = 1;
+    Cut cut;
+    hipError_t e = launch_product(p, PX_DZ, false, !x.classes_first, bf16, &cut, s);
     if (e != hipSuccess) return e;
+    p.parts = reinterpret_cast<float*>(ws + plan.parts);
     p.a = dz;
     p.N = x.width;
     p.K = n;
@@ -103,7 +147,7 @@ hipError_t launch_xent_backward(const XentArgs& x, const XentPlan& plan, char* w
     p.out_ld = x.dh_row;
     p.out_gs = x.rows * x.dh_row;
     p.sums = plan.pieces > 1 ? reinterpret_cast<float*>(ws + plan.sums) : nullptr;
-    if ((e = launch_product(p, PX_DH, false, x.classes_first, bf16, s)) != hipSuccess) return e;
+    if ((e = launch_gradient<PX_DH>(p, false, x.classes_first, bf16, s)) != hipSuccess) return e;
     p.a = x.classes_first ? dz : rows;
     p.b = x.classes_first ? rows : dz;
     p.M = x.classes_first ? n : x.width;
@@ -112,7 +156,7 @@ hipError_t launch_xent_backward(const XentArgs& x, const XentPlan& plan, char* w
     p.out = (char*)x.dw + dw_at * es;
     p.out_ld = x.dw_row;
     p.out_gs = x.dw_gs;
-    if ((e = launch_product(p, PX_DW, true, true, bf16, s)) != hipSuccess) return e;
+    if ((e = launch_gradient<PX_DW>(p, true, true, bf16, s)) != hipSuccess) return e;
   }
   return hipSuccess;
 }
@@ -133,6 +177,9 @@ XentPlan xent_plan(int workers, int64_t rows, int width, int classes, bool bf16,
     e.pieces = (classes + e.piece - 1) / e.piece;
     e.dz = take(n * e.piece * (bf16 ? 2 : 4));
     e.sums = e.pieces > 1 ? take(n * width * sizeof(float)) : 0;
+    const int last = classes - (e.pieces - 1) * e.piece;   // classes of the last piece: of fewer tiles, and so perhaps more parts
+    e.parts = take(std::max({parts_bytes(rows, width, e.piece, workers), parts_bytes(width, std::min(e.piece, classes), rows, workers),
+                             parts_bytes(width, last, rows, workers)}));
     e.real = take((size_t)workers * real_words(rows) * sizeof(uint32_t));
   }
   e.total = at;

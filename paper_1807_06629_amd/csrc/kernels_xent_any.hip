@@ -1,5 +1,5 @@
 // The cross entropy's products of operands of any alignment and size, in fp32 (products and sums) or bf16 (sums in fp32): tiles pass through registers into
-// LDS, [row][contraction] whichever way they lie in memory, 32 deep and twice, the next one on its way while the matrix cores take the last.
+// LDS, [row][contraction] whichever way they lie in memory and twice, the next one on its way while the matrix cores take the last.
 #include "xent_products.h"
 
 namespace prsgd {
@@ -22,55 +22,62 @@ template <typename T> __device__ __forceinline__ u32x4_t load16(const T* p, int 
   return v;
 }
 
-// ---- products of operands of any alignment and size --------------------------------------------
-// Tiles pass through registers into LDS, [row][contraction] either way: 32 deep, rows padded by 16 bytes.  Fragments are those of the grouped products.
-constexpr int kDepth = 32;
-template <typename T, int ROWS, bool TRANS> struct Stage {
-  static constexpr int ES = (int)sizeof(T), V = 16 / ES, LD = kDepth * ES + 16, BYTES = ROWS * LD;
-  // transposed: a thread has a block of 4 / ES contraction elements ... of 16 bytes of rows
-  static constexpr int BK = TRANS ? 4 / ES * (ES == 4 ? 4 : 1) : 1;            // fp32 4 x 4, bf16 2 x 8
-  static constexpr int UNITS = TRANS ? kDepth / BK * (ROWS / V) : ROWS * kDepth / V;
-  static constexpr int NPT = (UNITS + kThreads - 1) / kThreads;
+// An operand's tiles, D deep, rows padded by 16 bytes.
+template <typename T, int ROWS, bool TRANS, int D, int THREADS> struct Stage {
+  static constexpr int ES = (int)sizeof(T), V = 16 / ES, LD = D * ES + 16, BYTES = ROWS * LD;
+  // transposed: a thread has a block of 16 bytes of rows by BK contraction elements (fp32 4 x 4, bf16 8 x 2)
+  static constexpr int BK = TRANS ? (ES == 4 ? 4 : 2) : 1;
+  static constexpr int UNITS = ROWS * D / V / BK, NPT = (UNITS + THREADS - 1) / THREADS;
+  static __device__ __forceinline__ int row_of(int u) { return TRANS ? u % (ROWS / V) * V : u / (D / V); }
+  static __device__ __forceinline__ int depth_of(int u) { return TRANS ? u / (ROWS / V) * BK : u % (D / V) * V; }
   u32x4_t reg[NPT][BK];
-  // rows, depth: what is left of the operand from the tile's first element on; labels: of the contraction index (PX_DW)
-  __device__ __forceinline__ void load(const T* base, int64_t ld, int rows, int depth, const int32_t* labels, int classes) {
+  // rows, depth: what is left of the operand from the tile's first element on
+  __device__ __forceinline__ void load(const T* base, int64_t ld, int rows, int depth) {
 #pragma unroll
     for (int q = 0; q < NPT; ++q) {
-      const int u = q * kThreads + (int)threadIdx.x;
+      const int u = q * THREADS + (int)threadIdx.x, r = row_of(u), c = depth_of(u);
 #pragma unroll
       for (int k = 0; k < BK; ++k) reg[q][k] = (u32x4_t){0, 0, 0, 0};
-      if (UNITS % kThreads != 0 && u >= UNITS) continue;
+      if (UNITS % THREADS != 0 && u >= UNITS) continue;
       if constexpr (TRANS) {
-        const int c = u % (kDepth / BK) * BK, r = u / (kDepth / BK) * V;
 #pragma unroll
         for (int k = 0; k < BK; ++k)
-          if (c + k < depth && r < rows && (labels == nullptr || (unsigned)labels[c + k] < (unsigned)classes))
-            reg[q][k] = load16(base + (int64_t)(c + k) * ld + r, rows - r);
+          if (c + k < depth && r < rows) reg[q][k] = load16(base + (int64_t)(c + k) * ld + r, rows - r);
       } else {
-        const int r = u / (kDepth / V), c = u % (kDepth / V) * V;
         if (r < rows && c < depth) reg[q][0] = load16(base + (int64_t)r * ld + c, depth - c);
       }
     }
   }
-  __device__ __forceinline__ void store(unsigned char* tile) const {
+  // bits: of the tile's contraction elements those that take part (transposed operands)
+  template <int WORDS> __device__ __forceinline__ void store(unsigned char* tile, const uint32_t (&bits)[WORDS]) const {
 #pragma unroll
     for (int q = 0; q < NPT; ++q) {
-      const int u = q * kThreads + (int)threadIdx.x;
-      if (UNITS % kThreads != 0 && u >= UNITS) continue;
+      const int u = q * THREADS + (int)threadIdx.x, r = row_of(u), c = depth_of(u);
+      if (UNITS % THREADS != 0 && u >= UNITS) continue;
       if constexpr (TRANS) {
-        const int c = u % (kDepth / BK) * BK, r = u / (kDepth / BK) * V;
+        u32x4_t v[BK];
+        uint32_t part = ~0u;
+        if constexpr (WORDS > 0) {
+          part = bits[0];
+#pragma unroll
+          for (int w = 1; w < WORDS; ++w) part = c / 32 == w ? bits[w] : part;
+          part >>= c % 32;
+        }
+#pragma unroll
+        for (int k = 0; k < BK; ++k)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[k][e] = (part >> k & 1) != 0 ? reg[q][k][e] : 0;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           unsigned char* to = tile + (r + e) * LD + c * ES;
           if constexpr (ES == 4) {
-            *reinterpret_cast<u32x4_t*>(to) = (u32x4_t){reg[q][0][e], reg[q][1][e], reg[q][2][e], reg[q][3][e]};
+            *reinterpret_cast<u32x4_t*>(to) = (u32x4_t){v[0][e], v[1][e], v[2][e], v[3][e]};
           } else {
-            const uint32_t lo = reg[q][0][e / 2] >> (16 * (e & 1)) & 0xFFFFu, hi = reg[q][1][e / 2] >> (16 * (e & 1)) << 16;
+            const uint32_t lo = v[0][e / 2] >> (16 * (e & 1)) & 0xFFFFu, hi = v[1][e / 2] >> (16 * (e & 1)) << 16;
             *reinterpret_cast<uint32_t*>(to) = lo | hi;
           }
         }
       } else {
-        const int r = u / (kDepth / V), c = u % (kDepth / V) * V;
         *reinterpret_cast<u32x4_t*>(tile + r * LD + c * ES) = reg[q][0];
       }
     }
@@ -83,21 +90,28 @@ template <typename T, int ROWS, bool TRANS> struct Stage {
   }
 };
 
-constexpr int product_stage_bytes(int bm, int bn, int es) { return (bm + bn) * (kDepth * es + 16); }
-
-template <typename T, int BM, int BN, bool TA, bool TB, int EPI> __global__ void __launch_bounds__(kThreads) product_kernel(ProductArgs p) {
-  constexpr int WM = 2, WN = 2, TM = BM / WM / 32, TN = BN / WN / 32, KK = kDepth * (int)sizeof(T) / 32;
-  using A = Stage<T, BM, TA>;
-  using B = Stage<T, BN, TB>;
-  constexpr int STAGE = product_stage_bytes(BM, BN, (int)sizeof(T));
+// WM x WN wavefronts, WK of them at each place, which share out a tile's depth and join their sums at the end.
+template <typename T, int BM, int BN, int WM, int WN, int WK, int D, int EPI> constexpr int lds_bytes() {
+  constexpr int stages = 2 * (BM + BN) * (D * (int)sizeof(T) + 16), join = (WK - 1) * BM * BN * 4;
+  constexpr int epilogue = epilogue_lds_bytes<BM, BN, WM, WN, EPI>(), most = stages > join ? stages : join;
+  return most > epilogue ? most : epilogue;
+}
+template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bool TB, int EPI>
+__global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(ProductArgs p) {
+  constexpr int TM = BM / WM / 32, TN = BN / WN / 32, KK = D * (int)sizeof(T) / 32 / WK, THREADS = 64 * WM * WN * WK;
+  static_assert(D * (int)sizeof(T) % (32 * WK) == 0, "a tile's depth splits evenly");
+  constexpr int WORDS = EPI == PX_DW ? D / 32 : 0;
+  using A = Stage<T, BM, TA, D, THREADS>;
+  using B = Stage<T, BN, TB, D, THREADS>;
+  constexpr int STAGE = A::BYTES + B::BYTES;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wk = wave / (WM * WN), wm = wave / WN % WM, wn = wave % WN;
   const TilePosition at = tile_of_workgroup(p);
-  const int g = at.g, m0 = at.ti * BM, n0 = at.tj * BN;
-  const T* a = reinterpret_cast<const T*>(p.a.p) + g * p.a.gs + (int64_t)m0 * (TA ? 1 : p.a.ld);
-  const T* b = reinterpret_cast<const T*>(p.b.p) + g * p.b.gs + (int64_t)n0 * (TB ? 1 : p.b.ld);
-  const int64_t step_a = (int64_t)kDepth * (TA ? p.a.ld : 1), step_b = (int64_t)kDepth * (TB ? p.b.ld : 1);
-  const int32_t* labels = EPI == PX_DW ? p.labels + g * p.rows : nullptr;
+  const int g = at.g, m0 = at.ti * BM, n0 = at.tj * BN, k0 = at.split * p.split_steps * D, depth = min(p.K - k0, p.split_steps * D);
+  const T* a = reinterpret_cast<const T*>(p.a.p) + g * p.a.gs + (int64_t)m0 * (TA ? 1 : p.a.ld) + (int64_t)k0 * (TA ? p.a.ld : 1);
+  const T* b = reinterpret_cast<const T*>(p.b.p) + g * p.b.gs + (int64_t)n0 * (TB ? 1 : p.b.ld) + (int64_t)k0 * (TB ? p.b.ld : 1);
+  const int64_t step_a = (int64_t)D * (TA ? p.a.ld : 1), step_b = (int64_t)D * (TB ? p.b.ld : 1);
+  const uint32_t* real = p.real + g * real_words(p.rows);
   f32x16_t acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
@@ -107,21 +121,38 @@ template <typename T, int BM, int BN, bool TA, bool TB, int EPI> __global__ void
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
   A ra;
   B rb;
-  const int n_k = (p.K + kDepth - 1) / kDepth;
+  uint32_t bits[WORDS > 0 ? WORDS : 1];
+  const int n_k = (depth + D - 1) / D;
   auto load = [&](int t) __attribute__((always_inline)) {
-    const int32_t* of = EPI == PX_DW ? labels + t * kDepth : nullptr;
-    ra.load(a + t * step_a, p.a.ld, p.M - m0, p.K - t * kDepth, of, p.classes);
-    rb.load(b + t * step_b, p.b.ld, p.N - n0, p.K - t * kDepth, of, p.classes);
+    ra.load(a + t * step_a, p.a.ld, p.M - m0, depth - t * D);
+    rb.load(b + t * step_b, p.b.ld, p.N - n0, depth - t * D);
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) {
+      const int at_word = (k0 + t * D) / 32 + w;
+      bits[w] = at_word < real_words(p.rows) ? real[at_word] : 0;
+    }
   };
-  load(0);
-  ra.store(smem);
-  rb.store(smem + A::BYTES);
+  auto store = [&](unsigned char* stage) __attribute__((always_inline)) {
+    if constexpr (WORDS > 0) {
+      ra.store(stage, bits);
+      rb.store(stage + A::BYTES, bits);
+    } else {
+      const uint32_t all[1] = {~0u};
+      ra.store(stage, all);
+      rb.store(stage + A::BYTES, all);
+    }
+  };
+  if (n_k > 0) {
+    load(0);
+    store(smem);
+  }
   __syncthreads();
   for (int t = 0; t < n_k; ++t) {
     const unsigned char* here = smem + (t & 1) * STAGE;
     if (t + 1 < n_k) load(t + 1);
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
+    for (int k = 0; k < KK; ++k) {
+      const int kk = wk * KK + k;
       Frag<Tag<T>> fa[TM], fb[TN];
 #pragma unroll
       for (int i = 0; i < TM; ++i) fa[i] = A::frag(here, wm * TM + i, kk, lane);
@@ -132,41 +163,59 @@ template <typename T, int BM, int BN, bool TA, bool TB, int EPI> __global__ void
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = mma(fa[i], fb[j], acc[i][j]);
     }
-    if (t + 1 < n_k) {
-      unsigned char* next = smem + ((t + 1) & 1) * STAGE;
-      ra.store(next);
-      rb.store(next + A::BYTES);
+    if (t + 1 < n_k) store(smem + ((t + 1) & 1) * STAGE);
+    __syncthreads();
+  }
+  if constexpr (WK > 1) {
+    float* sums = reinterpret_cast<float*>(smem);            // [WK - 1][WM * WN][TM * TN][16][64]
+    constexpr int BLOCK = 16 * kWave, PLACE = TM * TN * BLOCK;
+    if (wk > 0) {
+      float* to = sums + ((wk - 1) * WM * WN + wm * WN + wn) * PLACE + lane;
+#pragma unroll
+      for (int i = 0; i < TM * TN; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) to[i * BLOCK + e * kWave] = acc[i / TN][i % TN][e];
+    }
+    __syncthreads();
+    if (wk == 0) {
+#pragma unroll
+      for (int w = 0; w < WK - 1; ++w)
+#pragma unroll
+        for (int i = 0; i < TM * TN; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[i / TN][i % TN][e] += sums[(w * WM * WN + wm * WN + wn) * PLACE + i * BLOCK + e * kWave + lane];
     }
     __syncthreads();
   }
-  product_epilogue<T, EPI, BM, BN, WM, WN>(p, acc, g, m0, n0, at.ti, wm, wn, lane, smem);
+  product_epilogue<T, EPI, BM, BN, WM, WN, WK>(p, acc, at, m0, n0, wm, wn, lane, wk == 0, smem);
 }
 
-template <typename T, int BM, int BN, bool TA, bool TB, int EPI> hipError_t launch_tile(ProductArgs p, int* tiles_m, hipStream_t s) {
-  constexpr int kStages = 2 * product_stage_bytes(BM, BN, (int)sizeof(T)), kEpilogue = epilogue_lds_bytes<BM, BN, 2, 2, EPI>();
-  constexpr int kLds = kStages > kEpilogue ? kStages : kEpilogue;
+template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bool TB, int EPI> hipError_t launch_tile(ProductArgs p, Cut* cut, hipStream_t s) {
+  constexpr int kLds = lds_bytes<T, BM, BN, WM, WN, WK, D, EPI>();
   static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
-  constexpr auto kernel = product_kernel<T, BM, BN, TA, TB, EPI>;
+  constexpr auto kernel = product_kernel<T, BM, BN, WM, WN, WK, D, TA, TB, EPI>;
   if (const hipError_t e = allow_lds<kernel>(kLds); e != hipSuccess) return e;
-  *tiles_m = p.tiles_m = (p.M + BM - 1) / BM;
-  p.tiles_n = (p.N + BN - 1) / BN;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)p.tiles_m * (unsigned)p.tiles_n * (unsigned)p.groups), dim3(kThreads), kLds, s, p);
+  const unsigned grid = cut_product(p, BM, BN, D, cut);
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * WM * WN * WK), kLds, s, p);
   return hipGetLastError();
 }
-template <typename T> hipError_t launch(const ProductArgs& p, int epi, bool ta, bool tb, int* tiles_m, hipStream_t s) {
-  constexpr int B = 128;
+template <typename T, bool TA, bool TB, int EPI> hipError_t launch_size(const ProductArgs& p, Cut* cut, hipStream_t s) {
+  if (tiles_of(p, 128) >= 192) return launch_tile<T, 128, 128, 2, 2, 1, 32, TA, TB, EPI>(p, cut, s);
+  return launch_tile<T, 32, 32, 1, 1, 4, 128, TA, TB, EPI>(p, cut, s);
+}
+template <typename T> hipError_t launch(const ProductArgs& p, int epi, bool ta, bool tb, Cut* cut, hipStream_t s) {
   switch (epi) {
-    case PX_STATS: return ta ? launch_tile<T, B, B, true, false, PX_STATS>(p, tiles_m, s) : launch_tile<T, B, B, false, false, PX_STATS>(p, tiles_m, s);
-    case PX_DZ: return tb ? launch_tile<T, B, B, false, true, PX_DZ>(p, tiles_m, s) : launch_tile<T, B, B, false, false, PX_DZ>(p, tiles_m, s);
-    case PX_DH: return tb ? launch_tile<T, B, B, false, true, PX_DH>(p, tiles_m, s) : launch_tile<T, B, B, false, false, PX_DH>(p, tiles_m, s);
-    default: return launch_tile<T, B, B, true, true, PX_DW>(p, tiles_m, s);
+    case PX_STATS: return ta ? launch_size<T, true, false, PX_STATS>(p, cut, s) : launch_size<T, false, false, PX_STATS>(p, cut, s);
+    case PX_DZ: return tb ? launch_size<T, false, true, PX_DZ>(p, cut, s) : launch_size<T, false, false, PX_DZ>(p, cut, s);
+    case PX_DH: return tb ? launch_size<T, false, true, PX_DH>(p, cut, s) : launch_size<T, false, false, PX_DH>(p, cut, s);
+    default: return launch_size<T, true, true, PX_DW>(p, cut, s);
   }
 }
 
 }  // namespace
 
-hipError_t launch_product_any(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, bool bf16, int* tiles_m, hipStream_t s) {
-  return bf16 ? launch<uint16_t>(p, epi, a_transposed, b_transposed, tiles_m, s) : launch<float>(p, epi, a_transposed, b_transposed, tiles_m, s);
+hipError_t launch_product_any(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, bool bf16, Cut* cut, hipStream_t s) {
+  return bf16 ? launch<uint16_t>(p, epi, a_transposed, b_transposed, cut, s) : launch<float>(p, epi, a_transposed, b_transposed, cut, s);
 }
 
 }  // namespace prsgd

@@ -95,13 +95,14 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) product_bf16_kernel(const Pro
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
   const TilePosition place_of = tile_of_workgroup(p);
-  const int g = place_of.g, m0 = place_of.ti * BM, n0 = place_of.tj * BN;
+  const int g = place_of.g, m0 = place_of.ti * BM, n0 = place_of.tj * BN, step0 = place_of.split * p.split_steps;
+  const int depth = min(p.K - step0 * kDepth, p.split_steps * kDepth);
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
-  const uint16_t* a = reinterpret_cast<const uint16_t*>(p.a.p) + g * p.a.gs + (int64_t)m0 * (TA ? 1 : p.a.ld);
-  const uint16_t* b = reinterpret_cast<const uint16_t*>(p.b.p) + g * p.b.gs + (int64_t)n0 * (TB ? 1 : p.b.ld);
   const int64_t a_step = (int64_t)kDepth * (TA ? p.a.ld : 1), b_step = (int64_t)kDepth * (TB ? p.b.ld : 1);
-  const int lda = (int)p.a.ld, ldb = (int)p.b.ld, n_k = (p.K + kDepth - 1) / kDepth, tail = p.K - (n_k - 1) * kDepth;
+  const uint16_t* a = reinterpret_cast<const uint16_t*>(p.a.p) + g * p.a.gs + (int64_t)m0 * (TA ? 1 : p.a.ld) + step0 * a_step;
+  const uint16_t* b = reinterpret_cast<const uint16_t*>(p.b.p) + g * p.b.gs + (int64_t)n0 * (TB ? 1 : p.b.ld) + step0 * b_step;
+  const int lda = (int)p.a.ld, ldb = (int)p.b.ld, n_k = (depth + kDepth - 1) / kDepth, tail = depth - (n_k - 1) * kDepth;
   ReqA ra;
   ReqB rb;
   ra.set(lda, p.M - m0, n_k == 1 ? tail : kDepth, wave, lane);
@@ -119,7 +120,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) product_bf16_kernel(const Pro
     }
   };
   // contraction elements of tile t that take part
-  const uint64_t* real = reinterpret_cast<const uint64_t*>(p.real + g * real_words(p.rows));
+  const uint64_t* real = reinterpret_cast<const uint64_t*>(p.real + g * real_words(p.rows)) + step0;
   auto bits_of = [&](int t) __attribute__((always_inline)) -> uint64_t {
     if constexpr (EPI == PX_DW) return ((const __attribute__((address_space(4))) uint64_t*)real)[t];
     return t == n_k - 1 && tail != kDepth ? (1ull << tail) - 1 : ~0ull;
@@ -192,32 +193,30 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) product_bf16_kernel(const Pro
   for (; t + S < n_k; ++t) step(t, std::true_type{});
   for (; t < n_k; ++t) step(t, std::false_type{});
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-  product_epilogue<uint16_t, EPI, BM, BN, WM, WN>(p, acc, g, m0, n0, place_of.ti, wm, wn, lane, smem);
+  product_epilogue<uint16_t, EPI, BM, BN, WM, WN, 1>(p, acc, place_of, m0, n0, wm, wn, lane, true, smem);
 }
 
-template <int BM, int BN, int WM, int WN, int S, bool TA, bool TB, int EPI> hipError_t launch_tile(ProductArgs p, int* tiles_m, hipStream_t s) {
+template <int BM, int BN, int WM, int WN, int S, bool TA, bool TB, int EPI> hipError_t launch_tile(ProductArgs p, Cut* cut, hipStream_t s) {
   static_assert(S >= 2, "a step's tile and the next one");
   constexpr int kLds = lds_bytes<BM, BN, WM, WN, S, EPI>();
   static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
   constexpr auto kernel = product_bf16_kernel<BM, BN, WM, WN, S, TA, TB, EPI>;
   if (const hipError_t e = allow_lds<kernel>(kLds); e != hipSuccess) return e;
-  *tiles_m = p.tiles_m = (p.M + BM - 1) / BM;
-  p.tiles_n = (p.N + BN - 1) / BN;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)p.tiles_m * (unsigned)p.tiles_n * (unsigned)p.groups), dim3(64 * WM * WN), kLds, s, p);
+  const unsigned grid = cut_product(p, BM, BN, kDepth, cut);
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * WM * WN), kLds, s, p);
   return hipGetLastError();
 }
 
-template <bool TA, bool TB, int EPI> hipError_t launch(const ProductArgs& p, int* tiles_m, hipStream_t s) {
+template <bool TA, bool TB, int EPI> hipError_t launch(const ProductArgs& p, Cut* cut, hipStream_t s) {
   // Time of a launch in units of a 64 x 64 tile's products: tiles per compute unit times their size over their efficiency.  Of tiles that a compute unit has
   // several of in hand, parts of a round count as such; of 256 x 256 tiles whole rounds.
-  auto tiles = [&](int64_t b) { return ((p.M + b - 1) / b) * ((p.N + b - 1) / b) * p.groups; };
   auto cost = [](int64_t n, int b, double efficiency) { return (n < 256 ? 1.0 : (double)n / 256.0) * (b / 64) * (b / 64) / efficiency; };
-  const int64_t n_middle = tiles(128), n_huge = (tiles(256) + 255) / 256 * 256;
-  const double middle = cost(n_middle, 128, n_middle > 256 ? 0.9 : 1.34), small = cost(tiles(64), 64, 0.68), huge = cost(n_huge, 256, 1.2);
-  if (huge <= middle && huge <= small) return launch_tile<256, 256, 4, 2, 2, TA, TB, EPI>(p, tiles_m, s);
-  if (middle > small) return launch_tile<64, 64, 2, 2, 4, TA, TB, EPI>(p, tiles_m, s);
-  if (n_middle <= 256) return launch_tile<128, 128, 4, 2, 3, TA, TB, EPI>(p, tiles_m, s);
-  return launch_tile<128, 128, 2, 2, 2, TA, TB, EPI>(p, tiles_m, s);
+  const int64_t n_middle = tiles_of(p, 128), n_huge = (tiles_of(p, 256) + 255) / 256 * 256;
+  const double middle = cost(n_middle, 128, n_middle > 256 ? 0.9 : 1.34), small = cost(tiles_of(p, 64), 64, 0.68), huge = cost(n_huge, 256, 1.2);
+  if (huge <= middle && huge <= small) return launch_tile<256, 256, 4, 2, 2, TA, TB, EPI>(p, cut, s);
+  if (middle > small) return launch_tile<64, 64, 2, 2, 4, TA, TB, EPI>(p, cut, s);
+  if (n_middle <= 256) return launch_tile<128, 128, 4, 2, 3, TA, TB, EPI>(p, cut, s);
+  return launch_tile<128, 128, 2, 2, 2, TA, TB, EPI>(p, cut, s);
 }
 
 bool operand_aligned(const Operand& o, int64_t contiguous, int64_t other, int groups) {
@@ -233,12 +232,12 @@ bool product_aligned(const ProductArgs& p, bool a_transposed, bool b_transposed)
          operand_aligned(p.b, whole(p.b, b_transposed ? p.N : p.K), b_transposed ? p.K : p.N, p.groups);
 }
 
-hipError_t launch_product_bf16(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, int* tiles_m, hipStream_t s) {
+hipError_t launch_product_bf16(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, Cut* cut, hipStream_t s) {
   switch (epi) {
-    case PX_STATS: return a_transposed ? launch<true, false, PX_STATS>(p, tiles_m, s) : launch<false, false, PX_STATS>(p, tiles_m, s);
-    case PX_DZ: return b_transposed ? launch<false, true, PX_DZ>(p, tiles_m, s) : launch<false, false, PX_DZ>(p, tiles_m, s);
-    case PX_DH: return b_transposed ? launch<false, true, PX_DH>(p, tiles_m, s) : launch<false, false, PX_DH>(p, tiles_m, s);
-    default: return launch<true, true, PX_DW>(p, tiles_m, s);
+    case PX_STATS: return a_transposed ? launch<true, false, PX_STATS>(p, cut, s) : launch<false, false, PX_STATS>(p, cut, s);
+    case PX_DZ: return b_transposed ? launch<false, true, PX_DZ>(p, cut, s) : launch<false, false, PX_DZ>(p, cut, s);
+    case PX_DH: return b_transposed ? launch<false, true, PX_DH>(p, cut, s) : launch<false, false, PX_DH>(p, cut, s);
+    default: return launch<true, true, PX_DW>(p, cut, s);
   }
 }
 

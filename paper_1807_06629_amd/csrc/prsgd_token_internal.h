@@ -96,7 +96,7 @@ struct XentArgs {
 };
 struct XentPlan {
   int piece, pieces;                     // backward: classes of a piece
-  size_t stats, picked, dz, sums, real, total;       // byte offsets
+  size_t stats, picked, dz, sums, parts, real, total;       // byte offsets
 };
 XentPlan xent_plan(int workers, int64_t rows, int width, int classes, bool bf16, bool backward);
 hipError_t launch_xent(const XentArgs& p, const XentPlan& plan, char* ws, bool bf16, hipStream_t s);

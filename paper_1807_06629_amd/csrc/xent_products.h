@@ -8,6 +8,7 @@
 
 #include <math.h>
 
+#include <algorithm>
 #include <atomic>
 #include <type_traits>
 
@@ -22,7 +23,9 @@ struct Operand { const void* p; int64_t gs, ld; bool dz; };
 struct ProductArgs {
   Operand a, b;
   int M, N, K;                           // rows of A, rows of B, contraction
-  int tiles_m, tiles_n, groups;          // tiles: filled in by the launcher
+  int groups;
+  int splits; float* parts;              // wished for: parts of the contraction, each to its own fp32 [groups][M][N] of `parts` (1: none)
+  int tiles_m, tiles_n, split_steps;     // filled in by the launcher: tiles, and steps of the contraction in a part
   // of the rows, `rows` in every worker
   const int32_t* labels;
   const float* lse; const float* dloss;
@@ -56,20 +59,56 @@ __device__ __forceinline__ void join_stats(float& m, float& s, float m2, float s
 // Rows of the accumulators: element e of a 32 x 32 block lies at row acc_row(e, lane), column lane % 32.
 __device__ __forceinline__ int acc_row(int e, int lane) { return 8 * (e / 4) + 4 * (lane >> 5) + (e & 3); }
 
+// Consecutive workgroups go to the XCDs in turn; each gets a contiguous range of the tiles, so that what neighbours share stays in its L2.
+struct TilePosition { int g, ti, tj, split; };
+__device__ __forceinline__ TilePosition tile_of_workgroup(const ProductArgs& p) {
+  const int tiles = p.tiles_m * p.tiles_n, total = tiles * p.groups * p.splits, xcd = blockIdx.x & 7;
+  const int idx = xcd * (total >> 3) + min(xcd, total & 7) + (int)(blockIdx.x >> 3), part = idx / tiles, in = idx - part * tiles, g = part % p.groups;
+  // strips four tiles high, column by column
+  constexpr int kHigh = 4;
+  const int strip = in / (kHigh * p.tiles_n), first = strip * kHigh, high = min(kHigh, p.tiles_m - first), rest = in - first * p.tiles_n;
+  return {g, first + rest % high, rest / high, part / p.groups};
+}
+
 constexpr int kStripPad = 8;             // floats: the four rows between a register's two halves lie 32 banks apart
 template <int BM, int BN, int WM, int WN, int EPI> constexpr int epilogue_lds_bytes() {
   return EPI == PX_STATS ? WM * BN * (int)sizeof(float2) : WM * WN * 32 * (BN / WN + kStripPad) * 4;
 }
 
-// Workgroup-wide: the last reads of the operands' tiles in smem are over.
-template <typename T, int EPI, int BM, int BN, int WM, int WN>
-__device__ __forceinline__ void product_epilogue(const ProductArgs& p, const f32x16_t (&acc)[BM / WM / 32][BN / WN / 32], int g, int m0, int n0, int ti,
-                                                 int wm, int wn, int lane, unsigned char* smem) {
+// Eight columns of a row of dh or dW, n of which exist.
+template <typename T, int EPI> __device__ __forceinline__ void finish(const ProductArgs& p, int g, int r, int c, int n, float (&v)[8]) {
+  if constexpr (EPI == PX_DH) {
+    const bool real = (unsigned)p.labels[g * p.rows + r] < (unsigned)p.classes;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = real ? v[e] : 0.0f;
+    if (p.sums != nullptr) {
+      float* sum = p.sums + ((int64_t)g * p.M + r) * p.N + c;
+      if (!p.first_piece) {
+        float before[8];
+        load8(sum, n, before);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += before[e];
+      }
+      if (!p.last_piece) {
+        store8(sum, n, v);
+        return;
+      }
+    }
+  }
+  store8(reinterpret_cast<T*>(p.out) + g * p.out_gs + (int64_t)r * p.out_ld + c, n, v);
+}
+
+// Workgroup-wide: the last reads of the operands' tiles in smem are over.  sums: this wavefront's accumulators are whole (of WK at a place one).
+template <typename T, int EPI, int BM, int BN, int WM, int WN, int WK>
+__device__ __forceinline__ void product_epilogue(const ProductArgs& p, const f32x16_t (&acc)[BM / WM / 32][BN / WN / 32], TilePosition at, int m0, int n0,
+                                                 int wm, int wn, int lane, bool sums, unsigned char* smem) {
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
+  const int g = at.g;
   if constexpr (EPI == PX_STATS) {
     float2* shared = reinterpret_cast<float2*>(smem);        // [WM][BN]
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
+      if (!sums) break;
       const int col = (wn * TN + j) * 32 + (lane & 31), row = n0 + col;
       const bool live = row < p.N;
       const int label = live ? p.labels[g * p.rows + row] : -1;
@@ -99,7 +138,7 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& p, const f32
       if (lane < 32) shared[wm * BN + col] = make_float2(m, s);
     }
     __syncthreads();
-    for (int col = threadIdx.x; col < BN; col += WM * WN * kWave) {
+    for (int col = threadIdx.x; col < BN; col += WM * WN * WK * kWave) {
       if (n0 + col >= p.N) continue;
       float2 v = shared[col];
 #pragma unroll
@@ -107,10 +146,11 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& p, const f32
         const float2 o = shared[w * BN + col];
         join_stats(v.x, v.y, o.x, o.y);
       }
-      p.stats[(g * p.rows + n0 + col) * p.tiles_m + ti] = v;
+      p.stats[(g * p.rows + n0 + col) * p.tiles_m + at.ti] = v;
     }
   } else {
     // a wavefront passes strips of 32 rows through LDS, from where a lane takes eight columns of a row at a time
+    if (!sums) return;
     constexpr int W = BN / WN, P = W + kStripPad, VPR = W / 8, RPP = kWave / VPR, PASSES = 32 / RPP;
     float* strip = reinterpret_cast<float*>(smem) + (wm * WN + wn) * 32 * P;
     const int c = n0 + wn * W + lane % VPR * 8, n = p.N - c;
@@ -125,10 +165,10 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& p, const f32
 #pragma unroll
       for (int q = 0; q < PASSES; ++q) {
         const int lr = q * RPP + lane / VPR, r = r0 + lr;
-        const float* at = strip + lr * P + lane % VPR * 8;
+        const float* from = strip + lr * P + lane % VPR * 8;
         float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = at[e];
+        for (int e = 0; e < 8; ++e) v[e] = from[e];
         const bool live = r < p.M;
         if constexpr (EPI == PX_DZ) {
           const int64_t row = g * p.rows + (live ? r : 0);
@@ -141,53 +181,27 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& p, const f32
           if (live && c < p.out_ld) store8(reinterpret_cast<T*>(p.out) + g * p.out_gs + (int64_t)r * p.out_ld + c, 8, v);
         } else {
           if (!live || n <= 0) continue;
-          if constexpr (EPI == PX_DH) {
-            const bool real = (unsigned)p.labels[g * p.rows + r] < (unsigned)p.classes;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = real ? v[e] : 0.0f;
-            if (p.sums != nullptr) {
-              float* sum = p.sums + ((int64_t)g * p.M + r) * p.N + c;
-              if (!p.first_piece) {
-                float before[8];
-                load8(sum, n, before);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += before[e];
-              }
-              if (!p.last_piece) {
-                store8(sum, n, v);
-                continue;
-              }
-            }
-          }
-          store8(reinterpret_cast<T*>(p.out) + g * p.out_gs + (int64_t)r * p.out_ld + c, n, v);
+          if (p.splits > 1) store8(p.parts + (((int64_t)at.split * p.groups + g) * p.M + r) * p.N + c, n, v);
+          else finish<T, EPI>(p, g, r, c, n, v);
         }
       }
       __builtin_amdgcn_wave_barrier();
     }
     if constexpr (EPI == PX_DZ) {
       if (p.first_piece && n0 == 0 && wn == 0) {
-        // rows of this wavefront: words of 32, and zeros behind the last row to the end of a pair of words
+        // rows of this wavefront: words of 32, of which behind the last row there may be one more, so that they are pairs
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
           const int r0 = m0 + (wm * TM + i) * 32, r = r0 + (lane & 31);
           const bool real = r < p.M && (unsigned)p.labels[g * p.rows + r] < (unsigned)p.classes;
           const uint64_t bits = __ballot(real);
-          if (lane == 0 && r0 / 32 < real_words(p.M)) p.real[g * real_words(p.M) + r0 / 32] = (uint32_t)bits;
+          uint32_t* words = p.real + g * real_words(p.M) + r0 / 32;
+          if (lane == 0 && r0 < p.M) words[0] = (uint32_t)bits;
+          if (lane == 0 && r0 < p.M && r0 + 32 >= p.M && r0 / 32 % 2 == 0) words[1] = 0;
         }
       }
     }
   }
-}
-
-// Consecutive workgroups go to the XCDs in turn; each gets a contiguous range of the tiles, so that what neighbours share stays in its L2.
-struct TilePosition { int g, ti, tj; };
-__device__ __forceinline__ TilePosition tile_of_workgroup(const ProductArgs& p) {
-  const int tiles = p.tiles_m * p.tiles_n, total = tiles * p.groups, xcd = blockIdx.x & 7;
-  const int idx = xcd * (total >> 3) + min(xcd, total & 7) + (int)(blockIdx.x >> 3), g = idx / tiles, in = idx - g * tiles;
-  // strips four tiles high, column by column
-  constexpr int kHigh = 4;
-  const int strip = in / (kHigh * p.tiles_n), first = strip * kHigh, high = min(kHigh, p.tiles_m - first), rest = in - first * p.tiles_n;
-  return {g, first + rest % high, rest / high};
 }
 
 // Limit of a kernel's dynamic LDS, raised once (twice is harmless).
@@ -200,12 +214,25 @@ template <auto KERNEL> hipError_t allow_lds(int bytes) {
   return e;
 }
 
+// Tiles of B x B, and those of all parts of the contraction.
+inline int64_t tiles_of(const ProductArgs& p, int64_t b) { return (p.M + b - 1) / b * ((p.N + b - 1) / b) * p.groups * p.splits; }
+// How a launch of tiles of bm x bn, `depth` a step, cuts the product: its grid.  No part of the contraction is empty.
+struct Cut { int tiles_m, splits; };
+inline unsigned cut_product(ProductArgs& p, int bm, int bn, int depth, Cut* cut) {
+  cut->tiles_m = p.tiles_m = (p.M + bm - 1) / bm;
+  p.tiles_n = (p.N + bn - 1) / bn;
+  const int steps = std::max((p.K + depth - 1) / depth, 1);
+  p.split_steps = (steps + p.splits - 1) / p.splits;
+  cut->splits = p.splits = (steps + p.split_steps - 1) / p.split_steps;
+  return (unsigned)p.tiles_m * (unsigned)p.tiles_n * (unsigned)p.groups * (unsigned)p.splits;
+}
+
 // transposed: (A, B) as (element (i, c) at c * ld + i).  Operands of any alignment and size (kernels_xent_any.hip) ...
-// tiles_m: how many tiles the rows of A were cut into, of kLeastTile rows at least
-constexpr int kLeastTile = 64;
-hipError_t launch_product_any(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, bool bf16, int* tiles_m, hipStream_t s);
+// cut: how the product was cut; tiles have kLeastTile rows at least
+constexpr int kLeastTile = 32;
+hipError_t launch_product_any(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, bool bf16, Cut* cut, hipStream_t s);
 // ... and bf16 operands whose rows start at 16 bytes and are as long in whole (kernels_xent_bf16.hip).
 bool product_aligned(const ProductArgs& p, bool a_transposed, bool b_transposed);
-hipError_t launch_product_bf16(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, int* tiles_m, hipStream_t s);
+hipError_t launch_product_bf16(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, Cut* cut, hipStream_t s);
 
 }  // namespace prsgd
