@@ -7,6 +7,7 @@
 // no numbers, and get zeros.
 #include <algorithm>
 
+#include "row_pieces.h"
 #include "xent_products.h"
 
 namespace prsgd {
@@ -20,22 +21,22 @@ int splits_of(int64_t m, int64_t n, int64_t k, int groups) {
 }
 size_t parts_bytes(int64_t m, int64_t n, int64_t k, int groups) {
   const int splits = splits_of(m, n, k, groups);
-  return splits > 1 ? (size_t)splits * groups * m * n * sizeof(float) : 0;
+  return splits > 1 ? (size_t)splits * groups * std::max(m * parts_row(n), n * parts_row(m)) * sizeof(float) : 0;
 }
 
 // dh or dW of the parts: a lane eight columns.
 template <typename T, int EPI> __global__ void __launch_bounds__(kThreads) join_parts_kernel(ProductArgs p) {
-  const int64_t per_row = (p.N + 7) / 8, matrix = (int64_t)p.M * p.N, total = per_row * p.M * p.groups;
+  const int64_t per_row = (p.N + 7) / 8, part = parts_row(p.N) * p.M * p.groups, total = per_row * p.M * p.groups;
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
     const int64_t row = i / per_row, g = row / p.M;
     const int r = (int)(row - g * p.M), c = (int)(i - row * per_row) * 8, n = p.N - c;
-    const float* from = p.parts + row * p.N + c;
+    const float* from = p.parts + row * parts_row(p.N) + c;
     float v[8];
-    load8(from, n, v);
+    load8(from, 8, v);
 #pragma unroll 4
     for (int q = 1; q < p.splits; ++q) {
       float more[8];
-      load8(from + q * matrix * p.groups, n, more);
+      load8(from + q * part, 8, more);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += more[e];
     }
@@ -62,18 +63,23 @@ template <int EPI> hipError_t launch_gradient(ProductArgs p, bool a_transposed, 
   return hipGetLastError();
 }
 
-// Loss and lse of every row from its tiles' statistics: a wavefront a row.
-__global__ void __launch_bounds__(kThreads) join_tiles_kernel(XentArgs p, const float2* stats, const float* picked, int tiles) {
-  const int lane = threadIdx.x % kWave;
+// Statistics of the classes' pieces, `stride` apart: [rows of all workers][tiles], in the last one [..][last_tiles].
+struct XentPieces { int pieces, tiles, last_tiles; int64_t stride; };
+
+// Loss and lse of every row from its tiles' statistics, by as many lanes as it has tiles, at most a wavefront.
+__global__ void __launch_bounds__(kThreads) join_tiles_kernel(XentArgs p, const float2* stats, const float* picked, XentPieces pieces, int lanes_log2) {
+  const int lanes = 1 << lanes_log2, lane = threadIdx.x & (lanes - 1), slots = kThreads >> lanes_log2;
   const int64_t rows = p.rows * p.workers;
-  for (int64_t r = (int64_t)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave; r < rows; r += (int64_t)gridDim.x * (kThreads / kWave)) {
+  for (int64_t r = (int64_t)blockIdx.x * slots + (threadIdx.x >> lanes_log2); r < rows; r += (int64_t)gridDim.x * slots) {
     float m = -INFINITY, s = 0.0f;
-    for (int t = lane; t < tiles; t += kWave) {
-      const float2 v = stats[r * tiles + t];
-      join_stats(m, s, v.x, v.y);
+    for (int k = 0; k < pieces.pieces; ++k) {
+      const int tiles = k + 1 == pieces.pieces ? pieces.last_tiles : pieces.tiles;
+      for (int t = lane; t < tiles; t += lanes) {
+        const float2 v = stats[k * pieces.stride + r * tiles + t];
+        join_stats(m, s, v.x, v.y);
+      }
     }
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) join_stats(m, s, __shfl_xor(m, d), __shfl_xor(s, d));
+    for (int d = 1; d < lanes; d <<= 1) join_stats(m, s, __shfl_xor(m, d), __shfl_xor(s, d));
     if (lane == 0) {
       const float lse = m + logf(s);
       const bool real = (unsigned)p.labels[r] < (unsigned)p.classes;
@@ -83,29 +89,97 @@ __global__ void __launch_bounds__(kThreads) join_tiles_kernel(XentArgs p, const 
   }
 }
 
-constexpr size_t kPieceBytes = (size_t)128 << 20;          // of dz
+constexpr size_t kPieceBytes = (size_t)128 << 20;          // of dz, and of a copy of W
+
+// Rows of bf16 whose length is no multiple of eight are copied to such a multiple, with zeros, where the products take long enough: aligned operands go to LDS
+// by themselves.  Gradients of 8 workers' rows x 1024 x 8001 classes, as they lie and by copies: 128 rows 174 and 175 us, 256 rows 289 and 222 us, 512 rows 491 and
+// 296 us; of 16 workers' 256 rows x 129 x 333 24 and 24 us.
+constexpr int kAlignRows = 192;
+constexpr int64_t eights(int64_t n) { return (n + 7) / 8 * 8; }
+
+__global__ void __launch_bounds__(kThreads) align_kernel(Operand from, Operand to, int rows, int width, int64_t total, int lanes_log2) {
+  const int lanes = 1 << lanes_log2, slots = kThreads >> lanes_log2;
+  for (int64_t i = (int64_t)blockIdx.x * slots + (threadIdx.x >> lanes_log2); i < total; i += (int64_t)gridDim.x * slots) {
+    const int64_t g = (uint32_t)i / (uint32_t)rows, r = i - g * rows;
+    const uint16_t* in = reinterpret_cast<const uint16_t*>(from.p) + g * from.gs + r * from.ld;
+    uint16_t* out = reinterpret_cast<uint16_t*>(const_cast<void*>(to.p)) + g * to.gs + r * to.ld;
+    for (int c = (threadIdx.x & (lanes - 1)) * 8; c < width; c += lanes * 8) {
+      const int n = width - c;
+      u32x4_t v;
+      if (n >= 8) v = reinterpret_cast<const Packed16<2>*>(in + c)->v;
+      else v = place_end<2>(load_end<2>(in + c, n, from.p), n);
+      *reinterpret_cast<u32x4_t*>(out + c) = v;
+    }
+  }
+}
+hipError_t launch_align(const Operand& from, const Operand& to, int rows, int width, int workers, hipStream_t s) {
+  const int lanes_log2 = lanes_for_row(width), slots = kThreads >> lanes_log2;
+  const int64_t total = (int64_t)rows * workers;
+  const unsigned grid = (unsigned)std::min<int64_t>((total + slots - 1) / slots, 256 * 64);
+  hipLaunchKernelGGL(align_kernel, dim3(grid), dim3(kThreads), 0, s, from, to, rows, width, total, lanes_log2);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+namespace {
+
+// What a piece of the classes, `first` .. `first` + n, works on: rows and matrices, as they lie or as copies in whole eights.
+hipError_t operands_of_piece(const XentArgs& x, const XentPlan& plan, char* ws, bool bf16, int first, int n, Operand* rows, Operand* matrix, hipStream_t s) {
+  const int64_t at = x.classes_first ? first * x.w_row : first;
+  *rows = {x.h, x.rows * x.h_row, x.h_row, false};
+  *matrix = {(const char*)x.w + at * (bf16 ? 2 : 4), x.w_gs, x.w_row, false};
+  if (plan.align_h) {
+    const Operand copy{ws + plan.h, x.rows * eights(x.width), eights(x.width), true};
+    if (first == 0)
+      if (const hipError_t e = launch_align(*rows, copy, (int)x.rows, x.width, x.workers, s); e != hipSuccess) return e;
+    *rows = copy;
+  }
+  if (plan.align_w) {
+    const int r = x.classes_first ? n : x.width, c = x.classes_first ? x.width : n;
+    const Operand copy{ws + plan.w, r * eights(c), eights(c), true};
+    if (const hipError_t e = launch_align(*matrix, copy, r, c, x.workers, s); e != hipSuccess) return e;
+    *matrix = copy;
+  }
+  return hipSuccess;
+}
 
 }  // namespace
 
 hipError_t launch_xent(const XentArgs& x, const XentPlan& plan, char* ws, bool bf16, hipStream_t s) {
-  ProductArgs p{};
-  p.a = {x.w, x.w_gs, x.w_row, false};
-  p.b = {x.h, x.rows * x.h_row, x.h_row, false};
-  p.M = x.classes;
-  p.N = (int)x.rows;
-  p.K = x.width;
-  p.groups = x.workers;
-  p.labels = x.labels;
-  p.rows = x.rows;
-  p.classes = x.classes;
-  p.stats = reinterpret_cast<float2*>(ws + plan.stats);
-  p.picked = reinterpret_cast<float*>(ws + plan.picked);
-  p.splits = 1;
-  Cut cut;
-  const hipError_t e = launch_product(p, PX_STATS, !x.classes_first, false, bf16, &cut, s);
-  if (e != hipSuccess) return e;
-  const unsigned grid = (unsigned)std::min<int64_t>((x.rows * x.workers + 3) / 4, 256 * 64);
-  hipLaunchKernelGGL(join_tiles_kernel, dim3(grid), dim3(kThreads), 0, s, x, (const float2*)p.stats, (const float*)p.picked, cut.tiles_m);
+  Cut cut{};
+  int64_t stats = 0;                     // of the pieces so far, one behind another
+  const int least = (plan.piece + kLeastTile - 1) / kLeastTile;
+  XentPieces pieces{};
+  for (int k = 0; k < plan.pieces; ++k) {
+    const int first = k * plan.piece, n = std::min(plan.piece, x.classes - first);
+    ProductArgs p{};
+    if (const hipError_t e = operands_of_piece(x, plan, ws, bf16, first, n, &p.b, &p.a, s); e != hipSuccess) return e;
+    p.M = n;
+    p.N = (int)x.rows;
+    p.K = x.width;
+    p.groups = x.workers;
+    p.splits = 1;
+    p.labels = x.labels;
+    p.rows = x.rows;
+    p.class0 = first;
+    p.classes = x.classes;
+    p.stats = reinterpret_cast<float2*>(ws + plan.stats) + stats;
+    p.picked = reinterpret_cast<float*>(ws + plan.picked);
+    if (const hipError_t e = launch_product(p, PX_STATS, !x.classes_first, false, bf16, &cut, s); e != hipSuccess) return e;
+    if (k == 0) pieces.tiles = cut.tiles_m;
+    pieces.last_tiles = cut.tiles_m;
+    stats += x.rows * x.workers * least;
+  }
+  pieces.pieces = plan.pieces;
+  pieces.stride = x.rows * x.workers * least;
+  const int tiles = (pieces.pieces - 1) * pieces.tiles + pieces.last_tiles;
+  int lanes_log2 = 0;
+  while (lanes_log2 < 6 && (1 << lanes_log2) < tiles) ++lanes_log2;
+  const int slots = kThreads >> lanes_log2;
+  const unsigned grid = (unsigned)std::min<int64_t>((x.rows * x.workers + slots - 1) / slots, 256 * 64);
+  hipLaunchKernelGGL(join_tiles_kernel, dim3(grid), dim3(kThreads), 0, s, x, reinterpret_cast<const float2*>(ws + plan.stats),
+                     reinterpret_cast<const float*>(ws + plan.picked), pieces, lanes_log2);
   return hipGetLastError();
 }
 
@@ -113,9 +187,11 @@ hipError_t launch_xent_backward(const XentArgs& x, const XentPlan& plan, char* w
   const int es = bf16 ? 2 : 4;
   for (int k = 0; k < plan.pieces; ++k) {
     const int first = k * plan.piece, n = std::min(plan.piece, x.classes - first);
-    const int64_t w_at = x.classes_first ? first * x.w_row : first, dw_at = x.classes_first ? first * x.dw_row : first;
-    const Operand rows{x.h, x.rows * x.h_row, x.h_row, false}, matrix{(const char*)x.w + w_at * es, x.w_gs, x.w_row, false};
+    const int64_t dw_at = x.classes_first ? first * x.dw_row : first;
     const Operand dz{ws + plan.dz, x.rows * plan.piece, plan.piece, true};
+    Operand rows, matrix;
+    hipError_t e = operands_of_piece(x, plan, ws, bf16, first, n, &rows, &matrix, s);
+    if (e != hipSuccess) return e;
     ProductArgs p{};
     p.groups = x.workers;
     p.labels = x.labels;
@@ -137,8 +213,7 @@ hipError_t launch_xent_backward(const XentArgs& x, const XentPlan& plan, char* w
     p.out_gs = dz.gs;
     p.splits = 1;
     Cut cut;
-    hipError_t e = launch_product(p, PX_DZ, false, !x.classes_first, bf16, &cut, s);
-    if (e != hipSuccess) return e;
+    if ((e = launch_product(p, PX_DZ, false, !x.classes_first, bf16, &cut, s)) != hipSuccess) return e;
     p.parts = reinterpret_cast<float*>(ws + plan.parts);
     p.a = dz;
     p.N = x.width;
@@ -161,27 +236,34 @@ hipError_t launch_xent_backward(const XentArgs& x, const XentPlan& plan, char* w
   return hipSuccess;
 }
 
-XentPlan xent_plan(int workers, int64_t rows, int width, int classes, bool bf16, bool backward) {
+XentPlan xent_plan(int workers, int64_t rows, int width, int classes, bool classes_first, bool bf16, bool backward) {
   XentPlan e{};
-  const size_t n = (size_t)workers * (size_t)rows;
+  const size_t n = (size_t)workers * (size_t)rows, es = bf16 ? 2 : 4;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t v = at; at += (bytes + 255) / 256 * 256; return v; };
+  e.align_h = bf16 && rows >= kAlignRows && width % 8 != 0;
+  e.align_w = bf16 && rows >= kAlignRows && (classes_first ? width : classes) % 8 != 0;
+  const int whole = (classes + 255) / 256;                 // in 256 classes
+  // of a class: what a piece holds of it
+  const size_t held = std::max(backward ? n : 0, e.align_w ? (size_t)workers * eights(width) : 0) * es;
+  const int64_t fit = held == 0 ? whole : std::max<int64_t>((int64_t)(kPieceBytes / (held * 256)), 1);
+  const int pieces = (int)std::min<int64_t>(whole, (whole + fit - 1) / fit);
+  e.piece = (whole + pieces - 1) / pieces * 256;
+  e.pieces = (classes + e.piece - 1) / e.piece;
   if (!backward) {
-    e.stats = take(n * ((classes + kLeastTile - 1) / kLeastTile) * sizeof(float2));
+    if (e.pieces == 1) e.piece = classes;
+    e.stats = take(n * e.pieces * ((e.piece + kLeastTile - 1) / kLeastTile) * sizeof(float2));
     e.picked = take(n * sizeof(float));
   } else {
-    const int whole = (classes + 255) / 256;               // in 256 classes
-    const int64_t fit = std::max<int64_t>((int64_t)(kPieceBytes / (std::max<size_t>(n, 1) * 256 * (bf16 ? 2 : 4))), 1);
-    const int pieces = (int)std::min<int64_t>(whole, (whole + fit - 1) / fit);
-    e.piece = (whole + pieces - 1) / pieces * 256;
-    e.pieces = (classes + e.piece - 1) / e.piece;
-    e.dz = take(n * e.piece * (bf16 ? 2 : 4));
+    e.dz = take(n * e.piece * es);
     e.sums = e.pieces > 1 ? take(n * width * sizeof(float)) : 0;
     const int last = classes - (e.pieces - 1) * e.piece;   // classes of the last piece: of fewer tiles, and so perhaps more parts
     e.parts = take(std::max({parts_bytes(rows, width, e.piece, workers), parts_bytes(width, std::min(e.piece, classes), rows, workers),
                              parts_bytes(width, last, rows, workers)}));
     e.real = take((size_t)workers * real_words(rows) * sizeof(uint32_t));
   }
+  e.h = e.align_h ? take(n * eights(width) * es) : 0;
+  e.w = e.align_w ? take((size_t)workers * eights(width) * eights(std::min(e.piece, classes)) * es) : 0;
   e.total = at;
   return e;
 }

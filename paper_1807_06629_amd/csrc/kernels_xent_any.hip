@@ -1,5 +1,6 @@
 // The cross entropy's products of operands of any alignment and size, in fp32 (products and sums) or bf16 (sums in fp32): tiles pass through registers into
 // LDS, [row][contraction] whichever way they lie in memory and twice, the next one on its way while the matrix cores take the last.
+#include "row_pieces.h"
 #include "xent_products.h"
 
 namespace prsgd {
@@ -7,20 +8,6 @@ namespace prsgd {
 namespace {
 
 template <typename T> using Tag = std::conditional_t<kIsBf16<T>, TBF16, TF32>;
-
-// n elements from p on (0 .. 16 bytes' worth)
-template <typename T> __device__ __forceinline__ u32x4_t load16(const T* p, int n) {
-  constexpr int V = 16 / (int)sizeof(T);
-  u32x4_t v = {0, 0, 0, 0};
-  if (n >= V) return reinterpret_cast<const Packed16<(int)sizeof(T)>*>(p)->v;
-#pragma unroll
-  for (int e = 0; e < V; ++e)
-    if (e < n) {
-      if constexpr (sizeof(T) == 4) v[e] = __float_as_uint(p[e]);
-      else v[e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
-    }
-  return v;
-}
 
 // An operand's tiles, D deep, rows padded by 16 bytes.
 template <typename T, int ROWS, bool TRANS, int D, int THREADS> struct Stage {
@@ -31,8 +18,11 @@ template <typename T, int ROWS, bool TRANS, int D, int THREADS> struct Stage {
   static __device__ __forceinline__ int row_of(int u) { return TRANS ? u % (ROWS / V) * V : u / (D / V); }
   static __device__ __forceinline__ int depth_of(int u) { return TRANS ? u / (ROWS / V) * BK : u % (D / V) * V; }
   u32x4_t reg[NPT][BK];
-  // rows, depth: what is left of the operand from the tile's first element on
-  __device__ __forceinline__ void load(const T* base, int64_t ld, int rows, int depth) {
+  static __device__ __forceinline__ u32x4_t piece(const T* p, int n, const void* first) {
+    return n >= V ? reinterpret_cast<const Packed16<ES>*>(p)->v : load_end<ES>(p, n, first);
+  }
+  // rows, depth: what is left of the operand from the tile's first element on; first: the operand's first
+  __device__ __forceinline__ void load(const T* base, int64_t ld, int rows, int depth, const void* first) {
 #pragma unroll
     for (int q = 0; q < NPT; ++q) {
       const int u = q * THREADS + (int)threadIdx.x, r = row_of(u), c = depth_of(u);
@@ -42,27 +32,29 @@ template <typename T, int ROWS, bool TRANS, int D, int THREADS> struct Stage {
       if constexpr (TRANS) {
 #pragma unroll
         for (int k = 0; k < BK; ++k)
-          if (c + k < depth && r < rows) reg[q][k] = load16(base + (int64_t)(c + k) * ld + r, rows - r);
+          if (c + k < depth && r < rows) reg[q][k] = piece(base + (int64_t)(c + k) * ld + r, rows - r, first);
       } else {
-        if (r < rows && c < depth) reg[q][0] = load16(base + (int64_t)r * ld + c, depth - c);
+        if (r < rows && c < depth) reg[q][0] = piece(base + (int64_t)r * ld + c, depth - c, first);
       }
     }
   }
-  // bits: of the tile's contraction elements those that take part (transposed operands)
-  template <int WORDS> __device__ __forceinline__ void store(unsigned char* tile, const uint32_t (&bits)[WORDS]) const {
+  // rows, depth: as they were loaded; bits: of the tile's contraction elements those that take part (transposed operands)
+  template <int WORDS> __device__ __forceinline__ void store(unsigned char* tile, int rows, int depth, const uint32_t (&bits)[WORDS]) {
 #pragma unroll
     for (int q = 0; q < NPT; ++q) {
       const int u = q * THREADS + (int)threadIdx.x, r = row_of(u), c = depth_of(u);
       if (UNITS % THREADS != 0 && u >= UNITS) continue;
+      const int n = TRANS ? rows - r : depth - c;
+      if (n > 0 && n < V) {
+#pragma unroll
+        for (int k = 0; k < BK; ++k) reg[q][k] = place_end<ES>(reg[q][k], n);
+      }
       if constexpr (TRANS) {
         u32x4_t v[BK];
-        uint32_t part = ~0u;
-        if constexpr (WORDS > 0) {
-          part = bits[0];
+        uint32_t part = bits[0];
 #pragma unroll
-          for (int w = 1; w < WORDS; ++w) part = c / 32 == w ? bits[w] : part;
-          part >>= c % 32;
-        }
+        for (int w = 1; w < WORDS; ++w) part = c / 32 == w ? bits[w] : part;
+        if constexpr (WORDS > 1 || D == 32) part >>= c % 32;
 #pragma unroll
         for (int k = 0; k < BK; ++k)
 #pragma unroll
@@ -121,30 +113,25 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(ProductArgs 
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
   A ra;
   B rb;
-  uint32_t bits[WORDS > 0 ? WORDS : 1];
+  uint32_t bits[WORDS > 0 ? WORDS : 1] = {~0u};
   const int n_k = (depth + D - 1) / D;
   auto load = [&](int t) __attribute__((always_inline)) {
-    ra.load(a + t * step_a, p.a.ld, p.M - m0, depth - t * D);
-    rb.load(b + t * step_b, p.b.ld, p.N - n0, depth - t * D);
+    ra.load(a + t * step_a, p.a.ld, p.M - m0, depth - t * D, p.a.p);
+    rb.load(b + t * step_b, p.b.ld, p.N - n0, depth - t * D, p.b.p);
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) {
       const int at_word = (k0 + t * D) / 32 + w;
       bits[w] = at_word < real_words(p.rows) ? real[at_word] : 0;
     }
   };
-  auto store = [&](unsigned char* stage) __attribute__((always_inline)) {
-    if constexpr (WORDS > 0) {
-      ra.store(stage, bits);
-      rb.store(stage + A::BYTES, bits);
-    } else {
-      const uint32_t all[1] = {~0u};
-      ra.store(stage, all);
-      rb.store(stage + A::BYTES, all);
-    }
+  auto store = [&](int t) __attribute__((always_inline)) {
+    unsigned char* stage = smem + (t & 1) * STAGE;
+    ra.store(stage, p.M - m0, depth - t * D, bits);
+    rb.store(stage + A::BYTES, p.N - n0, depth - t * D, bits);
   };
   if (n_k > 0) {
     load(0);
-    store(smem);
+    store(0);
   }
   __syncthreads();
   for (int t = 0; t < n_k; ++t) {
@@ -163,7 +150,7 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(ProductArgs 
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = mma(fa[i], fb[j], acc[i][j]);
     }
-    if (t + 1 < n_k) store(smem + ((t + 1) & 1) * STAGE);
+    if (t + 1 < n_k) store(t + 1);
     __syncthreads();
   }
   if constexpr (WK > 1) {
@@ -200,8 +187,16 @@ template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bo
   return hipGetLastError();
 }
 template <typename T, bool TA, bool TB, int EPI> hipError_t launch_size(const ProductArgs& p, Cut* cut, hipStream_t s) {
-  if (tiles_of(p, 128) >= 192) return launch_tile<T, 128, 128, 2, 2, 1, 32, TA, TB, EPI>(p, cut, s);
-  return launch_tile<T, 32, 32, 1, 1, 4, 128, TA, TB, EPI>(p, cut, s);
+  constexpr int M128 = sizeof(T) == 4 && EPI != PX_DW ? 4 : 2;
+  const int64_t huge = tiles_of(p, 128), large = tiles_of(p, 64);
+  if (tiles_of(p, 32) >= 512 && (p.M <= 32 || p.N <= 32)) {
+    if (p.K <= 64) return p.N <= 32 ? launch_tile<T, 128, 32, 4, 1, 1, 32, TA, TB, EPI>(p, cut, s) : launch_tile<T, 32, 128, 1, 4, 1, 32, TA, TB, EPI>(p, cut, s);
+    return p.N <= 32 ? launch_tile<T, 64, 32, 2, 1, 2, 64, TA, TB, EPI>(p, cut, s) : launch_tile<T, 32, 64, 1, 2, 2, 64, TA, TB, EPI>(p, cut, s);
+  }
+  if (huge >= 256 && huge * 16 <= large * 5) return launch_tile<T, 128, 128, M128, 2, 1, 32, TA, TB, EPI>(p, cut, s);
+  if (large < 256) return launch_tile<T, 32, 32, 1, 1, 4, 128, TA, TB, EPI>(p, cut, s);
+  if (p.K <= 64) return launch_tile<T, 64, 64, 2, 2, 1, 32, TA, TB, EPI>(p, cut, s);
+  return launch_tile<T, 64, 64, 2, 2, 1, 64, TA, TB, EPI>(p, cut, s);
 }
 template <typename T> hipError_t launch(const ProductArgs& p, int epi, bool ta, bool tb, Cut* cut, hipStream_t s) {
   switch (epi) {

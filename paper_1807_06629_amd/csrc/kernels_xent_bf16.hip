@@ -225,9 +225,8 @@ bool operand_aligned(const Operand& o, int64_t contiguous, int64_t other, int gr
 
 }  // namespace
 
-// dz has rows of a multiple of eight with zeros behind the last class, so that classes may end anywhere.
 bool product_aligned(const ProductArgs& p, bool a_transposed, bool b_transposed) {
-  auto whole = [](const Operand& o, int n) { return o.dz ? (n + 7) / 8 * 8 : n; };
+  auto whole = [](const Operand& o, int n) { return o.padded ? (n + 7) / 8 * 8 : n; };
   return operand_aligned(p.a, whole(p.a, a_transposed ? p.M : p.K), a_transposed ? p.K : p.M, p.groups) &&
          operand_aligned(p.b, whole(p.b, b_transposed ? p.N : p.K), b_transposed ? p.K : p.N, p.groups);
 }

@@ -134,7 +134,7 @@ XentArgs xent_args(const prsgd_xent_config* c) {
   return p;
 }
 XentPlan plan_of(const prsgd_xent_config* c, bool backward) {
-  return xent_plan(c->workers, c->rows_per_worker, c->width, c->classes, c->dtype == PRSGD_BF16, backward);
+  return xent_plan(c->workers, c->rows_per_worker, c->width, c->classes, c->classes_first != 0, c->dtype == PRSGD_BF16, backward);
 }
 size_t xent_bytes(const prsgd_xent_config* c, bool backward) {
   if (const char* e = xent_error(c)) {

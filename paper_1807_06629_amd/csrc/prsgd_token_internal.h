@@ -95,10 +95,11 @@ struct XentArgs {
   bool classes_first;
 };
 struct XentPlan {
-  int piece, pieces;                     // backward: classes of a piece
-  size_t stats, picked, dz, sums, parts, real, total;       // byte offsets
+  int piece, pieces;                     // classes of a piece
+  bool align_h, align_w;                 // h, a piece of W: copied, each row to a multiple of 16 bytes
+  size_t stats, picked, dz, sums, parts, real, h, w, total;         // byte offsets
 };
-XentPlan xent_plan(int workers, int64_t rows, int width, int classes, bool bf16, bool backward);
+XentPlan xent_plan(int workers, int64_t rows, int width, int classes, bool classes_first, bool bf16, bool backward);
 hipError_t launch_xent(const XentArgs& p, const XentPlan& plan, char* ws, bool bf16, hipStream_t s);
 hipError_t launch_xent_backward(const XentArgs& p, const XentPlan& plan, char* ws, bool bf16, hipStream_t s);
 

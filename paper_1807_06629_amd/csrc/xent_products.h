@@ -19,12 +19,13 @@
 namespace prsgd {
 
 // One matrix of every worker: element (i, c), c the contraction index, at p + g * gs + i * ld + c, or (transposed) + c * ld + i.
-struct Operand { const void* p; int64_t gs, ld; bool dz; };
+// padded: rows as they lie in memory go on with zeros up to a multiple of eight.
+struct Operand { const void* p; int64_t gs, ld; bool padded; };
 struct ProductArgs {
   Operand a, b;
   int M, N, K;                           // rows of A, rows of B, contraction
   int groups;
-  int splits; float* parts;              // wished for: parts of the contraction, each to its own fp32 [groups][M][N] of `parts` (1: none)
+  int splits; float* parts;              // wished for: parts of the contraction, each to its own fp32 [groups][M][parts_row(N)] of `parts` (1: none)
   int tiles_m, tiles_n, split_steps;     // filled in by the launcher: tiles, and steps of the contraction in a part
   // of the rows, `rows` in every worker
   const int32_t* labels;
@@ -40,6 +41,7 @@ struct ProductArgs {
 enum ProductEpilogue { PX_STATS = 0, PX_DZ = 1, PX_DH = 2, PX_DW = 3 };
 
 template <typename T> constexpr bool kIsBf16 = std::is_same_v<T, uint16_t>;
+__host__ __device__ constexpr int64_t parts_row(int64_t n) { return (n + 7) / 8 * 8; }
 __host__ __device__ constexpr int64_t real_words(int64_t rows) { return (rows + 63) / 64 * 2; }
 
 // exp of what is at most about zero.  bf16: on the hardware's base 2, which leaves |x| 2^-24 of the result, at most 2^-24 of the largest term.
@@ -122,7 +124,7 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& p, const f32
           if (c < p.M) {
             m = fmaxf(m, acc[i][j][e]);
             odd = odd || !(acc[i][j][e] <= INFINITY);          // fmaxf passes over what is no number
-            if (c == label) p.picked[g * p.rows + row] = acc[i][j][e];
+            if (p.class0 + c == label) p.picked[g * p.rows + row] = acc[i][j][e];
           }
         }
       const float top = m == -INFINITY ? 0.0f : m;
@@ -181,7 +183,7 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& p, const f32
           if (live && c < p.out_ld) store8(reinterpret_cast<T*>(p.out) + g * p.out_gs + (int64_t)r * p.out_ld + c, 8, v);
         } else {
           if (!live || n <= 0) continue;
-          if (p.splits > 1) store8(p.parts + (((int64_t)at.split * p.groups + g) * p.M + r) * p.N + c, n, v);
+          if (p.splits > 1) store8(p.parts + (((int64_t)at.split * p.groups + g) * p.M + r) * parts_row(p.N) + c, 8, v);
           else finish<T, EPI>(p, g, r, c, n, v);
         }
       }

@@ -127,6 +127,21 @@ def test_several_pieces_of_the_classes(P, dtype, first):
     _check_backward(P, _rand(9, rows), h, w, labels, lse, first)
 
 
+@pytest.mark.parametrize("first", [False, True])
+@pytest.mark.parametrize("workers,rows,width,classes", [(2, 191, 33, 1001), (2, 192, 33, 1001), (3, 300, 250, 129), (2, 200, 264, 7), (1, 230, 1023, 515), (300, 192, 1001, 515)])
+def test_rows_of_no_whole_eights(P, workers, rows, width, classes, first):
+    """bf16 that is copied for its products; the last case in several pieces of the classes, forward too."""
+    _check(P, workers, rows, width, classes, BF16, first)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("first", [False, True])
+@pytest.mark.parametrize("rows,width,classes", [(2, 18, 15255), (1, 3, 9001), (3330, 9, 30), (700, 5, 3), (33, 4001, 2), (4100, 20, 33), (20, 51, 9000)])
+def test_few_tiles_and_long_sums(P, rows, width, classes, dtype, first):
+    _check(P, 1, rows, width, classes, dtype, first)
+    _check(P, 3, rows, width, classes, dtype, first)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("first", [False, True])
 def test_strides_that_are_multiples_of_nothing(P, dtype, first):
