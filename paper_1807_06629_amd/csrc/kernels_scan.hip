@@ -4,11 +4,14 @@
 //   dv_t = (1 - f_t) g_t,  dgate_t = f_t (1 - f_t) (h_{t-1} - v_t) g_t,  dinitial = c of the first row
 // Both are x -> a x + b along a sequence, the second one from its end.  A workgroup has 64 channels of one sequence and walks along it: every lane
 // holds R rows of eight channels, composes them, and lanes, then wavefronts, compose theirs, so that a pass over NW * 8 * R rows reads
-// each of them once and needs no workgroup to wait for another.  States and compositions are fp32.
+// each of them once and needs no workgroup to wait for another.  States and compositions are fp32.  Bound by HBM where sequences are many (64 packed ones, 65536 x 2048
+// bf16: 189 us, 4.3 TB/s; gradients 351 us, 4.6 TB/s), by the 2 us of a pass where they are few.
 #include <algorithm>
+#include <cmath>
 
 #include "orth_rows.h"
 #include "prsgd_token_internal.h"
+#include "row_pieces.h"
 
 namespace prsgd {
 
@@ -44,12 +47,22 @@ __device__ __forceinline__ Span span_of(const ScanArgs& p, int s) {
   return {first, min(max(p.starts[s + 1], first), (int)p.rows)};
 }
 
-// Zeros in the rows that no sequence has, by workgroups behind those of the sequences.
+// Zeros in the rows that no sequence has, and (where rows are cut into parts) the states that pass sequences without rows, by workgroups behind the others.
+enum ScanMode { WHOLE = 0, COMPOSE = 1, APPLY = 2 };
 constexpr int kClearers = 64;
-template <typename T> __device__ __forceinline__ void clear_rest(const ScanArgs& p, int block) {
+template <typename T, bool BACK, int MODE> __device__ __forceinline__ void clear_rest(const ScanArgs& p, int block) {
+  if constexpr (MODE == APPLY) {
+    const float* from = BACK ? p.dlast : p.initial;
+    const int64_t from_row = BACK ? p.dlast_row : p.initial_row;
+    for (int s = block; s < p.sequences && p.last != nullptr; s += kClearers) {
+      const Span q = span_of(p, s);
+      if (q.end > q.first) continue;
+      for (int c = threadIdx.x; c < p.width; c += blockDim.x) p.last[s * p.last_row + c] = from != nullptr ? from[s * from_row + c] : 0.0f;
+    }
+  }
   const int first = min(max(p.starts[0], 0), (int)p.rows), end = min(max(p.starts[p.sequences], first), (int)p.rows);
   const float none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  for (int i = block; i < first + ((int)p.rows - end); i += kClearers) {
+  for (int i = block; i < first + ((int)p.rows - end) && p.clear != 0; i += kClearers) {
     const int64_t row = i < first ? i : end + (i - first);
     for (int c = threadIdx.x * 8; c < p.width; c += blockDim.x * 8) {
       if ((p.clear & 1) != 0) store8(reinterpret_cast<T*>(p.h) + row * p.h_row + c, p.width - c, none);
@@ -64,21 +77,22 @@ template <typename T> __device__ __forceinline__ float raw_at(const Raw<T>& v, i
   if constexpr (sizeof(T) == 4) return __uint_as_float(v.q[e / 4][e % 4]);
   else return __uint_as_float((e & 1) != 0 ? v.q[0][e / 2] & 0xFFFF0000u : v.q[0][e / 2] << 16);
 }
-// VEC: rows are whole eights, so that no lane has a part of one
-template <typename T, bool VEC> __device__ __forceinline__ void raw_load(Raw<T>& v, const T* p, int n) {
-  if (VEC || n >= 8) {
+// VEC: rows are whole eights, so that no lane has a part of one.  Otherwise such a part comes with what lies before it (its rows begin at `first`), and is moved
+// into place when it is used.
+template <typename T, bool VEC> __device__ __forceinline__ void raw_load(Raw<T>& v, const T* p, int n, const void* first) {
+  constexpr int ES = (int)sizeof(T), V = 16 / ES;
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) v.q[i] = reinterpret_cast<const Packed16<(int)sizeof(T)>*>(p + i * (16 / (int)sizeof(T)))->v;
-  } else {
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) v.q[i] = (u32x4_t){0, 0, 0, 0};
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < n) {
-        if constexpr (sizeof(T) == 4) v.q[e / 4][e % 4] = __float_as_uint(p[e]);
-        else v.q[0][e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
-      }
+  for (int i = 0; i < 8 / V; ++i) {
+    if (VEC || n >= (i + 1) * V) v.q[i] = reinterpret_cast<const Packed16<ES>*>(p + i * V)->v;
+    else if (n > i * V) v.q[i] = load_end<ES>(p + i * V, n - i * V, first);
+    else v.q[i] = (u32x4_t){0, 0, 0, 0};
   }
+}
+template <typename T> __device__ __forceinline__ void raw_place(Raw<T>& v, int n) {
+  constexpr int ES = (int)sizeof(T), V = 16 / ES;
+#pragma unroll
+  for (int i = 0; i < 8 / V; ++i)
+    if (n > i * V && n < (i + 1) * V) v.q[i] = place_end<ES>(v.q[i], n - i * V);
 }
 
 // Workgroups take packed sequences longest first, where these are few enough to be compared by each of them, so that the longest is not the last to start.
@@ -100,47 +114,63 @@ template <int THREADS> __device__ __forceinline__ int nth_longest(const ScanArgs
   return found;
 }
 
-// A long sequence may be cut into parts (p.parts), where there are too few workgroups otherwise: the first launch composes each part's rows, the second
-// (join_parts_kernel) finds the states in front of the parts, the third is the scan with these.
-enum ScanMode { WHOLE = 0, COMPOSE = 1, APPLY = 2 };
+// Where the longest sequence would be walked for longer than all others take, the rows of all sequences are cut into equal parts (p.parts), wherever
+// sequences end: a first launch composes each part's rows, a second composes the parts before its own, which gives the state that comes to it, and scans.
+// A sequence's first row replaces what comes to it by the sequence's state, which a composition x -> a x + b notes as a < 0, so that a NaN before it goes nowhere.
+constexpr int kTableRows = 4 * kPass;    // rows of which a workgroup knows at a time which are the first and the last of a sequence
 __device__ __forceinline__ Span part_of(Span s, int part, int parts) {
-  const int each = ((s.end - s.first + parts - 1) / parts + 63) / 64 * 64, from = min(s.first + part * each, s.end);
-  return {from, min(from + each, s.end)};
+  const int each = ((s.end - s.first + parts - 1) / parts + kPass - 1) / kPass * kPass, from = (int)min(s.first + (int64_t)part * each, (int64_t)s.end);
+  return {from, (int)min(from + (int64_t)each, (int64_t)s.end)};
+}
+template <bool RESETS> __device__ __forceinline__ void compose(float& a, float& b, float2 next) {
+  if constexpr (RESETS) {
+    b = next.x < 0.0f ? next.y : fmaf(next.x, b, next.y);
+    a = a < 0.0f || next.x < 0.0f ? -1.0f : a * next.x;
+  } else {
+    b = fmaf(next.x, b, next.y);
+    a *= next.x;
+  }
 }
 
 // NW wavefronts; CL lanes share a row, R rows a lane.  The next pass's rows are on their way while this one's are composed.
 template <typename T, bool BACK, int NW, int R, int CL, bool VEC, int OCC, int MODE> __global__ void __launch_bounds__(NW * kWave, OCC) scan_kernel(ScanArgs p, int tiles) {
   constexpr int CH = 8 * CL, PARTS = kWave / CL, PASS = NW * PARTS * R;
+  constexpr bool CUT = MODE != WHOLE;
   // compositions of the lanes' rows, then the states in front of them; of a wavefront, which alone reads them
   __shared__ __attribute__((aligned(16))) float composed[NW][PARTS][CH][2];
   __shared__ float total[2][NW][CH][2];
-  const int workgroups = tiles * p.sequences * (MODE == WHOLE ? 1 : p.parts);
+  __shared__ int head[CUT ? kTableRows : 1], tail[CUT ? kTableRows : 1];
+  const int workgroups = tiles * (CUT ? p.parts : p.sequences);
   if (blockIdx.x >= (unsigned)workgroups) {
-    clear_rest<T>(p, (int)(blockIdx.x - workgroups));
+    clear_rest<T, BACK, MODE>(p, (int)(blockIdx.x - workgroups));
     return;
   }
   const int slot = blockIdx.x / tiles, c_wg = (blockIdx.x - slot * tiles) * CH;
-  int sequence = MODE == WHOLE ? slot : slot / p.parts;
-  const int nth = MODE == WHOLE ? 0 : slot - sequence * p.parts;           // part, counted as the scan goes
-  if (MODE == WHOLE && NW > 1 && p.starts != nullptr && p.sequences <= kRanked) sequence = __builtin_amdgcn_readfirstlane(nth_longest<NW * kWave>(p, sequence));
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid % kWave, part = lane / CL, cl = lane % CL * 8;
   const int c = c_wg + cl, n = p.width - c;
-  const Span all = span_of(p, sequence), span = MODE == WHOLE ? all : part_of(all, BACK ? p.parts - 1 - nth : nth, p.parts);
+  int sequence = slot;                   // WHOLE
+  Span all, span;
+  if constexpr (CUT) {
+    all = {span_of(p, 0).first, span_of(p, p.sequences - 1).end};
+    all.end = max(all.end, all.first);
+    span = part_of(all, BACK ? p.parts - 1 - slot : slot, p.parts);
+  } else {
+    if (NW > 1 && p.starts != nullptr && p.sequences <= kRanked) sequence = __builtin_amdgcn_readfirstlane(nth_longest<NW * kWave>(p, sequence));
+    all = span = span_of(p, sequence);
+  }
   const int length = span.end - span.first;
   // of channel c_wg + lane % CH, in every wavefront alike
   const int own = lane % CH;
   const bool owns = c_wg + own < p.width;
-  float2* joint = MODE == WHOLE ? nullptr : p.joint + (int64_t)slot * p.width + c_wg + own;
-  float state = 0.0f;
-  if (owns && MODE == APPLY) state = joint->x;
-  if (owns && MODE == WHOLE) {
+  float2* joint = CUT ? p.joint + c_wg + own : nullptr;    // of the parts: their compositions
+  float state = 0.0f, product = 1.0f;
+  if (!CUT && owns) {
     if (BACK) state = p.dlast != nullptr ? p.dlast[sequence * p.dlast_row + c_wg + own] : 0.0f;
     else state = p.initial != nullptr ? p.initial[sequence * p.initial_row + c_wg + own] : 0.0f;
   }
-  float product = 1.0f;                  // COMPOSE: of all f
   struct Rows { Raw<T> gate, v, dh, h; };
   Rows ahead[R];
-  // Row `at` of this lane, counted from the sequence's end backward, and what lies one row and one pass further on.
+  // Row `at` of this lane, counted from the span's end backward, and what lies one row and one pass further on.
   int at = (wave * PARTS + part) * R, parity = 0;
   constexpr int64_t kOn = BACK ? -1 : 1;
   const int64_t row0 = BACK ? (int64_t)span.end - 1 - at : (int64_t)span.first + at;
@@ -154,11 +184,11 @@ template <typename T, bool BACK, int NW, int R, int CL, bool VEC, int OCC, int M
 #pragma unroll
     for (int j = 0; j < R; ++j)
       if (from + j < length && n > 0) {
-        raw_load<T, VEC>(ahead[j].gate, gate_at + j * kOn * p.gate_row, n);
-        if constexpr (!BACK || MODE != COMPOSE) raw_load<T, VEC>(ahead[j].v, v_at + j * kOn * p.v_row, n);
-        if constexpr (BACK) raw_load<T, VEC>(ahead[j].dh, dh_at + j * kOn * p.dh_row, n);
+        raw_load<T, VEC>(ahead[j].gate, gate_at + j * kOn * p.gate_row, n, p.gate);
+        if constexpr (!BACK || MODE != COMPOSE) raw_load<T, VEC>(ahead[j].v, v_at + j * kOn * p.v_row, n, p.v);
+        if constexpr (BACK) raw_load<T, VEC>(ahead[j].dh, dh_at + j * kOn * p.dh_row, n, p.dh);
         if constexpr (BACK && MODE != COMPOSE) {
-          if (from + j < length - 1 || span.first > all.first) raw_load<T, VEC>(ahead[j].h, h_at + j * kOn * p.h_in_row, n);
+          if (from + j < length - 1 || span.first > all.first) raw_load<T, VEC>(ahead[j].h, h_at + j * kOn * p.h_in_row, n, p.h_in);
         }
       } else {
         // past the end a gate that is open, and nothing else: such a row leaves what comes to it as it is
@@ -176,10 +206,53 @@ template <typename T, bool BACK, int NW, int R, int CL, bool VEC, int OCC, int M
       h_at += PASS * kOn * p.h_in_row;
     }
   };
+  // CUT: the state of sequence s that comes to its first row; kept aside by the first launch, as the second one may write `last` over it
+  auto entering = [&](int s, float (&v)[8]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+    const float* from = BACK ? p.dlast : p.initial;
+    if (from == nullptr || n <= 0) return;
+    float* aside = p.aside + (int64_t)s * p.width + c;
+    if constexpr (MODE == COMPOSE) {
+      load8(from + s * (BACK ? p.dlast_row : p.initial_row) + c, n, v);
+      store8(aside, n, v);
+    } else {
+      load8(aside, n, v);
+    }
+  };
   request(at);
+  if constexpr (MODE == APPLY) {
+    // the parts before this one: a wavefront composes its share of them, then each those of all
+    const int each = (slot + NW - 1) / NW, q1 = min(slot, (wave + 1) * each);
+    float a = 1.0f, b = 0.0f;
+    if (owns) {
+#pragma unroll 8
+      for (int q = wave * each; q < q1; ++q) compose<true>(a, b, joint[(int64_t)q * p.width]);
+    }
+    if (lane < CH) *reinterpret_cast<float2*>(&total[1][wave][own][0]) = make_float2(a, b);
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < NW; ++q) compose<true>(product, state, *reinterpret_cast<const float2*>(&total[1][q][own][0]));
+  }
   for (int base = 0; base < length; base += PASS, at += PASS, parity ^= 1) {
+    if constexpr (CUT) {
+      if (base % kTableRows == 0) {
+        __syncthreads();
+        for (int i = tid; i < kTableRows; i += NW * kWave) head[i] = tail[i] = -1;
+        __syncthreads();
+        for (int i = tid; i < p.sequences; i += NW * kWave) {
+          const Span q = span_of(p, i);
+          if (q.end <= q.first) continue;
+          const int from = (BACK ? span.end - q.end : q.first - span.first) - base, to = (BACK ? span.end - 1 - q.first : q.end - 1 - span.first) - base;
+          if ((unsigned)from < (unsigned)kTableRows) head[from] = i;
+          if ((unsigned)to < (unsigned)kTableRows) tail[to] = i;
+        }
+        __syncthreads();
+      }
+    }
     // forward: u = (1 - f) v; backward: u = dh, w = (1 - f) (h_{t-1} - v)
     float f[R][8], u[R][8], rest[BACK ? R : 1][8], w[BACK ? R : 1][8], a[8], b[8];
+    int first_of[R], last_of[R];         // CUT: the sequence whose first row, as the scan goes, this is, and whose last row
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       a[e] = 1.0f;
@@ -187,14 +260,31 @@ template <typename T, bool BACK, int NW, int R, int CL, bool VEC, int OCC, int M
     }
 #pragma unroll
     for (int j = 0; j < R; ++j) {
+      if constexpr (CUT) {
+        const bool row = at + j < length;
+        first_of[j] = row ? head[(at + j) % kTableRows] : -1;
+        last_of[j] = row ? tail[(at + j) % kTableRows] : -1;
+        if (first_of[j] >= 0) {
+          entering(first_of[j], b);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) a[e] = -1.0f;
+        }
+      }
+      if constexpr (!VEC) {
+        raw_place<T>(ahead[j].gate, n);
+        if constexpr (!BACK || MODE != COMPOSE) raw_place<T>(ahead[j].v, n);
+        if constexpr (BACK) raw_place<T>(ahead[j].dh, n);
+        if constexpr (BACK && MODE != COMPOSE) raw_place<T>(ahead[j].h, n);
+      }
       float past[8];
       if constexpr (BACK && MODE != COMPOSE) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) past[e] = raw_at<T>(ahead[j].h, e);
-        if (at + j == length - 1 && span.first == all.first) {           // the first row
+        const int s = CUT ? last_of[j] : at + j == length - 1 ? sequence : -1;
+        if (s >= 0) {                                      // the sequence's first row
 #pragma unroll
           for (int e = 0; e < 8; ++e) past[e] = 0.0f;
-          if (p.initial != nullptr && n > 0) load8(p.initial + sequence * p.initial_row + c, n, past);
+          if (p.initial != nullptr && n > 0) load8(p.initial + s * p.initial_row + c, n, past);
         }
       }
 #pragma unroll
@@ -212,7 +302,7 @@ template <typename T, bool BACK, int NW, int R, int CL, bool VEC, int OCC, int M
           u[j][e] = r * raw_at<T>(ahead[j].v, e);
           b[e] = fmaf(f[j][e], b[e], u[j][e]);
         }
-        a[e] *= f[j][e];
+        a[e] = CUT && a[e] < 0.0f ? -1.0f : a[e] * f[j][e];
       }
     }
     request(at + PASS);
@@ -224,27 +314,27 @@ template <typename T, bool BACK, int NW, int R, int CL, bool VEC, int OCC, int M
     float before_a[PARTS], before_b[PARTS], sum_a = 1.0f, sum_b = 0.0f;
 #pragma unroll
     for (int q = 0; q < PARTS; ++q) {
-      const float2 x = *reinterpret_cast<const float2*>(&composed[wave][q][own][0]);
       before_a[q] = sum_a;
       before_b[q] = sum_b;
-      sum_b = fmaf(x.x, sum_b, x.y);
-      sum_a *= x.x;
+      compose<CUT>(sum_a, sum_b, *reinterpret_cast<const float2*>(&composed[wave][q][own][0]));
     }
     if (lane < CH) *reinterpret_cast<float2*>(&total[parity][wave][own][0]) = make_float2(sum_a, sum_b);
     __syncthreads();
     float mine = state;
 #pragma unroll
     for (int q = 0; q < NW; ++q) {
-      const float2 x = *reinterpret_cast<const float2*>(&total[parity][q][own][0]);
       mine = q == wave ? state : mine;
-      state = fmaf(x.x, state, x.y);
-      if (MODE == COMPOSE) product *= x.x;
+      compose<CUT>(product, state, *reinterpret_cast<const float2*>(&total[parity][q][own][0]));
     }
     if constexpr (MODE == COMPOSE) continue;
     float* states = &composed[wave][0][0][0];              // [PARTS][CH]
     if (lane < CH) {
 #pragma unroll
-      for (int q = 0; q < PARTS; ++q) states[q * CH + own] = fmaf(before_a[q], mine, before_b[q]);
+      for (int q = 0; q < PARTS; ++q) {
+        float none = 1.0f, x = mine;
+        compose<CUT>(none, x, make_float2(before_a[q], before_b[q]));
+        states[q * CH + own] = x;
+      }
     }
     __builtin_amdgcn_wave_barrier();
     float h[8];
@@ -259,6 +349,9 @@ template <typename T, bool BACK, int NW, int R, int CL, bool VEC, int OCC, int M
 #pragma unroll
     for (int j = 0; j < R; ++j)
       if (at + j < length && n > 0) {
+        if constexpr (CUT) {
+          if (first_of[j] >= 0) entering(first_of[j], h);
+        }
         if constexpr (BACK) {
           float dv[8], dgate[8];
 #pragma unroll
@@ -275,31 +368,18 @@ template <typename T, bool BACK, int NW, int R, int CL, bool VEC, int OCC, int M
           for (int e = 0; e < 8; ++e) h[e] = fmaf(f[j][e], h[e], u[j][e]);
           store8(out_at + j * kOn * p.h_row, VEC ? 8 : n, h);
         }
+        if constexpr (CUT) {
+          if (last_of[j] >= 0 && p.last != nullptr) store8(p.last + last_of[j] * p.last_row + c, n, h);
+        }
       }
     out_at += PASS * kOn * p.h_row;
     if constexpr (BACK) dgate_at += PASS * kOn * p.dgate_row;
     __builtin_amdgcn_wave_barrier();
   }
   if (wave == 0 && lane < CH && owns) {
-    if (MODE == COMPOSE) *joint = make_float2(product, state);
+    if (MODE == COMPOSE) joint[(int64_t)slot * p.width] = make_float2(product, state);
     if (MODE == WHOLE && p.last != nullptr) p.last[sequence * p.last_row + c_wg + own] = state;
   }
-}
-
-// The state in front of every part, in the place of the part's composition.
-template <bool BACK> __global__ void __launch_bounds__(kThreads) join_parts_kernel(ScanArgs p) {
-  const int channels = (p.width + kThreads - 1) / kThreads, sequence = blockIdx.x / channels, c = (blockIdx.x - sequence * channels) * kThreads + threadIdx.x;
-  if (c >= p.width) return;
-  const float* from = BACK ? p.dlast : p.initial;
-  float state = from != nullptr ? from[sequence * (BACK ? p.dlast_row : p.initial_row) + c] : 0.0f;
-  float2* joint = p.joint + (int64_t)sequence * p.parts * p.width + c;
-#pragma unroll 8
-  for (int q = 0; q < p.parts; ++q, joint += p.width) {
-    const float2 x = *joint;
-    joint->x = state;
-    state = fmaf(x.x, state, x.y);
-  }
-  if (p.last != nullptr) p.last[sequence * p.last_row + c] = state;
 }
 
 // Sequences of one row: a token of each.
@@ -335,23 +415,24 @@ template <typename T, bool BACK> __global__ void __launch_bounds__(kThreads) sca
     }
 }
 
-template <typename T, bool BACK, int NW, bool VEC, int MODE> hipError_t launch_scan(const ScanArgs& p, hipStream_t s) {
-  constexpr int OCC = BACK ? 2 : 4;
-  const int tiles = (p.width + kTile - 1) / kTile;
-  const unsigned grid = (unsigned)tiles * (unsigned)p.sequences * (MODE == WHOLE ? 1u : (unsigned)p.parts) +
-                        (MODE != COMPOSE && p.starts != nullptr && p.clear != 0 ? kClearers : 0);
-  hipLaunchKernelGGL((scan_kernel<T, BACK, NW, 2, kTile / 8, VEC, OCC, MODE>), dim3(grid), dim3(NW * kWave), 0, s, p, tiles);
+template <typename T, bool BACK, int NW, bool VEC, int MODE, int R = 2, int CL = kTile / 8> hipError_t launch_scan(const ScanArgs& p, hipStream_t s) {
+  constexpr int OCC = BACK || R > 2 ? 2 : 4;
+  const int tiles = (p.width + 8 * CL - 1) / (8 * CL);
+  const unsigned others = MODE != COMPOSE && p.starts != nullptr && (p.clear != 0 || MODE == APPLY) ? kClearers : 0;
+  const unsigned grid = (unsigned)tiles * (unsigned)(MODE == WHOLE ? p.sequences : p.parts) + others;
+  hipLaunchKernelGGL((scan_kernel<T, BACK, NW, R, CL, VEC, OCC, MODE>), dim3(grid), dim3(NW * kWave), 0, s, p, tiles);
   return hipGetLastError();
 }
 template <typename T, bool BACK, bool VEC> hipError_t launch_passes(const ScanArgs& p, hipStream_t s) {
   if (p.parts > 1) {
-    hipError_t e = launch_scan<T, BACK, kWaves, VEC, COMPOSE>(p, s);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(join_parts_kernel<BACK>, dim3((unsigned)p.sequences * (unsigned)((p.width + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, p);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    return launch_scan<T, BACK, kWaves, VEC, APPLY>(p, s);
+    const hipError_t e = launch_scan<T, BACK, kWaves, VEC, COMPOSE>(p, s);
+    return e != hipSuccess ? e : launch_scan<T, BACK, kWaves, VEC, APPLY>(p, s);
   }
   if (p.rows / p.sequences <= 16) return launch_scan<T, BACK, 1, VEC, WHOLE>(p, s);
+  if constexpr (!BACK) {
+    // too few workgroups for the card, and long walks: half the channels and twice the rows in hand; 4 sequences of 16384 rows x 2048 bf16 330 -> 248 us, but 64 of 1024 216 -> 318 us
+    if ((int64_t)((p.width + kTile - 1) / kTile) * p.sequences <= 128 && p.rows / p.sequences >= 2048) return launch_scan<T, BACK, kWaves, VEC, WHOLE, 4, 4>(p, s);
+  }
   return launch_scan<T, BACK, kWaves, VEC, WHOLE>(p, s);
 }
 
@@ -368,10 +449,18 @@ template <typename T, bool BACK> hipError_t launch(const ScanArgs& p, hipStream_
 
 }  // namespace
 
-int scan_parts(int sequences, int64_t rows, int width) {
-  const int64_t workgroups = (int64_t)sequences * ((width + kTile - 1) / kTile), passes = rows / sequences / kPass;
-  if (workgroups > 64 || passes < 8) return 1;
-  return (int)std::min<int64_t>(std::min<int64_t>(512 / workgroups, 64), passes / 2);
+// Parts by what the two ways take, in microseconds: a pass of a workgroup 2, HBM 5.2 TB/s for the rows (and once more for what is composed), a launch more 8.  The
+// longest of n packed sequences that are cut at random has 1 + ln n times the rows of the average.
+int scan_parts(int sequences, int64_t rows, int width, int element_bytes, bool packed, bool backward) {
+  constexpr double kPassTime = 2.0, kLaunch = 8.0, kRate = 5.2e6;
+  if (sequences > 4096) return 1;        // a workgroup looks at all of them
+  const double tiles = (width + kTile - 1) / kTile, bytes = (double)rows * width * element_bytes;
+  const double longest = std::min((double)rows, (double)rows / sequences * (packed ? 1.0 + std::log((double)sequences) : 1.0));
+  const double whole = std::max(longest / kPass * kPassTime, (backward ? 6 : 3) * bytes / kRate);
+  const int64_t parts = std::min<int64_t>(std::max<int64_t>((int64_t)(512 / tiles), 1), (rows + kPass - 1) / kPass);
+  const double passes = std::ceil((double)rows / (double)parts / kPass);
+  const double cut = kLaunch + std::max(2.0 * passes * kPassTime, (backward ? 8 : 5) * bytes / kRate);
+  return parts > 1 && cut < whole ? (int)parts : 1;
 }
 
 hipError_t launch_gated_scan(const ScanArgs& p, bool bf16, bool backward, hipStream_t s) {

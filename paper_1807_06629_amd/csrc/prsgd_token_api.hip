@@ -76,9 +76,21 @@ const char* scan_error(const prsgd_scan_config* c, const int32_t* starts, int cl
   if (misaligned(starts, 4)) return "gated_scan: misaligned buffer";
   return nullptr;
 }
+int parts_of(const prsgd_scan_config* c, const int32_t* starts, bool backward) {
+  return scan_parts(c->sequences, c->rows, c->width, element_bytes(c->dtype), starts != nullptr, backward);
+}
+size_t joint_bytes(const prsgd_scan_config* c, int parts) { return ((size_t)parts * c->width * sizeof(float2) + 255) / 256 * 256; }
 size_t scan_bytes(const prsgd_scan_config* c) {
-  const int parts = scan_parts(c->sequences, c->rows, c->width);
-  return parts > 1 ? (size_t)c->sequences * parts * c->width * sizeof(float2) : 0;
+  // of any of the calls that the configuration allows
+  int most = 1;
+  for (int k = 0; k < 4; ++k) most = std::max(most, scan_parts(c->sequences, c->rows, c->width, element_bytes(c->dtype), (k & 1) != 0, (k & 2) != 0));
+  return most > 1 ? joint_bytes(c, most) + (size_t)c->sequences * c->width * sizeof(float) : 0;
+}
+void set_parts(ScanArgs& p, const prsgd_scan_config* c, bool backward, void* workspace) {
+  p.parts = parts_of(c, p.starts, backward);
+  if (p.parts <= 1) return;
+  p.joint = reinterpret_cast<float2*>(workspace);
+  p.aside = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + joint_bytes(c, p.parts));
 }
 struct ScanBuffer { const void* at; int64_t row; bool output, needed; };
 // Rows in the sequences' type and states in fp32: present, aligned, distances, and outputs nowhere else.
@@ -233,10 +245,9 @@ int prsgd_gated_scan(const prsgd_scan_config* cfg, const int32_t* starts_dev, co
   p.last_row = last_row;
   p.sequences = cfg->sequences;
   p.clear = cfg->clear;
-  p.parts = scan_parts(cfg->sequences, cfg->rows, cfg->width);
-  p.joint = reinterpret_cast<float2*>(workspace_dev);
   p.rows = cfg->rows;
   p.width = cfg->width;
+  set_parts(p, cfg, false, workspace_dev);
   return hip_result(launch_gated_scan(p, cfg->dtype == PRSGD_BF16, false, reinterpret_cast<hipStream_t>(hip_stream)), "gated_scan");
 }
 
@@ -274,10 +285,9 @@ int prsgd_gated_scan_backward(const prsgd_scan_config* cfg, const int32_t* start
   p.last_row = dinitial_row;
   p.sequences = cfg->sequences;
   p.clear = cfg->clear;
-  p.parts = scan_parts(cfg->sequences, cfg->rows, cfg->width);
-  p.joint = reinterpret_cast<float2*>(workspace_dev);
   p.rows = cfg->rows;
   p.width = cfg->width;
+  set_parts(p, cfg, true, workspace_dev);
   return hip_result(launch_gated_scan(p, cfg->dtype == PRSGD_BF16, true, reinterpret_cast<hipStream_t>(hip_stream)), "gated_scan backward");
 }
 

@@ -72,11 +72,12 @@ struct ScanArgs {
   int sequences;
   int64_t rows;
   int width;
-  int parts; float2* joint;
+  int parts; float2* joint; float* aside;
   int clear;                             // 1: h, 2: dgate hold zeros in rows before the first sequence and behind the last
 };
-// Parts that every sequence is cut into (1: none); their compositions and states lie in `joint` [sequences][parts][width].
-int scan_parts(int sequences, int64_t rows, int width);
+// Parts that the rows are cut into (1: they are not); their compositions lie in `joint` [parts][width], the sequences' states at their start in `aside`
+// [sequences][width].
+int scan_parts(int sequences, int64_t rows, int width, int element_bytes, bool packed, bool backward);
 hipError_t launch_gated_scan(const ScanArgs& p, bool bf16, bool backward, hipStream_t s);
 
 // ---- cross entropy of a last layer ---------------------------------------------------------------

@@ -86,6 +86,56 @@ def test_parts_and_any_workspace(P):
         P.prsgd_gated_scan(v, gate, workspace=torch.empty(n - 8, dtype=torch.uint8, device="cuda"))
 
 
+def _many_cuts(rows, sequences, seed):
+    """Sequences of any length, empty ones, ones of a row and ones that end where tables of 512 rows and parts do."""
+    cuts = torch.randint(7, rows - 9, (sequences - 9,), generator=torch.Generator().manual_seed(seed)).tolist()
+    return torch.tensor(sorted(cuts + [7, 7, 8, 512, 513, 1024, 1024 + 7, 1024 + 7, rows - 9, rows - 9]), dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("width,dtype", [(5, F32), (20, BF16), (72, F32), (72, BF16)])
+def test_many_sequences_of_any_length_are_cut_too(P, width, dtype):
+    rows, n = 9000, 30
+    starts = _many_cuts(rows, n, width)
+    assert starts.numel() == n + 1 and P.prsgd_gated_scan_workspace_bytes(torch.empty(rows, width, device="cuda", dtype=dtype), n) > 0
+    _check(P, rows, width, dtype, n, starts, shift=3.0)
+    _check(P, rows, width, dtype, n, starts, states=False, shift=3.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_long_walks_of_few_workgroups(P, dtype):
+    """Wide rows of a long sequence that is not cut (the forward pass has its own shape there)."""
+    rows, width = 2600, 8136
+    assert P.prsgd_gated_scan_workspace_bytes(torch.empty(rows, width, device="cuda", dtype=dtype), 1) == 0
+    _check(P, rows, width, dtype, shift=3.0)
+
+
+def test_parts_keep_sequences_apart_and_states_in_place(P):
+    rows, n, width = 9000, 30, 20
+    starts = _many_cuts(rows, n, 3)
+    v, gate, initial, dlast = _rand(1, rows, width), _rand(2, rows, width) + 2, _rand(3, n, width), _rand(4, n, width)
+    out = torch.full((rows, width), 9.0, device="cuda")
+    h, last = P.prsgd_gated_scan(v, gate, starts=starts, initial=initial, out=out)
+    assert bool((h[:7] == 9).all()) and bool((h[rows - 9:] == 9).all())
+    state = initial.clone()
+    again, s = P.prsgd_gated_scan(v, gate, starts=starts, initial=state, last=state)
+    assert torch.equal(again[7:rows - 9], h[7:rows - 9]) and not again[:7].any() and not again[rows - 9:].any() and torch.equal(s, last)
+    dh = _rand(5, rows, width)
+    a = P.prsgd_gated_scan_backward(dh, v, gate, h, starts=starts, initial=initial, dlast=dlast)
+    b = P.prsgd_gated_scan_backward(dh, v, gate, h, starts=starts, initial=initial, dlast=dlast, dinitial=dlast)
+    assert all(torch.equal(x, y) for x, y in zip(a, b)) and not a[0][:7].any() and not a[1][rows - 9:].any()
+    # what is no number, in one channel of the longest sequence, also where it is its state
+    lengths = (starts[1:] - starts[:-1]).tolist()
+    k = lengths.index(max(lengths))
+    first, end = int(starts[k]), int(starts[k + 1])
+    v[first + 3, 4], initial[k, 6] = float("nan"), float("inf")
+    bad, bad_last = P.prsgd_gated_scan(v, gate, starts=starts, initial=initial, out=out.clone())
+    touched = torch.zeros_like(v, dtype=torch.bool)
+    touched[first + 3:end, 4] = True
+    touched[first:end, 6] = True
+    assert bool(bad[touched].isfinite().logical_not().all()) and torch.equal(bad[~touched], h[~touched])
+    assert torch.equal(bad_last[:k], last[:k]) and torch.equal(bad_last[k + 1:], last[k + 1:])
+
+
 def test_rows_that_no_sequence_has(P):
     rows, width = 50, 20
     starts = torch.tensor([7, 20, 41], dtype=torch.int32, device="cuda")

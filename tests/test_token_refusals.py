@@ -112,10 +112,11 @@ def test_scan_backward_refuses_its_buffers(P, args):
     assert _call(P, "prsgd_gated_scan_backward", _scan(P), args) == P.PRSGD_EINVAL
 
 
-def test_few_long_sequences_need_a_workspace(P):
+def test_long_sequences_need_a_workspace(P):
+    """For what parts of 128 rows at least compose, up to 512 of them, and for the sequences' states."""
     cfg = _scan(P, sequences=1, rows=1 << 15)
     n = P._lib.prsgd_gated_scan_workspace_bytes(ctypes.byref(cfg))
-    assert 0 < n <= 64 * 50 * 8
+    assert 0 < n <= 256 * 50 * 8 + 50 * 4
     assert _call(P, "prsgd_gated_scan", cfg, SCAN) == P.PRSGD_EINVAL and _call(P, "prsgd_gated_scan_backward", cfg, SCAN_BACK) == P.PRSGD_EINVAL
     assert P._lib.prsgd_gated_scan_workspace_bytes(ctypes.byref(_scan(P))) == 0
     assert P._lib.prsgd_gated_scan_workspace_bytes(ctypes.byref(_scan(P, width=0))) == 0 and "width" in P.prsgd_last_error(None)
