@@ -1,13 +1,14 @@
 // Rows of the workers' tables by token, and the tables' gradients by sorted tokens.
 //   y[r] = scale T[token[r]],   dT[v] = scale * sum of dy[r] over the rows r whose token is v
-// Bound by HBM: a lookup moves rows, a gradient reads every row of dy once and writes every row of dT, mostly zeros, once.  So that a row of
-// dT has one writer and its sum one order, tokens are sorted with their rows (equal tokens stay in order): tiles of 2048 in LDS, then each
-// token finds its place by binary search in the other tiles.  Text has a few tokens that are a large share of all: sorted tokens are cut into chunks, a
-// workgroup each, which sum what of a run passes their ends; a row of dT then adds its own rows of dy, or such sums.
+// Bound by HBM: a lookup moves rows, a gradient reads every row of dy once and writes every row of dT, mostly zeros, once (named rows twice: zeros are written
+// beside the sort, which they take much longer than).  So that a row of dT has one writer and its sum one order, tokens are sorted with their rows (equal tokens stay
+// in order): tiles of 2048 in LDS, then each token finds its place by binary search in the other tiles.  Text has a few tokens that are a large share of all: sorted
+// tokens are cut into chunks, whose runs a few lanes sum and write; a run that passes a chunk's end leaves its parts, which another launch adds.
 #include <algorithm>
 
 #include "orth_rows.h"
 #include "prsgd_token_internal.h"
+#include "row_pieces.h"
 
 namespace prsgd {
 
@@ -17,7 +18,7 @@ constexpr int kTileBits = 11;
 static_assert(1 << kTileBits == kSortTile, "place in a tile");
 static_assert((uint64_t)(kMaxClasses + 1) << kTileBits < 0xFFFFFFFFull, "a token and its place in its tile fit 32 bits, with a value to spare");
 constexpr uint32_t kNoKey = 0xFFFFFFFFu;
-constexpr int kLeastChunk = 64;
+constexpr int kLeastChunk = 32;
 
 template <typename T> __global__ void __launch_bounds__(kThreads) embedding_kernel(EmbeddingArgs p, int lanes_log2) {
   const int lanes = 1 << lanes_log2, slots = kThreads >> lanes_log2;
@@ -38,11 +39,33 @@ template <typename T> __global__ void __launch_bounds__(kThreads) embedding_kern
 
 // ---- sorting -----------------------------------------------------------------------------------
 
-// A tile's tokens in order, each above its place in the tile; what is no token is above all that are.  Also clears the runs.
-__global__ void __launch_bounds__(kSortTile / 2) sort_tiles_kernel(EmbeddingArgs p, EmbeddingPlan plan, char* ws) {
+// Zeros in a worker's rows of dT, by `blocks` workgroups.
+template <typename T> __device__ __forceinline__ void clear_table(const EmbeddingArgs& p, int64_t g, int block, int blocks) {
+  T* table = reinterpret_cast<T*>(p.dtable) + g * p.dtable_gs;
+  const bool whole = p.dtable_row == p.width;              // one row
+  const int64_t width = whole ? (int64_t)p.classes * p.width : p.width, rows = whole ? 1 : p.classes, units = (width + 7) / 8;
+  const float none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  const int64_t step = (int64_t)blocks * blockDim.x;
+  if (whole) {
+    for (int64_t i = (int64_t)block * blockDim.x + threadIdx.x; i < units; i += step) store8(table + i * 8, (int)min(width - i * 8, (int64_t)8), none);
+  } else {
+    for (int64_t i = (int64_t)block * blockDim.x + threadIdx.x; i < units * rows; i += step) {
+      const int64_t r = i / units, c = (i - r * units) * 8;
+      store8(table + r * p.dtable_row + c, (int)min(width - c, (int64_t)8), none);
+    }
+  }
+}
+
+// A tile's tokens in order, each above its place in the tile; what is no token is above all that are.  Workgroups behind the tiles' clear dT.
+template <typename T> __global__ void __launch_bounds__(kSortTile / 2) sort_tiles_kernel(EmbeddingArgs p, EmbeddingPlan plan, char* ws) {
   __shared__ uint32_t key[kSortTile];
   const int64_t g = blockIdx.y, first = (int64_t)blockIdx.x * kSortTile;
-  const int n = (int)min((int64_t)kSortTile, p.rows - first), t = threadIdx.x, threads = blockDim.x;
+  const int t = threadIdx.x, threads = blockDim.x;
+  if ((int)blockIdx.x >= plan.tiles) {
+    clear_table<T>(p, g, blockIdx.x - plan.tiles, gridDim.x - plan.tiles);
+    return;
+  }
+  const int n = (int)min((int64_t)kSortTile, p.rows - first);
   const int32_t* tokens = p.tokens + g * p.rows + first;
   for (int i = t; i < 2 * threads; i += threads) {
     uint32_t k = kNoKey;
@@ -52,20 +75,22 @@ __global__ void __launch_bounds__(kSortTile / 2) sort_tiles_kernel(EmbeddingArgs
     }
     key[i] = k;
   }
-  int2* runs = reinterpret_cast<int2*>(ws + plan.runs) + g * p.classes;
-  for (int i = blockIdx.x * threads + t; i < p.classes; i += gridDim.x * threads) runs[i] = make_int2(0, 0);
   __syncthreads();
-  // bitonic: pairs j apart within blocks of k
+  // bitonic: pairs j apart within blocks of k.  Up to 64 apart a wavefront's 64 pairs are 128 keys that no other one has.
+  bool across = false;
   for (int k = 2; k <= 2 * threads; k <<= 1)
     for (int j = k >> 1; j > 0; j >>= 1) {
+      if (across || j > 64) __syncthreads();
+      else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      across = j > 64;
       const int lo = ((t & ~(j - 1)) << 1) | (t & (j - 1)), hi = lo | j;
       const uint32_t a = key[lo], b = key[hi];
       if ((a > b) == ((lo & k) == 0)) {
         key[lo] = b;
         key[hi] = a;
       }
-      __syncthreads();
     }
+  __syncthreads();
   if (plan.tiles == 1) {
     int* order = reinterpret_cast<int*>(ws + plan.order) + g * p.rows;
     int* sorted = reinterpret_cast<int*>(ws + plan.sorted) + g * p.rows;
@@ -119,131 +144,157 @@ __global__ void __launch_bounds__(kSortTile / 2) place_tokens_kernel(EmbeddingAr
 
 // ---- sums --------------------------------------------------------------------------------------
 
-constexpr int kSlice = 512;              // columns of a workgroup's sums: eight a lane, rows dealt to the wavefronts
+constexpr int kSlice = 8 * kWave;        // columns that a chunk's lanes take, at most
 __host__ __device__ constexpr int part_width(int width) { return (width + 7) / 8 * 8; }
 
-// Where the runs of a chunk of sorted tokens begin and end, and the sums of those that pass its ends: of the chunk's first run (part 0) and of
-// its last one if that is another (part 1).
-template <typename T> __global__ void __launch_bounds__(kThreads) chunk_sums_kernel(EmbeddingArgs p, EmbeddingPlan plan, char* ws) {
-  __shared__ float share[kThreads / kWave][kSlice];
-  const int64_t g = blockIdx.z;
-  const int n = (int)p.rows, c0 = blockIdx.x * plan.chunk, c1 = min(n, c0 + plan.chunk), t = threadIdx.x;
-  const int* sorted = reinterpret_cast<const int*>(ws + plan.sorted) + g * p.rows;
-  const int* order = reinterpret_cast<const int*>(ws + plan.order) + g * p.rows;
-  int2* runs = reinterpret_cast<int2*>(ws + plan.runs) + g * p.classes;
-  const int first = sorted[c0], last = sorted[c1 - 1];
-  const bool on = c1 < n && sorted[c1] == last;            // the last run goes on
-  const bool part0 = first < p.classes && ((c0 > 0 && sorted[c0 - 1] == first) || (on && first == last));
-  const bool part1 = last < p.classes && on && first != last;
-  int firsts = 0, lasts = 0;                               // tokens of the first and of the last run in the chunk
-  for (int i0 = c0; i0 < c1; i0 += kThreads) {
-    const int i = i0 + t, v = i < c1 ? sorted[i] : -1;
-    if (blockIdx.y == 0 && i < c1 && v < p.classes) {
-      if (i == 0 || sorted[i - 1] != v) runs[v].x = i;
-      if (i == n - 1 || sorted[i + 1] != v) runs[v].y = i + 1;
-    }
-    firsts += __syncthreads_count(v == first);
-    lasts += __syncthreads_count(v == last);
+// A chunk of sorted tokens and a slice of the columns, for lanes_log2 lanes: which these are, and what follows from them.
+struct ChunkPlace {
+  int64_t g;
+  int chunk, c, first, end;              // sorted tokens first .. end - 1; c: this lane's first column
+  const int *sorted, *order;
+  float* parts;                          // [2][part_width]: of the chunk's first run if it began before, of its last one if it goes on
+  __device__ __forceinline__ bool set(const EmbeddingArgs& p, const EmbeddingPlan& plan, char* ws, int lanes_log2) {
+    const int lanes = 1 << lanes_log2, slices = (p.width + kSlice - 1) / kSlice;
+    const int64_t unit = (int64_t)blockIdx.x * (kThreads >> lanes_log2) + (threadIdx.x >> lanes_log2), at = unit / slices;
+    if (at >= (int64_t)plan.chunks * p.workers) return false;
+    g = at / plan.chunks;
+    chunk = (int)(at - g * plan.chunks);
+    c = (int)(unit - at * slices) * kSlice + (threadIdx.x & (lanes - 1)) * 8;
+    first = chunk * plan.chunk;
+    end = (int)min(p.rows, (int64_t)first + plan.chunk);
+    sorted = reinterpret_cast<const int*>(ws + plan.sorted) + g * p.rows;
+    order = reinterpret_cast<const int*>(ws + plan.order) + g * p.rows;
+    parts = reinterpret_cast<float*>(ws + plan.parts) + (g * plan.chunks + chunk) * 2 * part_width(p.width) + c;
+    return c < p.width;
   }
-  const int wave = t / kWave, lane = t % kWave, c = blockIdx.y * kSlice + lane * 8;
-  for (int part = 0; part < 2; ++part) {
-    if (part == 0 ? !part0 : !part1) continue;
-    const int from = part == 0 ? c0 : c1 - lasts, to = part == 0 ? c0 + firsts : c1;
-    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (c < p.width)
-      for (int i = from + wave; i < to; i += kThreads / kWave) {
-        float v[8];
-        load8(reinterpret_cast<const T*>(p.y) + (g * p.rows + order[i]) * p.y_row + c, p.width - c, v);
+};
+template <typename T> __device__ __forceinline__ void store_row(const EmbeddingArgs& p, const ChunkPlace& at, int token, float (&sum)[8]) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] += v[e];
-      }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) share[wave][lane * 8 + e] = sum[e];
-    __syncthreads();
-    float* out = reinterpret_cast<float*>(ws + plan.parts) + ((g * plan.chunks + blockIdx.x) * 2 + part) * part_width(p.width);
-    for (int j = t; j < kSlice; j += kThreads) {
-      float s = share[0][j];
-#pragma unroll
-      for (int w = 1; w < kThreads / kWave; ++w) s += share[w][j];
-      if (blockIdx.y * kSlice + j < part_width(p.width)) out[blockIdx.y * kSlice + j] = s;
-    }
-    __syncthreads();
-  }
+  for (int e = 0; e < 8; ++e) sum[e] *= p.scale;
+  store8(reinterpret_cast<T*>(p.dtable) + at.g * p.dtable_gs + (int64_t)token * p.dtable_row + at.c, p.width - at.c, sum);
 }
 
-template <typename T> __global__ void __launch_bounds__(kThreads) table_rows_kernel(EmbeddingArgs p, EmbeddingPlan plan, const char* ws, int lanes_log2) {
-  const int lanes = 1 << lanes_log2, slots = kThreads >> lanes_log2;
-  const int64_t rows = (int64_t)p.classes * p.workers;
-  for (int64_t row = (int64_t)blockIdx.x * slots + (threadIdx.x >> lanes_log2); row < rows; row += (int64_t)gridDim.x * slots) {
-    const int64_t g = row / p.classes;
-    const int2 run = reinterpret_cast<const int2*>(ws + plan.runs)[row];
-    const int* order = reinterpret_cast<const int*>(ws + plan.order) + g * p.rows;
-    const int q0 = run.x / plan.chunk, q1 = run.y > run.x ? (run.y - 1) / plan.chunk : q0;
-    for (int c = (threadIdx.x & (lanes - 1)) * 8; c < p.width; c += lanes * 8) {
-      float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-      if (q0 == q1) {
-        for (int i = run.x; i < run.y; ++i) {
-          float v[8];
-          load8(reinterpret_cast<const T*>(p.y) + (g * p.rows + order[i]) * p.y_row + c, p.width - c, v);
+template <typename T> __global__ void __launch_bounds__(kThreads) chunk_sums_kernel(EmbeddingArgs p, EmbeddingPlan plan, char* ws, int lanes_log2) {
+  constexpr int U = 8;                   // rows on their way
+  ChunkPlace at;
+  if (!at.set(p, plan, ws, lanes_log2)) return;
+  const int n = p.width - at.c, before = at.first > 0 ? at.sorted[at.first - 1] : -1, behind = at.end < p.rows ? at.sorted[at.end] : -1;
+  const T* dy = reinterpret_cast<const T*>(p.y) + at.g * p.rows * p.y_row + at.c;
+  int token[U], row[U], now = -1;        // the run that is being summed
+  bool from_before = false;
+  float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  auto places = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sum[e] += v[e];
-        }
-      } else {
-        const float* parts = reinterpret_cast<const float*>(ws + plan.parts) + g * plan.chunks * 2 * part_width(p.width) + c;
-        for (int q = q0; q <= q1; ++q) {
-          float v[8];
-          load8(parts + (int64_t)(q * 2 + (q * plan.chunk < run.x ? 1 : 0)) * part_width(p.width), 8, v);
+    for (int k = 0; k < U; ++k) {
+      const int j = min(i + k, at.end - 1);
+      token[k] = i + k < at.end ? at.sorted[j] : -1;
+      row[k] = at.order[j];
+    }
+  };
+  auto finish_run = [&](bool goes_on) __attribute__((always_inline)) {
+    if ((unsigned)now >= (unsigned)p.classes) return;
+    if (from_before || goes_on) store8(at.parts + (from_before ? 0 : part_width(p.width)), 8, sum);
+    else store_row<T>(p, at, now, sum);
+  };
+  places(at.first);
+  for (int i = at.first; i < at.end; i += U) {
+    // no token comes last: nothing of its row is read
+    if ((unsigned)token[0] >= (unsigned)p.classes) break;
+    Raw8<T> v[U];
+    int of[U];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sum[e] += v[e];
+    for (int k = 0; k < U; ++k) {
+      of[k] = token[k];
+      raw_load(v[k], dy + row[k] * p.y_row, n, narrow_row<T>(p.width));
+    }
+    places(i + U);
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if ((unsigned)of[k] < (unsigned)p.classes) {
+        raw_place(v[k], n);
+        if (of[k] != now) {
+          finish_run(false);
+          now = of[k];
+          from_before = i + k == at.first && before == now;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
         }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += raw_at(v[k], e);
       }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum[e] *= p.scale;
-      store8(reinterpret_cast<T*>(p.dtable) + g * p.dtable_gs + (row - g * p.classes) * p.dtable_row + c, p.width - c, sum);
     }
   }
+  finish_run(behind == now);
 }
 
-template <typename K> hipError_t launch_rows(K kernel_of, int64_t rows, int width) {
-  const int lanes_log2 = lanes_for_row(width), slots = kThreads >> lanes_log2;
-  kernel_of(dim3((unsigned)std::min<int64_t>((rows + slots - 1) / slots, 256 * 64)), lanes_log2);
-  return hipGetLastError();
+// A run that passes ends of chunks: the parts that it left, by the lanes of the chunk that it begins in.
+template <typename T> __global__ void __launch_bounds__(kThreads) join_chunks_kernel(EmbeddingArgs p, EmbeddingPlan plan, char* ws, int lanes_log2) {
+  constexpr int U = 8;
+  ChunkPlace at;
+  if (!at.set(p, plan, ws, lanes_log2)) return;
+  const int token = at.sorted[at.end - 1];
+  if (at.end == p.rows || (unsigned)token >= (unsigned)p.classes || at.sorted[at.end] != token) return;
+  if (at.first > 0 && at.sorted[at.first] == token && at.sorted[at.first - 1] == token) return;
+  const int64_t apart = 2 * part_width(p.width);
+  float sum[8];
+  load8(at.parts + part_width(p.width), 8, sum);
+  bool more = true;
+  for (int q = at.chunk + 1; more; q += U) {
+    float part[U][8];
+    bool of_run[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const int chunk = min(q + k, plan.chunks - 1);
+      of_run[k] = q + k < plan.chunks && at.sorted[chunk * plan.chunk] == token;
+      load8(at.parts + (chunk - at.chunk) * apart, 8, part[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      more = more && of_run[k];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] += more ? part[k][e] : 0.0f;
+    }
+  }
+  store_row<T>(p, at, token, sum);
 }
 
 template <typename T> hipError_t backward(const EmbeddingArgs& p, const EmbeddingPlan& plan, char* ws, hipStream_t s) {
-  int threads = kWave;
+  int threads = kThreads;
   while (threads < kSortTile / 2 && 2 * threads < p.rows) threads *= 2;
-  const dim3 tiles((unsigned)plan.tiles, (unsigned)p.workers);
-  hipLaunchKernelGGL(sort_tiles_kernel, tiles, dim3(threads), 0, s, p, plan, ws);
+  // 64 KiB of zeros a workgroup, 16384 in all at most
+  const int64_t units = ((int64_t)p.classes * p.width * (int64_t)sizeof(T) + 65535) / 65536;
+  const int clearers = (int)std::min<int64_t>(units, std::max<int64_t>(16384 / p.workers, 1));
+  hipLaunchKernelGGL(sort_tiles_kernel<T>, dim3((unsigned)(plan.tiles + clearers), (unsigned)p.workers), dim3(threads), 0, s, p, plan, ws);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || p.rows == 0) return e;
   if (plan.tiles > 1) {
-    hipLaunchKernelGGL(place_tokens_kernel, tiles, dim3(kSortTile / 2), 0, s, p, plan, ws);
+    hipLaunchKernelGGL(place_tokens_kernel, dim3((unsigned)plan.tiles, (unsigned)p.workers), dim3(kSortTile / 2), 0, s, p, plan, ws);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  if (plan.chunks > 0)
-    hipLaunchKernelGGL(chunk_sums_kernel<T>, dim3((unsigned)plan.chunks, (unsigned)((p.width + kSlice - 1) / kSlice), (unsigned)p.workers), dim3(kThreads),
-                       0, s, p, plan, ws);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  return launch_rows([&](dim3 grid, int lanes_log2) {
-    hipLaunchKernelGGL(table_rows_kernel<T>, grid, dim3(kThreads), 0, s, p, plan, (const char*)ws, lanes_log2);
-  }, (int64_t)p.classes * p.workers, p.width);
+  const int lanes_log2 = std::min(lanes_for_row(p.width), 6), slots = kThreads >> lanes_log2;
+  const int64_t chunks = (int64_t)plan.chunks * p.workers * ((p.width + kSlice - 1) / kSlice);
+  const dim3 grid((unsigned)((chunks + slots - 1) / slots));
+  hipLaunchKernelGGL(chunk_sums_kernel<T>, grid, dim3(kThreads), 0, s, p, plan, ws, lanes_log2);
+  if ((e = hipGetLastError()) != hipSuccess || plan.chunks == 1) return e;
+  hipLaunchKernelGGL(join_chunks_kernel<T>, grid, dim3(kThreads), 0, s, p, plan, ws, lanes_log2);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_embedding(const EmbeddingArgs& p, bool bf16, hipStream_t s) {
-  return launch_rows([&](dim3 grid, int lanes_log2) {
-    if (bf16) hipLaunchKernelGGL(embedding_kernel<uint16_t>, grid, dim3(kThreads), 0, s, p, lanes_log2);
-    else hipLaunchKernelGGL(embedding_kernel<float>, grid, dim3(kThreads), 0, s, p, lanes_log2);
-  }, p.rows * p.workers, p.width);
+  const int lanes_log2 = lanes_for_row(p.width), slots = kThreads >> lanes_log2;
+  const dim3 grid((unsigned)std::min<int64_t>((p.rows * p.workers + slots - 1) / slots, 256 * 64));
+  if (bf16) hipLaunchKernelGGL(embedding_kernel<uint16_t>, grid, dim3(kThreads), 0, s, p, lanes_log2);
+  else hipLaunchKernelGGL(embedding_kernel<float>, grid, dim3(kThreads), 0, s, p, lanes_log2);
+  return hipGetLastError();
 }
 
-EmbeddingPlan embedding_plan(int workers, int64_t rows, int classes, int width) {
+EmbeddingPlan embedding_plan(int workers, int64_t rows, int width) {
   EmbeddingPlan e{};
   e.tiles = (int)std::max<int64_t>(1, (rows + kSortTile - 1) / kSortTile);
   // chunks grow with the rows, so that the commonest token's row has at most 256 of them to add
-  e.chunk = (int)std::max<int64_t>(kLeastChunk, ((rows + 255) / 256 + 63) / 64 * 64);
+  e.chunk = (int)std::max<int64_t>(kLeastChunk, ((rows + 255) / 256 + 31) / 32 * 32);
   e.chunks = (int)((rows + e.chunk - 1) / e.chunk);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t v = at; at += (bytes + 255) / 256 * 256; return v; };
@@ -251,9 +302,8 @@ EmbeddingPlan embedding_plan(int workers, int64_t rows, int classes, int width) 
   e.keys = e.tiles > 1 ? take(n * e.tiles * kSortTile * sizeof(uint32_t)) : 0;
   e.order = take(n * r * sizeof(int));
   e.sorted = take(n * r * sizeof(int));
-  e.runs = take(n * classes * sizeof(int2));
   e.parts = take(n * e.chunks * 2 * part_width(width) * sizeof(float));
-  e.total = at;
+  e.total = std::max<size_t>(at, 256);    // rows or none
   return e;
 }
 

@@ -17,18 +17,14 @@ namespace prsgd {
 
 namespace {
 
-// sigmoid(x) and sigmoid(-x), neither as a difference from 1.  The hardware's base-2 exponential takes an argument that is rounded, which leaves 1.3 |x| 2^-24 of
-// exp(-|x|), and its quotient is good to one rounding.  For gates in bf16, which are off by |x| 2^-9 themselves, that is nothing; for fp32 the rounding is made good.
-template <typename T> __device__ __forceinline__ void gates(float x, float& f, float& rest) {
-  float e;
-  if constexpr (sizeof(T) == 2) {
-    e = __builtin_amdgcn_exp2f(fabsf(x) * -1.44269502f);
-  } else {
-    const float t = fabsf(x) > 128.0f ? 128.0f : fabsf(x);       // NaN stays; from 104 on e is 0 anyway
-    const float hi = t * -1.44269502f, lo = fmaf(t, -1.44269502f, -hi), power = __builtin_amdgcn_exp2f(hi);
-    e = fmaf(power * 0.693147181f, lo, power);
-  }
-  const float r = __builtin_amdgcn_rcpf(1.0f + e), s = e * r;
+// sigmoid(x) and sigmoid(-x), neither as a difference from 1.  The hardware's base-2 exponential is good to a rounding of its own, but its argument's rounding
+// would leave 0.7 |x| 2^-23 of the result, which a product over a long sequence adds up: it is made good, and so is the reciprocal's.  (Rows in bf16 too: their
+// gates are exact numbers, and the states' gradient is fp32.  With neither, that of 4 x 16384 x 2048 was off by four times as much, in no less time.)
+__device__ __forceinline__ void gates(float x, float& f, float& rest) {
+  const float t = fabsf(x) > 128.0f ? 128.0f : fabsf(x);         // NaN stays; from 104 on e is 0 anyway
+  const float hi = t * -1.44269502f, lo = fmaf(t, -1.92596299e-8f, fmaf(t, -1.44269502f, -hi)), power = __builtin_amdgcn_exp2f(hi);
+  const float e = fmaf(power * 0.693147181f, lo, power), d = 1.0f + e, close = __builtin_amdgcn_rcpf(d);
+  const float r = fmaf(fmaf(-d, close, 1.0f), close, close), s = e * r;
   f = x >= 0.0f ? r : s;
   rest = x >= 0.0f ? s : r;
 }
@@ -71,15 +67,29 @@ template <typename T, bool BACK, int MODE> __device__ __forceinline__ void clear
   }
 }
 
-// Eight channels of a row as they lie in memory, and of it n that exist.
-template <typename T> struct Raw { u32x4_t q[sizeof(T) / 2]; };
-template <typename T> __device__ __forceinline__ float raw_at(const Raw<T>& v, int e) {
-  if constexpr (sizeof(T) == 4) return __uint_as_float(v.q[e / 4][e % 4]);
-  else return __uint_as_float((e & 1) != 0 ? v.q[0][e / 2] & 0xFFFF0000u : v.q[0][e / 2] << 16);
+// Of the 16 bytes from p on, n elements exist, 0 < n < 16 / ES: they come to lie at the end.  first: start of the buffer; the elements of a row's first piece
+// that has nothing in front of it are loaded one by one.
+template <int ES> __device__ __forceinline__ u32x4_t load_end(const void* p, int n, const void* first) {
+  constexpr int V = 16 / ES;
+  const char* from = reinterpret_cast<const char*>(p) - (V - n) * ES;
+  u32x4_t v = {0, 0, 0, 0};
+  if (from >= reinterpret_cast<const char*>(first)) {
+    v = reinterpret_cast<const Packed16<ES>*>(from)->v;
+  } else {
+    for (int e = 0; e < n; ++e) {
+      const int at = V - n + e;
+      uint32_t x;
+      if constexpr (ES == 4) x = reinterpret_cast<const uint32_t*>(p)[e];
+      else x = (uint32_t)reinterpret_cast<const uint16_t*>(p)[e] << (16 * (at & 1));
+#pragma unroll
+      for (int w = 0; w < 4; ++w) v[w] |= at * ES / 4 == w ? x : 0;
+    }
+  }
+  return v;
 }
-// VEC: rows are whole eights, so that no lane has a part of one.  Otherwise such a part comes with what lies before it (its rows begin at `first`), and is moved
-// into place when it is used.
-template <typename T, bool VEC> __device__ __forceinline__ void raw_load(Raw<T>& v, const T* p, int n, const void* first) {
+// Eight channels of a row.  VEC: rows are whole eights, so that no lane has a part of one.  Otherwise such a part comes with what lies before it (its rows begin at
+// `first`), and is moved into place when it is used.  (The branch between both costs a wait, but what load_piece needs would not stay in registers here.)
+template <bool VEC, typename T> __device__ __forceinline__ void load_channels(Raw8<T>& v, const T* p, int n, const void* first) {
   constexpr int ES = (int)sizeof(T), V = 16 / ES;
 #pragma unroll
   for (int i = 0; i < 8 / V; ++i) {
@@ -88,11 +98,11 @@ template <typename T, bool VEC> __device__ __forceinline__ void raw_load(Raw<T>&
     else v.q[i] = (u32x4_t){0, 0, 0, 0};
   }
 }
-template <typename T> __device__ __forceinline__ void raw_place(Raw<T>& v, int n) {
+template <typename T> __device__ __forceinline__ void place_channels(Raw8<T>& v, int n) {
   constexpr int ES = (int)sizeof(T), V = 16 / ES;
 #pragma unroll
   for (int i = 0; i < 8 / V; ++i)
-    if (n > i * V && n < (i + 1) * V) v.q[i] = place_end<ES>(v.q[i], n - i * V);
+    if (n > i * V && n < (i + 1) * V) v.q[i] = place_piece<ES>(v.q[i], n - i * V);
 }
 
 // Workgroups take packed sequences longest first, where these are few enough to be compared by each of them, so that the longest is not the last to start.
@@ -168,7 +178,7 @@ template <typename T, bool BACK, int NW, int R, int CL, bool VEC, int OCC, int M
     if (BACK) state = p.dlast != nullptr ? p.dlast[sequence * p.dlast_row + c_wg + own] : 0.0f;
     else state = p.initial != nullptr ? p.initial[sequence * p.initial_row + c_wg + own] : 0.0f;
   }
-  struct Rows { Raw<T> gate, v, dh, h; };
+  struct Rows { Raw8<T> gate, v, dh, h; };
   Rows ahead[R];
   // Row `at` of this lane, counted from the span's end backward, and what lies one row and one pass further on.
   int at = (wave * PARTS + part) * R, parity = 0;
@@ -184,11 +194,11 @@ template <typename T, bool BACK, int NW, int R, int CL, bool VEC, int OCC, int M
 #pragma unroll
     for (int j = 0; j < R; ++j)
       if (from + j < length && n > 0) {
-        raw_load<T, VEC>(ahead[j].gate, gate_at + j * kOn * p.gate_row, n, p.gate);
-        if constexpr (!BACK || MODE != COMPOSE) raw_load<T, VEC>(ahead[j].v, v_at + j * kOn * p.v_row, n, p.v);
-        if constexpr (BACK) raw_load<T, VEC>(ahead[j].dh, dh_at + j * kOn * p.dh_row, n, p.dh);
+        load_channels<VEC>(ahead[j].gate, gate_at + j * kOn * p.gate_row, n, p.gate);
+        if constexpr (!BACK || MODE != COMPOSE) load_channels<VEC>(ahead[j].v, v_at + j * kOn * p.v_row, n, p.v);
+        if constexpr (BACK) load_channels<VEC>(ahead[j].dh, dh_at + j * kOn * p.dh_row, n, p.dh);
         if constexpr (BACK && MODE != COMPOSE) {
-          if (from + j < length - 1 || span.first > all.first) raw_load<T, VEC>(ahead[j].h, h_at + j * kOn * p.h_in_row, n, p.h_in);
+          if (from + j < length - 1 || span.first > all.first) load_channels<VEC>(ahead[j].h, h_at + j * kOn * p.h_in_row, n, p.h_in);
         }
       } else {
         // past the end a gate that is open, and nothing else: such a row leaves what comes to it as it is
@@ -271,15 +281,15 @@ template <typename T, bool BACK, int NW, int R, int CL, bool VEC, int OCC, int M
         }
       }
       if constexpr (!VEC) {
-        raw_place<T>(ahead[j].gate, n);
-        if constexpr (!BACK || MODE != COMPOSE) raw_place<T>(ahead[j].v, n);
-        if constexpr (BACK) raw_place<T>(ahead[j].dh, n);
-        if constexpr (BACK && MODE != COMPOSE) raw_place<T>(ahead[j].h, n);
+        place_channels(ahead[j].gate, n);
+        if constexpr (!BACK || MODE != COMPOSE) place_channels(ahead[j].v, n);
+        if constexpr (BACK) place_channels(ahead[j].dh, n);
+        if constexpr (BACK && MODE != COMPOSE) place_channels(ahead[j].h, n);
       }
       float past[8];
       if constexpr (BACK && MODE != COMPOSE) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) past[e] = raw_at<T>(ahead[j].h, e);
+        for (int e = 0; e < 8; ++e) past[e] = raw_at(ahead[j].h, e);
         const int s = CUT ? last_of[j] : at + j == length - 1 ? sequence : -1;
         if (s >= 0) {                                      // the sequence's first row
 #pragma unroll
@@ -290,16 +300,16 @@ template <typename T, bool BACK, int NW, int R, int CL, bool VEC, int OCC, int M
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float r;
-        gates<T>(raw_at<T>(ahead[j].gate, e), f[j][e], r);
+        gates(raw_at(ahead[j].gate, e), f[j][e], r);
         if constexpr (BACK) {
-          u[j][e] = raw_at<T>(ahead[j].dh, e);
+          u[j][e] = raw_at(ahead[j].dh, e);
           if constexpr (MODE != COMPOSE) {
             rest[j][e] = r;
-            w[j][e] = r * (past[e] - raw_at<T>(ahead[j].v, e));
+            w[j][e] = r * (past[e] - raw_at(ahead[j].v, e));
           }
           b[e] = f[j][e] * (u[j][e] + b[e]);
         } else {
-          u[j][e] = r * raw_at<T>(ahead[j].v, e);
+          u[j][e] = r * raw_at(ahead[j].v, e);
           b[e] = fmaf(f[j][e], b[e], u[j][e]);
         }
         a[e] = CUT && a[e] < 0.0f ? -1.0f : a[e] * f[j][e];
@@ -399,7 +409,7 @@ template <typename T, bool BACK> __global__ void __launch_bounds__(kThreads) sca
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float f, rest;
-        gates<T>(gate[e], f, rest);
+        gates(gate[e], f, rest);
         if constexpr (BACK) {
           const float g = dh[e] + dlast[e];
           v[e] = f * rest * (state[e] - v[e]) * g;
@@ -415,8 +425,11 @@ template <typename T, bool BACK> __global__ void __launch_bounds__(kThreads) sca
     }
 }
 
-template <typename T, bool BACK, int NW, bool VEC, int MODE, int R = 2, int CL = kTile / 8> hipError_t launch_scan(const ScanArgs& p, hipStream_t s) {
-  constexpr int OCC = BACK || R > 2 ? 2 : 4;
+// What stays in registers: all of it (spilled registers would be, besides slow, many more places to go wrong).
+template <typename T, bool VEC, int MODE> constexpr bool kLarge = sizeof(T) == 4 && !VEC && MODE == APPLY;
+template <typename T, bool BACK, int NW, bool VEC, int MODE, int R = BACK && kLarge<T, VEC, MODE> ? 1 : 2, int CL = kTile / 8>
+hipError_t launch_scan(const ScanArgs& p, hipStream_t s) {
+  constexpr int OCC = BACK || R > 2 || kLarge<T, VEC, MODE> ? 2 : 4;
   const int tiles = (p.width + 8 * CL - 1) / (8 * CL);
   const unsigned others = MODE != COMPOSE && p.starts != nullptr && (p.clear != 0 || MODE == APPLY) ? kClearers : 0;
   const unsigned grid = (unsigned)tiles * (unsigned)(MODE == WHOLE ? p.sequences : p.parts) + others;

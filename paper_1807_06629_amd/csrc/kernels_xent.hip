@@ -105,9 +105,8 @@ __global__ void __launch_bounds__(kThreads) align_kernel(Operand from, Operand t
     uint16_t* out = reinterpret_cast<uint16_t*>(const_cast<void*>(to.p)) + g * to.gs + r * to.ld;
     for (int c = (threadIdx.x & (lanes - 1)) * 8; c < width; c += lanes * 8) {
       const int n = width - c;
-      u32x4_t v;
-      if (n >= 8) v = reinterpret_cast<const Packed16<2>*>(in + c)->v;
-      else v = place_end<2>(load_end<2>(in + c, n, from.p), n);
+      u32x4_t v = load_piece<2>(in + c, n, width < 8);
+      if (n < 8) v = place_piece<2>(v, n);
       *reinterpret_cast<u32x4_t*>(out + c) = v;
     }
   }

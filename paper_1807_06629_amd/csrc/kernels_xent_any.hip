@@ -18,11 +18,8 @@ template <typename T, int ROWS, bool TRANS, int D, int THREADS> struct Stage {
   static __device__ __forceinline__ int row_of(int u) { return TRANS ? u % (ROWS / V) * V : u / (D / V); }
   static __device__ __forceinline__ int depth_of(int u) { return TRANS ? u / (ROWS / V) * BK : u % (D / V) * V; }
   u32x4_t reg[NPT][BK];
-  static __device__ __forceinline__ u32x4_t piece(const T* p, int n, const void* first) {
-    return n >= V ? reinterpret_cast<const Packed16<ES>*>(p)->v : load_end<ES>(p, n, first);
-  }
-  // rows, depth: what is left of the operand from the tile's first element on; first: the operand's first
-  __device__ __forceinline__ void load(const T* base, int64_t ld, int rows, int depth, const void* first) {
+  // rows, depth: what is left of the operand from the tile's first element on; narrow: rows as they lie in memory are shorter than 16 bytes
+  __device__ __forceinline__ void load(const T* base, int64_t ld, int rows, int depth, bool narrow) {
 #pragma unroll
     for (int q = 0; q < NPT; ++q) {
       const int u = q * THREADS + (int)threadIdx.x, r = row_of(u), c = depth_of(u);
@@ -32,9 +29,9 @@ template <typename T, int ROWS, bool TRANS, int D, int THREADS> struct Stage {
       if constexpr (TRANS) {
 #pragma unroll
         for (int k = 0; k < BK; ++k)
-          if (c + k < depth && r < rows) reg[q][k] = piece(base + (int64_t)(c + k) * ld + r, rows - r, first);
+          if (c + k < depth && r < rows) reg[q][k] = load_piece<ES>(base + (int64_t)(c + k) * ld + r, rows - r, narrow);
       } else {
-        if (r < rows && c < depth) reg[q][0] = piece(base + (int64_t)r * ld + c, depth - c, first);
+        if (r < rows && c < depth) reg[q][0] = load_piece<ES>(base + (int64_t)r * ld + c, depth - c, narrow);
       }
     }
   }
@@ -47,7 +44,7 @@ template <typename T, int ROWS, bool TRANS, int D, int THREADS> struct Stage {
       const int n = TRANS ? rows - r : depth - c;
       if (n > 0 && n < V) {
 #pragma unroll
-        for (int k = 0; k < BK; ++k) reg[q][k] = place_end<ES>(reg[q][k], n);
+        for (int k = 0; k < BK; ++k) reg[q][k] = place_piece<ES>(reg[q][k], n);
       }
       if constexpr (TRANS) {
         u32x4_t v[BK];
@@ -116,8 +113,8 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(ProductArgs 
   uint32_t bits[WORDS > 0 ? WORDS : 1] = {~0u};
   const int n_k = (depth + D - 1) / D;
   auto load = [&](int t) __attribute__((always_inline)) {
-    ra.load(a + t * step_a, p.a.ld, p.M - m0, depth - t * D, p.a.p);
-    rb.load(b + t * step_b, p.b.ld, p.N - n0, depth - t * D, p.b.p);
+    ra.load(a + t * step_a, p.a.ld, p.M - m0, depth - t * D, narrow_row<T>(TA ? p.M : p.K));
+    rb.load(b + t * step_b, p.b.ld, p.N - n0, depth - t * D, narrow_row<T>(TB ? p.N : p.K));
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) {
       const int at_word = (k0 + t * D) / 32 + w;

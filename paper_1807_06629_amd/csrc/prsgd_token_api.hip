@@ -185,7 +185,7 @@ size_t prsgd_embedding_backward_workspace_bytes(const prsgd_embedding_config* cf
     bad(e);
     return 0;
   }
-  return embedding_plan(cfg->workers, cfg->rows_per_worker, cfg->classes, cfg->width).total;
+  return embedding_plan(cfg->workers, cfg->rows_per_worker, cfg->width).total;
 }
 
 int prsgd_embedding_backward(const prsgd_embedding_config* cfg, const int32_t* tokens_dev, const void* dy_dev, int64_t dy_row,
@@ -208,7 +208,7 @@ int prsgd_embedding_backward(const prsgd_embedding_config* cfg, const int32_t* t
   p.dtable = dtable_dev;
   p.dtable_gs = dtable_matrix;
   p.dtable_row = dtable_row;
-  return hip_result(launch_embedding_backward(p, embedding_plan(cfg->workers, cfg->rows_per_worker, cfg->classes, cfg->width),
+  return hip_result(launch_embedding_backward(p, embedding_plan(cfg->workers, cfg->rows_per_worker, cfg->width),
                                               reinterpret_cast<char*>(workspace_dev), cfg->dtype == PRSGD_BF16,
                                               reinterpret_cast<hipStream_t>(hip_stream)), "embedding backward");
 }

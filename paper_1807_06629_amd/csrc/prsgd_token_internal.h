@@ -51,9 +51,9 @@ hipError_t launch_embedding(const EmbeddingArgs& p, bool bf16, hipStream_t s);
 struct EmbeddingPlan {
   int tiles;                             // of kSortTile tokens, per worker
   int chunk, chunks;                     // sorted tokens whose sums one workgroup takes; per worker
-  size_t keys, order, sorted, runs, parts, total;    // byte offsets
+  size_t keys, order, sorted, parts, total;    // byte offsets
 };
-EmbeddingPlan embedding_plan(int workers, int64_t rows, int classes, int width);
+EmbeddingPlan embedding_plan(int workers, int64_t rows, int width);
 hipError_t launch_embedding_backward(const EmbeddingArgs& p, const EmbeddingPlan& plan, char* ws, bool bf16, hipStream_t s);
 
 // ---- gated scan --------------------------------------------------------------------------------

@@ -1,33 +1,28 @@
-// The ends of rows whose length is a multiple of nothing.  16 bytes that end where the row does take one load, and are moved into place when they
-// are used: elements loaded one by one would each be waited for where they are put together.
+// Rows whose length is a multiple of nothing, 16 bytes at a time.  The last bytes of a row come in one load that ends where the row does, and are moved into place when
+// they are used: elements loaded one by one would each be waited for where they are put together, and a branch between both ways of loading waits for what is on its way.
 #pragma once
 
 #include "orth_rows.h"
 
 namespace prsgd {
 
-// Of the 16 bytes from p on, n elements exist, 0 < n < 16 / ES: they come to lie at the end.  first: start of the buffer; the elements of a row's first piece
-// that has nothing in front of it are loaded one by one.
-template <int ES> __device__ __forceinline__ u32x4_t load_end(const void* p, int n, const void* first) {
+// 16 bytes of a row from p on, n > 0 elements of which exist; fewer than 16 / ES come to lie at the end, behind what lies before them.  narrow (of all lanes): the
+// row as a whole is shorter than that, and is loaded one by one.
+template <int ES> __device__ __forceinline__ u32x4_t load_piece(const void* p, int n, bool narrow) {
   constexpr int V = 16 / ES;
-  const char* from = reinterpret_cast<const char*>(p) - (V - n) * ES;
+  const int missing = n < V ? V - n : 0;
+  if (!narrow) return reinterpret_cast<const Packed16<ES>*>(reinterpret_cast<const char*>(p) - missing * ES)->v;
   u32x4_t v = {0, 0, 0, 0};
-  if (from >= reinterpret_cast<const char*>(first)) {
-    v = reinterpret_cast<const Packed16<ES>*>(from)->v;
-  } else {
-    for (int e = 0; e < n; ++e) {
-      const int at = V - n + e;
-      uint32_t x;
-      if constexpr (ES == 4) x = reinterpret_cast<const uint32_t*>(p)[e];
-      else x = (uint32_t)reinterpret_cast<const uint16_t*>(p)[e] << (16 * (at & 1));
 #pragma unroll
-      for (int w = 0; w < 4; ++w) v[w] |= at * ES / 4 == w ? x : 0;
-    }
+  for (int e = 0; e < V; ++e) {
+    const int from = e < missing ? 0 : e - missing;
+    if constexpr (ES == 4) v[e] = reinterpret_cast<const uint32_t*>(p)[from];
+    else v[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[from] << (16 * (e & 1));
   }
   return v;
 }
-// What load_end returned, with its n elements in front and zeros behind.
-template <int ES> __device__ __forceinline__ u32x4_t place_end(u32x4_t v, int n) {
+// What load_piece returned of n < 16 / ES elements, with these in front and zeros behind.
+template <int ES> __device__ __forceinline__ u32x4_t place_piece(u32x4_t v, int n) {
   const int bytes = (16 / ES - n) * ES;
   if constexpr (ES == 2) {
     const u32x4_t half = {v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
@@ -41,6 +36,31 @@ template <int ES> __device__ __forceinline__ u32x4_t place_end(u32x4_t v, int n)
 #pragma unroll
   for (int w = 0; w < 4; ++w) v[w] = (bytes & 8) != 0 ? two[w] : v[w];
   return v;
+}
+
+// Eight elements of a row as they lie in memory, n of which exist; until raw_place has moved them, the last ones of an odd row lie elsewhere.
+template <typename T> struct Raw8 { u32x4_t q[sizeof(T) / 2]; };
+template <typename T> __device__ __forceinline__ float raw_at(const Raw8<T>& v, int e) {
+  if constexpr (sizeof(T) == 4) return __uint_as_float(v.q[e / 4][e % 4]);
+  else return __uint_as_float((e & 1) != 0 ? v.q[0][e / 2] & 0xFFFF0000u : v.q[0][e / 2] << 16);
+}
+// WHOLE: rows are whole eights, so that no lane has a part of one; n > 0
+template <typename T> __device__ __forceinline__ bool narrow_row(int width) { return width < 16 / (int)sizeof(T); }
+template <bool WHOLE = false, typename T> __device__ __forceinline__ void raw_load(Raw8<T>& v, const T* p, int n, bool narrow) {
+  constexpr int ES = (int)sizeof(T), V = 16 / ES;
+#pragma unroll
+  for (int i = 0; i < 8 / V; ++i) {
+    if constexpr (WHOLE) v.q[i] = reinterpret_cast<const Packed16<ES>*>(p + i * V)->v;
+    else if (i == 0) v.q[i] = load_piece<ES>(p, n, narrow);
+    // of a second piece that does not exist the first one once more
+    else v.q[i] = load_piece<ES>(n > i * V ? p + i * V : p, n > i * V ? n - i * V : n, narrow);
+  }
+}
+template <typename T> __device__ __forceinline__ void raw_place(Raw8<T>& v, int n) {
+  constexpr int ES = (int)sizeof(T), V = 16 / ES;
+#pragma unroll
+  for (int i = 0; i < 8 / V; ++i)
+    if (n < (i + 1) * V) v.q[i] = n > i * V ? place_piece<ES>(v.q[i], n - i * V) : (u32x4_t){0, 0, 0, 0};
 }
 
 }  // namespace prsgd
