@@ -18,7 +18,7 @@ constexpr int kTileBits = 11;
 static_assert(1 << kTileBits == kSortTile, "place in a tile");
 static_assert((uint64_t)(kMaxClasses + 1) << kTileBits < 0xFFFFFFFFull, "a token and its place in its tile fit 32 bits, with a value to spare");
 constexpr uint32_t kNoKey = 0xFFFFFFFFu;
-constexpr int kLeastChunk = 32;
+constexpr int kLeastChunk = 8;
 
 template <typename T> __global__ void __launch_bounds__(kThreads) embedding_kernel(EmbeddingArgs p, int lanes_log2) {
   const int lanes = 1 << lanes_log2, slots = kThreads >> lanes_log2;
@@ -39,19 +39,24 @@ template <typename T> __global__ void __launch_bounds__(kThreads) embedding_kern
 
 // ---- sorting -----------------------------------------------------------------------------------
 
-// Zeros in a worker's rows of dT, by `blocks` workgroups.
+// Zeros in a worker's rows of dT, by `blocks` workgroups: 16 aligned bytes a lane where rows lie one behind another.
 template <typename T> __device__ __forceinline__ void clear_table(const EmbeddingArgs& p, int64_t g, int block, int blocks) {
+  constexpr int V = 16 / (int)sizeof(T);
   T* table = reinterpret_cast<T*>(p.dtable) + g * p.dtable_gs;
-  const bool whole = p.dtable_row == p.width;              // one row
-  const int64_t width = whole ? (int64_t)p.classes * p.width : p.width, rows = whole ? 1 : p.classes, units = (width + 7) / 8;
-  const float none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  const int64_t step = (int64_t)blocks * blockDim.x;
-  if (whole) {
-    for (int64_t i = (int64_t)block * blockDim.x + threadIdx.x; i < units; i += step) store8(table + i * 8, (int)min(width - i * 8, (int64_t)8), none);
+  const int64_t start = (int64_t)block * blockDim.x + threadIdx.x, step = (int64_t)blocks * blockDim.x;
+  if (p.dtable_row == p.width) {
+    const int64_t n = (int64_t)p.classes * p.width, front = min((int64_t)((16 - (uintptr_t)table % 16) % 16 / sizeof(T)), n), units = (n - front) / V;
+    u32x4_t* at = reinterpret_cast<u32x4_t*>(table + front);
+#pragma unroll 4
+    for (int64_t i = start; i < units; i += step) at[i] = (u32x4_t){0, 0, 0, 0};
+    if (start < front) table[start] = 0;
+    if (start < n - front - units * V) table[front + units * V + start] = 0;
   } else {
-    for (int64_t i = (int64_t)block * blockDim.x + threadIdx.x; i < units * rows; i += step) {
-      const int64_t r = i / units, c = (i - r * units) * 8;
-      store8(table + r * p.dtable_row + c, (int)min(width - c, (int64_t)8), none);
+    const float none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    const int64_t per_row = (p.width + 7) / 8;
+    for (int64_t i = start; i < per_row * p.classes; i += step) {
+      const int64_t r = i / per_row, c = (i - r * per_row) * 8;
+      store8(table + r * p.dtable_row + c, (int)min(p.width - c, (int64_t)8), none);
     }
   }
 }
@@ -293,8 +298,9 @@ hipError_t launch_embedding(const EmbeddingArgs& p, bool bf16, hipStream_t s) {
 EmbeddingPlan embedding_plan(int workers, int64_t rows, int width) {
   EmbeddingPlan e{};
   e.tiles = (int)std::max<int64_t>(1, (rows + kSortTile - 1) / kSortTile);
-  // chunks grow with the rows, so that the commonest token's row has at most 256 of them to add
-  e.chunk = (int)std::max<int64_t>(kLeastChunk, ((rows + 255) / 256 + 31) / 32 * 32);
+  // Few rows a chunk, so that many lanes work on them; chunks grow with the rows, so that the commonest token's row has at most 256 parts to add: chunks of 8, 16,
+  // 32 and 64 of 8 x 8192 tokens, 1024 wide, take 107, 89, 81 and 75 us for sums and parts, of 16 x 2013, 21 wide, 19, 21, 29 and 48 us.
+  e.chunk = (int)std::max<int64_t>(kLeastChunk, ((rows + 255) / 256 + kLeastChunk - 1) / kLeastChunk * kLeastChunk);
   e.chunks = (int)((rows + e.chunk - 1) / e.chunk);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t v = at; at += (bytes + 255) / 256 * 256; return v; };
