@@ -14,10 +14,11 @@ namespace prsgd {
 
 namespace {
 
-// Parts that a contraction is cut into where its product has few tiles: 512 tiles of 64 x 64 in all, a part at least eight steps of 64.
+// Parts that a contraction is cut into where its product has few tiles: 512 tiles of 64 x 64 in all, a part at least eight steps of 64.  The parts' addition takes
+// 4 us, and half of a contraction of 2048 not much more.
 int splits_of(int64_t m, int64_t n, int64_t k, int groups) {
   const int64_t tiles = (m + 63) / 64 * ((n + 63) / 64) * groups;
-  return tiles == 0 ? 1 : (int)std::max<int64_t>(std::min<int64_t>(512 / tiles, k / 512), 1);
+  return tiles == 0 || k < 2048 ? 1 : (int)std::max<int64_t>(std::min<int64_t>(512 / tiles, k / 512), 1);
 }
 size_t parts_bytes(int64_t m, int64_t n, int64_t k, int groups) {
   const int splits = splits_of(m, n, k, groups);
@@ -74,17 +75,19 @@ __global__ void __launch_bounds__(kThreads) join_tiles_kernel(XentArgs p, const 
     float m = -INFINITY, s = 0.0f;
     for (int k = 0; k < pieces.pieces; ++k) {
       const int tiles = k + 1 == pieces.pieces ? pieces.last_tiles : pieces.tiles;
-      for (int t = lane; t < tiles; t += lanes) {
-        const float2 v = stats[k * pieces.stride + r * tiles + t];
-        join_stats(m, s, v.x, v.y);
+      constexpr int U = 4;
+      for (int t = lane; t < tiles; t += lanes * U) {
+        float2 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = t + u * lanes < tiles ? stats[k * pieces.stride + r * tiles + t + u * lanes] : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+        for (int u = 0; u < U; ++u) join_stats(m, s, v[u].x, v[u].y);
       }
     }
     for (int d = 1; d < lanes; d <<= 1) join_stats(m, s, __shfl_xor(m, d), __shfl_xor(s, d));
     if (lane == 0) {
-      const float lse = m + logf(s);
       const bool real = (unsigned)p.labels[r] < (unsigned)p.classes;
-      p.lse[r] = lse;
-      p.loss[r] = real ? lse - picked[r] : 0.0f;
+      write_loss(p.loss, p.lse, r, m, s, real, real ? picked[r] : 0.0f);
     }
   }
 }
@@ -165,11 +168,14 @@ hipError_t launch_xent(const XentArgs& x, const XentPlan& plan, char* ws, bool b
     p.classes = x.classes;
     p.stats = reinterpret_cast<float2*>(ws + plan.stats) + stats;
     p.picked = reinterpret_cast<float*>(ws + plan.picked);
+    p.loss_out = plan.pieces == 1 ? x.loss : nullptr;
+    p.lse_out = x.lse;
     if (const hipError_t e = launch_product(p, PX_STATS, !x.classes_first, false, bf16, &cut, s); e != hipSuccess) return e;
     if (k == 0) pieces.tiles = cut.tiles_m;
     pieces.last_tiles = cut.tiles_m;
     stats += x.rows * x.workers * least;
   }
+  if (plan.pieces == 1 && cut.tiles_m == 1) return hipSuccess;             // done
   pieces.pieces = plan.pieces;
   pieces.stride = x.rows * x.workers * least;
   const int tiles = (pieces.pieces - 1) * pieces.tiles + pieces.last_tiles;
@@ -211,8 +217,10 @@ hipError_t launch_xent_backward(const XentArgs& x, const XentPlan& plan, char* w
     p.out_ld = dz.ld;
     p.out_gs = dz.gs;
     p.splits = 1;
+    const bool small = plan.pieces == 1 && small_gradients(x.rows, x.width, x.classes);
+    const ProductArgs dz_of = p;
     Cut cut;
-    if ((e = launch_product(p, PX_DZ, false, !x.classes_first, bf16, &cut, s)) != hipSuccess) return e;
+    if (!small && (e = launch_product(p, PX_DZ, false, !x.classes_first, bf16, &cut, s)) != hipSuccess) return e;
     p.parts = reinterpret_cast<float*>(ws + plan.parts);
     p.a = dz;
     p.N = x.width;
@@ -221,7 +229,8 @@ hipError_t launch_xent_backward(const XentArgs& x, const XentPlan& plan, char* w
     p.out_ld = x.dh_row;
     p.out_gs = x.rows * x.dh_row;
     p.sums = plan.pieces > 1 ? reinterpret_cast<float*>(ws + plan.sums) : nullptr;
-    if ((e = launch_gradient<PX_DH>(p, false, x.classes_first, bf16, s)) != hipSuccess) return e;
+    const ProductArgs dh_of = p;
+    if (!small && (e = launch_gradient<PX_DH>(p, false, x.classes_first, bf16, s)) != hipSuccess) return e;
     p.a = x.classes_first ? dz : rows;
     p.b = x.classes_first ? rows : dz;
     p.M = x.classes_first ? n : x.width;
@@ -230,6 +239,7 @@ hipError_t launch_xent_backward(const XentArgs& x, const XentPlan& plan, char* w
     p.out = (char*)x.dw + dw_at * es;
     p.out_ld = x.dw_row;
     p.out_gs = x.dw_gs;
+    if (small) return launch_small_gradients(dz_of, dh_of, p, x.classes_first, bf16, s);
     if ((e = launch_gradient<PX_DW>(p, true, true, bf16, s)) != hipSuccess) return e;
   }
   return hipSuccess;

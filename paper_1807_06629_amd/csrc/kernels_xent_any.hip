@@ -86,16 +86,14 @@ template <typename T, int BM, int BN, int WM, int WN, int WK, int D, int EPI> co
   return most > epilogue ? most : epilogue;
 }
 template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bool TB, int EPI>
-__global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(ProductArgs p) {
+__device__ __forceinline__ void product_tile(const ProductArgs& p, TilePosition at, unsigned char* smem) {
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32, KK = D * (int)sizeof(T) / 32 / WK, THREADS = 64 * WM * WN * WK;
   static_assert(D * (int)sizeof(T) % (32 * WK) == 0, "a tile's depth splits evenly");
   constexpr int WORDS = EPI == PX_DW ? D / 32 : 0;
   using A = Stage<T, BM, TA, D, THREADS>;
   using B = Stage<T, BN, TB, D, THREADS>;
   constexpr int STAGE = A::BYTES + B::BYTES;
-  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wk = wave / (WM * WN), wm = wave / WN % WM, wn = wave % WN;
-  const TilePosition at = tile_of_workgroup(p);
   const int g = at.g, m0 = at.ti * BM, n0 = at.tj * BN, k0 = at.split * p.split_steps * D, depth = min(p.K - k0, p.split_steps * D);
   const T* a = reinterpret_cast<const T*>(p.a.p) + g * p.a.gs + (int64_t)m0 * (TA ? 1 : p.a.ld) + (int64_t)k0 * (TA ? p.a.ld : 1);
   const T* b = reinterpret_cast<const T*>(p.b.p) + g * p.b.gs + (int64_t)n0 * (TB ? 1 : p.b.ld) + (int64_t)k0 * (TB ? p.b.ld : 1);
@@ -118,7 +116,8 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(ProductArgs 
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) {
       const int at_word = (k0 + t * D) / 32 + w;
-      bits[w] = at_word < real_words(p.rows) ? real[at_word] : 0;
+      // (written by this launch, where a workgroup makes all of a worker's products)
+      bits[w] = at_word < real_words(p.rows) ? __hip_atomic_load(const_cast<uint32_t*>(real) + at_word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) : 0;
     }
   };
   auto store = [&](int t) __attribute__((always_inline)) {
@@ -173,6 +172,44 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(ProductArgs 
   }
   product_epilogue<T, EPI, BM, BN, WM, WN, WK>(p, acc, at, m0, n0, wm, wn, lane, wk == 0, smem);
 }
+template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bool TB, int EPI>
+__global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(ProductArgs p) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  product_tile<T, BM, BN, WM, WN, WK, D, TA, TB, EPI>(p, tile_of_workgroup(p), smem);
+}
+
+// All of a worker's products one after another.
+template <typename T, bool CF> constexpr int small_lds_bytes() {
+  constexpr int dz = lds_bytes<T, 32, 32, 1, 1, 4, 128, PX_DZ>(), wide = lds_bytes<T, 32, 128, 1, 4, 1, 32, PX_DH>(), high = lds_bytes<T, 128, 32, 4, 1, 1, 32, PX_DW>();
+  return std::max(dz, std::max(wide, high));
+}
+template <typename T, bool CF> __global__ void __launch_bounds__(kThreads) small_gradients_kernel(ProductArgs dz, ProductArgs dh, ProductArgs dw) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int g = blockIdx.x;
+  for (int i = 0; i < dz.tiles_m * dz.tiles_n; ++i) {
+    product_tile<T, 32, 32, 1, 1, 4, 128, false, !CF, PX_DZ>(dz, {g, i / dz.tiles_n, i % dz.tiles_n, 0}, smem);
+    __syncthreads();
+  }
+  for (int i = 0; i < dh.tiles_m * dh.tiles_n; ++i) {
+    product_tile<T, 32, 128, 1, 4, 1, 32, false, CF, PX_DH>(dh, {g, i / dh.tiles_n, i % dh.tiles_n, 0}, smem);
+    __syncthreads();
+  }
+  for (int i = 0; i < dw.tiles_m * dw.tiles_n; ++i) {
+    product_tile<T, CF ? 32 : 128, CF ? 128 : 32, CF ? 1 : 4, CF ? 4 : 1, 1, 32, true, true, PX_DW>(dw, {g, i / dw.tiles_n, i % dw.tiles_n, 0}, smem);
+    __syncthreads();
+  }
+}
+template <typename T, bool CF> hipError_t launch_small(ProductArgs& dz, ProductArgs& dh, ProductArgs& dw, hipStream_t s) {
+  constexpr int kLds = small_lds_bytes<T, CF>();
+  constexpr auto kernel = small_gradients_kernel<T, CF>;
+  if (const hipError_t e = allow_lds<kernel>(kLds); e != hipSuccess) return e;
+  Cut cut;
+  cut_product(dz, 32, 32, 128, &cut);
+  cut_product(dh, 32, 128, 32, &cut);
+  cut_product(dw, CF ? 32 : 128, CF ? 128 : 32, 32, &cut);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)dz.groups), dim3(kThreads), kLds, s, dz, dh, dw);
+  return hipGetLastError();
+}
 
 template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bool TB, int EPI> hipError_t launch_tile(ProductArgs p, Cut* cut, hipStream_t s) {
   constexpr int kLds = lds_bytes<T, BM, BN, WM, WN, WK, D, EPI>();
@@ -186,6 +223,11 @@ template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bo
 template <typename T, bool TA, bool TB, int EPI> hipError_t launch_size(const ProductArgs& p, Cut* cut, hipStream_t s) {
   constexpr int M128 = sizeof(T) == 4 && EPI != PX_DW ? 4 : 2;
   const int64_t huge = tiles_of(p, 128), large = tiles_of(p, 64);
+  if constexpr (EPI == PX_STATS) {
+    // all classes in one tile need no other launch
+    if (large < 256 && p.M > 32 && p.M <= 64 && p.K <= 512) return launch_tile<T, 64, 32, 2, 1, 2, 64, TA, TB, EPI>(p, cut, s);
+    if (large < 256 && p.M > 64 && p.M <= 128 && p.K <= 128) return launch_tile<T, 128, 32, 4, 1, 1, 32, TA, TB, EPI>(p, cut, s);
+  }
   if (tiles_of(p, 32) >= 512 && (p.M <= 32 || p.N <= 32)) {
     if (p.K <= 64) return p.N <= 32 ? launch_tile<T, 128, 32, 4, 1, 1, 32, TA, TB, EPI>(p, cut, s) : launch_tile<T, 32, 128, 1, 4, 1, 32, TA, TB, EPI>(p, cut, s);
     return p.N <= 32 ? launch_tile<T, 64, 32, 2, 1, 2, 64, TA, TB, EPI>(p, cut, s) : launch_tile<T, 32, 64, 1, 2, 2, 64, TA, TB, EPI>(p, cut, s);
@@ -204,8 +246,22 @@ template <typename T> hipError_t launch(const ProductArgs& p, int epi, bool ta, 
   }
 }
 
+// A step takes a workgroup 1.3 us to 2 us, a launch 4 to 6 us: 64 workers' 8 rows x 128 x 10 fp32 (6 steps) 17.8 us as three launches, 12.7 us as one; 2 workers'
+// 3 x 370 x 6 (16 steps) 20.0 and 24.1 us.
+constexpr int64_t kSmallSteps = 8;
+
 }  // namespace
 
+bool small_gradients(int64_t rows, int width, int classes) {
+  auto t = [](int64_t n, int b) { return (n + b - 1) / b; };
+  const int64_t r = t(rows, 32), c = t(classes, 32), w = t(width, 128);
+  // steps of the contraction and a tile's beginning and end
+  return rows > 0 && r * c * (1 + w) + r * w * (1 + c) + w * c * (1 + r) <= kSmallSteps;
+}
+hipError_t launch_small_gradients(ProductArgs dz, ProductArgs dh, ProductArgs dw, bool classes_first, bool bf16, hipStream_t s) {
+  if (bf16) return classes_first ? launch_small<uint16_t, true>(dz, dh, dw, s) : launch_small<uint16_t, false>(dz, dh, dw, s);
+  return classes_first ? launch_small<float, true>(dz, dh, dw, s) : launch_small<float, false>(dz, dh, dw, s);
+}
 hipError_t launch_product_any(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, bool bf16, Cut* cut, hipStream_t s) {
   return bf16 ? launch<uint16_t>(p, epi, a_transposed, b_transposed, cut, s) : launch<float>(p, epi, a_transposed, b_transposed, cut, s);
 }

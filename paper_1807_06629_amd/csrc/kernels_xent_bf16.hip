@@ -214,7 +214,7 @@ template <bool TA, bool TB, int EPI> hipError_t launch(const ProductArgs& p, Cut
   const int64_t n_middle = tiles_of(p, 128), n_huge = (tiles_of(p, 256) + 255) / 256 * 256;
   const double middle = cost(n_middle, 128, n_middle > 256 ? 0.9 : 1.34), small = cost(tiles_of(p, 64), 64, 0.68), huge = cost(n_huge, 256, 1.2);
   if (huge <= middle && huge <= small) return launch_tile<256, 256, 4, 2, 2, TA, TB, EPI>(p, cut, s);
-  if (middle > small) return launch_tile<64, 64, 2, 2, 4, TA, TB, EPI>(p, cut, s);
+  if (middle > small) return launch_tile<64, 64, 2, 2, 3, TA, TB, EPI>(p, cut, s);
   if (n_middle <= 256) return launch_tile<128, 128, 4, 2, 3, TA, TB, EPI>(p, cut, s);
   return launch_tile<128, 128, 2, 2, 2, TA, TB, EPI>(p, cut, s);
 }

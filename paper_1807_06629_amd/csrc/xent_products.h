@@ -33,6 +33,7 @@ struct ProductArgs {
   int64_t rows;
   int class0, classes;                   // first class of the piece; of all
   float2* stats; float* picked;          // PX_STATS: [rows of all workers][tiles_m]
+  float* loss_out; float* lse_out;       // PX_STATS of all classes in one tile: what comes of its statistics (nullptr: these alone)
   void* out; int64_t out_gs, out_ld;     // the others
   float* sums;                           // PX_DH over several pieces: [groups][M][N] fp32
   bool first_piece, last_piece;
@@ -74,7 +75,13 @@ __device__ __forceinline__ TilePosition tile_of_workgroup(const ProductArgs& p) 
 
 constexpr int kStripPad = 8;             // floats: the four rows between a register's two halves lie 32 banks apart
 template <int BM, int BN, int WM, int WN, int EPI> constexpr int epilogue_lds_bytes() {
-  return EPI == PX_STATS ? WM * BN * (int)sizeof(float2) : WM * WN * 32 * (BN / WN + kStripPad) * 4;
+  return EPI == PX_STATS ? (WM * (int)sizeof(float2) + (int)sizeof(float)) * BN : WM * WN * 32 * (BN / WN + kStripPad) * 4;
+}
+
+__device__ __forceinline__ void write_loss(float* loss, float* lse_out, int64_t row, float m, float s, bool real, float picked) {
+  const float lse = m + logf(s);
+  lse_out[row] = lse;
+  loss[row] = real ? lse - picked : 0.0f;
 }
 
 // Eight columns of a row of dh or dW, n of which exist.
@@ -107,7 +114,9 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& p, const f32
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
   const int g = at.g;
   if constexpr (EPI == PX_STATS) {
-    float2* shared = reinterpret_cast<float2*>(smem);        // [WM][BN]
+    float2* shared = reinterpret_cast<float2*>(smem);        // [WM][BN], and the labels' logits
+    float* shared_picked = reinterpret_cast<float*>(shared + WM * BN);
+    const bool whole = p.loss_out != nullptr && p.tiles_m == 1;
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
       if (!sums) break;
@@ -124,7 +133,10 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& p, const f32
           if (c < p.M) {
             m = fmaxf(m, acc[i][j][e]);
             odd = odd || !(acc[i][j][e] <= INFINITY);          // fmaxf passes over what is no number
-            if (p.class0 + c == label) p.picked[g * p.rows + row] = acc[i][j][e];
+            if (p.class0 + c == label) {
+              if (whole) shared_picked[col] = acc[i][j][e];
+              else p.picked[g * p.rows + row] = acc[i][j][e];
+            }
           }
         }
       const float top = m == -INFINITY ? 0.0f : m;
@@ -148,7 +160,9 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& p, const f32
         const float2 o = shared[w * BN + col];
         join_stats(v.x, v.y, o.x, o.y);
       }
-      p.stats[(g * p.rows + n0 + col) * p.tiles_m + at.ti] = v;
+      const int64_t row = g * p.rows + n0 + col;
+      if (whole) write_loss(p.loss_out, p.lse_out, row, v.x, v.y, (unsigned)p.labels[row] < (unsigned)p.classes, shared_picked[col]);
+      else p.stats[row * p.tiles_m + at.ti] = v;
     }
   } else {
     // a wavefront passes strips of 32 rows through LDS, from where a lane takes eight columns of a row at a time
@@ -233,6 +247,9 @@ inline unsigned cut_product(ProductArgs& p, int bm, int bn, int depth, Cut* cut)
 // cut: how the product was cut; tiles have kLeastTile rows at least
 constexpr int kLeastTile = 32;
 hipError_t launch_product_any(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, bool bf16, Cut* cut, hipStream_t s);
+// The gradients' three products one after another, by a workgroup a worker, where that takes less than their launches.
+bool small_gradients(int64_t rows, int width, int classes);
+hipError_t launch_small_gradients(ProductArgs dz, ProductArgs dh, ProductArgs dw, bool classes_first, bool bf16, hipStream_t s);
 // ... and bf16 operands whose rows start at 16 bytes and are as long in whole (kernels_xent_bf16.hip).
 bool product_aligned(const ProductArgs& p, bool a_transposed, bool b_transposed);
 hipError_t launch_product_bf16(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, Cut* cut, hipStream_t s);
