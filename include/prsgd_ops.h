@@ -237,7 +237,7 @@ int prsgd_linear_cross_entropy(const prsgd_xent_config* cfg, const void* h_dev, 
  *   dz = dloss (exp(z - lse) - onehot(label)),   dh = dz W_i^T,   dW_i = sum over worker i's rows of h dz,
  * each rounded once from fp32 sums; dz itself, which the products take, is held in the rows' type.  Rows without a label get a dh of
  * zeros and are no part of dW, whatever h, lse and dloss hold there.  dw has W's layout; every worker has its own.  Without rows it is
- * zeros.  Classes are taken in pieces, of which the workspace holds one (128 MiB, or 256 classes if those are more).
+ * zeros.  Classes are taken in pieces, of which the workspace holds one (256 MiB, or 256 classes if those are more).
  */
 size_t prsgd_linear_cross_entropy_backward_workspace_bytes(const prsgd_xent_config* cfg);
 int prsgd_linear_cross_entropy_backward(const prsgd_xent_config* cfg, const float* dloss_dev, const void* h_dev, int64_t h_row,

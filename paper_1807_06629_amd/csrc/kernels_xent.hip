@@ -92,12 +92,13 @@ __global__ void __launch_bounds__(kThreads) join_tiles_kernel(XentArgs p, const 
   }
 }
 
-constexpr size_t kPieceBytes = (size_t)128 << 20;          // of dz, and of a copy of W
+constexpr size_t kPieceBytes = (size_t)256 << 20;          // of dz, and of a copy of W
 
-// Rows of bf16 whose length is no multiple of eight are copied to such a multiple, with zeros, where the products take long enough: aligned operands go to LDS
-// by themselves.  Gradients of 8 workers' rows x 1024 x 8001 classes, as they lie and by copies: 128 rows 174 and 175 us, 256 rows 289 and 222 us, 512 rows 491 and
-// 296 us; of 16 workers' 256 rows x 129 x 333 24 and 24 us.
-constexpr int kAlignRows = 192;
+// Rows of bf16 whose length is no multiple of eight are copied to such a multiple, with zeros, where the products gain more by it than the copies take: aligned operands
+// go to LDS by themselves.  An element of h is worth a copy from that many classes on, one of W from that many rows: gradients of 8 workers' rows x 1024 x 8001 classes, as
+// they lie and by copies of W: 128 rows 174 and 175 us, 256 rows 289 and 222 us, 512 rows 491 and 296 us; of 16 workers' 256 rows x 129 x 333 24 and 24 us.
+constexpr double kWorthACopy = 160, kWorthACopyForward = 256;
+constexpr int64_t kLeastAligned = (int64_t)1 << 28;        // products of two elements
 constexpr int64_t eights(int64_t n) { return (n + 7) / 8 * 8; }
 
 __global__ void __launch_bounds__(kThreads) align_kernel(Operand from, Operand to, int rows, int width, int64_t total, int lanes_log2) {
@@ -250,8 +251,13 @@ XentPlan xent_plan(int workers, int64_t rows, int width, int classes, bool class
   const size_t n = (size_t)workers * (size_t)rows, es = bf16 ? 2 : 4;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t v = at; at += (bytes + 255) / 256 * 256; return v; };
-  e.align_h = bf16 && rows >= kAlignRows && width % 8 != 0;
-  e.align_w = bf16 && rows >= kAlignRows && (classes_first ? width : classes) % 8 != 0;
+  const bool odd_h = width % 8 != 0, odd_w = (classes_first ? width : classes) % 8 != 0;
+  if (bf16 && rows > 0 && (double)n * width * classes >= (double)kLeastAligned) {
+    const double copies = (odd_h ? 1.0 / classes : 0.0) + (odd_w ? 1.0 / (double)rows : 0.0);
+    const bool worth = copies < 1.0 / (backward ? kWorthACopy : kWorthACopyForward);
+    e.align_h = odd_h && worth;
+    e.align_w = odd_w && worth;
+  }
   const int whole = (classes + 255) / 256;                 // in 256 classes
   // of a class: what a piece holds of it
   const size_t held = std::max(backward ? n : 0, e.align_w ? (size_t)workers * eights(width) : 0) * es;

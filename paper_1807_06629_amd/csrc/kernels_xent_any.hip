@@ -18,8 +18,16 @@ template <typename T, int ROWS, bool TRANS, int D, int THREADS> struct Stage {
   static __device__ __forceinline__ int row_of(int u) { return TRANS ? u % (ROWS / V) * V : u / (D / V); }
   static __device__ __forceinline__ int depth_of(int u) { return TRANS ? u / (ROWS / V) * BK : u % (D / V) * V; }
   u32x4_t reg[NPT][BK];
+  const T* at[NPT];                      // where this thread's pieces of the next tile lie
+  __device__ __forceinline__ void set(const T* base, int64_t ld) {
+#pragma unroll
+    for (int q = 0; q < NPT; ++q) {
+      const int u = q * THREADS + (int)threadIdx.x, r = row_of(u), c = depth_of(u);
+      at[q] = base + (TRANS ? (int64_t)c * ld + r : (int64_t)r * ld + c);
+    }
+  }
   // rows, depth: what is left of the operand from the tile's first element on; narrow: rows as they lie in memory are shorter than 16 bytes
-  __device__ __forceinline__ void load(const T* base, int64_t ld, int rows, int depth, bool narrow) {
+  __device__ __forceinline__ void load(int64_t ld, int rows, int depth, bool narrow) {
 #pragma unroll
     for (int q = 0; q < NPT; ++q) {
       const int u = q * THREADS + (int)threadIdx.x, r = row_of(u), c = depth_of(u);
@@ -29,10 +37,11 @@ template <typename T, int ROWS, bool TRANS, int D, int THREADS> struct Stage {
       if constexpr (TRANS) {
 #pragma unroll
         for (int k = 0; k < BK; ++k)
-          if (c + k < depth && r < rows) reg[q][k] = load_piece<ES>(base + (int64_t)(c + k) * ld + r, rows - r, narrow);
+          if (c + k < depth && r < rows) reg[q][k] = load_piece<ES>(at[q] + k * ld, rows - r, narrow);
       } else {
-        if (r < rows && c < depth) reg[q][0] = load_piece<ES>(base + (int64_t)r * ld + c, depth - c, narrow);
+        if (r < rows && c < depth) reg[q][0] = load_piece<ES>(at[q], depth - c, narrow);
       }
+      at[q] += TRANS ? D * ld : D;
     }
   }
   // rows, depth: as they were loaded; bits: of the tile's contraction elements those that take part (transposed operands)
@@ -97,7 +106,6 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, TilePosition 
   const int g = at.g, m0 = at.ti * BM, n0 = at.tj * BN, k0 = at.split * p.split_steps * D, depth = min(p.K - k0, p.split_steps * D);
   const T* a = reinterpret_cast<const T*>(p.a.p) + g * p.a.gs + (int64_t)m0 * (TA ? 1 : p.a.ld) + (int64_t)k0 * (TA ? p.a.ld : 1);
   const T* b = reinterpret_cast<const T*>(p.b.p) + g * p.b.gs + (int64_t)n0 * (TB ? 1 : p.b.ld) + (int64_t)k0 * (TB ? p.b.ld : 1);
-  const int64_t step_a = (int64_t)D * (TA ? p.a.ld : 1), step_b = (int64_t)D * (TB ? p.b.ld : 1);
   const uint32_t* real = p.real + g * real_words(p.rows);
   f32x16_t acc[TM][TN];
 #pragma unroll
@@ -108,11 +116,13 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, TilePosition 
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
   A ra;
   B rb;
+  ra.set(a, p.a.ld);
+  rb.set(b, p.b.ld);
   uint32_t bits[WORDS > 0 ? WORDS : 1] = {~0u};
   const int n_k = (depth + D - 1) / D;
-  auto load = [&](int t) __attribute__((always_inline)) {
-    ra.load(a + t * step_a, p.a.ld, p.M - m0, depth - t * D, narrow_row<T>(TA ? p.M : p.K));
-    rb.load(b + t * step_b, p.b.ld, p.N - n0, depth - t * D, narrow_row<T>(TB ? p.N : p.K));
+  auto load = [&](int t) __attribute__((always_inline)) {             // 0, 1, 2 ..
+    ra.load(p.a.ld, p.M - m0, depth - t * D, narrow_row<T>(TA ? p.M : p.K));
+    rb.load(p.b.ld, p.N - n0, depth - t * D, narrow_row<T>(TB ? p.N : p.K));
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) {
       const int at_word = (k0 + t * D) / 32 + w;
@@ -173,7 +183,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, TilePosition 
   product_epilogue<T, EPI, BM, BN, WM, WN, WK>(p, acc, at, m0, n0, wm, wn, lane, wk == 0, smem);
 }
 template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bool TB, int EPI>
-__global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(ProductArgs p) {
+__global__ void __launch_bounds__(64 * WM * WN * WK, WM * WN * WK == 8 ? 4 : 1) product_kernel(ProductArgs p) {        // eight wavefronts: two workgroups on a compute unit
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   product_tile<T, BM, BN, WM, WN, WK, D, TA, TB, EPI>(p, tile_of_workgroup(p), smem);
 }
@@ -232,8 +242,17 @@ template <typename T, bool TA, bool TB, int EPI> hipError_t launch_size(const Pr
     if (p.K <= 64) return p.N <= 32 ? launch_tile<T, 128, 32, 4, 1, 1, 32, TA, TB, EPI>(p, cut, s) : launch_tile<T, 32, 128, 1, 4, 1, 32, TA, TB, EPI>(p, cut, s);
     return p.N <= 32 ? launch_tile<T, 64, 32, 2, 1, 2, 64, TA, TB, EPI>(p, cut, s) : launch_tile<T, 32, 64, 1, 2, 2, 64, TA, TB, EPI>(p, cut, s);
   }
-  if (huge >= 256 && huge * 16 <= large * 5) return launch_tile<T, 128, 128, M128, 2, 1, 32, TA, TB, EPI>(p, cut, s);
-  if (large < 256) return launch_tile<T, 32, 32, 1, 1, 4, 128, TA, TB, EPI>(p, cut, s);
+  // What a round of tiles, one on every compute unit, takes in ns: an element of the contraction, at least what it waits for its loads, and a beginning and end
+  // (2 x 1024 rows x 1024 x 8192 fp32, logits' gradients by tiles of 128, 64 and 32: 308, 379 and 587 us; 9 x 768 x 77 x 2339: 68, 56 and 179 us).
+  auto cost = [&](int64_t tiles, int depth, double element, double wait, double ends) {
+    const double k = (double)((p.K + depth - 1) / depth * depth) / (double)p.splits, rounds = (double)((tiles + 255) / 256);
+    return rounds * (k * element + ends) > k * wait + ends ? rounds * (k * element + ends) : k * wait + ends;
+  };
+  constexpr bool F32 = sizeof(T) == 4;
+  const double by128 = cost(huge, 32, F32 ? 75 : 21.6, 47, 8000), by64 = cost(large, p.K <= 64 ? 32 : 64, F32 ? 23 : 6.4, 19, 1800);
+  const double by32 = cost(tiles_of(p, 32), 128, F32 ? 9.0 : 2.7, 9.4, 1700);
+  if (by128 <= by64 && by128 <= by32) return launch_tile<T, 128, 128, M128, 2, 1, 32, TA, TB, EPI>(p, cut, s);
+  if (by32 < by64) return launch_tile<T, 32, 32, 1, 1, 4, 128, TA, TB, EPI>(p, cut, s);
   if (p.K <= 64) return launch_tile<T, 64, 64, 2, 2, 1, 32, TA, TB, EPI>(p, cut, s);
   return launch_tile<T, 64, 64, 2, 2, 1, 64, TA, TB, EPI>(p, cut, s);
 }

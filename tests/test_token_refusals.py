@@ -178,11 +178,11 @@ def test_nothing_to_do_is_no_error(P):
 
 
 def test_workspaces_stay_bounded(P):
-    """Of the logits' gradients 128 MiB are held, or 256 classes of them; with them dh's sums, parts of products of few tiles
+    """Of the logits' gradients 256 MiB are held, or 256 classes of them; with them dh's sums, parts of products of few tiles
     (512 tiles of 64 x 64 in fp32), a bit a row, and what rounds each up to 256 bytes."""
     parts = 512 * 64 * 64 * 4
     cfg = _xent(P, dtype=1, workers=8, rows_per_worker=8192, width=64, classes=1 << 20)
-    assert P._lib.prsgd_linear_cross_entropy_backward_workspace_bytes(ctypes.byref(cfg)) <= (128 << 20) + 8 * 8192 * 64 * 4 + 8 * 8192 // 8 + parts + 4096
+    assert P._lib.prsgd_linear_cross_entropy_backward_workspace_bytes(ctypes.byref(cfg)) <= (256 << 20) + 8 * 8192 * 64 * 4 + 8 * 8192 // 8 + parts + 4096
     cfg = _xent(P, dtype=0, workers=1, rows_per_worker=1 << 20, width=64, classes=1000)
     assert P._lib.prsgd_linear_cross_entropy_backward_workspace_bytes(ctypes.byref(cfg)) <= (1 << 20) * (256 + 64) * 4 + (1 << 20) // 8 + parts + 4096
 
