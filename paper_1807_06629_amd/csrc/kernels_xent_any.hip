@@ -10,7 +10,10 @@ namespace {
 template <typename T> using Tag = std::conditional_t<kIsBf16<T>, TBF16, TF32>;
 
 // An operand's tiles, D deep, rows padded by 16 bytes.
-template <typename T, int ROWS, bool TRANS, int D, int THREADS> struct Stage {
+template <typename T_, int ROWS, bool TRANS_, int D, int THREADS_> struct Stage {
+  using T = T_;
+  static constexpr bool TRANS = TRANS_;
+  static constexpr int THREADS = THREADS_;
   static constexpr int ES = (int)sizeof(T), V = 16 / ES, LD = D * ES + 16, BYTES = ROWS * LD;
   // transposed: a thread has a block of 16 bytes of rows by BK contraction elements (fp32 4 x 4, bf16 8 x 2)
   static constexpr int BK = TRANS ? (ES == 4 ? 4 : 2) : 1;
@@ -18,16 +21,8 @@ template <typename T, int ROWS, bool TRANS, int D, int THREADS> struct Stage {
   static __device__ __forceinline__ int row_of(int u) { return TRANS ? u % (ROWS / V) * V : u / (D / V); }
   static __device__ __forceinline__ int depth_of(int u) { return TRANS ? u / (ROWS / V) * BK : u % (D / V) * V; }
   u32x4_t reg[NPT][BK];
-  const T* at[NPT];                      // where this thread's pieces of the next tile lie
-  __device__ __forceinline__ void set(const T* base, int64_t ld) {
-#pragma unroll
-    for (int q = 0; q < NPT; ++q) {
-      const int u = q * THREADS + (int)threadIdx.x, r = row_of(u), c = depth_of(u);
-      at[q] = base + (TRANS ? (int64_t)c * ld + r : (int64_t)r * ld + c);
-    }
-  }
   // rows, depth: what is left of the operand from the tile's first element on; narrow: rows as they lie in memory are shorter than 16 bytes
-  __device__ __forceinline__ void load(int64_t ld, int rows, int depth, bool narrow) {
+  template <typename P> __device__ __forceinline__ void load(P& places, int64_t ld, int rows, int depth, bool narrow) {
 #pragma unroll
     for (int q = 0; q < NPT; ++q) {
       const int u = q * THREADS + (int)threadIdx.x, r = row_of(u), c = depth_of(u);
@@ -37,11 +32,11 @@ template <typename T, int ROWS, bool TRANS, int D, int THREADS> struct Stage {
       if constexpr (TRANS) {
 #pragma unroll
         for (int k = 0; k < BK; ++k)
-          if (c + k < depth && r < rows) reg[q][k] = load_piece<ES>(at[q] + k * ld, rows - r, narrow);
+          if (c + k < depth && r < rows) reg[q][k] = load_piece<ES>(places.at[q] + k * ld, rows - r, narrow);
       } else {
-        if (r < rows && c < depth) reg[q][0] = load_piece<ES>(at[q], depth - c, narrow);
+        if (r < rows && c < depth) reg[q][0] = load_piece<ES>(places.at[q], depth - c, narrow);
       }
-      at[q] += TRANS ? D * ld : D;
+      places.at[q] += TRANS ? D * ld : D;
     }
   }
   // rows, depth: as they were loaded; bits: of the tile's contraction elements those that take part (transposed operands)
@@ -88,6 +83,18 @@ template <typename T, int ROWS, bool TRANS, int D, int THREADS> struct Stage {
   }
 };
 
+// Where a thread's pieces of the next tile lie.
+template <typename S> struct Places {
+  const typename S::T* at[S::NPT];
+  __device__ __forceinline__ void set(const typename S::T* base, int64_t ld) {
+#pragma unroll
+    for (int q = 0; q < S::NPT; ++q) {
+      const int u = q * S::THREADS + (int)threadIdx.x, r = S::row_of(u), c = S::depth_of(u);
+      at[q] = base + (S::TRANS ? (int64_t)c * ld + r : (int64_t)r * ld + c);
+    }
+  }
+};
+
 // WM x WN wavefronts, WK of them at each place, which share out a tile's depth and join their sums at the end.
 template <typename T, int BM, int BN, int WM, int WN, int WK, int D, int EPI> constexpr int lds_bytes() {
   constexpr int stages = 2 * (BM + BN) * (D * (int)sizeof(T) + 16), join = (WK - 1) * BM * BN * 4;
@@ -98,6 +105,7 @@ template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bo
 __device__ __forceinline__ void product_tile(const ProductArgs& p, TilePosition at, unsigned char* smem) {
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32, KK = D * (int)sizeof(T) / 32 / WK, THREADS = 64 * WM * WN * WK;
   static_assert(D * (int)sizeof(T) % (32 * WK) == 0, "a tile's depth splits evenly");
+  constexpr int AHEAD = WK == 4 ? 2 : 1;                   // small tiles, which are few: nothing else covers what they wait for
   constexpr int WORDS = EPI == PX_DW ? D / 32 : 0;
   using A = Stage<T, BM, TA, D, THREADS>;
   using B = Stage<T, BN, TB, D, THREADS>;
@@ -114,35 +122,46 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, TilePosition 
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-  A ra;
-  B rb;
-  ra.set(a, p.a.ld);
-  rb.set(b, p.b.ld);
-  uint32_t bits[WORDS > 0 ? WORDS : 1] = {~0u};
+  // AHEAD tiles on their way
+  A ra[AHEAD];
+  B rb[AHEAD];
+  uint32_t bits[AHEAD][WORDS > 0 ? WORDS : 1];
   const int n_k = (depth + D - 1) / D;
-  auto load = [&](int t) __attribute__((always_inline)) {             // 0, 1, 2 ..
-    ra.load(p.a.ld, p.M - m0, depth - t * D, narrow_row<T>(TA ? p.M : p.K));
-    rb.load(p.b.ld, p.N - n0, depth - t * D, narrow_row<T>(TB ? p.N : p.K));
+  Places<A> pa;
+  Places<B> pb;
+  pa.set(a, p.a.ld);
+  pb.set(b, p.b.ld);
+  auto load = [&](int t, auto set_) __attribute__((always_inline)) {         // 0, 1, 2 ..
+    constexpr int set = decltype(set_)::value;
+    if (t >= n_k) return;
+    ra[set].load(pa, p.a.ld, p.M - m0, depth - t * D, narrow_row<T>(TA ? p.M : p.K));
+    rb[set].load(pb, p.b.ld, p.N - n0, depth - t * D, narrow_row<T>(TB ? p.N : p.K));
+    if constexpr (WORDS == 0) bits[set][0] = ~0u;
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) {
       const int at_word = (k0 + t * D) / 32 + w;
       // (written by this launch, where a workgroup makes all of a worker's products)
-      bits[w] = at_word < real_words(p.rows) ? __hip_atomic_load(const_cast<uint32_t*>(real) + at_word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) : 0;
+      bits[set][w] = at_word < real_words(p.rows) ? __hip_atomic_load(const_cast<uint32_t*>(real) + at_word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) : 0;
     }
   };
-  auto store = [&](int t) __attribute__((always_inline)) {
+  auto store = [&](int t, auto set_) __attribute__((always_inline)) {
+    constexpr int set = decltype(set_)::value;
+    if (t >= n_k) return;
     unsigned char* stage = smem + (t & 1) * STAGE;
-    ra.store(stage, p.M - m0, depth - t * D, bits);
-    rb.store(stage + A::BYTES, p.N - n0, depth - t * D, bits);
+    ra[set].store(stage, p.M - m0, depth - t * D, bits[set]);
+    rb[set].store(stage + A::BYTES, p.N - n0, depth - t * D, bits[set]);
   };
-  if (n_k > 0) {
-    load(0);
-    store(0);
-  }
+  using First = std::integral_constant<int, 0>;
+  using Second = std::integral_constant<int, AHEAD - 1>;
+  load(0, First{});
+  if constexpr (AHEAD == 2) load(1, Second{});
+  store(0, First{});
+  if constexpr (AHEAD == 2) load(2, First{});
   __syncthreads();
-  for (int t = 0; t < n_k; ++t) {
+  // tile t + 1 is in set (t + 1) mod AHEAD
+  auto step = [&](int t, auto next_) __attribute__((always_inline)) {
     const unsigned char* here = smem + (t & 1) * STAGE;
-    if (t + 1 < n_k) load(t + 1);
+    if constexpr (AHEAD == 1) load(t + 1, next_);
 #pragma unroll
     for (int k = 0; k < KK; ++k) {
       const int kk = wk * KK + k;
@@ -156,8 +175,13 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, TilePosition 
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = mma(fa[i], fb[j], acc[i][j]);
     }
-    if (t + 1 < n_k) store(t + 1);
+    store(t + 1, next_);
+    if constexpr (AHEAD == 2) load(t + 3, next_);
     __syncthreads();
+  };
+  for (int t = 0; t < n_k; t += 2) {
+    step(t, Second{});
+    if (t + 1 < n_k) step(t + 1, First{});
   }
   if constexpr (WK > 1) {
     float* sums = reinterpret_cast<float*>(smem);            // [WK - 1][WM * WN][TM * TN][16][64]

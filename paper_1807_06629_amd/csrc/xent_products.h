@@ -220,13 +220,16 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& p, const f32
   }
 }
 
-// Limit of a kernel's dynamic LDS, raised once (twice is harmless).
+// Limit of a kernel's dynamic LDS, raised once on every device (twice is harmless).
 template <auto KERNEL> hipError_t allow_lds(int bytes) {
   if (bytes <= 64 * 1024) return hipSuccess;
-  static std::atomic<bool> configured{false};
-  if (configured.load(std::memory_order_acquire)) return hipSuccess;
+  static std::atomic<uint64_t> configured{0};
+  int device = 0;
+  if (const hipError_t e = hipGetDevice(&device); e != hipSuccess) return e;
+  const uint64_t bit = device < 64 ? (uint64_t)1 << device : 0;
+  if ((configured.load(std::memory_order_acquire) & bit) != 0) return hipSuccess;
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == hipSuccess) configured.store(true, std::memory_order_release);
+  if (e == hipSuccess) configured.fetch_or(bit, std::memory_order_release);
   return e;
 }
 
