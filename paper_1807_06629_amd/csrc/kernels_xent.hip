@@ -218,7 +218,7 @@ hipError_t launch_xent_backward(const XentArgs& x, const XentPlan& plan, char* w
     p.out_ld = dz.ld;
     p.out_gs = dz.gs;
     p.splits = 1;
-    const bool small = plan.pieces == 1 && small_gradients(x.rows, x.width, x.classes);
+    const bool small = plan.pieces == 1 && small_gradients(x.rows, x.width, x.classes, bf16);
     const ProductArgs dz_of = p;
     Cut cut;
     if (!small && (e = launch_product(p, PX_DZ, false, !x.classes_first, bf16, &cut, s)) != hipSuccess) return e;

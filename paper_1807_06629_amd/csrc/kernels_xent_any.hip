@@ -21,26 +21,31 @@ template <typename T_, int ROWS, bool TRANS_, int D, int THREADS_> struct Stage 
   static __device__ __forceinline__ int row_of(int u) { return TRANS ? u % (ROWS / V) * V : u / (D / V); }
   static __device__ __forceinline__ int depth_of(int u) { return TRANS ? u / (ROWS / V) * BK : u % (D / V) * V; }
   u32x4_t reg[NPT][BK];
-  // rows, depth: what is left of the operand from the tile's first element on; narrow: rows as they lie in memory are shorter than 16 bytes
-  template <typename P> __device__ __forceinline__ void load(P& places, int64_t ld, int rows, int depth, bool narrow) {
+  uint32_t part[NPT];                    // of 32 elements of the contraction, this thread's among them, those that take part (MASKED)
+  // rows, depth: what is left of the operand from the tile's first element on; NARROW: rows as they lie in memory may be shorter than 16 bytes; at: the tile's
+  // first element of the contraction, in `words` of 32
+  template <bool NARROW, bool MASKED, typename P>
+  __device__ __forceinline__ void load(P& places, int64_t ld, int rows, int depth, bool narrow, const uint32_t* words, int at, int last_word) {
 #pragma unroll
     for (int q = 0; q < NPT; ++q) {
       const int u = q * THREADS + (int)threadIdx.x, r = row_of(u), c = depth_of(u);
+      // (written by this launch, where a workgroup makes all of a worker's products; past the last word any, as no element is loaded there)
+      if constexpr (MASKED) part[q] = __hip_atomic_load(const_cast<uint32_t*>(words) + min((at + c) / 32, last_word), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
 #pragma unroll
       for (int k = 0; k < BK; ++k) reg[q][k] = (u32x4_t){0, 0, 0, 0};
       if (UNITS % THREADS != 0 && u >= UNITS) continue;
       if constexpr (TRANS) {
 #pragma unroll
         for (int k = 0; k < BK; ++k)
-          if (c + k < depth && r < rows) reg[q][k] = load_piece<ES>(places.at[q] + k * ld, rows - r, narrow);
+          if (c + k < depth && r < rows) reg[q][k] = load_piece<ES>(places.at[q] + k * ld, rows - r, NARROW && narrow);
       } else {
-        if (r < rows && c < depth) reg[q][0] = load_piece<ES>(places.at[q], depth - c, narrow);
+        if (r < rows && c < depth) reg[q][0] = load_piece<ES>(places.at[q], depth - c, NARROW && narrow);
       }
       places.at[q] += TRANS ? D * ld : D;
     }
   }
-  // rows, depth: as they were loaded; bits: of the tile's contraction elements those that take part (transposed operands)
-  template <int WORDS> __device__ __forceinline__ void store(unsigned char* tile, int rows, int depth, const uint32_t (&bits)[WORDS]) {
+  // rows, depth: as they were loaded
+  template <bool MASKED> __device__ __forceinline__ void store(unsigned char* tile, int rows, int depth) {
 #pragma unroll
     for (int q = 0; q < NPT; ++q) {
       const int u = q * THREADS + (int)threadIdx.x, r = row_of(u), c = depth_of(u);
@@ -52,14 +57,11 @@ template <typename T_, int ROWS, bool TRANS_, int D, int THREADS_> struct Stage 
       }
       if constexpr (TRANS) {
         u32x4_t v[BK];
-        uint32_t part = bits[0];
-#pragma unroll
-        for (int w = 1; w < WORDS; ++w) part = c / 32 == w ? bits[w] : part;
-        if constexpr (WORDS > 1 || D == 32) part >>= c % 32;
+        const uint32_t bits = MASKED ? part[q] >> c % 32 : ~0u;
 #pragma unroll
         for (int k = 0; k < BK; ++k)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[k][e] = (part >> k & 1) != 0 ? reg[q][k][e] : 0;
+          for (int e = 0; e < 4; ++e) v[k][e] = (bits >> k & 1) != 0 ? reg[q][k][e] : 0;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           unsigned char* to = tile + (r + e) * LD + c * ES;
@@ -83,6 +85,8 @@ template <typename T_, int ROWS, bool TRANS_, int D, int THREADS_> struct Stage 
   }
 };
 
+template <typename T> __host__ __device__ constexpr bool narrow_operand(const Operand& o, int contiguous) { return !o.padded && narrow_row<T>(contiguous); }
+
 // Where a thread's pieces of the next tile lie.
 template <typename S> struct Places {
   const typename S::T* at[S::NPT];
@@ -101,12 +105,13 @@ template <typename T, int BM, int BN, int WM, int WN, int WK, int D, int EPI> co
   constexpr int epilogue = epilogue_lds_bytes<BM, BN, WM, WN, EPI>(), most = stages > join ? stages : join;
   return most > epilogue ? most : epilogue;
 }
-template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bool TB, int EPI>
+template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bool TB, int EPI, bool NARROW = false>
 __device__ __forceinline__ void product_tile(const ProductArgs& p, TilePosition at, unsigned char* smem) {
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32, KK = D * (int)sizeof(T) / 32 / WK, THREADS = 64 * WM * WN * WK;
   static_assert(D * (int)sizeof(T) % (32 * WK) == 0, "a tile's depth splits evenly");
-  constexpr int AHEAD = WK == 4 ? 2 : 1;                   // small tiles, which are few: nothing else covers what they wait for
-  constexpr int WORDS = EPI == PX_DW ? D / 32 : 0;
+  constexpr int AHEAD = WK == 4 && !NARROW ? 2 : 1;                   // small tiles, which are few: nothing else covers what they wait for
+  constexpr bool MASKED = EPI == PX_DW;
+  static_assert(!MASKED || D % 32 == 0, "words of 32 rows");
   using A = Stage<T, BM, TA, D, THREADS>;
   using B = Stage<T, BN, TB, D, THREADS>;
   constexpr int STAGE = A::BYTES + B::BYTES;
@@ -125,8 +130,11 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, TilePosition 
   // AHEAD tiles on their way
   A ra[AHEAD];
   B rb[AHEAD];
-  uint32_t bits[AHEAD][WORDS > 0 ? WORDS : 1];
   const int n_k = (depth + D - 1) / D;
+  // what is left of the operands from the tile on; zeros behind the end of a padded one are loaded with the rest
+  auto whole = [](const Operand& o, int n) { return o.padded ? (n + 7) / 8 * 8 : n; };
+  const int a_rows = (TA ? whole(p.a, p.M) : p.M) - m0, b_rows = (TB ? whole(p.b, p.N) : p.N) - n0;
+  const int a_depth = TA ? depth : whole(p.a, depth), b_depth = TB ? depth : whole(p.b, depth);
   Places<A> pa;
   Places<B> pb;
   pa.set(a, p.a.ld);
@@ -134,22 +142,16 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, TilePosition 
   auto load = [&](int t, auto set_) __attribute__((always_inline)) {         // 0, 1, 2 ..
     constexpr int set = decltype(set_)::value;
     if (t >= n_k) return;
-    ra[set].load(pa, p.a.ld, p.M - m0, depth - t * D, narrow_row<T>(TA ? p.M : p.K));
-    rb[set].load(pb, p.b.ld, p.N - n0, depth - t * D, narrow_row<T>(TB ? p.N : p.K));
-    if constexpr (WORDS == 0) bits[set][0] = ~0u;
-#pragma unroll
-    for (int w = 0; w < WORDS; ++w) {
-      const int at_word = (k0 + t * D) / 32 + w;
-      // (written by this launch, where a workgroup makes all of a worker's products)
-      bits[set][w] = at_word < real_words(p.rows) ? __hip_atomic_load(const_cast<uint32_t*>(real) + at_word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) : 0;
-    }
+    const int last_word = (int)real_words(p.rows) - 1;
+    ra[set].template load<NARROW, MASKED>(pa, p.a.ld, a_rows, a_depth - t * D, narrow_operand<T>(p.a, TA ? p.M : p.K), real, k0 + t * D, last_word);
+    rb[set].template load<NARROW, MASKED>(pb, p.b.ld, b_rows, b_depth - t * D, narrow_operand<T>(p.b, TB ? p.N : p.K), real, k0 + t * D, last_word);
   };
   auto store = [&](int t, auto set_) __attribute__((always_inline)) {
     constexpr int set = decltype(set_)::value;
     if (t >= n_k) return;
     unsigned char* stage = smem + (t & 1) * STAGE;
-    ra[set].store(stage, p.M - m0, depth - t * D, bits[set]);
-    rb[set].store(stage + A::BYTES, p.N - n0, depth - t * D, bits[set]);
+    ra[set].template store<MASKED>(stage, a_rows, a_depth - t * D);
+    rb[set].template store<MASKED>(stage + A::BYTES, b_rows, b_depth - t * D);
   };
   using First = std::integral_constant<int, 0>;
   using Second = std::integral_constant<int, AHEAD - 1>;
@@ -206,10 +208,10 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, TilePosition 
   }
   product_epilogue<T, EPI, BM, BN, WM, WN, WK>(p, acc, at, m0, n0, wm, wn, lane, wk == 0, smem);
 }
-template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bool TB, int EPI>
+template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bool TB, int EPI, bool NARROW>
 __global__ void __launch_bounds__(64 * WM * WN * WK, WM * WN * WK == 8 ? 4 : 1) product_kernel(ProductArgs p) {        // eight wavefronts: two workgroups on a compute unit
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  product_tile<T, BM, BN, WM, WN, WK, D, TA, TB, EPI>(p, tile_of_workgroup(p), smem);
+  product_tile<T, BM, BN, WM, WN, WK, D, TA, TB, EPI, NARROW>(p, tile_of_workgroup(p), smem);
 }
 
 // All of a worker's products one after another.
@@ -245,16 +247,18 @@ template <typename T, bool CF> hipError_t launch_small(ProductArgs& dz, ProductA
   return hipGetLastError();
 }
 
-template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bool TB, int EPI> hipError_t launch_tile(ProductArgs p, Cut* cut, hipStream_t s) {
+template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bool TB, int EPI, bool NARROW = false> hipError_t launch_tile(ProductArgs p, Cut* cut, hipStream_t s) {
   constexpr int kLds = lds_bytes<T, BM, BN, WM, WN, WK, D, EPI>();
   static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
-  constexpr auto kernel = product_kernel<T, BM, BN, WM, WN, WK, D, TA, TB, EPI>;
+  constexpr auto kernel = product_kernel<T, BM, BN, WM, WN, WK, D, TA, TB, EPI, NARROW>;
   if (const hipError_t e = allow_lds<kernel>(kLds); e != hipSuccess) return e;
   const unsigned grid = cut_product(p, BM, BN, D, cut);
   hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * WM * WN * WK), kLds, s, p);
   return hipGetLastError();
 }
 template <typename T, bool TA, bool TB, int EPI> hipError_t launch_size(const ProductArgs& p, Cut* cut, hipStream_t s) {
+  // rows shorter than 16 bytes: one kernel, which alone has what it takes to load them
+  if (narrow_operand<T>(p.a, TA ? p.M : p.K) || narrow_operand<T>(p.b, TB ? p.N : p.K)) return launch_tile<T, 32, 32, 1, 1, 4, 128, TA, TB, EPI, true>(p, cut, s);
   constexpr int M128 = sizeof(T) == 4 && EPI != PX_DW ? 4 : 2;
   const int64_t huge = tiles_of(p, 128), large = tiles_of(p, 64);
   if constexpr (EPI == PX_STATS) {
@@ -295,11 +299,12 @@ constexpr int64_t kSmallSteps = 8;
 
 }  // namespace
 
-bool small_gradients(int64_t rows, int width, int classes) {
+bool small_gradients(int64_t rows, int width, int classes, bool bf16) {
   auto t = [](int64_t n, int b) { return (n + b - 1) / b; };
   const int64_t r = t(rows, 32), c = t(classes, 32), w = t(width, 128);
   // steps of the contraction and a tile's beginning and end
-  return rows > 0 && r * c * (1 + w) + r * w * (1 + c) + w * c * (1 + r) <= kSmallSteps;
+  const int least = bf16 ? 8 : 4;          // rows of 16 bytes
+  return rows > 0 && width >= least && classes >= least && r * c * (1 + w) + r * w * (1 + c) + w * c * (1 + r) <= kSmallSteps;
 }
 hipError_t launch_small_gradients(ProductArgs dz, ProductArgs dh, ProductArgs dw, bool classes_first, bool bf16, hipStream_t s) {
   if (bf16) return classes_first ? launch_small<uint16_t, true>(dz, dh, dw, s) : launch_small<uint16_t, false>(dz, dh, dw, s);

@@ -45,7 +45,7 @@ template <typename T> __device__ __forceinline__ float raw_at(const Raw8<T>& v, 
   else return __uint_as_float((e & 1) != 0 ? v.q[0][e / 2] & 0xFFFF0000u : v.q[0][e / 2] << 16);
 }
 // WHOLE: rows are whole eights, so that no lane has a part of one; n > 0
-template <typename T> __device__ __forceinline__ bool narrow_row(int width) { return width < 16 / (int)sizeof(T); }
+template <typename T> __host__ __device__ constexpr bool narrow_row(int width) { return width < 16 / (int)sizeof(T); }
 template <bool WHOLE = false, typename T> __device__ __forceinline__ void raw_load(Raw8<T>& v, const T* p, int n, bool narrow) {
   constexpr int ES = (int)sizeof(T), V = 16 / ES;
 #pragma unroll

@@ -251,7 +251,7 @@ inline unsigned cut_product(ProductArgs& p, int bm, int bn, int depth, Cut* cut)
 constexpr int kLeastTile = 32;
 hipError_t launch_product_any(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, bool bf16, Cut* cut, hipStream_t s);
 // The gradients' three products one after another, by a workgroup a worker, where that takes less than their launches.
-bool small_gradients(int64_t rows, int width, int classes);
+bool small_gradients(int64_t rows, int width, int classes, bool bf16);
 hipError_t launch_small_gradients(ProductArgs dz, ProductArgs dh, ProductArgs dw, bool classes_first, bool bf16, hipStream_t s);
 // ... and bf16 operands whose rows start at 16 bytes and are as long in whole (kernels_xent_bf16.hip).
 bool product_aligned(const ProductArgs& p, bool a_transposed, bool b_transposed);
