@@ -1,5 +1,6 @@
 // The cross entropy's products of operands of any alignment and size, in fp32 (products and sums) or bf16 (sums in fp32): tiles pass through registers into
 // LDS, [row][contraction] whichever way they lie in memory and twice, the next one on its way while the matrix cores take the last.
+// Tiles of 128 x 128 fp32 reach 90 to 105 TFLOP/s (a large library product 153), bound by the step's barrier; bf16 430 TFLOP/s.
 #include "row_pieces.h"
 #include "xent_products.h"
 

@@ -67,6 +67,16 @@ def test_gradients_of_every_length_and_of_common_tokens(P, rows, kind):
         _check_gradient(P, _rand(3, workers * rows, 12, dtype=BF16), _tokens(rows, workers * rows, classes, kind), table, 0.5)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kind", ["any", "few", "one", "none"])
+@pytest.mark.parametrize("rows", [1, 5, 127, 128, 130, 255, 256, 257])
+def test_gradients_of_few_rows(P, rows, kind, dtype):
+    """A launch has ranges of the table's rows up to 256 rows of a worker; tables of one range, of many and of ranges of a row each."""
+    for workers, classes, width in ((1, 7, 530), (3, 1000, 41), (1, 20000, 16), (600 if rows < 10 else 4, 3, 9)):
+        table = _rand(1, workers, classes, width, dtype=dtype)
+        _check_gradient(P, _rand(3, workers * rows, width, dtype=dtype), _tokens(rows, workers * rows, classes, kind), table, 1.5)
+
+
 def test_chunks_grow_with_the_rows(P):
     """More than 256 chunks of 64 sorted tokens: chunks are larger then."""
     rows, classes = 40001, 11
