@@ -56,7 +56,6 @@ hipError_t launch_product(const ProductArgs& p, int epi, bool a_transposed, bool
 }
 template <int EPI> hipError_t launch_gradient(ProductArgs p, bool a_transposed, bool b_transposed, bool bf16, hipStream_t s) {
   Cut cut;
-  p.splits = splits_of(p.M, p.N, p.K, p.groups);
   const hipError_t e = launch_product(p, EPI, a_transposed, b_transposed, bf16, &cut, s);
   if (e != hipSuccess || cut.splits == 1) return e;
   p.splits = cut.splits;
@@ -228,8 +227,7 @@ hipError_t launch_xent_backward(const XentArgs& x, const XentPlan& plan, char* w
     p.out_ld = x.dh_row;
     p.out_gs = x.rows * x.dh_row;
     p.sums = plan.pieces > 1 ? reinterpret_cast<float*>(ws + plan.sums) : nullptr;
-    const ProductArgs dh_of = p;
-    if (!small && (e = launch_gradient<PX_DH>(p, false, x.classes_first, bf16, s)) != hipSuccess) return e;
+    ProductArgs dh = p;
     p.a = x.classes_first ? dz : rows;
     p.b = x.classes_first ? rows : dz;
     p.M = x.classes_first ? n : x.width;
@@ -238,7 +236,15 @@ hipError_t launch_xent_backward(const XentArgs& x, const XentPlan& plan, char* w
     p.out = (char*)x.dw + dw_at * es;
     p.out_ld = x.dw_row;
     p.out_gs = x.dw_gs;
-    if (small) return launch_small_gradients(dz_of, dh_of, p, x.classes_first, bf16, s);
+    if (small) return launch_small_gradients(dz_of, dh, p, x.classes_first, bf16, s);
+    dh.splits = splits_of(dh.M, dh.N, dh.K, dh.groups);
+    p.splits = splits_of(p.M, p.N, p.K, p.groups);
+    if (pair_gradients(dh, p, n, x.width, bf16)) {
+      const bool aligned = bf16 && product_aligned(dh, false, x.classes_first) && product_aligned(p, true, true);
+      if ((e = aligned ? launch_pair_bf16(dh, p, x.classes_first, s) : launch_pair_any(dh, p, x.classes_first, bf16, s)) != hipSuccess) return e;
+      continue;
+    }
+    if ((e = launch_gradient<PX_DH>(dh, false, x.classes_first, bf16, s)) != hipSuccess) return e;
     if ((e = launch_gradient<PX_DW>(p, true, true, bf16, s)) != hipSuccess) return e;
   }
   return hipSuccess;

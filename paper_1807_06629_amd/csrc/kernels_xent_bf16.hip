@@ -89,14 +89,12 @@ template <int BM, int BN, int WM, int WN, int S, int EPI> constexpr int lds_byte
 
 // WM x WN wavefronts, S tiles in LDS.
 template <int BM, int BN, int WM, int WN, int S, bool TA, bool TB, int EPI>
-__global__ void __launch_bounds__(64 * WM * WN, 2) product_bf16_kernel(const ProductArgs p) {
+__device__ __forceinline__ void product_bf16_tile(const ProductArgs& p, const TilePosition place_of, unsigned char* smem) {
   constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, KK = 4, STAGE = (BM + BN) * kRowBytes, READS = TM + TN;
   using ReqA = Requests<BM, NW, TA>;
   using ReqB = Requests<BN, NW, TB>;
   constexpr int PER = ReqA::NPT + ReqB::NPT;
-  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
-  const TilePosition place_of = tile_of_workgroup(p);
   const int g = place_of.g, m0 = place_of.ti * BM, n0 = place_of.tj * BN, step0 = place_of.split * p.split_steps;
   const int depth = min(p.K - step0 * kDepth, p.split_steps * kDepth);
 
@@ -198,6 +196,27 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) product_bf16_kernel(const Pro
   product_epilogue<uint16_t, EPI, BM, BN, WM, WN, 1>(p, acc, place_of, m0, n0, wm, wn, lane, true, smem);
 }
 
+template <int BM, int BN, int WM, int WN, int S, bool TA, bool TB, int EPI>
+__global__ void __launch_bounds__(64 * WM * WN, 2) product_bf16_kernel(const ProductArgs p) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  product_bf16_tile<BM, BN, WM, WN, S, TA, TB, EPI>(p, tile_of_workgroup(p, blockIdx.x), smem);
+}
+// dh by the first workgroups, dW by the others
+template <bool CF> __global__ void __launch_bounds__(256, 2) pair_bf16_kernel(const ProductArgs dh, const ProductArgs dw, int first_dw) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  if ((int)blockIdx.x < first_dw) product_bf16_tile<64, 64, 2, 2, 3, false, CF, PX_DH>(dh, tile_of_workgroup(dh, blockIdx.x), smem);
+  else product_bf16_tile<64, 64, 2, 2, 3, true, true, PX_DW>(dw, tile_of_workgroup(dw, blockIdx.x - first_dw), smem);
+}
+template <bool CF> hipError_t launch_pair(ProductArgs dh, ProductArgs dw, hipStream_t s) {
+  constexpr int kLds = lds_bytes<64, 64, 2, 2, 3, PX_DH>();
+  constexpr auto kernel = pair_bf16_kernel<CF>;
+  if (const hipError_t e = allow_lds<kernel>(kLds); e != hipSuccess) return e;
+  Cut cut;
+  const unsigned n_dh = cut_product(dh, 64, 64, kDepth, &cut), n_dw = cut_product(dw, 64, 64, kDepth, &cut);
+  hipLaunchKernelGGL(kernel, dim3(n_dh + n_dw), dim3(256), kLds, s, dh, dw, (int)n_dh);
+  return hipGetLastError();
+}
+
 template <int BM, int BN, int WM, int WN, int S, bool TA, bool TB, int EPI> hipError_t launch_tile(ProductArgs p, Cut* cut, hipStream_t s) {
   static_assert(S >= 2, "a step's tile and the next one");
   constexpr int kLds = lds_bytes<BM, BN, WM, WN, S, EPI>();
@@ -233,6 +252,9 @@ bool product_aligned(const ProductArgs& p, bool a_transposed, bool b_transposed)
          operand_aligned(p.b, whole(p.b, b_transposed ? p.N : p.K), b_transposed ? p.K : p.N, p.groups);
 }
 
+hipError_t launch_pair_bf16(const ProductArgs& dh, const ProductArgs& dw, bool classes_first, hipStream_t s) {
+  return classes_first ? launch_pair<true>(dh, dw, s) : launch_pair<false>(dh, dw, s);
+}
 hipError_t launch_product_bf16(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, Cut* cut, hipStream_t s) {
   switch (epi) {
     case PX_STATS: return a_transposed ? launch<true, false, PX_STATS>(p, cut, s) : launch<false, false, PX_STATS>(p, cut, s);

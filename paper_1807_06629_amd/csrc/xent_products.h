@@ -64,9 +64,9 @@ __device__ __forceinline__ int acc_row(int e, int lane) { return 8 * (e / 4) + 4
 
 // Consecutive workgroups go to the XCDs in turn; each gets a contiguous range of the tiles, so that what neighbours share stays in its L2.
 struct TilePosition { int g, ti, tj, split; };
-__device__ __forceinline__ TilePosition tile_of_workgroup(const ProductArgs& p) {
-  const int tiles = p.tiles_m * p.tiles_n, total = tiles * p.groups * p.splits, xcd = blockIdx.x & 7;
-  const int idx = xcd * (total >> 3) + min(xcd, total & 7) + (int)(blockIdx.x >> 3), part = idx / tiles, in = idx - part * tiles, g = part % p.groups;
+__device__ __forceinline__ TilePosition tile_of_workgroup(const ProductArgs& p, unsigned block) {
+  const int tiles = p.tiles_m * p.tiles_n, total = tiles * p.groups * p.splits, xcd = block & 7;
+  const int idx = xcd * (total >> 3) + min(xcd, total & 7) + (int)(block >> 3), part = idx / tiles, in = idx - part * tiles, g = part % p.groups;
   // strips four tiles high, column by column
   constexpr int kHigh = 4;
   const int strip = in / (kHigh * p.tiles_n), first = strip * kHigh, high = min(kHigh, p.tiles_m - first), rest = in - first * p.tiles_n;
@@ -253,6 +253,10 @@ hipError_t launch_product_any(const ProductArgs& p, int epi, bool a_transposed, 
 // The gradients' three products one after another, by a workgroup a worker, where that takes less than their launches.
 bool small_gradients(int64_t rows, int width, int classes, bool bf16);
 hipError_t launch_small_gradients(ProductArgs dz, ProductArgs dh, ProductArgs dw, bool classes_first, bool bf16, hipStream_t s);
+// dh and dW in one launch, where they are small (splits is set as wished in both).
+bool pair_gradients(const ProductArgs& dh, const ProductArgs& dw, int classes, int width, bool bf16);
+hipError_t launch_pair_any(const ProductArgs& dh, const ProductArgs& dw, bool classes_first, bool bf16, hipStream_t s);
+hipError_t launch_pair_bf16(const ProductArgs& dh, const ProductArgs& dw, bool classes_first, hipStream_t s);
 // ... and bf16 operands whose rows start at 16 bytes and are as long in whole (kernels_xent_bf16.hip).
 bool product_aligned(const ProductArgs& p, bool a_transposed, bool b_transposed);
 hipError_t launch_product_bf16(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, Cut* cut, hipStream_t s);
