@@ -155,7 +155,10 @@ template <typename T, bool BACK, int NW, int R, int CL, bool VEC, int OCC, int M
     clear_rest<T, BACK, MODE>(p, (int)(blockIdx.x - workgroups));
     return;
   }
-  const int slot = blockIdx.x / tiles, c_wg = (blockIdx.x - slot * tiles) * CH;
+  // Workgroups go to the XCDs in turn.  Those of half a line of bf16 that lie side by side go to one, so that they meet in its L2.
+  int block = blockIdx.x;
+  if constexpr (CL < 8) block = (block & 7) * (workgroups >> 3) + min(block & 7, workgroups & 7) + (block >> 3);
+  const int slot = block / tiles, c_wg = (block - slot * tiles) * CH;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid % kWave, part = lane / CL, cl = lane % CL * 8;
   const int c = c_wg + cl, n = p.width - c;
   int sequence = slot;                   // WHOLE
@@ -429,7 +432,7 @@ template <typename T, bool BACK> __global__ void __launch_bounds__(kThreads) sca
 template <typename T, bool VEC, int MODE> constexpr bool kLarge = sizeof(T) == 4 && !VEC && MODE == APPLY;
 template <typename T, bool BACK, int NW, bool VEC, int MODE, int R = BACK && kLarge<T, VEC, MODE> ? 1 : 2, int CL = kTile / 8>
 hipError_t launch_scan(const ScanArgs& p, hipStream_t s) {
-  constexpr int OCC = BACK || R > 2 || kLarge<T, VEC, MODE> ? 2 : 4;
+  constexpr int OCC = BACK || CL < 8 || kLarge<T, VEC, MODE> ? 2 : 4;
   const int tiles = (p.width + 8 * CL - 1) / (8 * CL);
   const unsigned others = MODE != COMPOSE && p.starts != nullptr && (p.clear != 0 || MODE == APPLY) ? kClearers : 0;
   const unsigned grid = (unsigned)tiles * (unsigned)(MODE == WHOLE ? p.sequences : p.parts) + others;
@@ -442,9 +445,15 @@ template <typename T, bool BACK, bool VEC> hipError_t launch_passes(const ScanAr
     return e != hipSuccess ? e : launch_scan<T, BACK, kWaves, VEC, APPLY>(p, s);
   }
   if (p.rows / p.sequences <= 16) return launch_scan<T, BACK, 1, VEC, WHOLE>(p, s);
-  if constexpr (!BACK) {
-    // too few workgroups for the card, and long walks: half the channels and twice the rows in hand; 4 sequences of 16384 rows x 2048 bf16 330 -> 248 us, but 64 of 1024 216 -> 318 us
-    if ((int64_t)((p.width + kTile - 1) / kTile) * p.sequences <= 128 && p.rows / p.sequences >= 2048) return launch_scan<T, BACK, kWaves, VEC, WHOLE, 4, 4>(p, s);
+  // too few workgroups for the card, and walks of some length: half the channels, and for long walks forward twice the rows in hand.  4 sequences of 16384 rows x 2048
+  // bf16 330 -> 235 us, gradients 450 -> 397 us, gradients of 3 of 605 rows x 448 fp32 18.9 -> 13.7 us; but 64 of 1024 rows 219 -> 638 us, gradients of 2 packed ones of 900 rows
+  // x 1048 17 -> 20 us.  (Odd rows in fp32 backward leave room for one row in hand: 1500 rows x 3001 93 -> 55 us.)
+  const int64_t workgroups = (int64_t)((p.width + kTile - 1) / kTile) * p.sequences, each = p.rows / p.sequences;
+  if (workgroups <= 128 && each >= (p.starts == nullptr ? 256 : 2048)) {
+    if constexpr (!BACK) {
+      if (each >= 2048) return launch_scan<T, BACK, kWaves, VEC, WHOLE, 4, 4>(p, s);
+    }
+    return launch_scan<T, BACK, kWaves, VEC, WHOLE, BACK && sizeof(T) == 4 && !VEC ? 1 : 2, 4>(p, s);
   }
   return launch_scan<T, BACK, kWaves, VEC, WHOLE>(p, s);
 }

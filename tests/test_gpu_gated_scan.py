@@ -102,9 +102,9 @@ def test_many_sequences_of_any_length_are_cut_too(P, width, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-def test_long_walks_of_few_workgroups(P, dtype):
-    """Wide rows of a long sequence that is not cut (the forward pass has its own shape there)."""
-    rows, width = 2600, 8136
+@pytest.mark.parametrize("rows,width", [(2600, 8136), (2100, 7001), (300, 3000), (256, 513), (513, 2002)])
+def test_long_walks_of_few_workgroups(P, rows, width, dtype):
+    """Wide rows of a long sequence that is not cut: workgroups have 32 channels there."""
     assert P.prsgd_gated_scan_workspace_bytes(torch.empty(rows, width, device="cuda", dtype=dtype), 1) == 0
     _check(P, rows, width, dtype, shift=3.0)
 
