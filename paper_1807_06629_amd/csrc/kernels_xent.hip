@@ -22,12 +22,17 @@ int splits_of(int64_t m, int64_t n, int64_t k, int groups) {
   const int64_t tiles = (m + 63) / 64 * ((n + 63) / 64) * groups;
   return tiles == 0 || k < 2048 ? 1 : (int)std::max<int64_t>(std::min<int64_t>(512 / tiles, k / 512), 1);
 }
-size_t parts_bytes(int64_t m, int64_t n, int64_t k, int groups) {
-  const int splits = splits_of(m, n, k, groups);
+// Of the logits' gradients: 256 tiles of 128 x 128 in all (smaller ones wait for L2), a part at least 512 deep.  Gradients of 3 workers' 31 rows x 2704 x 938 fp32 67 -> 52 us,
+// of 33 x 12 x 3010 x 20 52 -> 34 us, of 8 x 128 x 4096 x 1000 bf16 66.7 -> 64.8 us.
+int splits_of_logits(int64_t m, int64_t n, int64_t k, int groups) {
+  const int64_t tiles = (m + 127) / 128 * ((n + 127) / 128) * groups;
+  return tiles == 0 || k < 1024 ? 1 : (int)std::max<int64_t>(std::min<int64_t>(256 / tiles, k / 512), 1);
+}
+size_t parts_bytes(int64_t m, int64_t n, int splits, int groups) {
   return splits > 1 ? (size_t)splits * groups * std::max(m * parts_row(n), n * parts_row(m)) * sizeof(float) : 0;
 }
 
-// dh or dW of the parts: a lane eight columns.
+// dz, dh or dW of the parts: a lane eight columns.
 template <typename T, int EPI> __global__ void __launch_bounds__(kThreads) join_parts_kernel(ProductArgs p) {
   const int64_t per_row = (p.N + 7) / 8, part = parts_row(p.N) * p.M * p.groups, total = per_row * p.M * p.groups;
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
@@ -215,11 +220,14 @@ hipError_t launch_xent_backward(const XentArgs& x, const XentPlan& plan, char* w
     p.out_ld = dz.ld;
     p.out_gs = dz.gs;
     p.splits = 1;
+    p.parts = reinterpret_cast<float*>(ws + plan.parts);
     const bool small = plan.pieces == 1 && small_gradients(x.rows, x.width, x.classes, bf16);
     const ProductArgs dz_of = p;
-    Cut cut;
-    if (!small && (e = launch_product(p, PX_DZ, false, !x.classes_first, bf16, &cut, s)) != hipSuccess) return e;
-    p.parts = reinterpret_cast<float*>(ws + plan.parts);
+    if (!small) {
+      p.splits = splits_of_logits(p.M, p.N, p.K, p.groups);
+      if ((e = launch_gradient<PX_DZ>(p, false, !x.classes_first, bf16, s)) != hipSuccess) return e;
+      p.splits = 1;
+    }
     p.a = dz;
     p.N = x.width;
     p.K = n;
@@ -276,9 +284,12 @@ XentPlan xent_plan(int workers, int64_t rows, int width, int classes, bool class
   } else {
     e.dz = take(n * e.piece * es);
     e.sums = e.pieces > 1 ? take(n * width * sizeof(float)) : 0;
-    const int last = classes - (e.pieces - 1) * e.piece;   // classes of the last piece: of fewer tiles, and so perhaps more parts
-    e.parts = take(std::max({parts_bytes(rows, width, e.piece, workers), parts_bytes(width, std::min(e.piece, classes), rows, workers),
-                             parts_bytes(width, last, rows, workers)}));
+    size_t parts = 0;
+    for (const int n_of : {std::min(e.piece, classes), classes - (e.pieces - 1) * e.piece}) {          // the last piece has fewer tiles, and so perhaps more parts
+      parts = std::max({parts, parts_bytes(rows, n_of, splits_of_logits(rows, n_of, width, workers), workers),
+                        parts_bytes(rows, width, splits_of(rows, width, n_of, workers), workers), parts_bytes(width, n_of, splits_of(width, n_of, rows, workers), workers)});
+    }
+    e.parts = take(parts);
     e.real = take((size_t)workers * real_words(rows) * sizeof(uint32_t));
   }
   e.h = e.align_h ? take(n * eights(width) * es) : 0;

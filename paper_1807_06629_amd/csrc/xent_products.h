@@ -84,8 +84,19 @@ __device__ __forceinline__ void write_loss(float* loss, float* lse_out, int64_t 
   loss[row] = real ? lse - picked : 0.0f;
 }
 
-// Eight columns of a row of dh or dW, n of which exist.
+// Eight columns of a row of dz, dh or dW, n of which exist.
 template <typename T, int EPI> __device__ __forceinline__ void finish(const ProductArgs& p, int g, int r, int c, int n, float (&v)[8]) {
+  if constexpr (EPI == PX_DZ) {
+    const int64_t row = g * p.rows + r;
+    const int label = p.labels[row];
+    const bool real = (unsigned)label < (unsigned)p.classes;
+    const float lse = p.lse[row], weight = p.dloss[row];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = real && e < n ? weight * (exp_of<T>(v[e] - lse) - (p.class0 + c + e == label ? 1.0f : 0.0f)) : 0.0f;
+    // zeros behind the last class
+    store8(reinterpret_cast<T*>(p.out) + g * p.out_gs + (int64_t)r * p.out_ld + c, 8, v);
+    return;
+  }
   if constexpr (EPI == PX_DH) {
     const bool real = (unsigned)p.labels[g * p.rows + r] < (unsigned)p.classes;
 #pragma unroll
@@ -186,25 +197,14 @@ __device__ __forceinline__ void product_epilogue(const ProductArgs& p, const f32
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = from[e];
         const bool live = r < p.M;
-        if constexpr (EPI == PX_DZ) {
-          const int64_t row = g * p.rows + (live ? r : 0);
-          const int label = p.labels[row];
-          const bool real = live && (unsigned)label < (unsigned)p.classes;
-          const float lse = p.lse[row], weight = p.dloss[row];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = real && e < n ? weight * (exp_of<T>(v[e] - lse) - (p.class0 + c + e == label ? 1.0f : 0.0f)) : 0.0f;
-          // zeros behind the last class, up to the end of the tile or of the rows of dz (a multiple of eight)
-          if (live && c < p.out_ld) store8(reinterpret_cast<T*>(p.out) + g * p.out_gs + (int64_t)r * p.out_ld + c, 8, v);
-        } else {
-          if (!live || n <= 0) continue;
-          if (p.splits > 1) store8(p.parts + (((int64_t)at.split * p.groups + g) * p.M + r) * parts_row(p.N) + c, 8, v);
-          else finish<T, EPI>(p, g, r, c, n, v);
-        }
+        if (!live || n <= 0) continue;
+        if (p.splits > 1) store8(p.parts + (((int64_t)at.split * p.groups + g) * p.M + r) * parts_row(p.N) + c, 8, v);
+        else finish<T, EPI>(p, g, r, c, n, v);
       }
       __builtin_amdgcn_wave_barrier();
     }
     if constexpr (EPI == PX_DZ) {
-      if (p.first_piece && n0 == 0 && wn == 0) {
+      if (p.first_piece && n0 == 0 && wn == 0 && at.split == 0) {
         // rows of this wavefront: words of 32, of which behind the last row there may be one more, so that they are pairs
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
