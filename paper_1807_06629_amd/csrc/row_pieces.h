@@ -44,14 +44,13 @@ template <typename T> __device__ __forceinline__ float raw_at(const Raw8<T>& v, 
   if constexpr (sizeof(T) == 4) return __uint_as_float(v.q[e / 4][e % 4]);
   else return __uint_as_float((e & 1) != 0 ? v.q[0][e / 2] & 0xFFFF0000u : v.q[0][e / 2] << 16);
 }
-// WHOLE: rows are whole eights, so that no lane has a part of one; n > 0
+// n > 0
 template <typename T> __host__ __device__ constexpr bool narrow_row(int width) { return width < 16 / (int)sizeof(T); }
-template <bool WHOLE = false, typename T> __device__ __forceinline__ void raw_load(Raw8<T>& v, const T* p, int n, bool narrow) {
+template <typename T> __device__ __forceinline__ void raw_load(Raw8<T>& v, const T* p, int n, bool narrow) {
   constexpr int ES = (int)sizeof(T), V = 16 / ES;
 #pragma unroll
   for (int i = 0; i < 8 / V; ++i) {
-    if constexpr (WHOLE) v.q[i] = reinterpret_cast<const Packed16<ES>*>(p + i * V)->v;
-    else if (i == 0) v.q[i] = load_piece<ES>(p, n, narrow);
+    if (i == 0) v.q[i] = load_piece<ES>(p, n, narrow);
     // of a second piece that does not exist the first one once more
     else v.q[i] = load_piece<ES>(n > i * V ? p + i * V : p, n > i * V ? n - i * V : n, narrow);
   }
