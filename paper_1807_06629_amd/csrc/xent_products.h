@@ -78,10 +78,11 @@ template <int BM, int BN, int WM, int WN, int EPI> constexpr int epilogue_lds_by
   return EPI == PX_STATS ? (WM * (int)sizeof(float2) + (int)sizeof(float)) * BN : WM * WN * 32 * (BN / WN + kStripPad) * 4;
 }
 
+// The loss goes from the row's maximum, not from lse, which is rounded at the logits' size: of a label whose logit is the maximum it is log s itself.
 __device__ __forceinline__ void write_loss(float* loss, float* lse_out, int64_t row, float m, float s, bool real, float picked) {
-  const float lse = m + logf(s);
-  lse_out[row] = lse;
-  loss[row] = real ? lse - picked : 0.0f;
+  const float log_s = logf(s);
+  lse_out[row] = m + log_s;
+  loss[row] = real ? (m - picked) + log_s : 0.0f;
 }
 
 // Eight columns of a row of dz, dh or dW, n of which exist.
