@@ -220,7 +220,7 @@ int prsgd_dropout(const prsgd_dropout_config* cfg, const int64_t* step_dev, cons
 typedef struct {
   int32_t dtype;                   /* PRSGD_F32 | PRSGD_BF16: type of h, W and their gradients       */
   int32_t workers;                 /* 1..65535                                                       */
-  int64_t rows_per_worker;         /* >= 0; workers * rows_per_worker < 2^31                         */
+  int64_t rows_per_worker;         /* 0..2^31 - 256; workers * rows_per_worker < 2^31                */
   int32_t width;                   /* 1..32768                                                       */
   int32_t classes;                 /* 1..2^20                                                        */
   int32_t classes_first;           /* 0: W_i [width][classes]; 1: [classes][width], as a table of embeddings */

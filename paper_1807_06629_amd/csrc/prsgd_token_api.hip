@@ -120,10 +120,13 @@ const char* scan_buffers_error(const prsgd_scan_config* c, const ScanBuffer* row
 
 // ---- cross entropy -----------------------------------------------------------------------------
 
+// Tiles of up to 256 rows are counted in 32 bits.
+constexpr int64_t kMaxTiledRows = ((int64_t)1 << 31) - 256;
 const char* xent_error(const prsgd_xent_config* c) {
   if (c == nullptr) return "linear_cross_entropy: config is null";
   if (!type_ok(c->dtype)) return "linear_cross_entropy: unknown dtype";
   if (!rows_of_workers_ok(c->workers, c->rows_per_worker)) return "linear_cross_entropy: workers (1..65535) or rows (below 2^31 in all) out of range";
+  if (c->rows_per_worker > kMaxTiledRows) return "linear_cross_entropy: more than 2^31 - 256 rows of a worker";
   if (!classes_ok(c->classes)) return "linear_cross_entropy: classes out of range (1..2^20)";
   if (!width_ok(c->width)) return "linear_cross_entropy: width out of range (1..32768)";
   if (c->classes_first != 0 && c->classes_first != 1) return "linear_cross_entropy: classes_first must be 0 or 1";

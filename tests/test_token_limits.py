@@ -1,0 +1,45 @@
+"""Sizes at the ends of the token operators' documented ranges: refused one past them, with bounded workspaces up to them (no GPU; the addresses are never read)."""
+import ctypes
+import os
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+A = 1 << 20                                                # an aligned address that is no buffer
+
+
+@pytest.fixture(scope="module")
+def P():
+    if not os.path.exists(os.path.join(ROOT, "paper_1807_06629_amd", "libprsgd.so")):
+        from paper_1807_06629_amd.build import build
+        build()
+    from paper_1807_06629_amd import prsgd
+    return prsgd
+
+
+def _xent(P, **kw):
+    base = dict(dtype=P.PRSGD_F32, workers=1, rows_per_worker=3, width=8, classes=8, classes_first=0)
+    base.update(kw)
+    return P.prsgd_xent_config(*(base[k] for k, _ in P.prsgd_xent_config._fields_))
+
+
+def _xent_bytes(P, cfg):
+    return (P._lib.prsgd_linear_cross_entropy_workspace_bytes(ctypes.byref(cfg)),
+            P._lib.prsgd_linear_cross_entropy_backward_workspace_bytes(ctypes.byref(cfg)))
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("first", [0, 1])
+@pytest.mark.parametrize("short", [1, 2, 31, 32, 127, 255])
+def test_cross_entropy_refuses_rows_that_no_tile_can_count(P, short, first, dtype):
+    """Rows rounded up to a tile of 256 have to stay in 32 bits."""
+    cfg = _xent(P, dtype=dtype, rows_per_worker=2 ** 31 - short, classes_first=first)
+    assert _xent_bytes(P, cfg) == (0, 0) and "rows" in P.prsgd_last_error(None)
+    assert P._lib.prsgd_linear_cross_entropy(ctypes.byref(cfg), A, 8, 2 * A, 64, 8, 3 * A, 4 * A, 5 * A, 6 * A, None) == P.PRSGD_EINVAL
+    assert P._lib.prsgd_linear_cross_entropy_backward(ctypes.byref(cfg), A, 2 * A, 8, 3 * A, 64, 8, 4 * A, 5 * A, 6 * A, 8, 7 * A, 64, 8, 8 * A, None) == P.PRSGD_EINVAL
+    most = _xent(P, dtype=dtype, rows_per_worker=2 ** 31 - 256, classes_first=first)
+    assert min(_xent_bytes(P, most)) > 0
+
+
+def test_rows_of_all_workers_may_be_more(P):
+    assert min(_xent_bytes(P, _xent(P, workers=7, rows_per_worker=(2 ** 31 - 1) // 7))) > 0
