@@ -161,7 +161,7 @@ struct ChunkPlace {
   float* parts;                          // [2][part_width]: of the chunk's first run if it began before, of its last one if it goes on
   __device__ __forceinline__ bool set(const EmbeddingArgs& p, const EmbeddingPlan& plan, char* ws, int lanes_log2) {
     const int lanes = 1 << lanes_log2, slices = (p.width + kSlice - 1) / kSlice;
-    const int64_t unit = (int64_t)blockIdx.x * (kThreads >> lanes_log2) + (threadIdx.x >> lanes_log2), at = unit / slices;
+    const int64_t unit = (int64_t)workgroup_of_grid() * (kThreads >> lanes_log2) + (threadIdx.x >> lanes_log2), at = unit / slices;
     if (at >= (int64_t)plan.chunks * p.workers) return false;
     g = at / plan.chunks;
     chunk = (int)(at - g * plan.chunks);
@@ -383,7 +383,7 @@ template <typename T> hipError_t backward(const EmbeddingArgs& p, const Embeddin
   }
   const int lanes_log2 = std::min(lanes_for_row(p.width), 6), slots = kThreads >> lanes_log2;
   const int64_t chunks = (int64_t)plan.chunks * p.workers * ((p.width + kSlice - 1) / kSlice);
-  const dim3 grid((unsigned)((chunks + slots - 1) / slots));
+  const dim3 grid = grid_of((chunks + slots - 1) / slots);
   hipLaunchKernelGGL(chunk_sums_kernel<T>, grid, dim3(kThreads), 0, s, p, plan, ws, lanes_log2);
   if ((e = hipGetLastError()) != hipSuccess || plan.chunks == 1) return e;
   hipLaunchKernelGGL(join_chunks_kernel<T>, grid, dim3(kThreads), 0, s, p, plan, ws, lanes_log2);

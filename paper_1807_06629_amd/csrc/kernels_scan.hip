@@ -151,12 +151,13 @@ template <typename T, bool BACK, int NW, int R, int CL, bool VEC, int OCC, int M
   __shared__ float total[2][NW][CH][2];
   __shared__ int head[CUT ? kTableRows : 1], tail[CUT ? kTableRows : 1];
   const int workgroups = tiles * (CUT ? p.parts : p.sequences);
-  if (blockIdx.x >= (unsigned)workgroups) {
-    clear_rest<T, BACK, MODE>(p, (int)(blockIdx.x - workgroups));
+  const unsigned workgroup = workgroup_of_grid();
+  if (workgroup >= (unsigned)workgroups) {
+    if (MODE != COMPOSE && p.starts != nullptr && workgroup - workgroups < (unsigned)kClearers) clear_rest<T, BACK, MODE>(p, (int)(workgroup - workgroups));
     return;
   }
   // Workgroups go to the XCDs in turn.  Those of half a line of bf16 that lie side by side go to one, so that they meet in its L2.
-  int block = blockIdx.x;
+  int block = workgroup;
   if constexpr (CL < 8) block = (block & 7) * (workgroups >> 3) + min(block & 7, workgroups & 7) + (block >> 3);
   const int slot = block / tiles, c_wg = (block - slot * tiles) * CH;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid % kWave, part = lane / CL, cl = lane % CL * 8;
@@ -436,7 +437,7 @@ hipError_t launch_scan(const ScanArgs& p, hipStream_t s) {
   const int tiles = (p.width + 8 * CL - 1) / (8 * CL);
   const unsigned others = MODE != COMPOSE && p.starts != nullptr && (p.clear != 0 || MODE == APPLY) ? kClearers : 0;
   const unsigned grid = (unsigned)tiles * (unsigned)(MODE == WHOLE ? p.sequences : p.parts) + others;
-  hipLaunchKernelGGL((scan_kernel<T, BACK, NW, R, CL, VEC, OCC, MODE>), dim3(grid), dim3(NW * kWave), 0, s, p, tiles);
+  hipLaunchKernelGGL((scan_kernel<T, BACK, NW, R, CL, VEC, OCC, MODE>), grid_of(grid), dim3(NW * kWave), 0, s, p, tiles);
   return hipGetLastError();
 }
 template <typename T, bool BACK, bool VEC> hipError_t launch_passes(const ScanArgs& p, hipStream_t s) {

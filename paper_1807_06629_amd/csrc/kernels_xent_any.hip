@@ -9,7 +9,9 @@ namespace {
 template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bool TB, int EPI, bool NARROW>
 __global__ void __launch_bounds__(64 * WM * WN * WK, WM * WN * WK == 8 ? 4 : 1) product_kernel(ProductArgs p) {        // eight wavefronts: two workgroups on a compute unit
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  product_tile<T, BM, BN, WM, WN, WK, D, TA, TB, EPI, NARROW>(p, tile_of_workgroup(p, blockIdx.x), smem);
+  const unsigned workgroup = workgroup_of_grid();
+  if (workgroup >= workgroups_of(p)) return;
+  product_tile<T, BM, BN, WM, WN, WK, D, TA, TB, EPI, NARROW>(p, tile_of_workgroup(p, workgroup), smem);
 }
 
 template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bool TB, int EPI, bool NARROW = false> hipError_t launch_tile(ProductArgs p, Cut* cut, hipStream_t s) {
@@ -18,7 +20,7 @@ template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bo
   constexpr auto kernel = product_kernel<T, BM, BN, WM, WN, WK, D, TA, TB, EPI, NARROW>;
   if (const hipError_t e = allow_lds<kernel>(kLds); e != hipSuccess) return e;
   const unsigned grid = cut_product(p, BM, BN, D, cut);
-  hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * WM * WN * WK), kLds, s, p);
+  hipLaunchKernelGGL(kernel, grid_of(grid), dim3(64 * WM * WN * WK), kLds, s, p);
   return hipGetLastError();
 }
 template <typename T, bool TA, bool TB, int EPI> hipError_t launch_size(const ProductArgs& p, Cut* cut, hipStream_t s) {

@@ -199,7 +199,9 @@ __device__ __forceinline__ void product_bf16_tile(const ProductArgs& p, const Ti
 template <int BM, int BN, int WM, int WN, int S, bool TA, bool TB, int EPI>
 __global__ void __launch_bounds__(64 * WM * WN, 2) product_bf16_kernel(const ProductArgs p) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-  product_bf16_tile<BM, BN, WM, WN, S, TA, TB, EPI>(p, tile_of_workgroup(p, blockIdx.x), smem);
+  const unsigned workgroup = workgroup_of_grid();
+  if (workgroup >= workgroups_of(p)) return;
+  product_bf16_tile<BM, BN, WM, WN, S, TA, TB, EPI>(p, tile_of_workgroup(p, workgroup), smem);
 }
 // dh by the first workgroups, dW by the others
 template <bool CF> __global__ void __launch_bounds__(256, 2) pair_bf16_kernel(const ProductArgs dh, const ProductArgs dw, int first_dw) {
@@ -224,7 +226,7 @@ template <int BM, int BN, int WM, int WN, int S, bool TA, bool TB, int EPI> hipE
   constexpr auto kernel = product_bf16_kernel<BM, BN, WM, WN, S, TA, TB, EPI>;
   if (const hipError_t e = allow_lds<kernel>(kLds); e != hipSuccess) return e;
   const unsigned grid = cut_product(p, BM, BN, kDepth, cut);
-  hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * WM * WN), kLds, s, p);
+  hipLaunchKernelGGL(kernel, grid_of(grid), dim3(64 * WM * WN), kLds, s, p);
   return hipGetLastError();
 }
 

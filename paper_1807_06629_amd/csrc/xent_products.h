@@ -62,6 +62,10 @@ __device__ __forceinline__ void join_stats(float& m, float& s, float m2, float s
 // Rows of the accumulators: element e of a 32 x 32 block lies at row acc_row(e, lane), column lane % 32.
 __device__ __forceinline__ int acc_row(int e, int lane) { return 8 * (e / 4) + 4 * (lane >> 5) + (e & 3); }
 
+// Of a launch: below 2^31, as the calls' checks see to.
+__host__ __device__ inline unsigned workgroups_of(const ProductArgs& p) {
+  return (unsigned)p.tiles_m * (unsigned)p.tiles_n * (unsigned)p.groups * (unsigned)p.splits;
+}
 // Consecutive workgroups go to the XCDs in turn; each gets a contiguous range of the tiles, so that what neighbours share stays in its L2.
 struct TilePosition { int g, ti, tj, split; };
 __device__ __forceinline__ TilePosition tile_of_workgroup(const ProductArgs& p, unsigned block) {
@@ -244,7 +248,7 @@ inline unsigned cut_product(ProductArgs& p, int bm, int bn, int depth, Cut* cut)
   const int steps = std::max((p.K + depth - 1) / depth, 1);
   p.split_steps = (steps + p.splits - 1) / p.splits;
   cut->splits = p.splits = (steps + p.split_steps - 1) / p.split_steps;
-  return (unsigned)p.tiles_m * (unsigned)p.tiles_n * (unsigned)p.groups * (unsigned)p.splits;
+  return workgroups_of(p);
 }
 
 // transposed: (A, B) as (element (i, c) at c * ld + i).  Operands of any alignment and size (kernels_xent_any.hip) ...
