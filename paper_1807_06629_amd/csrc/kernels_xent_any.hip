@@ -10,7 +10,7 @@ template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bo
 __global__ void __launch_bounds__(64 * WM * WN * WK, WM * WN * WK == 8 ? 4 : 1) product_kernel(ProductArgs p) {        // eight wavefronts: two workgroups on a compute unit
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const unsigned workgroup = workgroup_of_grid();
-  if (workgroup >= workgroups_of(p)) return;
+  if (blockIdx.y != 0 && workgroup >= workgroups_of(p)) return;          // (nothing is waited for in a launch along one axis)
   product_tile<T, BM, BN, WM, WN, WK, D, TA, TB, EPI, NARROW>(p, tile_of_workgroup(p, workgroup), smem);
 }
 

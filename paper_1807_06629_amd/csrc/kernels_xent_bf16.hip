@@ -200,7 +200,7 @@ template <int BM, int BN, int WM, int WN, int S, bool TA, bool TB, int EPI>
 __global__ void __launch_bounds__(64 * WM * WN, 2) product_bf16_kernel(const ProductArgs p) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const unsigned workgroup = workgroup_of_grid();
-  if (workgroup >= workgroups_of(p)) return;
+  if (blockIdx.y != 0 && workgroup >= workgroups_of(p)) return;          // (nothing is waited for in a launch along one axis)
   product_bf16_tile<BM, BN, WM, WN, S, TA, TB, EPI>(p, tile_of_workgroup(p, workgroup), smem);
 }
 // dh by the first workgroups, dW by the others
