@@ -226,7 +226,10 @@ typedef struct {
   int32_t classes_first;           /* 0: W_i [width][classes]; 1: [classes][width], as a table of embeddings */
 } prsgd_xent_config;
 
-/* labels_dev, loss_dev, lse_dev [workers * rows_per_worker]; w_matrix elements from worker to worker (0: all share one). */
+/*
+ * labels_dev, loss_dev, lse_dev [workers * rows_per_worker]; w_matrix elements from worker to worker (0: all share one).  The workspace
+ * holds 8 bytes a row for every tile of classes, 32 of them where products are small, 128 or 256 where they are large.
+ */
 size_t prsgd_linear_cross_entropy_workspace_bytes(const prsgd_xent_config* cfg);
 int prsgd_linear_cross_entropy(const prsgd_xent_config* cfg, const void* h_dev, int64_t h_row, const void* w_dev,
                                int64_t w_matrix, int64_t w_row, const int32_t* labels_dev, float* loss_dev, float* lse_dev,

@@ -154,7 +154,6 @@ hipError_t operands_of_piece(const XentArgs& x, const XentPlan& plan, char* ws, 
 hipError_t launch_xent(const XentArgs& x, const XentPlan& plan, char* ws, bool bf16, hipStream_t s) {
   Cut cut{};
   int64_t stats = 0;                     // of the pieces so far, one behind another
-  const int least = (plan.piece + kLeastTile - 1) / kLeastTile;
   XentPieces pieces{};
   for (int k = 0; k < plan.pieces; ++k) {
     const int first = k * plan.piece, n = std::min(plan.piece, x.classes - first);
@@ -171,16 +170,17 @@ hipError_t launch_xent(const XentArgs& x, const XentPlan& plan, char* ws, bool b
     p.classes = x.classes;
     p.stats = reinterpret_cast<float2*>(ws + plan.stats) + stats;
     p.picked = reinterpret_cast<float*>(ws + plan.picked);
+    p.most_tiles = plan.tiles;
     p.loss_out = plan.pieces == 1 ? x.loss : nullptr;
     p.lse_out = x.lse;
     if (const hipError_t e = launch_product(p, PX_STATS, !x.classes_first, false, bf16, &cut, s); e != hipSuccess) return e;
     if (k == 0) pieces.tiles = cut.tiles_m;
     pieces.last_tiles = cut.tiles_m;
-    stats += x.rows * x.workers * least;
+    stats += x.rows * x.workers * plan.tiles;
   }
   if (plan.pieces == 1 && cut.tiles_m == 1) return hipSuccess;             // done
   pieces.pieces = plan.pieces;
-  pieces.stride = x.rows * x.workers * least;
+  pieces.stride = x.rows * x.workers * plan.tiles;
   const int tiles = (pieces.pieces - 1) * pieces.tiles + pieces.last_tiles;
   int lanes_log2 = 0;
   while (lanes_log2 < 6 && (1 << lanes_log2) < tiles) ++lanes_log2;
@@ -279,7 +279,21 @@ XentPlan xent_plan(int workers, int64_t rows, int width, int classes, bool class
   e.pieces = (classes + e.piece - 1) / e.piece;
   if (!backward) {
     if (e.pieces == 1) e.piece = classes;
-    e.stats = take(n * e.pieces * ((e.piece + kLeastTile - 1) / kLeastTile) * sizeof(float2));
+    // as many tiles as a piece gets, by whichever kernels take its operands
+    for (const int n_of : {e.piece, classes - (e.pieces - 1) * e.piece}) {
+      ProductArgs p{};
+      p.a.padded = e.align_w;
+      p.b.padded = e.align_h;
+      p.M = n_of;
+      p.N = (int)rows;
+      p.K = width;
+      p.groups = workers;
+      p.splits = 1;
+      int tile = stats_rows_any(p, !classes_first, bf16);
+      if (bf16) tile = std::min(tile, stats_rows_bf16(p));
+      e.tiles = std::max(e.tiles, (n_of + tile - 1) / tile);
+    }
+    e.stats = take(n * e.pieces * e.tiles * sizeof(float2));
     e.picked = take(n * sizeof(float));
   } else {
     e.dz = take(n * e.piece * es);

@@ -226,20 +226,30 @@ template <int BM, int BN, int WM, int WN, int S, bool TA, bool TB, int EPI> hipE
   constexpr auto kernel = product_bf16_kernel<BM, BN, WM, WN, S, TA, TB, EPI>;
   if (const hipError_t e = allow_lds<kernel>(kLds); e != hipSuccess) return e;
   const unsigned grid = cut_product(p, BM, BN, kDepth, cut);
+  if (EPI == PX_STATS && p.tiles_m > p.most_tiles) return hipErrorInvalidValue;
   hipLaunchKernelGGL(kernel, grid_of(grid), dim3(64 * WM * WN), kLds, s, p);
   return hipGetLastError();
 }
 
-template <bool TA, bool TB, int EPI> hipError_t launch(const ProductArgs& p, Cut* cut, hipStream_t s) {
+// 256 square, 128 by eight or four wavefronts, 64.
+enum Tiles { BY_256, BY_128_EIGHT, BY_128_FOUR, BY_64 };
+Tiles choose_tiles(const ProductArgs& p) {
   // Time of a launch in units of a 64 x 64 tile's products: tiles per compute unit times their size over their efficiency.  Of tiles that a compute unit has
   // several of in hand, parts of a round count as such; of 256 x 256 tiles whole rounds.
   auto cost = [](int64_t n, int b, double efficiency) { return (n < 256 ? 1.0 : (double)n / 256.0) * (b / 64) * (b / 64) / efficiency; };
   const int64_t n_middle = tiles_of(p, 128), n_huge = (tiles_of(p, 256) + 255) / 256 * 256;
   const double middle = cost(n_middle, 128, n_middle > 256 ? 0.9 : 1.34), small = cost(tiles_of(p, 64), 64, 0.68), huge = cost(n_huge, 256, 1.2);
-  if (huge <= middle && huge <= small) return launch_tile<256, 256, 4, 2, 2, TA, TB, EPI>(p, cut, s);
-  if (middle > small) return launch_tile<64, 64, 2, 2, 3, TA, TB, EPI>(p, cut, s);
-  if (n_middle <= 256) return launch_tile<128, 128, 4, 2, 3, TA, TB, EPI>(p, cut, s);
-  return launch_tile<128, 128, 2, 2, 2, TA, TB, EPI>(p, cut, s);
+  if (huge <= middle && huge <= small) return BY_256;
+  if (middle > small) return BY_64;
+  return n_middle <= 256 ? BY_128_EIGHT : BY_128_FOUR;
+}
+template <bool TA, bool TB, int EPI> hipError_t launch(const ProductArgs& p, Cut* cut, hipStream_t s) {
+  switch (choose_tiles(p)) {
+    case BY_256: return launch_tile<256, 256, 4, 2, 2, TA, TB, EPI>(p, cut, s);
+    case BY_128_EIGHT: return launch_tile<128, 128, 4, 2, 3, TA, TB, EPI>(p, cut, s);
+    case BY_128_FOUR: return launch_tile<128, 128, 2, 2, 2, TA, TB, EPI>(p, cut, s);
+    default: return launch_tile<64, 64, 2, 2, 3, TA, TB, EPI>(p, cut, s);
+  }
 }
 
 bool operand_aligned(const Operand& o, int64_t contiguous, int64_t other, int groups) {
@@ -254,6 +264,10 @@ bool product_aligned(const ProductArgs& p, bool a_transposed, bool b_transposed)
          operand_aligned(p.b, whole(p.b, b_transposed ? p.N : p.K), b_transposed ? p.K : p.N, p.groups);
 }
 
+int stats_rows_bf16(const ProductArgs& p) {
+  const Tiles t = choose_tiles(p);
+  return t == BY_256 ? 256 : t == BY_64 ? 64 : 128;
+}
 hipError_t launch_pair_bf16(const ProductArgs& dh, const ProductArgs& dw, bool classes_first, hipStream_t s) {
   return classes_first ? launch_pair<true>(dh, dw, s) : launch_pair<false>(dh, dw, s);
 }

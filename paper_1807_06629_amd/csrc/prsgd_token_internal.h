@@ -105,6 +105,7 @@ struct XentArgs {
 };
 struct XentPlan {
   int piece, pieces;                     // classes of a piece
+  int tiles;                             // forward: of a piece, at most
   bool align_h, align_w;                 // h, a piece of W: copied, each row to a multiple of 16 bytes
   size_t stats, picked, dz, sums, parts, real, h, w, total;         // byte offsets
 };

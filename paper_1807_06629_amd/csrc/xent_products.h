@@ -33,6 +33,7 @@ struct ProductArgs {
   int64_t rows;
   int class0, classes;                   // first class of the piece; of all
   float2* stats; float* picked;          // PX_STATS: [rows of all workers][tiles_m]
+  int most_tiles;                        // ... of which there is room for that many
   float* loss_out; float* lse_out;       // PX_STATS of all classes in one tile: what comes of its statistics (nullptr: these alone)
   void* out; int64_t out_gs, out_ld;     // the others
   float* sums;                           // PX_DH over several pieces: [groups][M][N] fp32
@@ -252,9 +253,11 @@ inline unsigned cut_product(ProductArgs& p, int bm, int bn, int depth, Cut* cut)
 }
 
 // transposed: (A, B) as (element (i, c) at c * ld + i).  Operands of any alignment and size (kernels_xent_any.hip) ...
-// cut: how the product was cut; tiles have kLeastTile rows at least
-constexpr int kLeastTile = 32;
+// cut: how the product was cut
 hipError_t launch_product_any(const ProductArgs& p, int epi, bool a_transposed, bool b_transposed, bool bf16, Cut* cut, hipStream_t s);
+// Rows of the tiles that PX_STATS of this size gets, by its sizes and by which operands are padded alone.
+int stats_rows_any(const ProductArgs& p, bool a_transposed, bool bf16);
+int stats_rows_bf16(const ProductArgs& p);
 // The gradients' three products one after another, by a workgroup a worker, where that takes less than their launches.
 bool small_gradients(int64_t rows, int width, int classes, bool bf16);
 hipError_t launch_small_gradients(ProductArgs dz, ProductArgs dh, ProductArgs dw, bool classes_first, bool bf16, hipStream_t s);

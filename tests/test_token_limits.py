@@ -43,3 +43,13 @@ def test_cross_entropy_refuses_rows_that_no_tile_can_count(P, short, first, dtyp
 
 def test_rows_of_all_workers_may_be_more(P):
     assert min(_xent_bytes(P, _xent(P, workers=7, rows_per_worker=(2 ** 31 - 1) // 7))) > 0
+
+
+@pytest.mark.parametrize("dtype,first,workers,rows,width,classes", [(1, 1, 8, 8192, 1024, 131072), (1, 0, 8, 8192, 1024, 131072), (0, 1, 8, 8192, 1024, 131072),
+                                                                    (1, 0, 2, 4096, 2047, 32767), (0, 0, 1, 65536, 250, 50001)])
+def test_statistics_of_large_launches_take_what_their_tiles_write(P, dtype, first, workers, rows, width, classes):
+    """Tiles of 128 classes at least: 8 bytes a row and tile, 4 a row for the label's logit, and copies of what is not aligned."""
+    cfg = _xent(P, dtype=dtype, workers=workers, rows_per_worker=rows, width=width, classes=classes, classes_first=first)
+    n, eights = workers * rows, lambda k: (k + 7) // 8 * 8
+    copies = 2 * (n * eights(width) + workers * eights(width) * eights(classes)) if dtype == 1 and (width % 8 or classes % 8) else 0
+    assert P._lib.prsgd_linear_cross_entropy_workspace_bytes(ctypes.byref(cfg)) <= 8 * n * ((classes + 127) // 128) + 4 * n + copies + 2048
