@@ -296,6 +296,8 @@ XentPlan xent_plan(int workers, int64_t rows, int width, int classes, bool class
     e.stats = take(n * e.pieces * e.tiles * sizeof(float2));
     e.picked = take(n * sizeof(float));
   } else {
+    // rows of dz start at 16 bytes, at whole lines where they are longer than those
+    if (e.pieces == 1) e.piece = classes < 64 ? (int)eights(classes) : (classes + 63) / 64 * 64;
     e.dz = take(n * e.piece * es);
     e.sums = e.pieces > 1 ? take(n * width * sizeof(float)) : 0;
     size_t parts = 0;

@@ -53,3 +53,13 @@ def test_statistics_of_large_launches_take_what_their_tiles_write(P, dtype, firs
     n, eights = workers * rows, lambda k: (k + 7) // 8 * 8
     copies = 2 * (n * eights(width) + workers * eights(width) * eights(classes)) if dtype == 1 and (width % 8 or classes % 8) else 0
     assert P._lib.prsgd_linear_cross_entropy_workspace_bytes(ctypes.byref(cfg)) <= 8 * n * ((classes + 127) // 128) + 4 * n + copies + 2048
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,classes", [(1 << 20, 1), (1 << 20, 2), (1 << 20, 10), (1 << 18, 100), (1 << 16, 333)])
+def test_gradients_of_few_classes_take_what_they_hold(P, rows, classes, dtype):
+    """A row's classes rounded up to 64 (to 8 below that), the parts of products of few tiles (512 of 64 x 64 in fp32), a copy of W and a bit a row."""
+    cfg = _xent(P, dtype=dtype, rows_per_worker=rows, width=64, classes=classes)
+    each = (classes + 7) // 8 * 8 if classes < 64 else (classes + 63) // 64 * 64
+    n = P._lib.prsgd_linear_cross_entropy_backward_workspace_bytes(ctypes.byref(cfg))
+    assert n <= rows * each * (2 if dtype == 1 else 4) + 512 * 64 * 64 * 4 + rows // 8 + 2 * 64 * each + 4096
