@@ -369,20 +369,24 @@ ScanCall scan_call(const Tensor& v, PyObject* sequences, PyObject* starts, PyObj
   ScanCall c{};
   require(v.dim() == 2, "rows must be a [rows][width] tensor");
   c.cfg.dtype = operand_type(v, "rows must be a device tensor of float32 or bfloat16");
-  int64_t n = sequences != Py_None ? integer(sequences) : -1;
+  bool known = sequences != Py_None;
+  int64_t n = known ? integer(sequences) : 1;
+  require(n >= 0, "the number of sequences must not be negative");
   if (starts != Py_None) {
     const Tensor& t = operand(starts, "starts");
     c.starts = ids_of(t, v, "starts");
-    if (n < 0) n = t.size(0) - 1;
+    if (!known) n = t.size(0) - 1;
+    known = true;
     require(t.size(0) == n + 1 && n >= 1, "starts must have one value more than there are sequences");
   }
-  for (int i = 0; i < n_states && n < 0; ++i)
+  for (int i = 0; i < n_states && !known; ++i)
     if (states[i] != Py_None) {
       const Tensor& t = operand(states[i], "states");
       require(t.dim() == 2, "states must be [sequences][width]");
       n = t.size(0);
+      known = true;
     }
-  c.cfg.sequences = n < 0 ? 1 : size32(n);
+  c.cfg.sequences = size32(n);
   c.cfg.rows = v.size(0);
   c.cfg.width = size32(v.size(1));
   return c;
