@@ -5,6 +5,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
@@ -47,6 +48,8 @@ const Tensor& operand(PyObject* o, const char* what) {
   const Tensor& t = tensor(o, what);
   if (t.requires_grad() && c10::GradMode::is_enabled())
     throw Refused(std::string(what) + " requires grad, and the operators record nothing: call them under torch.no_grad() or in a torch.autograd.Function");
+  if (c10::AutogradState::get_tls_state().get_fw_grad_mode() && t._fw_grad(0).defined())
+    throw Refused(std::string(what) + " has a forward-mode tangent, which the operators would drop: call them in a torch.autograd.Function with a jvp");
   return t;
 }
 // ... and one that it has written: autograd's check of what it saved has to see that
