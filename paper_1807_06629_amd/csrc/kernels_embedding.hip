@@ -32,7 +32,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) embedding_kern
       float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
       if (real) load8(from + c, p.width - c, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = real ? v[e] * p.scale : 0.0f;   // a scale of infinity leaves padding alone
+      for (int e = 0; e < 8; ++e) v[e] = real ? v[e] * p.scale : 0.0f;   // +0 in padding, also under a negative scale
       store8(reinterpret_cast<T*>(p.y) + row * p.y_row + c, p.width - c, v);
     }
   }
@@ -376,7 +376,7 @@ template <typename T> hipError_t backward(const EmbeddingArgs& p, const Embeddin
   const int clearers = (int)std::min<int64_t>(units, std::max<int64_t>(16384 / p.workers, 1));
   hipLaunchKernelGGL(sort_tiles_kernel<T>, dim3((unsigned)(plan.tiles + clearers), (unsigned)p.workers), dim3(threads), 0, s, p, plan, ws);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.rows == 0) return e;
+  if (e != hipSuccess) return e;
   if (plan.tiles > 1) {
     hipLaunchKernelGGL(place_tokens_kernel, dim3((unsigned)plan.tiles, (unsigned)p.workers), dim3(kSortTile / 2), 0, s, p, plan, ws);
     if ((e = hipGetLastError()) != hipSuccess) return e;
@@ -385,7 +385,7 @@ template <typename T> hipError_t backward(const EmbeddingArgs& p, const Embeddin
   const int64_t chunks = (int64_t)plan.chunks * p.workers * ((p.width + kSlice - 1) / kSlice);
   const dim3 grid = grid_of((chunks + slots - 1) / slots);
   hipLaunchKernelGGL(chunk_sums_kernel<T>, grid, dim3(kThreads), 0, s, p, plan, ws, lanes_log2);
-  if ((e = hipGetLastError()) != hipSuccess || plan.chunks == 1) return e;
+  if ((e = hipGetLastError()) != hipSuccess) return e;
   hipLaunchKernelGGL(join_chunks_kernel<T>, grid, dim3(kThreads), 0, s, p, plan, ws, lanes_log2);
   return hipGetLastError();
 }
@@ -402,7 +402,9 @@ hipError_t launch_embedding(const EmbeddingArgs& p, bool bf16, hipStream_t s) {
 
 EmbeddingPlan embedding_plan(int workers, int64_t rows, int width) {
   EmbeddingPlan e{};
-  e.tiles = (int)std::max<int64_t>(1, (rows + kSortTile - 1) / kSortTile);
+  e.total = 256;
+  if (rows <= kFewRows) return e;        // no rows, or few: nothing of the workspace is used
+  e.tiles = (int)((rows + kSortTile - 1) / kSortTile);
   // Few rows a chunk, so that many lanes work on them; chunks grow with the rows, so that the commonest token's row has at most 256 parts to add: chunks of 8, 16,
   // 32 and 64 of 8 x 8192 tokens, 1024 wide, take 107, 89, 81 and 75 us for sums and parts, of 16 x 2013, 21 wide, 19, 21, 29 and 48 us.
   e.chunk = (int)std::max<int64_t>(kLeastChunk, ((rows + 255) / 256 + kLeastChunk - 1) / kLeastChunk * kLeastChunk);
@@ -414,7 +416,7 @@ EmbeddingPlan embedding_plan(int workers, int64_t rows, int width) {
   e.order = take(n * r * sizeof(int));
   e.sorted = take(n * r * sizeof(int));
   e.parts = take(n * e.chunks * 2 * part_width(width) * sizeof(float));
-  e.total = std::max<size_t>(at, 256);    // rows or none
+  e.total = at;
   return e;
 }
 

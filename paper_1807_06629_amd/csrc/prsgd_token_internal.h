@@ -58,7 +58,7 @@ hipError_t launch_embedding(const EmbeddingArgs& p, bool bf16, hipStream_t s);
 // Sorted order of every worker's tokens, runs of equal ones, and partial sums of runs that pass a chunk's end.
 struct EmbeddingPlan {
   int tiles;                             // of kSortTile tokens, per worker
-  int chunk, chunks;                     // sorted tokens whose sums one workgroup takes; per worker
+  int chunk, chunks;                     // sorted tokens whose sums some lanes take; per worker
   size_t keys, order, sorted, parts, total;    // byte offsets
 };
 EmbeddingPlan embedding_plan(int workers, int64_t rows, int width);

@@ -63,3 +63,12 @@ def test_gradients_of_few_classes_take_what_they_hold(P, rows, classes, dtype):
     each = (classes + 7) // 8 * 8 if classes < 64 else (classes + 63) // 64 * 64
     n = P._lib.prsgd_linear_cross_entropy_backward_workspace_bytes(ctypes.byref(cfg))
     assert n <= rows * each * (2 if dtype == 1 else 4) + 512 * 64 * 64 * 4 + rows // 8 + 2 * 64 * each + 4096
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_the_embeddings_gradient_of_few_rows_needs_no_workspace(P, dtype):
+    """Up to 256 rows a worker one launch does without: what every call asks for at least is all. Beyond, sorted tokens with their rows, and two fp32 rows for eight tokens."""
+    def need(rows, workers=5, width=250):
+        return P._lib.prsgd_embedding_backward_workspace_bytes(ctypes.byref(P.prsgd_embedding_config(dtype, workers, rows, 1000, width, 1.0)))
+    assert [need(r) for r in (0, 1, 8, 255, 256)] == [256] * 5
+    assert 5 * 257 * 8 < need(257) <= 5 * (257 * 8 + 33 * 2 * 256 * 4) + 3 * 256
