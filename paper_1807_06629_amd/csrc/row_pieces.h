@@ -6,16 +6,34 @@
 
 namespace prsgd {
 
+// Where a piece of V elements is read, n > 0 of which exist from its place on: that many before it ...
+constexpr int missing_of(int n, int V) { return n < V ? V - n : 0; }
+// ... or, of a row that is shorter than a piece, its element e there.
+constexpr int narrow_element(int e, int missing) { return e < missing ? 0 : e - missing; }
+// No element outside a row is read, of rows of any width at any place that is a multiple of V: what a piece reads depends on these modulo V, and on whether a whole one
+// lies before it.
+constexpr bool pieces_stay_in_rows(int V) {
+  for (int width = 1; width <= 4 * V; ++width)
+    for (int c = 0; c < width; c += V) {
+      const int n = width - c, missing = missing_of(n, V);
+      if (width >= V && (c - missing < 0 || c - missing + V > width)) return false;
+      for (int e = 0; e < V && width < V; ++e)
+        if (narrow_element(e, missing) < 0 || c + narrow_element(e, missing) >= width) return false;
+    }
+  return true;
+}
+static_assert(pieces_stay_in_rows(4) && pieces_stay_in_rows(8), "pieces of fp32 and bf16");
+
 // 16 bytes of a row from p on, n > 0 elements of which exist; fewer than 16 / ES come to lie at the end, behind what lies before them.  narrow (of all lanes): the
 // row as a whole is shorter than that, and is loaded one by one.
 template <int ES> __device__ __forceinline__ u32x4_t load_piece(const void* p, int n, bool narrow) {
   constexpr int V = 16 / ES;
-  const int missing = n < V ? V - n : 0;
+  const int missing = missing_of(n, V);
   if (!narrow) return reinterpret_cast<const Packed16<ES>*>(reinterpret_cast<const char*>(p) - missing * ES)->v;
   u32x4_t v = {0, 0, 0, 0};
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    const int from = e < missing ? 0 : e - missing;
+    const int from = narrow_element(e, missing);
     if constexpr (ES == 4) v[e] = reinterpret_cast<const uint32_t*>(p)[from];
     else v[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[from] << (16 * (e & 1));
   }
