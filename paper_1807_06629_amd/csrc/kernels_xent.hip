@@ -22,11 +22,13 @@ int splits_of(int64_t m, int64_t n, int64_t k, int groups) {
   const int64_t tiles = (m + 63) / 64 * ((n + 63) / 64) * groups;
   return tiles == 0 || k < 2048 ? 1 : (int)std::max<int64_t>(std::min<int64_t>(512 / tiles, k / 512), 1);
 }
-// Of the logits' gradients: 256 tiles of 128 x 128 in all (smaller ones wait for L2), a part at least 512 deep.  Gradients of 3 workers' 31 rows x 2704 x 938 fp32 67 -> 52 us,
-// of 33 x 12 x 3010 x 20 52 -> 34 us, of 8 x 128 x 4096 x 1000 bf16 66.7 -> 64.8 us.
-int splits_of_logits(int64_t m, int64_t n, int64_t k, int groups) {
-  const int64_t tiles = (m + 127) / 128 * ((n + 127) / 128) * groups;
-  return tiles == 0 || k < 1024 ? 1 : (int)std::max<int64_t>(std::min<int64_t>(256 / tiles, k / 512), 1);
+// Of the logits' gradients: 256 tiles of 128 x 128 in all (smaller ones wait for L2), a part at least 512 deep.  A bf16 step takes a third of an fp32 one's time, so that the parts'
+// addition is worth it from longer contractions on only, and longer yet where whole tiles nearly fill the card.  Gradients in parts and whole: 3 workers' 31 rows x 2704 x 938 fp32 48 and
+// 63 us, 33 x 12 x 3010 x 20 31 and 51 us, 8 x 128 x 1024 x 1000 91 and 92 us; bf16 of the first 32 and 37 us, 4 x 64 x 2048 x 512 21.1 and 22.3 us, of 1024 15.2 and 14.5 us,
+// 8 x 128 x 1000 classes by widths of 1024, 2048, 4096 and 8192 30.1, 42.2, 60.1, 102 and 24.2, 36.2, 57.5, 108 us, 12 x 128 x 4096 x 1000 82 and 89 us.
+int splits_of_logits(int64_t m, int64_t n, int64_t k, int groups, bool bf16) {
+  const int64_t tiles = (m + 127) / 128 * ((n + 127) / 128) * groups, least = !bf16 ? 1024 : tiles < 64 ? 2048 : 4096;
+  return tiles == 0 || k < least ? 1 : (int)std::max<int64_t>(std::min<int64_t>(256 / tiles, k / 512), 1);
 }
 size_t parts_bytes(int64_t m, int64_t n, int splits, int groups) {
   return splits > 1 ? (size_t)splits * groups * std::max(m * parts_row(n), n * parts_row(m)) * sizeof(float) : 0;
@@ -224,7 +226,7 @@ hipError_t launch_xent_backward(const XentArgs& x, const XentPlan& plan, char* w
     const bool small = plan.pieces == 1 && small_gradients(x.rows, x.width, x.classes, bf16);
     const ProductArgs dz_of = p;
     if (!small) {
-      p.splits = splits_of_logits(p.M, p.N, p.K, p.groups);
+      p.splits = splits_of_logits(p.M, p.N, p.K, p.groups, bf16);
       if ((e = launch_gradient<PX_DZ>(p, false, !x.classes_first, bf16, s)) != hipSuccess) return e;
       p.splits = 1;
     }
@@ -302,7 +304,7 @@ XentPlan xent_plan(int workers, int64_t rows, int width, int classes, bool class
     e.sums = e.pieces > 1 ? take(n * width * sizeof(float)) : 0;
     size_t parts = 0;
     for (const int n_of : {std::min(e.piece, classes), classes - (e.pieces - 1) * e.piece}) {          // the last piece has fewer tiles, and so perhaps more parts
-      parts = std::max({parts, parts_bytes(rows, n_of, splits_of_logits(rows, n_of, width, workers), workers),
+      parts = std::max({parts, parts_bytes(rows, n_of, splits_of_logits(rows, n_of, width, workers, bf16), workers),
                         parts_bytes(rows, width, splits_of(rows, width, n_of, workers), workers), parts_bytes(width, n_of, splits_of(width, n_of, rows, workers), workers)});
     }
     e.parts = take(parts);

@@ -72,3 +72,10 @@ def test_the_embeddings_gradient_of_few_rows_needs_no_workspace(P, dtype):
         return P._lib.prsgd_embedding_backward_workspace_bytes(ctypes.byref(P.prsgd_embedding_config(dtype, workers, rows, 1000, width, 1.0)))
     assert [need(r) for r in (0, 1, 8, 255, 256)] == [256] * 5
     assert 5 * 257 * 8 < need(257) <= 5 * (257 * 8 + 33 * 2 * 256 * 4) + 3 * 256
+
+
+@pytest.mark.parametrize("workers,rows,width,classes", [(8, 128, 1024, 1000), (8, 128, 2048, 1000), (64, 16, 1024, 100), (4, 64, 1024, 512)])
+def test_short_contractions_of_bf16_stay_whole(P, workers, rows, width, classes):
+    """No room is asked for parts that would take longer to add than they save: dz, a bit a row, and roundings to 256 bytes alone."""
+    n = P._lib.prsgd_linear_cross_entropy_backward_workspace_bytes(ctypes.byref(_xent(P, dtype=1, workers=workers, rows_per_worker=rows, width=width, classes=classes)))
+    assert n <= workers * rows * ((classes + 63) // 64 * 64) * 2 + workers * ((rows + 63) // 64 * 8) + 1024
