@@ -445,11 +445,14 @@ template <typename T, bool BACK, bool VEC> hipError_t launch_passes(const ScanAr
     const hipError_t e = launch_scan<T, BACK, kWaves, VEC, COMPOSE>(p, s);
     return e != hipSuccess ? e : launch_scan<T, BACK, kWaves, VEC, APPLY>(p, s);
   }
-  if (p.rows / p.sequences <= 16) return launch_scan<T, BACK, 1, VEC, WHOLE>(p, s);
+  const int64_t workgroups = (int64_t)((p.width + kTile - 1) / kTile) * p.sequences, each = p.rows / p.sequences;
+  // one wavefront, where eight would have no rows to walk: 4096 sequences of 12 rows x 512 bf16 24 us, by eight 164.  Where the card has enough of them, equal sequences of up to 64 rows
+  // too: 16384 of 17, 32 and 64 rows x 64 bf16 32, 38 and 82 us, by eight 126, 127 and 138 (gradients 46, 67 and 132 of 218, 231 and 243), 1024 of 64 rows 8.8 and 10.7 us, but 256 of
+  // them 7.1 and 4.9.  Of packed ones one may be much longer than the others, which a wavefront walks in four times the time that eight take.
+  if (each <= 16 || (p.starts == nullptr && each <= 64 && workgroups >= 1024)) return launch_scan<T, BACK, 1, VEC, WHOLE>(p, s);
   // too few workgroups for the card, and walks of some length: half the channels, and for long walks forward twice the rows in hand.  4 sequences of 16384 rows x 2048
   // bf16 330 -> 235 us, gradients 450 -> 397 us, gradients of 3 of 605 rows x 448 fp32 18.9 -> 13.7 us; but 64 of 1024 rows 219 -> 638 us, gradients of 2 packed ones of 900 rows
   // x 1048 17 -> 20 us.  (Odd rows in fp32 backward leave room for one row in hand: 1500 rows x 3001 93 -> 55 us.)
-  const int64_t workgroups = (int64_t)((p.width + kTile - 1) / kTile) * p.sequences, each = p.rows / p.sequences;
   if (workgroups <= 128 && each >= (p.starts == nullptr ? 256 : 2048)) {
     if constexpr (!BACK) {
       if (each >= 2048) return launch_scan<T, BACK, kWaves, VEC, WHOLE, 4, 4>(p, s);
