@@ -25,7 +25,7 @@ int splits_of(int64_t m, int64_t n, int64_t k, int groups) {
 // Of the logits' gradients: 256 tiles of 128 x 128 in all (smaller ones wait for L2), a part at least 512 deep.  A bf16 step takes a third of an fp32 one's time, so that the parts'
 // addition is worth it from longer contractions on only, and longer yet where whole tiles nearly fill the card.  Gradients in parts and whole: 3 workers' 31 rows x 2704 x 938 fp32 48 and
 // 63 us, 33 x 12 x 3010 x 20 31 and 51 us, 8 x 128 x 1024 x 1000 91 and 92 us; bf16 of the first 32 and 37 us, 4 x 64 x 2048 x 512 21.1 and 22.3 us, of 1024 15.2 and 14.5 us,
-// 8 x 128 x 1000 classes by widths of 1024, 2048, 4096 and 8192 30.1, 42.2, 60.1, 102 and 24.2, 36.2, 57.5, 108 us, 12 x 128 x 4096 x 1000 82 and 89 us.
+// 8 x 128 x 1000 classes by widths of 1024, 2048, 4096 and 8192 30.1, 42.2, 60.1, 102 and 24.2, 36.2, 57.5, 108 us (4096 with inputs out of the caches 72 and 74), 12 x 128 x 4096 x 1000 82 and 89 us.
 int splits_of_logits(int64_t m, int64_t n, int64_t k, int groups, bool bf16) {
   const int64_t tiles = (m + 127) / 128 * ((n + 127) / 128) * groups, least = !bf16 ? 1024 : tiles < 64 ? 2048 : 4096;
   return tiles == 0 || k < least ? 1 : (int)std::max<int64_t>(std::min<int64_t>(256 / tiles, k / 512), 1);
