@@ -151,13 +151,12 @@ template <typename T, bool BACK, int NW, int R, int CL, bool VEC, int OCC, int M
   __shared__ float total[2][NW][CH][2];
   __shared__ int head[CUT ? kTableRows : 1], tail[CUT ? kTableRows : 1];
   const int workgroups = tiles * (CUT ? p.parts : p.sequences);
-  const unsigned workgroup = workgroup_of_grid();
-  if (workgroup >= (unsigned)workgroups) {
-    if (MODE != COMPOSE && p.starts != nullptr && workgroup - workgroups < (unsigned)kClearers) clear_rest<T, BACK, MODE>(p, (int)(workgroup - workgroups));
+  if (blockIdx.x >= (unsigned)workgroups) {
+    clear_rest<T, BACK, MODE>(p, (int)(blockIdx.x - workgroups));
     return;
   }
   // Workgroups go to the XCDs in turn.  Those of half a line of bf16 that lie side by side go to one, so that they meet in its L2.
-  int block = workgroup;
+  int block = blockIdx.x;
   if constexpr (CL < 8) block = (block & 7) * (workgroups >> 3) + min(block & 7, workgroups & 7) + (block >> 3);
   const int slot = block / tiles, c_wg = (block - slot * tiles) * CH;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid % kWave, part = lane / CL, cl = lane % CL * 8;
@@ -429,15 +428,58 @@ template <typename T, bool BACK> __global__ void __launch_bounds__(kThreads) sca
     }
 }
 
+// Sequences first .. first + n of p.
+template <typename T> ScanArgs sequences_of(const ScanArgs& p, int first, int n) {
+  ScanArgs q = p;
+  q.sequences = n;
+  q.clear = 0;
+  if (p.starts != nullptr) {
+    q.starts += first;
+  } else {
+    const int64_t length = p.rows / p.sequences, row = first * length;
+    q.rows = n * length;
+    auto on = [&](auto& at, int64_t distance) {
+      if (at != nullptr) at = (decltype(+at))((const T*)at + row * distance);
+    };
+    on(q.v, p.v_row);
+    on(q.gate, p.gate_row);
+    on(q.h_in, p.h_in_row);
+    on(q.dh, p.dh_row);
+    on(q.h, p.h_row);
+    on(q.dgate, p.dgate_row);
+  }
+  if (p.initial != nullptr) q.initial += first * p.initial_row;
+  if (p.dlast != nullptr) q.dlast += first * p.dlast_row;
+  if (p.last != nullptr) q.last += first * p.last_row;
+  return q;
+}
+template <typename T, bool BACK> __global__ void __launch_bounds__(kThreads) clear_kernel(ScanArgs p) { clear_rest<T, BACK, WHOLE>(p, (int)blockIdx.x); }
+// An axis of a grid holds fewer than 2^32 threads, and a launch of more is cut without an error: more sequences than that go by several launches.
+constexpr int kMostWorkgroups = 1 << 22;
+template <typename T, bool BACK, int NW, int R, int CL, bool VEC, int OCC> hipError_t launch_in_turn(const ScanArgs& p, int tiles, hipStream_t s) {
+  const int most = kMostWorkgroups / tiles;
+  for (int first = 0; first < p.sequences; first += most) {
+    const ScanArgs q = sequences_of<T>(p, first, std::min(most, p.sequences - first));
+    hipLaunchKernelGGL((scan_kernel<T, BACK, NW, R, CL, VEC, OCC, WHOLE>), dim3((unsigned)tiles * (unsigned)q.sequences), dim3(NW * kWave), 0, s, q, tiles);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  if (p.starts == nullptr || p.clear == 0) return hipSuccess;
+  hipLaunchKernelGGL((clear_kernel<T, BACK>), dim3(kClearers), dim3(kThreads), 0, s, p);
+  return hipGetLastError();
+}
+
 // What stays in registers: all of it (spilled registers would be, besides slow, many more places to go wrong).
 template <typename T, bool VEC, int MODE> constexpr bool kLarge = sizeof(T) == 4 && !VEC && MODE == APPLY;
 template <typename T, bool BACK, int NW, bool VEC, int MODE, int R = BACK && kLarge<T, VEC, MODE> ? 1 : 2, int CL = kTile / 8>
 hipError_t launch_scan(const ScanArgs& p, hipStream_t s) {
   constexpr int OCC = BACK || CL < 8 || kLarge<T, VEC, MODE> ? 2 : 4;
   const int tiles = (p.width + 8 * CL - 1) / (8 * CL);
+  if constexpr (MODE == WHOLE) {
+    if (p.sequences > kMostWorkgroups / tiles) return launch_in_turn<T, BACK, NW, R, CL, VEC, OCC>(p, tiles, s);
+  }
   const unsigned others = MODE != COMPOSE && p.starts != nullptr && (p.clear != 0 || MODE == APPLY) ? kClearers : 0;
   const unsigned grid = (unsigned)tiles * (unsigned)(MODE == WHOLE ? p.sequences : p.parts) + others;
-  hipLaunchKernelGGL((scan_kernel<T, BACK, NW, R, CL, VEC, OCC, MODE>), grid_of(grid), dim3(NW * kWave), 0, s, p, tiles);
+  hipLaunchKernelGGL((scan_kernel<T, BACK, NW, R, CL, VEC, OCC, MODE>), dim3(grid), dim3(NW * kWave), 0, s, p, tiles);
   return hipGetLastError();
 }
 template <typename T, bool BACK, bool VEC> hipError_t launch_passes(const ScanArgs& p, hipStream_t s) {

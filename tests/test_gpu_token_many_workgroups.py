@@ -1,4 +1,4 @@
-"""Calls whose launches have 2^32 threads and more, which no axis of a grid holds.
+"""Calls whose launches would have 2^32 threads and more, which no axis of a grid holds.
 
 A scan's workgroups of 512 threads, 2^23 of them, and the logits' tiles of rows shorter than 16 bytes, 2^24 workgroups of 256.  Tolerances are those of the operators' own tests.
 """
