@@ -153,6 +153,13 @@ __global__ void __launch_bounds__(kSortTile / 2) place_tokens_kernel(EmbeddingAr
 constexpr int kSlice = 8 * kWave;        // columns that a chunk's lanes take, at most
 __host__ __device__ constexpr int part_width(int width) { return (width + 7) / 8 * 8; }
 
+// An axis of a grid holds fewer than 2^32 threads, and a launch of more is cut without an error: workgroups lie along two, the last of which may be too many.
+constexpr int kGridBits = 22;
+dim3 grid_of(int64_t workgroups) {
+  const int64_t along = (int64_t)1 << kGridBits;
+  return dim3((unsigned)std::min(workgroups, along), (unsigned)((workgroups + along - 1) / along));
+}
+
 // A chunk of sorted tokens and a slice of the columns, for lanes_log2 lanes: which these are, and what follows from them.
 struct ChunkPlace {
   int64_t g;
@@ -161,7 +168,7 @@ struct ChunkPlace {
   float* parts;                          // [2][part_width]: of the chunk's first run if it began before, of its last one if it goes on
   __device__ __forceinline__ bool set(const EmbeddingArgs& p, const EmbeddingPlan& plan, char* ws, int lanes_log2) {
     const int lanes = 1 << lanes_log2, slices = (p.width + kSlice - 1) / kSlice;
-    const int64_t unit = (int64_t)workgroup_of_grid() * (kThreads >> lanes_log2) + (threadIdx.x >> lanes_log2), at = unit / slices;
+    const int64_t unit = (int64_t)(blockIdx.y << kGridBits | blockIdx.x) * (kThreads >> lanes_log2) + (threadIdx.x >> lanes_log2), at = unit / slices;
     if (at >= (int64_t)plan.chunks * p.workers) return false;
     g = at / plan.chunks;
     chunk = (int)(at - g * plan.chunks);

@@ -282,19 +282,20 @@ XentPlan xent_plan(int workers, int64_t rows, int width, int classes, bool class
   if (!backward) {
     if (e.pieces == 1) e.piece = classes;
     // as many tiles as a piece gets, by whichever kernels take its operands
-    for (const int n_of : {e.piece, classes - (e.pieces - 1) * e.piece}) {
+    auto tiles_of_piece = [&](int classes_of) {
       ProductArgs p{};
       p.a.padded = e.align_w;
       p.b.padded = e.align_h;
-      p.M = n_of;
+      p.M = classes_of;
       p.N = (int)rows;
       p.K = width;
       p.groups = workers;
       p.splits = 1;
-      int tile = stats_rows_any(p, !classes_first, bf16);
-      if (bf16) tile = std::min(tile, stats_rows_bf16(p));
-      e.tiles = std::max(e.tiles, (n_of + tile - 1) / tile);
-    }
+      const int any = stats_rows_any(p, !classes_first, bf16), tile = bf16 ? std::min(any, stats_rows_bf16(p)) : any;
+      return (classes_of + tile - 1) / tile;
+    };
+    e.tiles = tiles_of_piece(e.piece);
+    if (e.pieces > 1) e.tiles = std::max(e.tiles, tiles_of_piece(classes - (e.pieces - 1) * e.piece));
     e.stats = take(n * e.pieces * e.tiles * sizeof(float2));
     e.picked = take(n * sizeof(float));
   } else {

@@ -9,9 +9,7 @@ namespace {
 template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bool TB, int EPI, bool NARROW>
 __global__ void __launch_bounds__(64 * WM * WN * WK, WM * WN * WK == 8 ? 4 : 1) product_kernel(ProductArgs p) {        // eight wavefronts: two workgroups on a compute unit
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  const unsigned workgroup = workgroup_of_grid();
-  if (blockIdx.y != 0 && workgroup >= workgroups_of(p)) return;          // (nothing is waited for in a launch along one axis)
-  product_tile<T, BM, BN, WM, WN, WK, D, TA, TB, EPI, NARROW>(p, tile_of_workgroup(p, workgroup), smem);
+  product_tile<T, BM, BN, WM, WN, WK, D, TA, TB, EPI, NARROW>(p, tile_of_workgroup(p, p.first + blockIdx.x), smem);
 }
 
 template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bool TB, int EPI, bool NARROW = false> hipError_t launch_tile(ProductArgs p, Cut* cut, hipStream_t s) {
@@ -21,8 +19,7 @@ template <typename T, int BM, int BN, int WM, int WN, int WK, int D, bool TA, bo
   if (const hipError_t e = allow_lds<kernel>(kLds); e != hipSuccess) return e;
   const unsigned grid = cut_product(p, BM, BN, D, cut);
   if (EPI == PX_STATS && p.tiles_m > p.most_tiles) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(kernel, grid_of(grid), dim3(64 * WM * WN * WK), kLds, s, p);
-  return hipGetLastError();
+  return in_turn(p, grid, [&](unsigned n) { hipLaunchKernelGGL(kernel, dim3(n), dim3(64 * WM * WN * WK), kLds, s, p); });
 }
 // Tiles: rows, columns and, where several wavefronts share it, depth of a step.  NARROW: of rows shorter than 16 bytes, the one kernel that has what it takes to load them.
 enum Tiles { NARROW, R32_C32, R32_C64, R64_C32, R32_C128, R128_C32, R64_C64, R64_C64_DEEP, R128_C128 };

@@ -199,9 +199,7 @@ __device__ __forceinline__ void product_bf16_tile(const ProductArgs& p, const Ti
 template <int BM, int BN, int WM, int WN, int S, bool TA, bool TB, int EPI>
 __global__ void __launch_bounds__(64 * WM * WN, 2) product_bf16_kernel(const ProductArgs p) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-  const unsigned workgroup = workgroup_of_grid();
-  if (blockIdx.y != 0 && workgroup >= workgroups_of(p)) return;          // (nothing is waited for in a launch along one axis)
-  product_bf16_tile<BM, BN, WM, WN, S, TA, TB, EPI>(p, tile_of_workgroup(p, workgroup), smem);
+  product_bf16_tile<BM, BN, WM, WN, S, TA, TB, EPI>(p, tile_of_workgroup(p, p.first + blockIdx.x), smem);
 }
 // dh by the first workgroups, dW by the others
 template <bool CF> __global__ void __launch_bounds__(256, 2) pair_bf16_kernel(const ProductArgs dh, const ProductArgs dw, int first_dw) {
@@ -227,8 +225,7 @@ template <int BM, int BN, int WM, int WN, int S, bool TA, bool TB, int EPI> hipE
   if (const hipError_t e = allow_lds<kernel>(kLds); e != hipSuccess) return e;
   const unsigned grid = cut_product(p, BM, BN, kDepth, cut);
   if (EPI == PX_STATS && p.tiles_m > p.most_tiles) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(kernel, grid_of(grid), dim3(64 * WM * WN), kLds, s, p);
-  return hipGetLastError();
+  return in_turn(p, grid, [&](unsigned n) { hipLaunchKernelGGL(kernel, dim3(n), dim3(64 * WM * WN), kLds, s, p); });
 }
 
 // 256 square, 128 by eight or four wavefronts, 64.

@@ -18,14 +18,6 @@ constexpr int lanes_for_row(int width) {
   return log2;
 }
 
-// HIP takes fewer than 2^32 threads along an axis of a grid: the workgroups of a launch of any size lie along two, the last of which may be too many.
-constexpr int kGridBits = 22;
-inline dim3 grid_of(int64_t workgroups) {
-  const int64_t along = (int64_t)1 << kGridBits;
-  return dim3((unsigned)(workgroups < along ? workgroups : along), (unsigned)((workgroups + along - 1) / along));
-}
-__device__ __forceinline__ unsigned workgroup_of_grid() { return blockIdx.y << kGridBits | blockIdx.x; }
-
 // ---- dropout -----------------------------------------------------------------------------------
 
 constexpr int kDropLayers = 1 << 15;

@@ -27,6 +27,7 @@ struct ProductArgs {
   int groups;
   int splits; float* parts;              // wished for: parts of the contraction, each to its own fp32 [groups][M][parts_row(N)] of `parts` (1: none)
   int tiles_m, tiles_n, split_steps;     // filled in by the launcher: tiles, and steps of the contraction in a part
+  unsigned first;                        // ... and the launch's first workgroup of all
   // of the rows, `rows` in every worker
   const int32_t* labels;
   const float* lse; const float* dloss;
@@ -63,10 +64,6 @@ __device__ __forceinline__ void join_stats(float& m, float& s, float m2, float s
 // Rows of the accumulators: element e of a 32 x 32 block lies at row acc_row(e, lane), column lane % 32.
 __device__ __forceinline__ int acc_row(int e, int lane) { return 8 * (e / 4) + 4 * (lane >> 5) + (e & 3); }
 
-// Of a launch: below 2^31, as the calls' checks see to.
-__host__ __device__ inline unsigned workgroups_of(const ProductArgs& p) {
-  return (unsigned)p.tiles_m * (unsigned)p.tiles_n * (unsigned)p.groups * (unsigned)p.splits;
-}
 // Consecutive workgroups go to the XCDs in turn; each gets a contiguous range of the tiles, so that what neighbours share stays in its L2.
 struct TilePosition { int g, ti, tj, split; };
 __device__ __forceinline__ TilePosition tile_of_workgroup(const ProductArgs& p, unsigned block) {
@@ -249,7 +246,16 @@ inline unsigned cut_product(ProductArgs& p, int bm, int bn, int depth, Cut* cut)
   const int steps = std::max((p.K + depth - 1) / depth, 1);
   p.split_steps = (steps + p.splits - 1) / p.splits;
   cut->splits = p.splits = (steps + p.split_steps - 1) / p.split_steps;
-  return workgroups_of(p);
+  return (unsigned)p.tiles_m * (unsigned)p.tiles_n * (unsigned)p.groups * (unsigned)p.splits;
+}
+// An axis of a grid holds fewer than 2^32 threads, and a launch of more is cut without an error: 2^22 workgroups a launch.
+template <typename F> hipError_t in_turn(ProductArgs& p, unsigned grid, const F& launch) {
+  constexpr unsigned kMost = 1u << 22;
+  for (p.first = 0; p.first < grid; p.first += kMost) {
+    launch(std::min(grid - p.first, kMost));
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 // transposed: (A, B) as (element (i, c) at c * ld + i).  Operands of any alignment and size (kernels_xent_any.hip) ...
