@@ -5,7 +5,7 @@
 // Both are x -> a x + b along a sequence, the second one from its end.  A workgroup has 64 channels of one sequence and walks along it: every lane
 // holds R rows of eight channels, composes them, and lanes, then wavefronts, compose theirs, so that a pass over NW * 8 * R rows reads
 // each of them once and needs no workgroup to wait for another.  States and compositions are fp32.  Bound by HBM where sequences are many (64 packed ones, 65536 x 2048
-// bf16: 189 us, 4.3 TB/s; gradients 351 us, 4.6 TB/s), by the 2 us of a pass where they are few.
+// bf16: 187 to 213 us by where they are cut, 3.8 to 4.3 TB/s; gradients 368 us, 4.4 TB/s), by the 2 us of a pass where they are few.
 #include <algorithm>
 #include <cmath>
 
@@ -468,7 +468,7 @@ template <typename T, bool BACK, int NW, int R, int CL, bool VEC, int OCC> hipEr
   return hipGetLastError();
 }
 
-// What stays in registers: all of it (spilled registers would be, besides slow, many more places to go wrong).
+// Rows in hand such that no vector register goes to scratch.  Scalar registers do not all fit: in 22 of the 48 kernels 2 to 105 of them are kept in lanes of vector registers.
 template <typename T, bool VEC, int MODE> constexpr bool kLarge = sizeof(T) == 4 && !VEC && MODE == APPLY;
 template <typename T, bool BACK, int NW, bool VEC, int MODE, int R = BACK && kLarge<T, VEC, MODE> ? 1 : 2, int CL = kTile / 8>
 hipError_t launch_scan(const ScanArgs& p, hipStream_t s) {

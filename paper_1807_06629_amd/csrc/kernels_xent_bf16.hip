@@ -232,7 +232,10 @@ template <int BM, int BN, int WM, int WN, int S, bool TA, bool TB, int EPI> hipE
 enum Tiles { BY_256, BY_128_EIGHT, BY_128_FOUR, BY_64 };
 Tiles choose_tiles(const ProductArgs& p) {
   // Time of a launch in units of a 64 x 64 tile's products: tiles per compute unit times their size over their efficiency.  Of tiles that a compute unit has
-  // several of in hand, parts of a round count as such; of 256 x 256 tiles whole rounds.
+  // several of in hand, parts of a round count as such; of 256 x 256 tiles whole rounds.  The efficiencies are fitted: logits by 256, 128 (eight wavefronts), 128 (four) and 64, the
+  // rule's first, of 2 x 4096 rows x 2048 x 32768 977, 1304, 1123 and 1594 us, 8 x 512 x 64 x 4096 19, 28, 21 and 28; by 128 (eight), 256, 128 (four) and 64 of 8 x 256 x 2048 x 2048
+  // 25, 52, 34 and 34; by 128 (four), 256, 128 (eight) and 64 of 16 x 512 x 1024 x 1024 26, 36, 29 and 34; by 64, 256, 128 (eight) and 128 (four) of 8 x 128 x 4096 x 1000 24, 84, 34 and 48,
+  // 4 x 256 x 512 x 2048 12, 26, 14 and 15.  Of 14 such sizes the rule took the best one or one within 1 %.
   auto cost = [](int64_t n, int b, double efficiency) { return (n < 256 ? 1.0 : (double)n / 256.0) * (b / 64) * (b / 64) / efficiency; };
   const int64_t n_middle = tiles_of(p, 128), n_huge = (tiles_of(p, 256) + 255) / 256 * 256;
   const double middle = cost(n_middle, 128, n_middle > 256 ? 0.9 : 1.34), small = cost(tiles_of(p, 64), 64, 0.68), huge = cost(n_huge, 256, 1.2);

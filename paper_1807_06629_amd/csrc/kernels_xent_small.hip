@@ -6,7 +6,8 @@ namespace prsgd {
 
 namespace {
 
-// All of a worker's products one after another.
+// All of a worker's products one after another.  (The arguments of all three do not fit the scalar registers: 14 to 34 of these are kept in lanes of vector registers, and 36 bytes a
+// lane in scratch.)
 template <typename T, bool CF> constexpr int small_lds_bytes() {
   constexpr int dz = lds_bytes<T, 32, 32, 1, 1, 4, 128, PX_DZ>(), wide = lds_bytes<T, 32, 128, 1, 4, 1, 32, PX_DH>(), high = lds_bytes<T, 128, 32, 4, 1, 1, 32, PX_DW>();
   return std::max(dz, std::max(wide, high));
