@@ -468,7 +468,7 @@ template <typename T, bool BACK, int NW, int R, int CL, bool VEC, int OCC> hipEr
   return hipGetLastError();
 }
 
-// Rows in hand such that no vector register goes to scratch.  Scalar registers do not all fit: in 22 of the 48 kernels 2 to 105 of them are kept in lanes of vector registers.
+// Rows in hand such that no vector register goes to scratch.  Scalar registers do not all fit: in 22 of these 44 kernels 2 to 105 of them are kept in lanes of vector registers.
 template <typename T, bool VEC, int MODE> constexpr bool kLarge = sizeof(T) == 4 && !VEC && MODE == APPLY;
 template <typename T, bool BACK, int NW, bool VEC, int MODE, int R = BACK && kLarge<T, VEC, MODE> ? 1 : 2, int CL = kTile / 8>
 hipError_t launch_scan(const ScanArgs& p, hipStream_t s) {
