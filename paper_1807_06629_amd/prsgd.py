@@ -475,7 +475,7 @@ def prsgd_last_error(h: Optional[Handle]) -> str:
 # Tensors are taken as they are: rows have to be contiguous, distances between rows and matrices are read off the strides.
 # Work goes to the current stream of the tensors' device.  Outputs and workspaces that are not given are allocated.
 # Nothing is recorded for autograd: tensors that require grad are refused (ValueError) unless under torch.no_grad() or in a
-# torch.autograd.Function's own forward; tensors written in place count as changed, so that its check of saved tensors sees it.
+# torch.autograd.Function's own forward, and tensors with a forward-mode tangent unless in such a forward; tensors written in place count as changed, so that its check of saved tensors sees it.
 # The marshalling is compiled (csrc/binding): ValueError for a tensor that no call takes, PrsgdError for what the library refuses.
 
 NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
